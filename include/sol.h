@@ -475,6 +475,80 @@ int sol_attn_fwd_records(const void* rec, const void* k_prep, const void* v_prep
                          int H, int N, int n_kv, int D, int out_format, sol_stream_t stream);
 
 /*
+ * Linear attention with a decay for each head: attention whose cost grows with
+ * the token count, beside the softmax attention above (whose cost grows with
+ * its square), for layers that read a sequence in order -- a long video, a
+ * stream of frames, a prompt and its continuation token by token.  For every
+ * batch b and head h, with g = log_decay[h] and a state S of D x D floats,
+ *     S_t = e^g S_(t-1) + k_t v_t^T,     o_t = scale q_t^T S_t .
+ * q and k enter as they are: sol_qknorm_rope3d normalises and rotates them.
+ *
+ * Tensors: q, out [B][H][N][D] and k, v [B][Hk][N][D] bf16, H a multiple of
+ * Hk (query head h reads key and value head h / (H / Hk)).  Each has its
+ * strides: row (b, h, n) starts at element b*b + h*h + n*n of its pointer, its
+ * D values contiguous; a NULL strides pointer means contiguous
+ * [B][heads][N][D].  Strides are multiples of 8 elements, at least 0 for
+ * inputs (0 broadcasts) and such that rows do not meet for outputs; pointers
+ * are 16-byte aligned.  An output may not overlap the span of an input or of
+ * another output.  log_decay: H floats, <= 0 (-inf: a head without memory).
+ * States: float [B][H][D][D], row = the dim of k, column = the dim of v.  lens:
+ * B int32 on the device, or NULL (all N): sequence b has its first lens[b]
+ * tokens (taken into 0..N); no token behind them is read.
+ *
+ * Products run in bf16 with fp32 accumulation; the states are fp32, and what
+ * enters them keeps 16 bits or more.  Every call repeats bit for bit.
+ *
+ * sol_lin_attn_fwd: out for all tokens.  state_in: the state before the first
+ * token (NULL: zero); state_out: receives the one after the last (NULL: not
+ * wanted; state_in itself is allowed).  Rows of out behind a sequence are left
+ * as they are.
+ *
+ * sol_lin_attn_bwd: with dout the gradient of out and dstate_out that of
+ * state_out (NULL: zero), dq, dk, dv (bf16, zero behind a sequence; the
+ * gradient of a shared head is the sum over its query heads, in fp32) and
+ * dstate_in, the gradient of state_in (NULL: not wanted; dstate_out itself is
+ * allowed).  The decays are constants of the model.
+ *
+ * sol_lin_attn_step: the next token of R requests, one per request: q, out
+ * [R][H][D], k, v [R][Hk][D] (strides b and h; n unused), the states in place
+ * in a pool [n_slots][H][D][D].  slots: R int32 on the device, the slot of each
+ * request, or NULL (request r has slot r, R <= n_slots).  A request whose slot
+ * is negative is an empty place of the batch: its out is zero.  One whose slot
+ * is past the pool, or is an earlier request's of the same call, gets NaN and
+ * leaves the pool alone.
+ *
+ * workspace: sol_lin_attn_fwd_workspace_bytes / _bwd_workspace_bytes bytes of
+ * device memory (0: none is needed and NULL is taken), 16-byte aligned, not
+ * overlapping any tensor; its contents are scratch.  Those return 0 for
+ * invalid sizes too.  D = 128; 1 <= N <= SOL_MAX_TOKENS.
+ */
+typedef struct sol_strides {
+  int64_t b, h, n;
+} sol_strides;
+
+size_t sol_lin_attn_fwd_workspace_bytes(int B, int H, int N, int D);
+size_t sol_lin_attn_bwd_workspace_bytes(int B, int H, int Hk, int N, int D);
+int sol_lin_attn_fwd(const void* q, const sol_strides* q_strides, const void* k,
+                     const sol_strides* k_strides, const void* v, const sol_strides* v_strides,
+                     void* out, const sol_strides* out_strides, const float* log_decay,
+                     const float* state_in, float* state_out, const int32_t* lens, int B, int H,
+                     int Hk, int N, int D, float scale, void* workspace, size_t workspace_bytes,
+                     sol_stream_t stream);
+int sol_lin_attn_bwd(const void* dout, const sol_strides* dout_strides, const void* q,
+                     const sol_strides* q_strides, const void* k, const sol_strides* k_strides,
+                     const void* v, const sol_strides* v_strides, void* dq,
+                     const sol_strides* dq_strides, void* dk, const sol_strides* dk_strides,
+                     void* dv, const sol_strides* dv_strides, const float* log_decay,
+                     const float* state_in, const float* dstate_out, float* dstate_in,
+                     const int32_t* lens, int B, int H, int Hk, int N, int D, float scale,
+                     void* workspace, size_t workspace_bytes, sol_stream_t stream);
+int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k,
+                      const sol_strides* k_strides, const void* v, const sol_strides* v_strides,
+                      void* out, const sol_strides* out_strides, const float* log_decay,
+                      float* state, const int32_t* slots, int R, int H, int Hk, int n_slots, int D,
+                      float scale, sol_stream_t stream);
+
+/*
  * Measurement aid: the dense matrix rate of this GPU at the attention
  * kernels' launch shape.  Launches `workgroups` workgroups of four waves (one
  * per SIMD, as the attention kernels run), each wave issuing iters * 16 fp16

@@ -1,0 +1,76 @@
+// Internal interface of the linear (sol_lin_attn_*) and differential
+// (sol_diff_attn_*) attention: what the front end (sol_api_ops.cpp) hands the
+// HIP launchers (sol_lin_attn.hip, sol_diff_attn.hip).  Arguments reaching the
+// launchers have been validated already.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "sol.h"
+#include "sol_internal.h"
+
+namespace sol {
+
+// Rows of 128 bf16: row (b, h, n) at element b sb + h sh + n sn of p.
+struct Rows {
+  uint16_t* p;
+  int64_t sb, sh, sn;
+};
+
+// ------------------------------------------------- linear attention, decayed
+
+constexpr int kLinRows = 64;                      // tokens per chunk of the scan
+constexpr int kStateElems = kHeadDim * kHeadDim;  // fp32 values of a head's state
+
+// Tokens of a sequence that one workgroup walks, and the segments that makes:
+// the scan is sequential in the tokens, so a call of few (b, h) slabs splits
+// its tokens into segments whose states are found first (one pass over k and v
+// and one over the segments' states).
+struct LinPlan {
+  int seg_rows;  // a multiple of kLinRows
+  int nseg;
+};
+LinPlan lin_plan(int64_t slabs, int N);
+// Bytes of the segments' states (0 for one segment).
+size_t lin_states_bytes(int64_t slabs, int N);
+
+// out = scale (scan of q, k, v), state_out = the final state (fp32, may be
+// null or state_in itself); states: lin_states_bytes of workspace.
+struct LinFwd {
+  Rows q, k, v, out;
+  const float* log_decay;
+  const float* state_in;  // may be null (zero)
+  float* state_out;
+  const int32_t* lens;  // may be null (all N)
+  int B, H, Hk, N;
+  float scale;
+  float* states;
+};
+hipError_t launch_lin_fwd(const LinFwd& a, hipStream_t stream);
+
+struct LinBwd {
+  Rows q, k, v, dout, dq, dk, dv;
+  const float* log_decay;
+  const float* state_in;   // may be null
+  const float* dstate_in;  // gradient of the final state, may be null
+  float* dstate_out;       // gradient of the initial state, may be null
+  const int32_t* lens;
+  int B, H, Hk, N;
+  float scale;
+  float* states;
+  float* partial;  // fp32 [2][B][H][N][128] when Hk < H, else null
+};
+hipError_t launch_lin_bwd(const LinBwd& a, hipStream_t stream);
+
+struct LinStep {
+  Rows q, k, v, out;  // sn unused
+  const float* log_decay;
+  float* state;  // fp32 [n_slots][H][128][128]
+  const int32_t* slots;  // may be null (request r has slot r)
+  int R, H, Hk, n_slots;
+  float scale;
+};
+hipError_t launch_lin_step(const LinStep& a, hipStream_t stream);
+
+}  // namespace sol

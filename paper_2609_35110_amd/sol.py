@@ -706,6 +706,205 @@ def attn_fwd_records(rec, k_prep, v_prep, n_kv=None, out=None, fp8=False, int8_r
     return out
 
 
+# ------------------------------------------- linear and differential attention
+
+# sol_lin_attn_* and sol_diff_attn_* (include/sol.h), bound when first called.
+_P, _I32, _SZ, _F32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
+_SIGNATURES = {
+    "sol_lin_attn_fwd_workspace_bytes": ([_I32] * 4, _SZ),
+    "sol_lin_attn_bwd_workspace_bytes": ([_I32] * 5, _SZ),
+    "sol_lin_attn_fwd": ([_P] * 12 + [_I32] * 5 + [_F32, _P, _SZ, _P], _I32),
+    "sol_lin_attn_bwd": ([_P] * 19 + [_I32] * 5 + [_F32, _P, _SZ, _P], _I32),
+    "sol_lin_attn_step": ([_P] * 11 + [_I32] * 5 + [_F32, _P], _I32),
+}
+
+
+@functools.lru_cache(maxsize=None)
+def _entry(name):
+    f = getattr(lib(), name)
+    f.argtypes, f.restype = _SIGNATURES[name]
+    return f
+
+
+def sol_lin_attn_fwd_workspace_bytes(B, H, N, D):
+    return _entry("sol_lin_attn_fwd_workspace_bytes")(B, H, N, D)
+
+
+def sol_lin_attn_bwd_workspace_bytes(B, H, Hk, N, D):
+    return _entry("sol_lin_attn_bwd_workspace_bytes")(B, H, Hk, N, D)
+
+
+def sol_lin_attn_fwd(*args):
+    return _entry("sol_lin_attn_fwd")(*args)
+
+
+def sol_lin_attn_bwd(*args):
+    return _entry("sol_lin_attn_bwd")(*args)
+
+
+def sol_lin_attn_step(*args):
+    return _entry("sol_lin_attn_step")(*args)
+
+
+def strides(b, h, n):
+    """A sol_strides: the elements between batches, heads and tokens."""
+    return (ctypes.c_int64 * 3)(b, h, n)
+
+
+def _rows(name, t, dev=None, shape=None):
+    """(pointer, strides) of a bf16 tensor [B, heads, N, D] (or [R, heads, D])
+    whose rows of D are contiguous; strides None when all of it is."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype is not torch.bfloat16:
+        raise TypeError("%s must be bfloat16, got %s" % (name, t.dtype))
+    if not t.is_cuda or (dev is not None and t.device != dev):
+        raise ValueError("%s must be on %s" % (name, "a HIP device" if dev is None else dev))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.is_contiguous():
+        return t.data_ptr(), None
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] != 1:
+        raise ValueError("%s must have contiguous rows (the last dimension's stride is %d)" % (name, st[-1]))
+    return t.data_ptr(), strides(st[0], st[1], st[2] if t.dim() == 4 else 0)
+
+
+def _dims(name, t, n):
+    if not isinstance(t, torch.Tensor) or t.dim() != n:
+        raise ValueError("%s must be a tensor of %d dimensions" % (name, n))
+    return t.shape
+
+
+def _device_array(name, t, dev, dtype, shape):
+    """The pointer of a contiguous device tensor, None for None."""
+    if t is None:
+        return None
+    if (not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != dev or t.shape != shape
+            or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), dev))
+    return t.data_ptr()
+
+
+def _scratch(workspace, nbytes, dev):
+    """(pointer, bytes) of the caller's workspace, or of one from torch's
+    allocator (the tensor comes along: it lives until the call is enqueued, and
+    the allocator hands its memory on in stream order)."""
+    if workspace is None:
+        if nbytes == 0:
+            return None, None, 0
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        _check_workspace(workspace, nbytes, dev)
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _call(entry, dev, *args):
+    """entry(*args, stream), on the tensors' device and its current stream."""
+    i = dev.index
+    if i == torch.cuda.current_device():
+        check(entry(*args, torch._C._cuda_getCurrentRawStream(i)))
+    else:
+        with torch.cuda.device(dev):
+            check(entry(*args, torch._C._cuda_getCurrentRawStream(i)))
+
+
+def _scale(scale):
+    return HEAD_DIM ** -0.5 if scale is None else float(scale)
+
+
+def lin_attn_fwd(q, k, v, log_decay, scale=None, state=None, final_state=False, lens=None, out=None,
+                 workspace=None):
+    """Linear attention with a decay for each head: S = e^g S + k v^T, out =
+    scale q^T S, token by token (scale None: 1/sqrt(D)).
+
+    q [B, H, N, D], k, v [B, Hk, N, D] bf16 (any strides that keep rows
+    contiguous and 16-byte aligned), log_decay float32 [H], state float32
+    [B, H, D, D] (None: zero), lens int32 [B] on the device (None: all N; rows
+    of out behind a sequence are not written).  final_state: also return the
+    state after the last token; True, or the tensor that receives it (state
+    itself is allowed).  Returns out, or (out, final state)."""
+    B, H, N, D = _dims("q", q, 4)
+    dev = q.device
+    Hk = _dims("k", k, 4)[1]
+    qp, qs = _rows("q", q)
+    kp, ks = _rows("k", k, dev, (B, Hk, N, D))
+    vp, vs = _rows("v", v, dev, (B, Hk, N, D))
+    if out is None:
+        out = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+    op, os_ = _rows("out", out, dev, (B, H, N, D))
+    if final_state is True:
+        final_state = torch.empty((B, H, D, D), dtype=torch.float32, device=dev)
+    elif final_state is False:
+        final_state = None
+    if log_decay is None:
+        raise ValueError("log_decay must be given")
+    ws, wp, wn = _scratch(workspace, sol_lin_attn_fwd_workspace_bytes(B, H, N, D), dev)
+    _call(sol_lin_attn_fwd, dev, qp, qs, kp, ks, vp, vs, op, os_,
+          _device_array("log_decay", log_decay, dev, torch.float32, (H,)),
+          _device_array("state", state, dev, torch.float32, (B, H, D, D)),
+          _device_array("final_state", final_state, dev, torch.float32, (B, H, D, D)),
+          _device_array("lens", lens, dev, torch.int32, (B,)), B, H, Hk, N, D, _scale(scale), wp, wn)
+    return out if final_state is None else (out, final_state)
+
+
+def lin_attn_bwd(dout, q, k, v, log_decay, scale=None, state=None, dfinal_state=None, lens=None,
+                 dstate=None, dq=None, dk=None, dv=None, workspace=None):
+    """The gradients of lin_attn_fwd: (dq, dk, dv), bf16 and zero behind a
+    sequence, and where state or dfinal_state (the gradient of the final
+    state) is given the gradient of state as well, float32, in dstate when
+    that is given (dfinal_state itself is allowed)."""
+    B, H, N, D = _dims("q", q, 4)
+    dev = q.device
+    Hk = _dims("k", k, 4)[1]
+    qp, qs = _rows("q", q)
+    kp, ks = _rows("k", k, dev, (B, Hk, N, D))
+    vp, vs = _rows("v", v, dev, (B, Hk, N, D))
+    gp, gs = _rows("dout", dout, dev, (B, H, N, D))
+    grads = []
+    for name, t, h in (("dq", dq, H), ("dk", dk, Hk), ("dv", dv, Hk)):
+        if t is None:
+            t = torch.empty((B, h, N, D), dtype=torch.bfloat16, device=dev)
+        grads.append((t,) + _rows(name, t, dev, (B, h, N, D)))
+    if dstate is None and (state is not None or dfinal_state is not None):
+        dstate = torch.empty((B, H, D, D), dtype=torch.float32, device=dev)
+    if log_decay is None:
+        raise ValueError("log_decay must be given")
+    ws, wp, wn = _scratch(workspace, sol_lin_attn_bwd_workspace_bytes(B, H, Hk, N, D), dev)
+    (dq, dqp, dqs), (dk, dkp, dks), (dv, dvp, dvs) = grads
+    _call(sol_lin_attn_bwd, dev, gp, gs, qp, qs, kp, ks, vp, vs, dqp, dqs, dkp, dks, dvp, dvs,
+          _device_array("log_decay", log_decay, dev, torch.float32, (H,)),
+          _device_array("state", state, dev, torch.float32, (B, H, D, D)),
+          _device_array("dfinal_state", dfinal_state, dev, torch.float32, (B, H, D, D)),
+          _device_array("dstate", dstate, dev, torch.float32, (B, H, D, D)),
+          _device_array("lens", lens, dev, torch.int32, (B,)), B, H, Hk, N, D, _scale(scale), wp, wn)
+    return (dq, dk, dv) if dstate is None else (dq, dk, dv, dstate)
+
+
+def lin_attn_step(q, k, v, log_decay, state, slots=None, scale=None, out=None):
+    """One token for each of R requests: q [R, H, D], k, v [R, Hk, D] bf16; state,
+    float32 [n_slots, H, D, D], is updated in place at slots (int32 [R] on the
+    device; None: request r has slot r; below 0: an empty place, whose out is
+    zero; a slot past the pool or named twice: NaN).  Returns out [R, H, D]."""
+    R, H, D = _dims("q", q, 3)
+    dev = q.device
+    Hk = _dims("k", k, 3)[1]
+    n_slots = _dims("state", state, 4)[0]
+    qp, qs = _rows("q", q)
+    kp, ks = _rows("k", k, dev, (R, Hk, D))
+    vp, vs = _rows("v", v, dev, (R, Hk, D))
+    if out is None:
+        out = torch.empty((R, H, D), dtype=torch.bfloat16, device=dev)
+    op, os_ = _rows("out", out, dev, (R, H, D))
+    if log_decay is None:
+        raise ValueError("log_decay must be given")
+    _call(sol_lin_attn_step, dev, qp, qs, kp, ks, vp, vs, op, os_,
+          _device_array("log_decay", log_decay, dev, torch.float32, (H,)),
+          _device_array("state", state, dev, torch.float32, (n_slots, H, D, D)),
+          _device_array("slots", slots, dev, torch.int32, (R,)), R, H, Hk, n_slots, D, _scale(scale))
+    return out
+
+
 # ------------------------------------------------------------ measurement aid
 
 def mfma_probe_flops(workgroups, iters):

@@ -1,0 +1,146 @@
+"""The C ABI of the linear and differential attention without a GPU: every
+refusal happens on the host, before any HIP call (the pointers here are never
+read)."""
+import ctypes
+import os
+
+import pytest
+
+from paper_2609_35110_amd import sol
+
+P = ctypes.c_void_p
+MB = 1 << 20
+
+
+def at(i):
+    return i * 64 * MB
+
+
+@pytest.fixture(scope="module", autouse=True)
+def L():
+    if not os.path.exists(sol.LIB_PATH):
+        from paper_2609_35110_amd import build
+        build.build()
+    return sol.lib()
+
+
+def refused(status, fragment, st):
+    assert st == status, sol.sol_last_error()
+    assert fragment in sol.sol_last_error()
+
+
+S = sol.strides
+SMALL = dict(B=2, H=4, Hk=2, N=100, D=128, scale=1.0)
+COMMON = [
+    (dict(B=0), -1, ">= 1"),
+    (dict(N=0), -1, ">= 1"),
+    (dict(Hk=3), -1, "multiple"),
+    (dict(Hk=0), -1, ">= 1"),
+    (dict(D=64), -2, "head dim"),
+    (dict(N=(1 << 23) + 1), -2, "exceeds"),
+    (dict(B=1 << 20, H=1 << 10, Hk=1), -2, "too large"),
+    (dict(scale=float("nan")), -1, "scale"),
+    (dict(scale=float("inf")), -1, "scale"),
+    (dict(q=None), -1, "q must not be NULL"),
+    (dict(k=at(2) + 8), -1, "k must be 16-byte aligned"),
+    (dict(log_decay=None), -1, "log_decay"),
+    (dict(log_decay=at(6) + 2), -1, "log_decay must be 4-byte"),
+    (dict(lens=at(7) + 1), -1, "lens must be 4-byte"),
+    (dict(q_st=S(4 * 100 * 128, 100 * 128, 127)), -1, "q strides"),
+    (dict(v_st=S(-8, 100 * 128, 128)), -1, "v strides"),
+    (dict(k_st=S(1 << 41, 100 * 128, 128)), -1, "k strides"),
+]
+
+
+def fwd(**kw):
+    a = dict(SMALL, q=at(1), q_st=None, k=at(2), k_st=None, v=at(3), v_st=None, out=at(4), out_st=None, log_decay=at(6),
+             state_in=None, state_out=None, lens=None, ws=None, ws_bytes=0)
+    a.update(kw)
+    return sol.sol_lin_attn_fwd(a["q"], a["q_st"], a["k"], a["k_st"], a["v"], a["v_st"], a["out"], a["out_st"],
+                                a["log_decay"], a["state_in"], a["state_out"], a["lens"], a["B"], a["H"], a["Hk"],
+                                a["N"], a["D"], a["scale"], a["ws"], a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("kw,status,fragment", COMMON + [
+    (dict(out=None), -1, "out must not be NULL"),
+    (dict(out=at(1) + 16), -1, "out overlaps q"),
+    (dict(out=at(7), lens=at(7) + 64), -1, "out overlaps lens"),
+    (dict(out_st=S(4 * 100 * 128, 100 * 128, 0)), -1, "rows of out overlap"),
+    (dict(out_st=S(100 * 128, 100 * 128, 128)), -1, "rows of out overlap"),
+    (dict(out_st=S(64, 2 * 100 * 128, 128)), -1, "rows of out overlap"),
+    (dict(state_out=at(8) + 4), -1, "16-byte"),
+    (dict(state_in=at(8), state_out=at(8) + 1024), -1, "state_out overlaps state_in"),
+    (dict(state_in=at(4), state_out=at(4)), -1, "overlaps"),
+    (dict(N=20000), -1, "workspace is NULL"),
+    (dict(N=20000, ws=at(9) + 4, ws_bytes=1 << 30), -1, "workspace must be 16-byte"),
+    (dict(N=20000, ws=at(9), ws_bytes=1000), -1, "workspace needs"),
+    (dict(N=20000, ws=at(1), ws_bytes=1 << 30), -1, "workspace overlaps"),
+])
+def test_lin_fwd_refusals(kw, status, fragment):
+    refused(status, fragment, fwd(**kw))
+
+
+def bwd(**kw):
+    a = dict(SMALL, dout=at(5), q=at(1), q_st=None, k=at(2), k_st=None, v=at(3), v_st=None, dq=at(10), dk=at(11),
+             dv=at(12), dv_st=None, log_decay=at(6), state_in=None, dstate_out=None, dstate_in=None, lens=None,
+             ws=at(13), ws_bytes=1 << 25)
+    a.update(kw)
+    return sol.sol_lin_attn_bwd(a["dout"], None, a["q"], a["q_st"], a["k"], a["k_st"], a["v"], a["v_st"], a["dq"], None,
+                                a["dk"], None, a["dv"], a["dv_st"], a["log_decay"], a["state_in"], a["dstate_out"],
+                                a["dstate_in"], a["lens"], a["B"], a["H"], a["Hk"], a["N"], a["D"], a["scale"], a["ws"],
+                                a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("kw,status,fragment", COMMON + [
+    (dict(dout=None), -1, "dout must not be NULL"),
+    (dict(dq=at(10) + 8), -1, "dq must be 16-byte"),
+    (dict(dk=at(10)), -1, "dk overlaps dq"),
+    (dict(dv=at(5)), -1, "dv overlaps dout"),
+    (dict(dv_st=S(2 * 100 * 128, 0, 128)), -1, "rows of dv overlap"),
+    (dict(dstate_out=at(14), dstate_in=at(14) + 4096), -1, "dstate_in overlaps dstate_out"),
+    (dict(state_in=at(14), dstate_in=at(14)), -1, "dstate_in overlaps state_in"),
+    (dict(dstate_out=at(14) + 8), -1, "16-byte"),
+    (dict(ws_bytes=100), -1, "workspace needs"),
+    (dict(ws=at(2)), -1, "workspace overlaps k"),
+])
+def test_lin_bwd_refusals(kw, status, fragment):
+    refused(status, fragment, bwd(**kw))
+
+
+def step(**kw):
+    a = dict(SMALL, q=at(1), q_st=None, k=at(2), k_st=None, v=at(3), v_st=None, out=at(4), out_st=None, log_decay=at(6),
+             state=at(8), slots=at(7), n_slots=3)
+    a.update(kw)
+    return sol.sol_lin_attn_step(a["q"], a["q_st"], a["k"], a["k_st"], a["v"], a["v_st"], a["out"], a["out_st"],
+                                 a["log_decay"], a["state"], a["slots"], a["B"], a["H"], a["Hk"], a["n_slots"], a["D"],
+                                 a["scale"], None)
+
+
+@pytest.mark.parametrize("kw,status,fragment", [
+    (dict(B=0), -1, ">= 1"),
+    (dict(Hk=3), -1, "multiple"),
+    (dict(D=64), -2, "head dim"),
+    (dict(B=1 << 21, H=1 << 10, Hk=1), -2, "too large"),
+    (dict(n_slots=0), -1, "n_slots"),
+    (dict(slots=None, B=4), -1, "without slots"),
+    (dict(slots=at(7) + 2), -1, "slots must be 4-byte"),
+    (dict(state=None), -1, "state must not be NULL"),
+    (dict(state=at(8) + 8), -1, "state must be 16-byte"),
+    (dict(q=at(8) + 64), -1, "state overlaps q"),
+    (dict(out=at(8) + 64), -1, "state overlaps out"),
+    (dict(out_st=S(4 * 128, 64, 0)), -1, "rows of out overlap"),
+    (dict(scale=float("nan")), -1, "scale"),
+])
+def test_lin_step_refusals(kw, status, fragment):
+    refused(status, fragment, step(**kw))
+
+
+def test_lin_workspaces():
+    assert sol.sol_lin_attn_fwd_workspace_bytes(1, 2, 192, 128) == 0          # one segment
+    assert sol.sol_lin_attn_fwd_workspace_bytes(1, 1, 20000, 128) > 0
+    assert sol.sol_lin_attn_fwd_workspace_bytes(4, 1024, 20000, 128) == 0     # enough slabs as they are
+    for bad in ((0, 1, 1, 128), (1, 1, 1, 64), (1, 1, (1 << 23) + 1, 128), (1 << 20, 1 << 10, 1, 128)):
+        assert sol.sol_lin_attn_fwd_workspace_bytes(*bad) == 0
+    one = sol.sol_lin_attn_bwd_workspace_bytes(1, 4, 4, 100, 128)
+    assert sol.sol_lin_attn_bwd_workspace_bytes(1, 4, 2, 100, 128) == one + 2 * 4 * 100 * 128 * 4
+    assert sol.sol_lin_attn_bwd_workspace_bytes(1, 4, 3, 100, 128) == 0
