@@ -549,6 +549,65 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
                       float scale, sol_stream_t stream);
 
 /*
+ * Differential attention: for every output head h the difference of two
+ * softmax maps over the same values, the second with a learned weight,
+ *     out_h = softmax(scale q_2h k^T) v - lambda[h] softmax(scale q_(2h+1) k'^T) v
+ * (what both maps give the whole sequence cancels).  q and k enter as they are:
+ * sol_qknorm_rope3d normalises and rotates them.
+ *
+ * Tensors (bf16, strides, alignment and overlaps as in sol_lin_attn_fwd): q
+ * [B][2H][N][D], heads 2h and 2h + 1 the maps of output head h; v
+ * [B][Hv][M][D], H a multiple of Hv, output head h reading value head
+ * hv = h / (H / Hv); k [B][Hk][M][D] with Hk = 2 Hv (the maps read key heads
+ * 2 hv and 2 hv + 1) or Hk = Hv (both read key head hv); out [B][H][N][D].
+ * lambda: H floats on the device; scale > 0.
+ *
+ * Masks: q_lens, kv_lens: B int32 on the device, or NULL (all N, all M): the
+ * rows and keys of each sequence (taken into 0..N, 0..M); nothing behind them
+ * is read.  causal: the last row of a sequence sees its last key, the row
+ * before it one key less: row i sees keys up to i + kv_lens[b] - q_lens[b], as
+ * new tokens at the end of a cache do.  A row that sees no key has out = 0.
+ *
+ * Scores and row sums are fp32; probabilities are rounded to bf16 for the
+ * product with v.  Every call repeats bit for bit.  A call with few rows over
+ * many keys splits the keys over workgroups and joins them through the
+ * workspace.
+ *
+ * sol_diff_attn_fwd: rows of out behind a sequence are left as they are.  For
+ * training, out2 ([B][H][N][D] bf16, contiguous) receives the second map's own
+ * output and lse ([B][2H][N] floats) the logarithm of each row's sum of
+ * exponentials, -inf for a row that sees no key; both may be NULL, and both are
+ * left as they are behind a sequence.
+ *
+ * sol_diff_attn_bwd: from dout, the gradient of out, and the forward call's
+ * out, out2 and lse: dq, dk, dv (bf16, zero behind a sequence; shared heads'
+ * gradients summed in fp32) and dlambda (H floats, summed over the batch).
+ *
+ * workspace: sol_diff_attn_fwd_workspace_bytes / _bwd_workspace_bytes bytes of
+ * device memory (0: none is needed and NULL is taken), 16-byte aligned, not
+ * overlapping any tensor; its contents are scratch.  Those return 0 for
+ * invalid sizes too.  D = 128; 1 <= N, M <= SOL_MAX_TOKENS; B*H <= 2^22,
+ * B*H*N and B*Hv*M < 2^31.
+ */
+size_t sol_diff_attn_fwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D);
+size_t sol_diff_attn_bwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D);
+int sol_diff_attn_fwd(const void* q, const sol_strides* q_strides, const void* k,
+                      const sol_strides* k_strides, const void* v, const sol_strides* v_strides,
+                      void* out, const sol_strides* out_strides, void* out2, float* lse,
+                      const float* lambda, const int32_t* q_lens, const int32_t* kv_lens, int B,
+                      int H, int Hv, int Hk, int N, int M, int D, float scale, int causal,
+                      void* workspace, size_t workspace_bytes, sol_stream_t stream);
+int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const void* q,
+                      const sol_strides* q_strides, const void* k, const sol_strides* k_strides,
+                      const void* v, const sol_strides* v_strides, const void* out,
+                      const sol_strides* out_strides, const void* out2, const float* lse,
+                      const float* lambda, void* dq, const sol_strides* dq_strides, void* dk,
+                      const sol_strides* dk_strides, void* dv, const sol_strides* dv_strides,
+                      float* dlambda, const int32_t* q_lens, const int32_t* kv_lens, int B, int H,
+                      int Hv, int Hk, int N, int M, int D, float scale, int causal,
+                      void* workspace, size_t workspace_bytes, sol_stream_t stream);
+
+/*
  * Measurement aid: the dense matrix rate of this GPU at the attention
  * kernels' launch shape.  Launches `workgroups` workgroups of four waves (one
  * per SIMD, as the attention kernels run), each wave issuing iters * 16 fp16

@@ -130,6 +130,27 @@ int check_lin_grid(int64_t slabs) {
   return SOL_OK;
 }
 
+// The shape of a differential call.
+int check_diff(const sol::DiffShape& s, int D) {
+  if (s.B < 1 || s.H < 1 || s.Hv < 1 || s.N < 1 || s.M < 1)
+    return fail(SOL_ERR_INVALID_ARG, "B, H, Hv, N, M must be >= 1 (got %d, %d, %d, %d, %d)", s.B, s.H, s.Hv, s.N, s.M);
+  if (s.H % s.Hv) return fail(SOL_ERR_INVALID_ARG, "H = %d is not a multiple of Hv = %d", s.H, s.Hv);
+  if (s.Hk != s.Hv && s.Hk != 2 * (int64_t)s.Hv)
+    return fail(SOL_ERR_INVALID_ARG, "Hk must be Hv or 2 Hv (got %d for Hv = %d)", s.Hk, s.Hv);
+  if (D != sol::kHeadDim) return fail(SOL_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", D);
+  if (s.N > SOL_MAX_TOKENS || s.M > SOL_MAX_TOKENS)
+    return fail(SOL_ERR_UNSUPPORTED, "N=%d or M=%d exceeds %d", s.N, s.M, SOL_MAX_TOKENS);
+  // rows and keys stay below 2^31 (16 and more of each to a workgroup, times
+  // the splits of the few-row calls, at most 256)
+  if ((int64_t)s.B * s.H > (1 << 22) || (int64_t)s.B * s.H * s.N > INT32_MAX || (int64_t)s.B * s.Hv * s.M > INT32_MAX)
+    return fail(SOL_ERR_UNSUPPORTED, "B*H, B*H*N or B*Hv*M too large");
+  if (!std::isfinite(s.scale) || !(s.scale > 0.0f)) return fail(SOL_ERR_INVALID_ARG, "scale must be finite and > 0");
+  SOL_TRY(check_small("lambda", s.lambda, false));
+  SOL_TRY(check_small("q_lens", s.q_lens, true));
+  SOL_TRY(check_small("kv_lens", s.kv_lens, true));
+  return SOL_OK;
+}
+
 constexpr uint64_t kStateBytes = (uint64_t)sol::kStateElems * sizeof(float);
 
 }  // namespace
@@ -276,6 +297,96 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
   a.n_slots = n_slots;
   a.scale = scale;
   return done(sol::launch_lin_step(a, reinterpret_cast<hipStream_t>(stream)), "lin_attn_step");
+}
+
+size_t sol_diff_attn_fwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D) {
+  sol::DiffShape s = {B, H, Hv, Hv, N, M, 1.0f, 0, nullptr, nullptr, nullptr};
+  if (B < 1 || H < 1 || Hv < 1 || N < 1 || M < 1 || H % Hv || D != sol::kHeadDim || N > SOL_MAX_TOKENS ||
+      M > SOL_MAX_TOKENS || (int64_t)B * H * N > INT32_MAX)
+    return 0;
+  return sol::diff_fwd_bytes(s);
+}
+
+size_t sol_diff_attn_bwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D) {
+  sol::DiffShape s = {B, H, Hv, Hv, N, M, 1.0f, 0, nullptr, nullptr, nullptr};
+  if (B < 1 || H < 1 || Hv < 1 || N < 1 || M < 1 || H % Hv || D != sol::kHeadDim || N > SOL_MAX_TOKENS ||
+      M > SOL_MAX_TOKENS || (int64_t)B * H * N > INT32_MAX)
+    return 0;
+  size_t at;
+  int parts;
+  return sol::diff_bwd_bytes(s, &at, &parts);
+}
+
+int sol_diff_attn_fwd(const void* q, const sol_strides* q_strides, const void* k, const sol_strides* k_strides,
+                      const void* v, const sol_strides* v_strides, void* out, const sol_strides* out_strides,
+                      void* out2, float* lse, const float* lambda, const int32_t* q_lens, const int32_t* kv_lens, int B,
+                      int H, int Hv, int Hk, int N, int M, int D, float scale, int causal, void* workspace,
+                      size_t workspace_bytes, sol_stream_t stream) {
+  sol::DiffFwd a = {};
+  a.s = {B, H, Hv, Hk, N, M, scale, causal != 0, q_lens, kv_lens, lambda};
+  SOL_TRY(check_diff(a.s, D));
+  Span in[6], outs[4];
+  SOL_TRY(take_rows("q", q, q_strides, B, 2 * H, N, false, &a.q, &in[0]));
+  SOL_TRY(take_rows("k", k, k_strides, B, Hk, M, false, &a.k, &in[1]));
+  SOL_TRY(take_rows("v", v, v_strides, B, Hv, M, false, &a.v, &in[2]));
+  SOL_TRY(take_rows("out", out, out_strides, B, H, N, true, &a.out, &outs[0]));
+  if (!aligned16(out2)) return fail(SOL_ERR_INVALID_ARG, "out2 must be 16-byte aligned");
+  SOL_TRY(check_small("lse", lse, true));
+  const size_t need = sol::diff_fwd_bytes(a.s);
+  SOL_TRY(check_workspace(workspace, workspace_bytes, need));
+  in[3] = span("lambda", lambda, (uint64_t)H * 4);
+  in[4] = span("q_lens", q_lens, (uint64_t)B * 4);
+  in[5] = span("kv_lens", kv_lens, (uint64_t)B * 4);
+  outs[1] = span("out2", out2, (uint64_t)B * H * N * D * 2);
+  outs[2] = span("lse", lse, (uint64_t)B * 2 * H * N * 4);
+  outs[3] = span("workspace", workspace, need);
+  SOL_TRY(check_apart(in, 6, outs, 4));
+  a.out2 = static_cast<uint16_t*>(out2);
+  a.lse = lse;
+  a.ws = static_cast<float*>(workspace);
+  return done(sol::launch_diff_fwd(a, reinterpret_cast<hipStream_t>(stream)), "diff_attn_fwd");
+}
+
+int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const void* q, const sol_strides* q_strides,
+                      const void* k, const sol_strides* k_strides, const void* v, const sol_strides* v_strides,
+                      const void* out, const sol_strides* out_strides, const void* out2, const float* lse,
+                      const float* lambda, void* dq, const sol_strides* dq_strides, void* dk,
+                      const sol_strides* dk_strides, void* dv, const sol_strides* dv_strides, float* dlambda,
+                      const int32_t* q_lens, const int32_t* kv_lens, int B, int H, int Hv, int Hk, int N, int M, int D,
+                      float scale, int causal, void* workspace, size_t workspace_bytes, sol_stream_t stream) {
+  sol::DiffBwd a = {};
+  a.s = {B, H, Hv, Hk, N, M, scale, causal != 0, q_lens, kv_lens, lambda};
+  SOL_TRY(check_diff(a.s, D));
+  Span in[10], outs[5];
+  SOL_TRY(take_rows("dout", dout, dout_strides, B, H, N, false, &a.dout, &in[0]));
+  SOL_TRY(take_rows("q", q, q_strides, B, 2 * H, N, false, &a.q, &in[1]));
+  SOL_TRY(take_rows("k", k, k_strides, B, Hk, M, false, &a.k, &in[2]));
+  SOL_TRY(take_rows("v", v, v_strides, B, Hv, M, false, &a.v, &in[3]));
+  SOL_TRY(take_rows("out", out, out_strides, B, H, N, false, &a.out, &in[4]));
+  SOL_TRY(take_rows("dq", dq, dq_strides, B, 2 * H, N, true, &a.dq, &outs[0]));
+  SOL_TRY(take_rows("dk", dk, dk_strides, B, Hk, M, true, &a.dk, &outs[1]));
+  SOL_TRY(take_rows("dv", dv, dv_strides, B, Hv, M, true, &a.dv, &outs[2]));
+  if (!out2) return fail(SOL_ERR_INVALID_ARG, "out2 must not be NULL");
+  if (!aligned16(out2)) return fail(SOL_ERR_INVALID_ARG, "out2 must be 16-byte aligned");
+  SOL_TRY(check_small("lse", lse, false));
+  SOL_TRY(check_small("dlambda", dlambda, false));
+  size_t partial_at;
+  const size_t need = sol::diff_bwd_bytes(a.s, &partial_at, &a.parts);
+  SOL_TRY(check_workspace(workspace, workspace_bytes, need));
+  in[5] = span("out2", out2, (uint64_t)B * H * N * D * 2);
+  in[6] = span("lse", lse, (uint64_t)B * 2 * H * N * 4);
+  in[7] = span("lambda", lambda, (uint64_t)H * 4);
+  in[8] = span("q_lens", q_lens, (uint64_t)B * 4);
+  in[9] = span("kv_lens", kv_lens, (uint64_t)B * 4);
+  outs[3] = span("dlambda", dlambda, (uint64_t)H * 4);
+  outs[4] = span("workspace", workspace, need);
+  SOL_TRY(check_apart(in, 10, outs, 5));
+  a.out2 = static_cast<const uint16_t*>(out2);
+  a.lse = lse;
+  a.dlambda = dlambda;
+  a.stats = static_cast<float2*>(workspace);
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + partial_at);
+  return done(sol::launch_diff_bwd(a, reinterpret_cast<hipStream_t>(stream)), "diff_attn_bwd");
 }
 
 }  // extern "C"

@@ -21,19 +21,14 @@
 // before it is decayed), tokens reversed by a negative row stride.
 #include <hip/hip_runtime.h>
 
-#include "sol_device.h"
 #include "sol_ops.h"
+#include "sol_tiles.h"
 
 namespace sol {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kC = kLinRows;
-// LDS row stride of a staged tile, elements: 288 bytes = 8 banks past a whole
-// turn of the 64, so that the 16-byte reads along rows (8 rows at a time) and
-// the transpose reads (4 rows of 32 bytes) both touch every bank once.
-constexpr int kStride = D + 16;
-
 struct ScanArgs {
   const uint16_t *a, *b, *c;
   int64_t a_b, a_h, a_n, b_b, b_h, b_n, c_b, c_h, c_n;
@@ -59,37 +54,7 @@ __device__ __forceinline__ float decay_log2(const float* log_decay, int h) {
   return fmaxf(log_decay[h], -1e30f) * 1.44269504088896341f;
 }
 
-// Eight bf16 of one column of a staged tile, rows {0..3, 8..11} + 4 (lane / 32)
-// from p on: the row order in which an MFMA leaves its 32 x 32 result.
-__device__ __forceinline__ bf16x8 column8(const uint16_t* p) {
-  const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
-  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 8 * kStride));
-  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
-__device__ __forceinline__ f32x16 mfma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-
-// One chunk of rows on its way into LDS: thread t holds 16-byte chunk t % 16 of
-// rows t / 16 + 16 u.  Rows past the sequence are zero.
-struct Stage {
-  uint4 x[kC / 16];
-  __device__ __forceinline__ void load(const uint16_t* p, int64_t sn, int row0, int rows) {
-    const int r = threadIdx.x >> 4, cc = threadIdx.x & 15;
-#pragma unroll
-    for (int u = 0; u < kC / 16; ++u) {
-      const int i = row0 + r + 16 * u;
-      x[u] = make_uint4(0, 0, 0, 0);
-      if (i < rows) x[u] = *reinterpret_cast<const uint4*>(p + (int64_t)i * sn + cc * 8);
-    }
-  }
-  __device__ __forceinline__ void store(uint16_t* lds) const {
-    const int r = threadIdx.x >> 4, cc = threadIdx.x & 15;
-#pragma unroll
-    for (int u = 0; u < kC / 16; ++u) *reinterpret_cast<uint4*>(lds + (r + 16 * u) * kStride + cc * 8) = x[u];
-  }
-};
+using Tile = Stage<kC, kThreads>;
 
 // The wave's 32 columns of the state as four 32 x 32 MFMA results: s[t][r] of
 // lane l is S[32t + 8(r/4) + 4(l/32) + r%4][32 wave + l%32].
@@ -199,20 +164,19 @@ __global__ __launch_bounds__(kThreads, 2) void lin_state_kernel(ScanArgs A) {
   const int id = xcd_local_id(blockIdx.x, gridDim.x);
   const Walk W = make_walk(A, id);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, hh = lane >> 5, l32 = lane & 31;
-  const int g16 = lane >> 4, i16 = lane & 15;
-  const int tr_off = (4 * (g16 >> 1) + (i16 >> 2)) * kStride + 16 * (g16 & 1) + 4 * (i16 & 3);
+  const int tr_off = column_offset(lane);
   State st{};
-  Stage sb, sc;
-  sb.load(W.bb, W.bn, W.row0, W.rows);
-  sc.load(W.c, W.cn, W.row0, W.rows);
+  Tile sb, sc;
+  sb.load(W.bb, W.bn, W.row0, W.rows, threadIdx.x);
+  sc.load(W.c, W.cn, W.row0, W.rows, threadIdx.x);
   for (int row = W.row0; row < W.rows; row += kC) {
     const int m = min(kC, W.rows - row);
-    sb.store(tb);
-    sc.store(tc);
+    sb.store(tb, threadIdx.x);
+    sc.store(tc, threadIdx.x);
     if (row == W.row0 || m < kC) fill_weights(wt, A, W.g2, m);
     __syncthreads();
-    sb.load(W.bb, W.bn, row + kC, W.rows);
-    sc.load(W.c, W.cn, row + kC, W.rows);
+    sb.load(W.bb, W.bn, row + kC, W.rows, threadIdx.x);
+    sc.load(W.c, W.cn, row + kC, W.rows, threadIdx.x);
     bf16x8 cf[4];
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) cf[ks] = column8(tc + 16 * ks * kStride + 32 * wave + tr_off);
@@ -275,8 +239,7 @@ __global__ __launch_bounds__(kThreads, 2) void lin_scan_kernel(ScanArgs A) {
   const Walk W = make_walk(A, id);
   const int slab = W.b * A.H + W.h;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, hh = lane >> 5, l32 = lane & 31;
-  const int g16 = lane >> 4, i16 = lane & 15;
-  const int tr_off = (4 * (g16 >> 1) + (i16 >> 2)) * kStride + 16 * (g16 & 1) + 4 * (i16 & 3);
+  const int tr_off = column_offset(lane);
   const int col = 32 * wave + l32;
 
   if (A.zero_tail) {  // rows of this segment behind the sequence
@@ -311,27 +274,25 @@ __global__ __launch_bounds__(kThreads, 2) void lin_scan_kernel(ScanArgs A) {
   const float win[2] = {A.r * __builtin_amdgcn_exp2f(W.g2 * (float)(l32 + A.off)),
                         A.r * __builtin_amdgcn_exp2f(W.g2 * (float)(32 + l32 + A.off))};
 
-  Stage sa, sb, sc;
-  sa.load(W.a, W.an, W.row0, W.rows);
-  sb.load(W.bb, W.bn, W.row0, W.rows);
-  sc.load(W.c, W.cn, W.row0, W.rows);
+  Tile sa, sb, sc;
+  sa.load(W.a, W.an, W.row0, W.rows, threadIdx.x);
+  sb.load(W.bb, W.bn, W.row0, W.rows, threadIdx.x);
+  sc.load(W.c, W.cn, W.row0, W.rows, threadIdx.x);
   for (int row = W.row0; row < W.rows; row += kC) {
     const int m = min(kC, W.rows - row);
-    sa.store(ta);
-    sb.store(tb);
-    sc.store(tc);
+    sa.store(ta, threadIdx.x);
+    sb.store(tb, threadIdx.x);
+    sc.store(tc, threadIdx.x);
     if (row == W.row0 || m < kC) fill_weights(wt, A, W.g2, m);
     __syncthreads();
-    sa.load(W.a, W.an, row + kC, W.rows);
-    sb.load(W.bb, W.bn, row + kC, W.rows);
-    sc.load(W.c, W.cn, row + kC, W.rows);
+    sa.load(W.a, W.an, row + kC, W.rows, threadIdx.x);
+    sb.load(W.bb, W.bn, row + kC, W.rows, threadIdx.x);
+    sc.load(W.c, W.cn, row + kC, W.rows, threadIdx.x);
     if (wave < 3) {
       f32x16 s = {};
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) {
-        const bf16x8 bf = *reinterpret_cast<const bf16x8*>(tb + (32 * J + l32) * kStride + 16 * kk + 8 * hh);
-        const bf16x8 af = *reinterpret_cast<const bf16x8*>(ta + (32 * I + l32) * kStride + 16 * kk + 8 * hh);
-        s = mfma(bf, af, s);
+        s = mfma(row8(tb + 32 * J * kStride, lane, kk), row8(ta + 32 * I * kStride, lane, kk), s);
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
@@ -347,10 +308,7 @@ __global__ __launch_bounds__(kThreads, 2) void lin_scan_kernel(ScanArgs A) {
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        float f[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = st.s[t][8 * x + i];
-        const bf16x8 sf = __builtin_bit_cast(bf16x8, pack_bf16x8(f));
+        const bf16x8 sf = operand8(st.s[t], x);
 #pragma unroll
         for (int i2 = 0; i2 < 2; ++i2) {
           const uint16_t* p = ta + (32 * i2 + l32) * kStride + 32 * t + 16 * x + 4 * hh;

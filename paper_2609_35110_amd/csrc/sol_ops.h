@@ -73,4 +73,53 @@ struct LinStep {
 };
 hipError_t launch_lin_step(const LinStep& a, hipStream_t stream);
 
+// ------------------------------------------------------ differential attention
+
+constexpr int kDiffRows = 128;  // query rows of a workgroup
+constexpr int kDiffKeys = 64;   // keys of a tile
+constexpr int kFewRows = 32;    // (head of a group, token) rows of the few-row kernel
+
+// What both directions share.  Hk is Hv (both maps read one key head) or 2 Hv.
+struct DiffShape {
+  int B, H, Hv, Hk, N, M;
+  float scale;
+  int causal;
+  const int32_t* q_lens;   // may be null
+  const int32_t* kv_lens;  // may be null
+  const float* lambda;
+};
+
+// How a forward call runs: with so few rows that a group's fit one wave (few),
+// and over how many pieces of the keys (their results joined by a second
+// launch through the workspace).
+struct DiffPlan {
+  bool few;
+  int nsplit;
+};
+DiffPlan diff_plan(const DiffShape& s);
+size_t diff_fwd_bytes(const DiffShape& s);
+
+struct DiffFwd {
+  DiffShape s;
+  Rows q, k, v, out;
+  uint16_t* out2;  // second map's own output, [B][H][N][128], may be null
+  float* lse;      // [B][2H][N], may be null
+  float* ws;
+};
+hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream);
+
+struct DiffBwd {
+  DiffShape s;
+  Rows q, k, v, out, dout, dq, dk, dv;
+  const uint16_t* out2;
+  const float* lse;
+  float* dlambda;
+  float2* stats;   // [B][2H][N]
+  float* partial;  // [H][B][parts]
+  int parts;
+};
+// Workspace: the rows' stats, then dlambda's parts.
+size_t diff_bwd_bytes(const DiffShape& s, size_t* partial_at, int* parts);
+hipError_t launch_diff_bwd(const DiffBwd& a, hipStream_t stream);
+
 }  // namespace sol

@@ -716,6 +716,10 @@ _SIGNATURES = {
     "sol_lin_attn_fwd": ([_P] * 12 + [_I32] * 5 + [_F32, _P, _SZ, _P], _I32),
     "sol_lin_attn_bwd": ([_P] * 19 + [_I32] * 5 + [_F32, _P, _SZ, _P], _I32),
     "sol_lin_attn_step": ([_P] * 11 + [_I32] * 5 + [_F32, _P], _I32),
+    "sol_diff_attn_fwd_workspace_bytes": ([_I32] * 6, _SZ),
+    "sol_diff_attn_bwd_workspace_bytes": ([_I32] * 6, _SZ),
+    "sol_diff_attn_fwd": ([_P] * 13 + [_I32] * 7 + [_F32, _I32, _P, _SZ, _P], _I32),
+    "sol_diff_attn_bwd": ([_P] * 22 + [_I32] * 7 + [_F32, _I32, _P, _SZ, _P], _I32),
 }
 
 
@@ -744,6 +748,22 @@ def sol_lin_attn_bwd(*args):
 
 def sol_lin_attn_step(*args):
     return _entry("sol_lin_attn_step")(*args)
+
+
+def sol_diff_attn_fwd_workspace_bytes(B, H, Hv, N, M, D):
+    return _entry("sol_diff_attn_fwd_workspace_bytes")(B, H, Hv, N, M, D)
+
+
+def sol_diff_attn_bwd_workspace_bytes(B, H, Hv, N, M, D):
+    return _entry("sol_diff_attn_bwd_workspace_bytes")(B, H, Hv, N, M, D)
+
+
+def sol_diff_attn_fwd(*args):
+    return _entry("sol_diff_attn_fwd")(*args)
+
+
+def sol_diff_attn_bwd(*args):
+    return _entry("sol_diff_attn_bwd")(*args)
 
 
 def strides(b, h, n):
@@ -903,6 +923,81 @@ def lin_attn_step(q, k, v, log_decay, state, slots=None, scale=None, out=None):
           _device_array("state", state, dev, torch.float32, (n_slots, H, D, D)),
           _device_array("slots", slots, dev, torch.int32, (R,)), R, H, Hk, n_slots, D, _scale(scale))
     return out
+
+
+def _diff_shape(q, k, v):
+    B, H2, N, D = _dims("q", q, 4)
+    if H2 % 2:
+        raise ValueError("q must have two heads (maps) for each output head, got %d" % H2)
+    _, Hk, M, _ = _dims("k", k, 4)
+    return B, H2 // 2, _dims("v", v, 4)[1], Hk, N, M, D
+
+
+def diff_attn_fwd(q, k, v, lam, scale=None, causal=False, q_lens=None, kv_lens=None, out=None, training=False,
+                  workspace=None):
+    """Differential attention: out[:, h] = softmax(scale q[:, 2h] k^T) v -
+    lam[h] softmax(scale q[:, 2h + 1] k'^T) v (scale None: 1/sqrt(D)).
+
+    q [B, 2H, N, D], v [B, Hv, M, D], k [B, 2 Hv, M, D] (keys of its own for
+    each map) or [B, Hv, M, D] (both maps on one key head), bf16 (any strides
+    that keep rows contiguous and 16-byte aligned); lam float32 [H]; q_lens,
+    kv_lens int32 [B] on the device (None: all); causal: row i sees keys up to
+    i + kv_len - q_len.  Rows of out behind a sequence are not written.
+    Returns out, or with training (out, out2, lse), which diff_attn_bwd takes:
+    the second map's own output and the rows' log sums, float32 [B, 2H, N]."""
+    B, H, Hv, Hk, N, M, D = _diff_shape(q, k, v)
+    dev = q.device
+    qp, qs = _rows("q", q)
+    kp, ks = _rows("k", k, dev, (B, Hk, M, D))
+    vp, vs = _rows("v", v, dev, (B, Hv, M, D))
+    if out is None:
+        out = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+    op, os_ = _rows("out", out, dev, (B, H, N, D))
+    out2 = lse = None
+    if training:
+        out2 = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+        lse = torch.empty((B, 2 * H, N), dtype=torch.float32, device=dev)
+    if lam is None:
+        raise ValueError("lam must be given")
+    ws, wp, wn = _scratch(workspace, sol_diff_attn_fwd_workspace_bytes(B, H, Hv, N, M, D), dev)
+    _call(sol_diff_attn_fwd, dev, qp, qs, kp, ks, vp, vs, op, os_, out2.data_ptr() if training else None,
+          lse.data_ptr() if training else None, _device_array("lam", lam, dev, torch.float32, (H,)),
+          _device_array("q_lens", q_lens, dev, torch.int32, (B,)),
+          _device_array("kv_lens", kv_lens, dev, torch.int32, (B,)), B, H, Hv, Hk, N, M, D, _scale(scale),
+          1 if causal else 0, wp, wn)
+    return (out, out2, lse) if training else out
+
+
+def diff_attn_bwd(dout, q, k, v, lam, out, out2, lse, scale=None, causal=False, q_lens=None, kv_lens=None,
+                  dq=None, dk=None, dv=None, workspace=None):
+    """The gradients of diff_attn_fwd from dout and the out, out2 and lse of
+    its call with training: (dq, dk, dv, dlam), the first three bf16 and zero
+    behind a sequence, dlam float32 [H]."""
+    B, H, Hv, Hk, N, M, D = _diff_shape(q, k, v)
+    dev = q.device
+    qp, qs = _rows("q", q)
+    kp, ks = _rows("k", k, dev, (B, Hk, M, D))
+    vp, vs = _rows("v", v, dev, (B, Hv, M, D))
+    gp, gs = _rows("dout", dout, dev, (B, H, N, D))
+    op, os_ = _rows("out", out, dev, (B, H, N, D))
+    grads = []
+    for name, t, h, n in (("dq", dq, 2 * H, N), ("dk", dk, Hk, M), ("dv", dv, Hv, M)):
+        if t is None:
+            t = torch.empty((B, h, n, D), dtype=torch.bfloat16, device=dev)
+        grads.append((t,) + _rows(name, t, dev, (B, h, n, D)))
+    dlam = torch.empty(H, dtype=torch.float32, device=dev)
+    if lam is None or out2 is None or lse is None:
+        raise ValueError("lam, out2 and lse must be given")
+    ws, wp, wn = _scratch(workspace, sol_diff_attn_bwd_workspace_bytes(B, H, Hv, N, M, D), dev)
+    (dq, dqp, dqs), (dk, dkp, dks), (dv, dvp, dvs) = grads
+    _call(sol_diff_attn_bwd, dev, gp, gs, qp, qs, kp, ks, vp, vs, op, os_,
+          _device_array("out2", out2, dev, torch.bfloat16, (B, H, N, D)),
+          _device_array("lse", lse, dev, torch.float32, (B, 2 * H, N)),
+          _device_array("lam", lam, dev, torch.float32, (H,)), dqp, dqs, dkp, dks, dvp, dvs, dlam.data_ptr(),
+          _device_array("q_lens", q_lens, dev, torch.int32, (B,)),
+          _device_array("kv_lens", kv_lens, dev, torch.int32, (B,)), B, H, Hv, Hk, N, M, D, _scale(scale),
+          1 if causal else 0, wp, wn)
+    return dq, dk, dv, dlam
 
 
 # ------------------------------------------------------------ measurement aid

@@ -144,3 +144,88 @@ def test_lin_workspaces():
     one = sol.sol_lin_attn_bwd_workspace_bytes(1, 4, 4, 100, 128)
     assert sol.sol_lin_attn_bwd_workspace_bytes(1, 4, 2, 100, 128) == one + 2 * 4 * 100 * 128 * 4
     assert sol.sol_lin_attn_bwd_workspace_bytes(1, 4, 3, 100, 128) == 0
+
+
+DIFF = dict(B=2, H=4, Hv=2, Hk=4, N=100, M=120, D=128, scale=1.0, causal=1, q_lens=None, kv_lens=None, lam=at(6))
+DIFF_COMMON = [
+    (dict(B=0), -1, ">= 1"),
+    (dict(M=0), -1, ">= 1"),
+    (dict(Hv=3, Hk=3), -1, "multiple"),
+    (dict(Hk=1), -1, "Hk must be"),
+    (dict(Hk=8), -1, "Hk must be"),
+    (dict(D=256), -2, "head dim"),
+    (dict(N=(1 << 23) + 1), -2, "exceeds"),
+    (dict(M=(1 << 23) + 1), -2, "exceeds"),
+    (dict(B=1 << 12, H=1 << 12, Hv=1, Hk=1), -2, "too large"),
+    (dict(B=1 << 10, N=1 << 20), -2, "too large"),
+    (dict(scale=0.0), -1, "scale"),
+    (dict(scale=-1.0), -1, "scale"),
+    (dict(scale=float("nan")), -1, "scale"),
+    (dict(lam=None), -1, "lambda must not be NULL"),
+    (dict(q_lens=at(7) + 1), -1, "q_lens must be 4-byte"),
+    (dict(kv_lens=at(7) + 2), -1, "kv_lens must be 4-byte"),
+    (dict(q=at(1) + 2), -1, "q must be 16-byte"),
+    (dict(v=None), -1, "v must not be NULL"),
+    (dict(k_st=S(0, 0, 4)), -1, "k strides"),
+]
+
+
+def diff_fwd(**kw):
+    a = dict(DIFF, q=at(1), k=at(2), k_st=None, v=at(3), out=at(4), out_st=None, out2=at(5), lse=at(8), ws=None, ws_bytes=0)
+    a.update(kw)
+    return sol.sol_diff_attn_fwd(a["q"], None, a["k"], a["k_st"], a["v"], None, a["out"], a["out_st"], a["out2"], a["lse"],
+                                 a["lam"], a["q_lens"], a["kv_lens"], a["B"], a["H"], a["Hv"], a["Hk"], a["N"], a["M"],
+                                 a["D"], a["scale"], a["causal"], a["ws"], a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("kw,status,fragment", DIFF_COMMON + [
+    (dict(out=None), -1, "out must not be NULL"),
+    (dict(out=at(3)), -1, "out overlaps v"),
+    (dict(out2=at(5) + 8), -1, "out2 must be 16-byte"),
+    (dict(out2=at(4)), -1, "out2 overlaps out"),
+    (dict(lse=at(8) + 2), -1, "lse must be 4-byte"),
+    (dict(lse=at(6)), -1, "lse overlaps lambda"),
+    (dict(out_st=S(0, 100 * 128, 128)), -1, "rows of out overlap"),
+    (dict(N=1, M=100000), -1, "workspace is NULL"),
+    (dict(N=1, M=100000, ws=at(9) + 8, ws_bytes=1 << 30), -1, "workspace must be 16-byte"),
+    (dict(N=1, M=100000, ws=at(9), ws_bytes=64), -1, "workspace needs"),
+    (dict(N=1, M=100000, ws=at(3), ws_bytes=1 << 30), -1, "workspace overlaps"),
+])
+def test_diff_fwd_refusals(kw, status, fragment):
+    refused(status, fragment, diff_fwd(**kw))
+
+
+def diff_bwd(**kw):
+    a = dict(DIFF, dout=at(10), q=at(1), k=at(2), k_st=None, v=at(3), out=at(4), out2=at(5), lse=at(8), dq=at(11),
+             dk=at(12), dv=at(13), dlam=at(14), ws=at(15), ws_bytes=1 << 25)
+    a.update(kw)
+    return sol.sol_diff_attn_bwd(a["dout"], None, a["q"], None, a["k"], a["k_st"], a["v"], None, a["out"], None, a["out2"],
+                                 a["lse"], a["lam"], a["dq"], None, a["dk"], None, a["dv"], None, a["dlam"], a["q_lens"],
+                                 a["kv_lens"], a["B"], a["H"], a["Hv"], a["Hk"], a["N"], a["M"], a["D"], a["scale"],
+                                 a["causal"], a["ws"], a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("kw,status,fragment", DIFF_COMMON + [
+    (dict(out=None), -1, "out must not be NULL"),
+    (dict(out2=None), -1, "out2 must not be NULL"),
+    (dict(lse=None), -1, "lse must not be NULL"),
+    (dict(dlam=None), -1, "dlambda must not be NULL"),
+    (dict(dq=at(1)), -1, "dq overlaps q"),
+    (dict(dk=at(11)), -1, "dk overlaps dq"),
+    (dict(dv=at(8)), -1, "dv overlaps lse"),
+    (dict(dlam=at(6)), -1, "dlambda overlaps lambda"),
+    (dict(ws=None), -1, "workspace is NULL"),
+    (dict(ws_bytes=1000), -1, "workspace needs"),
+    (dict(ws=at(13)), -1, "workspace overlaps dv"),
+])
+def test_diff_bwd_refusals(kw, status, fragment):
+    refused(status, fragment, diff_bwd(**kw))
+
+
+def test_diff_workspaces():
+    assert sol.sol_diff_attn_fwd_workspace_bytes(1, 40, 40, 4096, 4096, 128) == 0
+    assert sol.sol_diff_attn_fwd_workspace_bytes(1, 1, 1, 1, 100000, 128) > 0
+    assert sol.sol_diff_attn_bwd_workspace_bytes(1, 2, 1, 100, 120, 128) >= 2 * 2 * 100 * 8
+    for bad in ((0, 1, 1, 1, 1, 128), (1, 3, 2, 1, 1, 128), (1, 1, 1, 1, 1, 64), (1, 1, 1, 1, (1 << 23) + 1, 128)):
+        assert sol.sol_diff_attn_fwd_workspace_bytes(*bad) == 0
+        assert sol.sol_diff_attn_bwd_workspace_bytes(*bad) == 0
