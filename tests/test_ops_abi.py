@@ -186,10 +186,10 @@ def diff_fwd(**kw):
     (dict(lse=at(8) + 2), -1, "lse must be 4-byte"),
     (dict(lse=at(6)), -1, "lse overlaps lambda"),
     (dict(out_st=S(0, 100 * 128, 128)), -1, "rows of out overlap"),
-    (dict(N=1, M=100000), -1, "workspace is NULL"),
-    (dict(N=1, M=100000, ws=at(9) + 8, ws_bytes=1 << 30), -1, "workspace must be 16-byte"),
-    (dict(N=1, M=100000, ws=at(9), ws_bytes=64), -1, "workspace needs"),
-    (dict(N=1, M=100000, ws=at(3), ws_bytes=1 << 30), -1, "workspace overlaps"),
+    (dict(N=1, M=30000), -1, "workspace is NULL"),
+    (dict(N=1, M=30000, ws=at(9) + 8, ws_bytes=1 << 30), -1, "workspace must be 16-byte"),
+    (dict(N=1, M=30000, ws=at(9), ws_bytes=64), -1, "workspace needs"),
+    (dict(N=1, M=30000, ws=at(3), ws_bytes=1 << 30), -1, "workspace overlaps"),
 ])
 def test_diff_fwd_refusals(kw, status, fragment):
     refused(status, fragment, diff_fwd(**kw))
