@@ -487,9 +487,9 @@ int sol_attn_fwd_records(const void* rec, const void* k_prep, const void* v_prep
  * Hk (query head h reads key and value head h / (H / Hk)).  Each has its
  * strides: row (b, h, n) starts at element b*b + h*h + n*n of its pointer, its
  * D values contiguous; a NULL strides pointer means contiguous
- * [B][heads][N][D].  Strides are multiples of 8 elements, at least 0 for
- * inputs (0 broadcasts) and such that rows do not meet for outputs; pointers
- * are 16-byte aligned.  An output may not overlap the span of an input or of
+ * [B][heads][N][D].  Strides are multiples of 8 elements (n: at most 2^24), at
+ * least 0 for inputs (0 broadcasts) and such that rows do not meet for
+ * outputs; pointers are 16-byte aligned.  An output may not overlap the span of an input or of
  * another output.  log_decay: H floats, <= 0 (-inf: a head without memory).
  * States: float [B][H][D][D], row = the dim of k, column = the dim of v.  lens:
  * B int32 on the device, or NULL (all N): sequence b has its first lens[b]

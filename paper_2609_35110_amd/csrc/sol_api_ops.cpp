@@ -37,6 +37,8 @@ bool meet(const Span& x, const Span& y) { return x.bytes && y.bytes && x.at < y.
 Span span(const char* name, const void* p, uint64_t bytes) { return {name, reinterpret_cast<uintptr_t>(p), p ? bytes : 0}; }
 
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
+// Elements between tokens: the kernels' copies address the rows of a tile by 32-bit byte offsets.
+constexpr int64_t kMaxRowStride = (int64_t)1 << 24;
 
 // The rows of one tensor: its strides (contiguous when null) checked, its span
 // found.  An output's rows must not meet: from the finest dimension up, each
@@ -54,6 +56,8 @@ int take_rows(const char* name, const void* p, const sol_strides* st, int B, int
     if (s[i] < 0 || s[i] % 8 || s[i] > kMaxStride)
       return fail(SOL_ERR_INVALID_ARG, "%s strides must be non-negative multiples of 8 elements (got %lld, %lld, %lld)",
                   name, (long long)s[0], (long long)s[1], (long long)s[2]);
+    if (i == 2 && s[i] > kMaxRowStride)
+      return fail(SOL_ERR_UNSUPPORTED, "%s: %lld elements between tokens (at most 2^24)", name, (long long)s[i]);
     last += (uint64_t)(n[i] - 1) * (uint64_t)s[i];
   }
   if (out) {
@@ -384,7 +388,7 @@ int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const v
   a.out2 = static_cast<const uint16_t*>(out2);
   a.lse = lse;
   a.dlambda = dlambda;
-  a.stats = static_cast<float2*>(workspace);
+  a.stats = static_cast<float*>(workspace);
   a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + partial_at);
   return done(sol::launch_diff_bwd(a, reinterpret_cast<hipStream_t>(stream)), "diff_attn_bwd");
 }

@@ -139,20 +139,45 @@ __device__ __forceinline__ Parts parts_of(float* ws, const DiffShape& s, int nsp
 
 // ------------------------------------------------------------------- forward
 
-// 128 rows of one head: waves 0..3 take 32 rows each of map 0, waves 4..7 the
-// same rows of map 1, so that the two waves of a SIMD run one's exponentials
-// under the other's MFMAs.  K and V tiles of 64 keys pass through LDS, two
-// buffers, one barrier a tile.
+// These kernels are one wave a SIMD, whose MFMAs, exponentials and LDS reads
+// have to overlap inside the wave: a turn of the loop is a list of slots, each
+// an MFMA, the LDS read of a fragment some slots on and a share of the
+// arithmetic on scores that are done, and nothing moves between slots.  Tiles
+// come through LDS in a ring of four, copied two turns ahead.
+constexpr int kRing = 4;
+
+// A value that all lanes hold, read to the end here: left in flight into a
+// loop, a load would have the loop wait for all its copies.
+__device__ __forceinline__ float uniform(float x) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+// Keeps a value where it is computed: the compiler moves what is used once to
+// where it is used.
+__device__ __forceinline__ void pin(float& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
+// 128 rows of one head, 32 a wave, both maps in the wave (a fragment of V, and
+// of a shared K, is read once for two MFMAs).  Turn t: the products P V of tile
+// t - 1, under them map 0's exponentials of tile t; then the scores of tile
+// t + 1, under them map 1's.
+//
+// A row is held to the maximum of its first tile: P and the sums have 8 exponent
+// bits, so scores far above it cost no precision, and most rows' stay within a
+// few binades.  A row whose P add up to more than 2^80 (55 above it in the
+// exponent) has its workgroup walk the keys again, held to the rows' own maxima,
+// found by a walk for scores alone.
+constexpr int kFwdKeys = 32;
+constexpr float kTooMuch = 1.2089258e24f;
 template <bool kShared>
-__global__ __launch_bounds__(512, 2) void diff_fwd_kernel(DiffFwd A, int nsplit) {
-  constexpr int kTileElems = kDiffKeys * kStride;
-  constexpr int kKTiles = kShared ? 1 : 2;
-  __shared__ __attribute__((aligned(16))) uint16_t lds[2][(kKTiles + 1) * kTileElems];
+__global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, int nsplit) {
+  constexpr int kTiles = kShared ? 2 : 3;  // K (of each map), V
+  constexpr int kV = kTiles - 1;
+  constexpr int kKFrags = kShared ? 8 : 16, kFrags = 8 + kKFrags, kAhead = 6, kHold = 8;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing][kTiles][kTile32];
   lds_poison(lds, sizeof(lds));
   lds_poison_done();
   const DiffShape& s = A.s;
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63, hh = lane >> 5, l32 = lane & 31;
-  const int map = wave >> 2, group = wave & 3;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
   const int tiles = (s.N + kDiffRows - 1) / kDiffRows;
   int id = xcd_local_id(blockIdx.x, gridDim.x);
   const int split = id % nsplit;
@@ -164,128 +189,254 @@ __global__ __launch_bounds__(512, 2) void diff_fwd_kernel(DiffFwd A, int nsplit)
   const int row0 = tile * kDiffRows;
   if (row0 >= sq.qlen) return;
   const int per = s.H / s.Hv, hv = h / per;
-  const int row = row0 + 32 * group + l32;
+  const int row = row0 + 32 * wave + l32;
   const bool valid = row < sq.qlen;
   const float c = s.scale * kLog2e;
 
   const uint16_t* k0 = A.k.p + b * A.k.sb + (kShared ? hv : 2 * hv) * A.k.sh;
-  const uint16_t* k1 = k0 + (kShared ? 0 : A.k.sh);
-  const uint16_t* v = A.v.p + b * A.v.sb + hv * A.v.sh;
-  bf16x8 qf[8];
-  load_row(qf, A.q.p + b * A.q.sb + (2 * h + map) * A.q.sh + (int64_t)row * A.q.sn, valid, hh);
+  const uint16_t* v0 = A.v.p + b * A.v.sb + hv * A.v.sh;
+  bf16x8 qf[2][8];
+  load_row(qf[0], A.q.p + b * A.q.sb + 2 * h * A.q.sh + (int64_t)row * A.q.sn, valid, hh);
+  load_row(qf[1], A.q.p + b * A.q.sb + (2 * h + 1) * A.q.sh + (int64_t)row * A.q.sn, valid, hh);
 
   const int2 range = split_keys(sq.klen, split, nsplit, kDiffKeys);
   const int last = min(row + sq.shift, sq.klen - 1);  // of this lane's row
   const int last_row = min(row0 + kDiffRows, sq.qlen) - 1;
   const int kend = min(range.y, min(last_row + sq.shift, sq.klen - 1) + 1);
-  // what every row of the wave sees, and what none does
-  const int wave_row = row0 + 32 * group;
-  const int all_to = min(wave_row + sq.shift, sq.klen - 1);
-  const int none_from = wave_row < sq.qlen ? min(wave_row + 31 + sq.shift, sq.klen - 1) : -1;
+  const int turns = kend > range.x ? (kend - range.x + kFwdKeys - 1) / kFwdKeys : 0;
+  const int all_to = min(row0 + 32 * wave + sq.shift, sq.klen - 1);  // every row of the wave sees these
 
-  MapRows x;
-  clear(x);
-  const int tr = column_offset(lane);
-  Stage<kDiffKeys, 512> sk0, sk1, sv;
-  auto load = [&](int key) __attribute__((always_inline)) {
-    sk0.load(k0, A.k.sn, key, kend, t);
-    if (!kShared) sk1.load(k1, A.k.sn, key, kend, t);
-    sv.load(v, A.v.sn, key, kend, t);
+  const uint32_t at0 = lds_address(&lds[0][0][0]) + wave * kRowBlock;
+  const int copy_row = 8 * wave + (lane >> 3);
+  // Tile after tile into place `place` of the ring, one kilobyte at a time; past
+  // the last tile it comes again, and is not used.
+  constexpr int kCopies = 2 * kTiles;
+  struct Copy {
+    const uint16_t *k, *v;
+    int key;
+    uint32_t to, ok, ov;
+  } cp_ = {};
+  auto copy_start = [&](int i, int place) __attribute__((always_inline)) {
+    if (i == 0) {
+      cp_.key = range.x;
+      cp_.k = k0 + (int64_t)range.x * A.k.sn;
+      cp_.v = v0 + (int64_t)range.x * A.v.sn;
+      cp_.ok = copy_offset(copy_row, A.k.sn, lane);
+      cp_.ov = copy_offset(copy_row, A.v.sn, lane);
+    }
+    const bool on = i > 0 && i < turns;
+    cp_.k += on ? kFwdKeys * A.k.sn : 0;
+    cp_.v += on ? kFwdKeys * A.v.sn : 0;
+    cp_.key += on ? kFwdKeys : 0;
+    cp_.to = __builtin_amdgcn_readfirstlane(at0 + (place % kRing) * (kTiles * kTile32));
+    if (cp_.key + kFwdKeys > sq.klen) {  // keys past the sequence: its last key again (their scores are masked)
+      const int r = min(copy_row, sq.klen - 1 - cp_.key);
+      cp_.ok = copy_offset(r, A.k.sn, lane);
+      cp_.ov = copy_offset(r, A.v.sn, lane);
+    }
   };
-  auto store = [&](int buf) __attribute__((always_inline)) {
-    sk0.store(lds[buf], t);
-    if (!kShared) sk1.store(lds[buf] + kTileElems, t);
-    sv.store(lds[buf] + kKTiles * kTileElems, t);
+  auto copy_part = [&](int n) __attribute__((always_inline)) {
+    const uint16_t* p = n / 2 == kV ? cp_.v : n / 2 == 0 ? cp_.k : cp_.k + A.k.sh;
+    copy_1k(cp_.to + n / 2 * kTile32 + n % 2 * 1024, p, (n / 2 == kV ? cp_.ov : cp_.ok) + n % 2 * 128);
   };
-  if (range.x < kend) {
-    load(range.x);
-    store(0);
-  }
-  int buf = 0;
-  for (int key = range.x; key < kend; key += kDiffKeys, buf ^= 1) {
-    __syncthreads();
-    const bool more = key + kDiffKeys < kend;
-    if (more) load(key + kDiffKeys);
-    if (key <= none_from) {
-      const uint16_t* tk = lds[buf] + (kShared ? 0 : map * kTileElems);
-      const uint16_t* tv = lds[buf] + kKTiles * kTileElems + tr;
-      f32x16 sc[2] = {scores(tk, qf, lane), scores(tk + 32 * kStride, qf, lane)};
-      if (key + kDiffKeys - 1 > all_to) {
-        mask(sc[0], key + 4 * hh, last);
-        mask(sc[1], key + 32 + 4 * hh, last);
+  auto copy = [&](int i, int place) __attribute__((always_inline)) {
+    copy_start(i, place);
+#pragma unroll
+    for (int n = 0; n < kCopies; ++n) copy_part(n);
+  };
+
+  struct Tile {
+    f32x16 s[2];         // scores
+    uint32_t pw[2][8];   // P, packed
+  } ta, tb;
+  MapRows x[2];
+  clear(x[0]);
+  clear(x[1]);
+  float mc[2];
+  bf16x8 ring[kHold];
+  const RowPlace rp = row_place(lane);
+  const int cp = col_place(lane);
+  // the fragments of a turn in order: V of tile t - 1, then K of tile t + 1
+  auto fragment = [&](int f, const uint8_t* then, const uint8_t* next) __attribute__((always_inline)) {
+    if (f < 8) return col_frag(then + kV * kTile32 + cp, f >> 2, f & 3);
+    const int j = f - 8;
+    return row_frag(next + (kShared ? 0 : (j & 1) * kTile32), rp, kShared ? j : j >> 1);
+  };
+  auto mask_tile = [&](Tile& now, int i) __attribute__((always_inline)) {
+    const int key = range.x + i * kFwdKeys;
+    if (key + kFwdKeys - 1 > all_to || i >= turns) {
+      const int to = i < turns ? last : -1;  // (past the last tile: none)
+      settle(now.s[0], now.s[1]);
+      mask(now.s[0], key + 4 * hh, to);
+      mask(now.s[1], key + 4 * hh, to);
+    }
+  };
+  // one exponential; its pair is summed and packed with the next one's (an
+  // exponential's result is not there at once)
+  float e[2];
+  auto take = [&](Tile& now, int m, int r) __attribute__((always_inline)) {  // rows r, r + 1
+    x[m].l += e[0];
+    now.pw[m][r >> 1] = pack_bf16x2(e[0], e[1]);
+    x[m].l += e[1];
+    pin(now.pw[m][r >> 1]);
+    pin(x[m].l);
+  };
+  auto exponential = [&](Tile& now, int m, int r) __attribute__((always_inline)) {
+    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(now.s[m][r], c, -mc[m]));
+    if (r % 2 == 0 && r > 0) take(now, m, r - 2);
+    if (r == 0 && m == 1) take(now, 0, 14);
+    e[r & 1] = p;
+    pin(e[r & 1]);
+  };
+  auto operand = [&](const Tile& z, int m, int y) __attribute__((always_inline)) {
+    return __builtin_bit_cast(bf16x8, make_uint4(z.pw[m][4 * y], z.pw[m][4 * y + 1], z.pw[m][4 * y + 2], z.pw[m][4 * y + 3]));
+  };
+  // old: tile i - 1's P, and room for tile i + 1's scores
+  auto turn = [&](int i, Tile& now, Tile& old) __attribute__((always_inline)) {
+    const uint8_t* to = &lds[(i + kRing - 1) % kRing][0][0];
+    const uint8_t* tn = &lds[i % kRing][0][0];
+    const uint8_t* next = &lds[(i + 1) % kRing][0][0];
+    mask_tile(now, i);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) asm volatile("" : "+a"(x[0].o[d]), "+a"(x[1].o[d]));
+    hold_in_agprs(qf[0]);
+    hold_in_agprs(qf[1]);
+    each<0, 32>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int j = slot.value;
+      if constexpr (j == 2) {
+        copies_landed<0>();
+        copy_start(i + 2, i + 2);
+        slot_end();
       }
-      raise_max(x, sc, c);
+      if constexpr (j >= 3 && j < 3 + kCopies) copy_part(j - 3);
+      constexpr bool kFirstUse = j < 16 ? j % 2 == 0 : !kShared || j % 2 == 0;
+      constexpr int f = j < 16 ? j / 2 : 8 + (kShared ? (j - 16) / 2 : j - 16);
+      if constexpr (j < 16) {
+        constexpr int m = j & 1, d = (j >> 1) & 3, y = j >> 3;
+        x[m].o[d] = mfma(ring[f % kHold], operand(old, m, y), x[m].o[d]);
+      } else {
+        constexpr int m = j & 1, kk = (j - 16) >> 1;
+        if constexpr (kk == 0) score_first_a(old.s[m], ring[f % kHold], qf[m][kk]);
+        else score_a(old.s[m], ring[f % kHold], qf[m][kk]);
+      }
+      if constexpr (kFirstUse) {
+        constexpr int g = f + kAhead;
+        ring[g % kHold] = g < kFrags ? fragment(g, to, next) : fragment(g - kFrags, tn, nullptr);
+      }
+      if constexpr (j >= 2 && j < 16) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        exponentials(x, sc[u], c);
+        for (int e = (j - 2) * 8 / 7; e < (j - 1) * 8 / 7; ++e) exponential(now, 0, e);
+      }
+      if constexpr (j >= 16) exponential(now, 1, j - 16);
+      slot_end();
+    });
+    take(now, 1, 14);
+  };
+  // scores of tile i, which is in the ring's place 0, all at once
+  auto scores_of = [&](Tile& z, int i) __attribute__((always_inline)) {
+    const uint8_t* tk = &lds[0][0][0];
+    hold_in_agprs(qf[0]);
+    hold_in_agprs(qf[1]);
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const bf16x8 pf = operand8(sc[u], y);
-#pragma unroll
-          for (int d = 0; d < 4; ++d)
-            x.o[d] = mfma(column8(tv + (32 * u + 16 * y) * kStride + 32 * d), pf, x.o[d]);
-        }
+    for (int kk = 0; kk < 8; ++kk) {
+      const bf16x8 f0 = row_frag(tk, rp, kk), f1 = kShared ? f0 : row_frag(tk + kTile32, rp, kk);
+      if (kk == 0) {
+        score_first_a(z.s[0], f0, qf[0][kk]);
+        score_first_a(z.s[1], f1, qf[1][kk]);
+      } else {
+        score_a(z.s[0], f0, qf[0][kk]);
+        score_a(z.s[1], f1, qf[1][kk]);
       }
     }
-    if (more) store(buf ^ 1);
+    settle(z.s[0], z.s[1]);
+    mask_tile(z, i);
+  };
+  auto raise = [&](const Tile& z) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      float top = z.s[m][0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, z.s[m][r]);
+      x[m].m = fmaxf(x[m].m, both_max(top));
+    }
+  };
+  for (int attempt = 0; turns > 0; ++attempt) {
+    copy(0, 0);
+    copy(0, kRing - 1);  // turn 0's products, of P = 0
+    copies_landed<0>();
+    all_landed();
+    copy(1, 1);
+    scores_of(ta, 0);
+    raise(ta);
+    mc[0] = x[0].m * c;
+    mc[1] = x[1].m * c;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) tb.pw[0][w] = tb.pw[1][w] = 0;
+#pragma unroll
+    for (int f = 0; f < kAhead; ++f) ring[f] = fragment(f, &lds[kRing - 1][0][0], nullptr);
+    for (int i = 0; i <= turns; i += 2) {
+      turn(i, ta, tb);
+      turn(i + 1, tb, ta);
+    }
+    copies_landed<0>();  // none is under way when the wave ends
+    if (attempt || !__syncthreads_or(!(x[0].l < kTooMuch && x[1].l < kTooMuch))) break;
+    clear(x[0]);
+    clear(x[1]);
+    for (int i = 0; i < turns; ++i) {
+      __syncthreads();
+      copy(i, 0);
+      copies_landed<0>();
+      scores_of(ta, i);
+      raise(ta);
+    }
+    __syncthreads();
   }
 
-  const float l = both_sum(x.l);
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  const float l2 = log2_sum(x.m, l, c);
+  float l2[2];
 #pragma unroll
-  for (int d = 0; d < 4; ++d)
+  for (int m = 0; m < 2; ++m) {
+    const float l = both_sum(x[m].l);
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    l2[m] = log2_sum(x[m].m, l, c);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x.o[d][r] *= inv;
-  const int64_t at = ((int64_t)(b * 2 * s.H + 2 * h + map)) * s.N + row;
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[m].o[d][r] *= inv;
+  }
+  if (!valid) return;
+  const int64_t at = ((int64_t)(b * 2 * s.H + 2 * h)) * s.N + row;
   if (nsplit > 1) {
     const Parts p = parts_of(A.ws, s, nsplit);
-    if (valid) {
-      float* o = p.o + (split * p.rows + at) * D + 4 * hh;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int64_t am = split * p.rows + at + m * s.N;
+      float* o = p.o + am * D + 4 * hh;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<float4*>(o + 32 * d + 8 * q) =
-              make_float4(x.o[d][4 * q], x.o[d][4 * q + 1], x.o[d][4 * q + 2], x.o[d][4 * q + 3]);
-      if (hh == 0) p.l[split * p.rows + at] = l2;
+          *reinterpret_cast<float4*>(o + 32 * d + 8 * q) = make_float4(
+              x[m].o[d][4 * q], x[m].o[d][4 * q + 1], x[m].o[d][4 * q + 2], x[m].o[d][4 * q + 3]);
+      if (hh == 0) p.l[am] = l2[m];
     }
     return;
   }
-  if (A.lse && valid && hh == 0) A.lse[at] = l2 * kLn2;
-  // map 1's rows to map 0's waves through LDS (fp32, rows 528 bytes apart)
-  __syncthreads();
-  constexpr int kRow = D + 4;
-  static_assert(kDiffRows * kRow * 4 <= (int)sizeof(lds), "the second map's rows fit the tiles' LDS");
-  float* other = reinterpret_cast<float*>(&lds[0][0]) + (32 * group + l32) * kRow + 4 * hh;
-  if (map == 1) {
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        *reinterpret_cast<float4*>(other + 32 * d + 8 * q) =
-            make_float4(x.o[d][4 * q], x.o[d][4 * q + 1], x.o[d][4 * q + 2], x.o[d][4 * q + 3]);
-        if (A.out2 && valid)
-          *reinterpret_cast<uint2*>(A.out2 + (((int64_t)b * s.H + h) * s.N + row) * D + 32 * d + 8 * q + 4 * hh) =
-              pack4(x.o[d], q);
-      }
+  if (A.lse && hh == 0) {
+    A.lse[at] = l2[0] * kLn2;
+    A.lse[at + s.N] = l2[1] * kLn2;
   }
-  __syncthreads();
-  if (map == 0 && valid) {
-    const float lam = s.lambda[h];
-    uint16_t* o = A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)row * A.out.sn + 4 * hh;
+  const float lam = s.lambda[h];
+  uint16_t* o = A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)row * A.out.sn + 4 * hh;
+  uint16_t* o2 = A.out2 ? A.out2 + (((int64_t)b * s.H + h) * s.N + row) * D + 4 * hh : nullptr;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+  for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float4 y = *reinterpret_cast<const float4*>(other + 32 * d + 8 * q);
-        x.o[d][4 * q] = __builtin_fmaf(-lam, y.x, x.o[d][4 * q]);
-        x.o[d][4 * q + 1] = __builtin_fmaf(-lam, y.y, x.o[d][4 * q + 1]);
-        x.o[d][4 * q + 2] = __builtin_fmaf(-lam, y.z, x.o[d][4 * q + 2]);
-        x.o[d][4 * q + 3] = __builtin_fmaf(-lam, y.w, x.o[d][4 * q + 3]);
-        *reinterpret_cast<uint2*>(o + 32 * d + 8 * q) = pack4(x.o[d], q);
-      }
-  }
+    for (int q = 0; q < 4; ++q) {
+      if (o2) *reinterpret_cast<uint2*>(o2 + 32 * d + 8 * q) = pack4(x[1].o[d], q);
+#pragma unroll
+      for (int r = 4 * q; r < 4 * q + 4; ++r) x[0].o[d][r] = __builtin_fmaf(-lam, x[1].o[d][r], x[0].o[d][r]);
+      *reinterpret_cast<uint2*>(o + 32 * d + 8 * q) = pack4(x[0].o[d], q);
+    }
 }
 
 // Few rows over many keys (a token or some drafted ones over a cache): the rows
@@ -497,22 +648,28 @@ __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, int nsplit) {
 // (dq) and one that owns keys (dk, dv, dlambda): no atomics, and every sum in a
 // fixed order.
 
-// Per row and map: the log2 sum that turns scores into P (+inf where the row
-// has no keys or is not the sequence's: P is 0 there) and delta.
+// What the backward kernels know of a row, 32 rows together: kStatLse0, kStatLse1:
+// -lse / scale of the maps, which added to raw scores and scaled gives log2 P
+// (-inf, and so P = 0, where the row has no keys or is not the sequence's);
+// kStatDelta0: -delta_0; kStatStep: delta_0 - delta_1; 32 floats each.
+constexpr int kBwdRows = 32;
+constexpr int kStatFloats = 4 * kBwdRows;
+enum { kStatLse0 = 0, kStatLse1 = kBwdRows, kStatDelta0 = 2 * kBwdRows, kStatStep = 3 * kBwdRows };
+
 __global__ __launch_bounds__(256) void diff_stats_kernel(DiffBwd A) {
   const DiffShape& s = A.s;
+  const int row_tiles = (s.N + kBwdRows - 1) / kBwdRows;
   const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  if (i >= (int64_t)s.B * s.H * s.N) return;
+  if (i >= (int64_t)s.B * s.H * row_tiles * kBwdRows) return;
   const int cc = threadIdx.x & 15;
-  const int n = (int)(i % s.N);
-  const int bh = (int)(i / s.N), h = bh % s.H, b = bh / s.H;
+  const int n = (int)(i % (row_tiles * kBwdRows));
+  const int bh = (int)(i / (row_tiles * kBwdRows)), h = bh % s.H, b = bh / s.H;
   const bool valid = n < sequence(s, b).qlen;
   float d0 = 0.0f, d1 = 0.0f;
-  const int64_t at = ((int64_t)(b * 2 * s.H + 2 * h)) * s.N + n;
   if (valid) {
     float o[8], o1[8], g[8];
     unpack_bf16x8(*reinterpret_cast<const uint4*>(A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)n * A.out.sn + 8 * cc), o);
-    unpack_bf16x8(*reinterpret_cast<const uint4*>(A.out2 + i * D + 8 * cc), o1);
+    unpack_bf16x8(*reinterpret_cast<const uint4*>(A.out2 + ((int64_t)bh * s.N + n) * D + 8 * cc), o1);
     unpack_bf16x8(*reinterpret_cast<const uint4*>(A.dout.p + b * A.dout.sb + h * A.dout.sh + (int64_t)n * A.dout.sn + 8 * cc), g);
     const float lam = s.lambda[h];
 #pragma unroll
@@ -527,26 +684,42 @@ __global__ __launch_bounds__(256) void diff_stats_kernel(DiffBwd A) {
     d1 += __shfl_xor(d1, m);
   }
   if (cc < 2) {
-    const float lse = valid ? A.lse[at + cc * s.N] : 0.0f;
+    const float lse = valid ? A.lse[((int64_t)bh * 2 + cc) * s.N + n] : 0.0f;
     const bool some = valid && lse > -3e38f;
-    A.stats[at + cc * s.N] = make_float2(some ? lse * kLog2e : __builtin_inff(), some ? (cc ? d1 : d0) : 0.0f);
+    float* st = A.stats + ((int64_t)bh * row_tiles + n / kBwdRows) * kStatFloats + n % kBwdRows;
+    st[cc ? kStatLse1 : kStatLse0] = some ? -lse / s.scale : -__builtin_inff();
+    st[cc ? kStatStep : kStatDelta0] = !some ? 0.0f : cc ? d0 - d1 : -d0;
   }
 }
 
+// A backward turn t finds the scores and X of tile t, the exponentials of tile t
+// (from the slot where its scores are done), what is left of tile t - 1 to its
+// operands, and the gradient products of tile t - 1.  A turn's slot j reads the
+// fragment of slot j + kAhead (kAhead a divisor of the list's length: a
+// fragment's register is the same in every turn); the barrier stands where the
+// last eight slots begin, so that the next tile's first fragments are read
+// before the turn ends.
+struct Scores {
+  f32x16 s[2], x;  // scores of the maps, X
+  float p[2][16];  // P of the maps
+};
+
 // dq of 128 rows of one head, both maps in a wave (X is found once): 32 rows a
-// wave over all the keys they see, tiles as in the forward pass.
+// wave over all the keys they see.
+constexpr int kDqKeys = 32;
 template <bool kShared>
 __global__ __launch_bounds__(256, 1) void diff_dq_kernel(DiffBwd A) {
-  constexpr int kTileElems = kDiffKeys * kStride;
-  constexpr int kKTiles = kShared ? 1 : 2;
-  __shared__ __attribute__((aligned(16))) uint16_t lds[2][(kKTiles + 1) * kTileElems];
+  constexpr int kTiles = kShared ? 2 : 3;  // K (of each map), V
+  constexpr int kV = kTiles - 1;
+  constexpr int kAhead = 8;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing][kTiles][kTile32];
   lds_poison(lds, sizeof(lds));
   lds_poison_done();
   const DiffShape& s = A.s;
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63, hh = lane >> 5, l32 = lane & 31;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
   const int tiles = (s.N + kDiffRows - 1) / kDiffRows;
   int id = xcd_local_id(blockIdx.x, gridDim.x);
-  const int tile = tiles - 1 - id % tiles;
+  const int tile = tiles - 1 - id % tiles;  // causal: the long rows first
   id /= tiles;
   const int h = id % s.H, b = id / s.H;
   const Seq sq = sequence(s, b);
@@ -557,77 +730,151 @@ __global__ __launch_bounds__(256, 1) void diff_dq_kernel(DiffBwd A) {
   const float c = s.scale * kLog2e, lam = s.lambda[h];
 
   const uint16_t* k0 = A.k.p + b * A.k.sb + (kShared ? hv : 2 * hv) * A.k.sh;
-  const uint16_t* k1 = k0 + (kShared ? 0 : A.k.sh);
-  const uint16_t* v = A.v.p + b * A.v.sb + hv * A.v.sh;
+  const uint16_t* v0 = A.v.p + b * A.v.sb + hv * A.v.sh;
   bf16x8 qf[2][8], gf[8];
   load_row(qf[0], A.q.p + b * A.q.sb + 2 * h * A.q.sh + (int64_t)row * A.q.sn, valid, hh);
   load_row(qf[1], A.q.p + b * A.q.sb + (2 * h + 1) * A.q.sh + (int64_t)row * A.q.sn, valid, hh);
   load_row(gf, A.dout.p + b * A.dout.sb + h * A.dout.sh + (int64_t)row * A.dout.sn, valid, hh);
-  float2 st[2] = {make_float2(__builtin_inff(), 0.0f), make_float2(__builtin_inff(), 0.0f)};
+  float lse[2] = {-__builtin_inff(), -__builtin_inff()}, del[2] = {0.0f, 0.0f};
   if (valid) {
-    const int64_t at = ((int64_t)(b * 2 * s.H + 2 * h)) * s.N + row;
-    st[0] = A.stats[at];
-    st[1] = A.stats[at + s.N];
+    const float* st = A.stats + ((int64_t)(b * s.H + h) * ((s.N + kBwdRows - 1) / kBwdRows) + row / kBwdRows) * kStatFloats +
+                      row % kBwdRows;
+    lse[0] = st[kStatLse0] * c;
+    lse[1] = st[kStatLse1] * c;
+    del[0] = -st[kStatDelta0];
+    del[1] = del[0] - st[kStatStep];
   }
 
   const int last = min(row + sq.shift, sq.klen - 1);
   const int last_row = min(row0 + kDiffRows, sq.qlen) - 1;
   const int kend = row0 < sq.qlen ? min(last_row + sq.shift, sq.klen - 1) + 1 : 0;
-  const int wave_row = row0 + 32 * wave;
-  const int all_to = min(wave_row + sq.shift, sq.klen - 1);
-  const int none_from = wave_row < sq.qlen ? min(wave_row + 31 + sq.shift, sq.klen - 1) : -1;
+  const int turns = kend > 0 ? (kend + kDqKeys - 1) / kDqKeys : 0;
+  const int all_to = min(row0 + 32 * wave + sq.shift, sq.klen - 1);  // every row of the wave sees these
+
+  const uint32_t at0 = lds_address(&lds[0][0][0]) + wave * kRowBlock;
+  const int copy_row = 8 * wave + (lane >> 3);
+  // Tile after tile into place `place` of the ring, one kilobyte at a time; past
+  // the last tile it comes again, and is not used.
+  constexpr int kCopies = 2 * kTiles;
+  struct Copy {
+    const uint16_t *k, *v;
+    int key;
+    uint32_t to, ok, ov;
+  } cp_ = {k0 + (int64_t)0 * A.k.sn, v0 + (int64_t)0 * A.v.sn, 0, 0u, copy_offset(copy_row, A.k.sn, lane),
+           copy_offset(copy_row, A.v.sn, lane)};
+  auto copy_start = [&](int i, int place) __attribute__((always_inline)) {
+    const bool on = i > 0 && i < turns;
+    cp_.k += on ? kDqKeys * A.k.sn : 0;
+    cp_.v += on ? kDqKeys * A.v.sn : 0;
+    cp_.key += on ? kDqKeys : 0;
+    cp_.to = __builtin_amdgcn_readfirstlane(at0 + (place % kRing) * (kTiles * kTile32));
+    if (cp_.key + kDqKeys > sq.klen) {  // keys past the sequence: its last key again (their scores are masked)
+      const int r = min(copy_row, sq.klen - 1 - cp_.key);
+      cp_.ok = copy_offset(r, A.k.sn, lane);
+      cp_.ov = copy_offset(r, A.v.sn, lane);
+    }
+  };
+  auto copy_part = [&](int n) __attribute__((always_inline)) {
+    const uint16_t* p = n / 2 == kV ? cp_.v : n / 2 == 0 ? cp_.k : cp_.k + A.k.sh;
+    copy_1k(cp_.to + n / 2 * kTile32 + n % 2 * 1024, p, (n / 2 == kV ? cp_.ov : cp_.ok) + n % 2 * 128);
+  };
+  auto copy = [&](int i, int place) __attribute__((always_inline)) {
+    copy_start(i, place);
+#pragma unroll
+    for (int n = 0; n < kCopies; ++n) copy_part(n);
+  };
 
   f32x16 dq[2][4] = {};
-  const int tr = column_offset(lane);
-  Stage<kDiffKeys, 256> sk0, sk1, sv;
-  auto load = [&](int key) __attribute__((always_inline)) {
-    sk0.load(k0, A.k.sn, key, kend, t);
-    if (!kShared) sk1.load(k1, A.k.sn, key, kend, t);
-    sv.load(v, A.v.sn, key, kend, t);
+  Scores sa, sb;
+  bf16x8 ring[kAhead];
+  uint32_t pw[2][8];  // dS of the maps, but for the factors scale and -lambda
+  const RowPlace rp = row_place(lane);
+  const int cp = col_place(lane);
+  // the fragment of slot i of a turn on tile `now` whose products read tile `then`
+  auto fragment = [&](int i, const uint8_t* now, const uint8_t* then) __attribute__((always_inline)) {
+    if (i < 16) return row_frag(now + (kShared ? 0 : (i & 1) * kTile32), rp, i >> 1);
+    if (i < 24) return row_frag(now + kV * kTile32, rp, i - 16);
+    const int j = i - 24;  // y, d, map
+    return col_frag(then + (kShared ? 0 : (j & 1) * kTile32) + cp, j >> 3, (j >> 1) & 3);
   };
-  auto store = [&](int buf) __attribute__((always_inline)) {
-    sk0.store(lds[buf], t);
-    if (!kShared) sk1.store(lds[buf] + kTileElems, t);
-    sv.store(lds[buf] + kKTiles * kTileElems, t);
+  auto finish = [&](const Scores& old, int r) __attribute__((always_inline)) {  // rows r, r + 1
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      pw[m][r >> 1] = pack_bf16x2(old.p[m][r] * (old.x[r] - del[m]), old.p[m][r + 1] * (old.x[r + 1] - del[m]));
+      pin(pw[m][r >> 1]);
+    }
   };
-  if (kend > 0) {
-    load(0);
-    store(0);
-  }
-  int buf = 0;
-  for (int key = 0; key < kend; key += kDiffKeys, buf ^= 1) {
-    __syncthreads();
-    const bool more = key + kDiffKeys < kend;
-    if (more) load(key + kDiffKeys);
-    if (key <= none_from) {
+  auto turn = [&](int i, Scores& now, Scores& old) __attribute__((always_inline)) {
+    constexpr int kSlots = 40;
+    const uint8_t* tn = &lds[i % kRing][0][0];
+    const uint8_t* to = &lds[(i + kRing - 1) % kRing][0][0];
+    const uint8_t* next = &lds[(i + 1) % kRing][0][0];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint16_t* tk0 = lds[buf] + 32 * u * kStride;
-        const uint16_t* tk1 = kShared ? tk0 : tk0 + kTileElems;
-        const uint16_t* tv = lds[buf] + kKTiles * kTileElems + 32 * u * kStride;
-        f32x16 s0 = scores(tk0, qf[0], lane), s1 = scores(tk1, qf[1], lane), x = scores(tv, gf, lane);
-        if (key + 32 * u + 31 > all_to) {
-          mask(s0, key + 32 * u + 4 * hh, last);
-          mask(s1, key + 32 * u + 4 * hh, last);
-        }
+    for (int d = 0; d < 4; ++d) asm volatile("" : "+a"(dq[0][d]), "+a"(dq[1][d]));
+    hold_in_agprs(qf[0]);
+    hold_in_agprs(qf[1]);
+    hold_in_agprs(gf);
+    each<0, kSlots>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int j = slot.value;
+      if constexpr (j == kSlots - 8) {
+        copies_landed<0>();
+        copy_start(i + 2, i + 2);
+        slot_end();
+      }
+      if constexpr (j >= kSlots - 7 && j < kSlots - 7 + kCopies) copy_part(j - (kSlots - 7));
+      const bf16x8 f = ring[j % kAhead];
+      if constexpr (j < 16) {
+        if constexpr (j < 2) score_first_a(now.s[j & 1], f, qf[j & 1][j >> 1]);
+        else score_a(now.s[j & 1], f, qf[j & 1][j >> 1]);
+      } else if constexpr (j < 24) {
+        if constexpr (j == 16) score_first_a(now.x, f, gf[j - 16]);
+        else score_a(now.x, f, gf[j - 16]);
+      } else {
+        constexpr int m = (j - 24) & 1, d = ((j - 24) >> 1) & 3, y = (j - 24) >> 3;
+        const uint4 w = make_uint4(pw[m][4 * y], pw[m][4 * y + 1], pw[m][4 * y + 2], pw[m][4 * y + 3]);
+        dq[m][d] = mfma(f, __builtin_bit_cast(bf16x8, w), dq[m][d]);
+      }
+      constexpr int k = j + kAhead;
+      ring[j % kAhead] = k < kSlots ? fragment(k, tn, to) : fragment(k - kSlots, next, tn);
+      if constexpr (j < 16 && j % 2 == 0) finish(old, j);
+      if constexpr (j >= 18) {  // the exponentials: 32 in 22 slots
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s0[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s0[r], c, -st[0].x)) * (x[r] - st[0].y);
-          s1[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s1[r], c, -st[1].x)) * (x[r] - st[1].y);
-        }
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const bf16x8 d0 = operand8(s0, y), d1 = operand8(s1, y);
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const bf16x8 kf = column8(tk0 + 16 * y * kStride + 32 * d + tr);
-            dq[0][d] = mfma(kf, d0, dq[0][d]);
-            dq[1][d] = mfma(kShared ? kf : column8(tk1 + 16 * y * kStride + 32 * d + tr), d1, dq[1][d]);
-          }
+        for (int e = (j - 18) * 16 / 11; e < (j - 17) * 16 / 11; ++e) {
+          now.p[e & 1][e >> 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(now.s[e & 1][e >> 1], c, lse[e & 1]));
+          pin(now.p[e & 1][e >> 1]);
         }
       }
+      slot_end();
+    });
+    if (i * kDqKeys + kDqKeys - 1 > all_to || i >= turns) {
+      const int to_key = i < turns ? last : -1;  // (past the last tile: none)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (i * kDqKeys + 4 * hh + 8 * (r >> 2) + (r & 3) > to_key) now.p[0][r] = now.p[1][r] = 0.0f;
     }
-    if (more) store(buf ^ 1);
+  };
+  if (turns > 0) {
+    copy(0, 0);
+    copy(0, kRing - 1);  // turn 0's products, of dS = 0
+    copies_landed<0>();
+    hold_in_agprs(qf[0]);
+    hold_in_agprs(qf[1]);
+    hold_in_agprs(gf);
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      pin(lse[m]);
+      pin(del[m]);
+    }
+    all_landed();
+    copy(1, 1);
+    sb = Scores{};
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) ring[j] = fragment(j, &lds[0][0][0], nullptr);
+    for (int i = 0; i <= turns; i += 2) {
+      turn(i, sa, sb);
+      turn(i + 1, sb, sa);
+    }
+    copies_landed<0>();  // none is under way when the wave ends
   }
   if (row < s.N) {  // zero behind the sequence
 #pragma unroll
@@ -647,19 +894,21 @@ __global__ __launch_bounds__(256, 1) void diff_dq_kernel(DiffBwd A) {
 
 // dk, dv of 128 keys of one value head, 32 keys a wave, over the rows of every
 // head of its group (so a shared head's gradient is summed in registers, heads
-// in order); dlambda's parts of these keys.
-constexpr int kBwdRows = 32;  // query rows of a tile
+// in order); dlambda's parts of these keys:
+//   sum P_1 (X - delta_1), which with sum delta_1 is sum P_1 X
+// (the rows of P_1 sum to 1; delta_1 comes from a rounded output, and that
+// rounding cancels here).
 template <bool kShared>
 __global__ __launch_bounds__(256, 1) void diff_dkv_kernel(DiffBwd A) {
-  constexpr int kTileElems = kBwdRows * kStride;
   constexpr int kK = kShared ? 1 : 2;
-  __shared__ __attribute__((aligned(16))) uint16_t lds[2][3 * kTileElems];
-  __shared__ __attribute__((aligned(16))) float rowstat[2][4][kBwdRows];  // log2 sums of the maps, deltas of the maps
+  constexpr int kAhead = kShared ? 6 : 4;  // (registers)
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing][3][kTile32];  // q of map 0, of map 1, dout
+  __shared__ __attribute__((aligned(1024))) float stat[kRing][kStatFloats];
   lds_poison(lds, sizeof(lds));
-  lds_poison(rowstat, sizeof(rowstat));
+  lds_poison(stat, sizeof(stat));
   lds_poison_done();
   const DiffShape& s = A.s;
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63, hh = lane >> 5, l32 = lane & 31;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
   const int tiles = (s.M + kDiffRows - 1) / kDiffRows;
   int id = xcd_local_id(blockIdx.x, gridDim.x);
   const int tile = id % tiles;  // causal: the long columns first
@@ -678,100 +927,218 @@ __global__ __launch_bounds__(256, 1) void diff_dkv_kernel(DiffBwd A) {
   if (!kShared) load_row(kf[kK - 1], kp + A.k.sh, valid, hh);
   load_row(vf, A.v.p + b * A.v.sb + hv * A.v.sh + (int64_t)key * A.v.sn, valid, hh);
 
-  // rows that see any key of this tile: from key0 - shift on
-  const int first = key0 < sq.klen ? min(max(key0 - sq.shift, 0), sq.qlen) / kBwdRows * kBwdRows : sq.qlen;
+  // the tiles of rows that see any key of this workgroup, head after head
+  const int first = key0 < sq.klen ? min(max(key0 - sq.shift, 0), sq.qlen) / kBwdRows : 0;
+  const int end = key0 < sq.klen ? (sq.qlen + kBwdRows - 1) / kBwdRows : 0;
+  const int head_turns = max(end - first, 0), turns = head_turns * per;
+  const int row_tiles = (s.N + kBwdRows - 1) / kBwdRows;
   const int wave_last_key = key0 + 32 * wave + 31;
 
+  const uint32_t at0 = lds_address(&lds[0][0][0]) + wave * kRowBlock;
+  const uint32_t stat0 = lds_address(&stat[0][0]) + (wave & 1) * 256;
+  const int copy_row = 8 * wave + (lane >> 3);
+  const uint16_t* qh = A.q.p + b * A.q.sb + 2 * (int64_t)hv * per * A.q.sh;
+  const uint16_t* gh = A.dout.p + b * A.dout.sb + (int64_t)hv * per * A.dout.sh;
+  const float* sth = A.stats + (int64_t)(b * s.H + hv * per) * row_tiles * kStatFloats + (wave & 1) * 64;
+  // Tile after tile (head after head) into the ring, one kilobyte at a time; past
+  // the last tile it comes again, and is not used.
+  constexpr int kCopies = 7;
+  struct Copy {
+    const uint16_t *q, *g;
+    const float* st;
+    int u, t;  // head of the group and row tile
+    uint32_t to, to_st, oq, og;
+  } cp_ = {};
+  auto copy_start = [&](int i, int place) __attribute__((always_inline)) {
+    const bool on = i > 0 && i < turns;
+    if (i == 0 || (on && cp_.t + 1 == end)) {
+      cp_.u += i > 0;
+      cp_.t = first;
+      cp_.q = qh + 2 * cp_.u * A.q.sh + (int64_t)first * kBwdRows * A.q.sn;
+      cp_.g = gh + cp_.u * A.dout.sh + (int64_t)first * kBwdRows * A.dout.sn;
+      cp_.st = sth + ((int64_t)cp_.u * row_tiles + first) * kStatFloats;
+      cp_.oq = copy_offset(copy_row, A.q.sn, lane);
+      cp_.og = copy_offset(copy_row, A.dout.sn, lane);
+    } else {
+      cp_.t += on;
+      cp_.q += on ? kBwdRows * A.q.sn : 0;
+      cp_.g += on ? kBwdRows * A.dout.sn : 0;
+      cp_.st += on ? kStatFloats : 0;
+    }
+    cp_.to = __builtin_amdgcn_readfirstlane(at0 + (place % kRing) * (3 * kTile32));
+    cp_.to_st = __builtin_amdgcn_readfirstlane(stat0 + (place % kRing) * (kStatFloats * 4));
+    if (cp_.t + 1 == end) {  // rows past the sequence: its last row again (their P is 0)
+      const int r = min(copy_row, sq.qlen - 1 - cp_.t * kBwdRows);
+      cp_.oq = copy_offset(r, A.q.sn, lane);
+      cp_.og = copy_offset(r, A.dout.sn, lane);
+    }
+  };
+  auto copy_part = [&](int n) __attribute__((always_inline)) {
+    if (n == 6) {
+      copy_256(cp_.to_st, cp_.st, lane * 4);
+    } else {
+      const uint16_t* p = n / 2 == 2 ? cp_.g : n / 2 == 0 ? cp_.q : cp_.q + A.q.sh;
+      copy_1k(cp_.to + n / 2 * kTile32 + n % 2 * 1024, p, (n / 2 == 2 ? cp_.og : cp_.oq) + n % 2 * 128);
+    }
+  };
+  auto copy = [&](int i, int place) __attribute__((always_inline)) {
+    copy_start(i, place);
+#pragma unroll
+    for (int n = 0; n < kCopies; ++n) copy_part(n);
+  };
+
   f32x16 dv[4] = {}, dk[kK][4] = {};
-  const int tr = column_offset(lane);
-  for (int u = 0; u < per; ++u) {
-    const int h = hv * per + u;
-    const float lam = s.lambda[h];
-    const uint16_t* q0 = A.q.p + b * A.q.sb + 2 * h * A.q.sh;
-    const uint16_t* q1 = q0 + A.q.sh;
-    const uint16_t* g = A.dout.p + b * A.dout.sb + h * A.dout.sh;
-    const float2* st = A.stats + ((int64_t)(b * 2 * s.H + 2 * h)) * s.N;
-    float dlam = 0.0f;
-    Stage<kBwdRows, 256> s0, s1, sg;
-    float2 stat;
-    auto load = [&](int row) __attribute__((always_inline)) {
-      s0.load(q0, A.q.sn, row, sq.qlen, t);
-      s1.load(q1, A.q.sn, row, sq.qlen, t);
-      sg.load(g, A.dout.sn, row, sq.qlen, t);
-      const int r = row + (t & 31);
-      stat = make_float2(__builtin_inff(), 0.0f);
-      if (t < 64 && r < sq.qlen) stat = st[(t >> 5) * s.N + r];
-    };
-    auto store = [&](int buf) __attribute__((always_inline)) {
-      s0.store(lds[buf], t);
-      s1.store(lds[buf] + kTileElems, t);
-      sg.store(lds[buf] + 2 * kTileElems, t);
-      if (t < 64) {
-        rowstat[buf][t >> 5][t & 31] = stat.x;
-        rowstat[buf][2 + (t >> 5)][t & 31] = stat.y;
-      }
-    };
-    __syncthreads();  // the last head's tiles are read
-    if (first < sq.qlen) {
-      load(first);
-      store(0);
+  Scores sa, sb;
+  bf16x8 ring[kAhead];
+  float4 step;        // delta_0 - delta_1 of four of the last tile's rows
+  uint32_t pw[3][8];  // P_0 - lambda P_1, dS_0, dS_1
+  float dlam = 0.0f;
+  const RowPlace rp = row_place(lane);
+  const int cp = col_place(lane);
+  int u = 0, left = head_turns;  // of the last tile: its head, and the tiles of that head from it on
+  int rt = first;                // row tile of the turn's scores
+  float lam = uniform(s.lambda[hv * per]);
+  // of the keys' operands, the first map's beside the gradients, and V's where
+  // there is room; the second map's beside the scores
+  auto hold_operands = [&]() __attribute__((always_inline)) {
+    hold_in_agprs(kf[0]);
+    if constexpr (kShared) {
+      hold_in_agprs(vf);
+    } else {
+      hold_in_vgprs(kf[1]);
+      hold_in_vgprs(vf);
     }
-    int buf = 0;
-    for (int row = first; row < sq.qlen; row += kBwdRows, buf ^= 1) {
-      __syncthreads();
-      const bool more = row + kBwdRows < sq.qlen;
-      if (more) load(row + kBwdRows);
-      if (row + kBwdRows - 1 + sq.shift >= key0 + 32 * wave) {
-        const uint16_t *t0 = lds[buf], *t1 = t0 + kTileElems, *tg = t1 + kTileElems;
-        // rows of q (lane) times keys: result row = row of q, column = key
-        f32x16 p0 = {}, p1 = {}, x = {};
+  };
+  auto fragment = [&](int i, const uint8_t* now, const uint8_t* then) __attribute__((always_inline)) {
+    if (i < 16) return row_frag(now + (i & 1) * kTile32, rp, i >> 1);
+    if (i < 24) return row_frag(now + 2 * kTile32, rp, i - 16);
+    const int j = i - 24, d = (j / 3) & 3, y = j / 12;  // y, d, which: dv, dk of map 0, of map 1
+    return col_frag(then + (j % 3 == 0 ? 2 : j % 3 - 1) * kTile32 + cp, y, d);
+  };
+  // rows 4 q .. 4 q + 3 of a lane's sixteen
+  auto quad = [&](const float* st, int q) __attribute__((always_inline)) {
+    return *reinterpret_cast<const float4*>(st + 8 * q + 4 * hh);
+  };
+  auto put = [](f32x16& x, int q, const float4& f) __attribute__((always_inline)) {
+    x[4 * q] = f.x;
+    x[4 * q + 1] = f.y;
+    x[4 * q + 2] = f.z;
+    x[4 * q + 3] = f.w;
+  };
+  // P_0 - lambda P_1, dS_0 and dS_1 of rows r, r + 1 of a lane's sixteen of the last tile
+  auto finish = [&](const Scores& old, int r) __attribute__((always_inline)) {
+    const float w0 = old.p[1][r] * (old.x[r] + (r & 2 ? step.z : step.x));
+    const float w1 = old.p[1][r + 1] * (old.x[r + 1] + (r & 2 ? step.w : step.y));
+    dlam += w0 + w1;
+    pw[0][r >> 1] = pack_bf16x2(__builtin_fmaf(-lam, old.p[1][r], old.p[0][r]),
+                                __builtin_fmaf(-lam, old.p[1][r + 1], old.p[0][r + 1]));
+    pw[1][r >> 1] = pack_bf16x2(old.p[0][r] * old.x[r], old.p[0][r + 1] * old.x[r + 1]);
+    pw[2][r >> 1] = pack_bf16x2(-lam * w0, -lam * w1);
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-          p0 = mfma(row8(t0, lane, kk), kf[0][kk], p0);
-          p1 = mfma(row8(t1, lane, kk), kf[kK - 1][kk], p1);
-          x = mfma(row8(tg, lane, kk), vf[kk], x);
-        }
-        const bool edge = wave_last_key >= sq.klen || wave_last_key > row + sq.shift;
-        float l0[16], l1[16], e0[16], e1[16];
+    for (int m = 0; m < 3; ++m) pin(pw[m][r >> 1]);
+  };
+  // the last tile is done: a head's last one ends its part of dlambda
+  auto end_of_tile = [&]() __attribute__((always_inline)) {
+    if (--left == 0) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          *reinterpret_cast<float4*>(&l0[4 * q]) = *reinterpret_cast<const float4*>(&rowstat[buf][0][8 * q + 4 * hh]);
-          *reinterpret_cast<float4*>(&l1[4 * q]) = *reinterpret_cast<const float4*>(&rowstat[buf][1][8 * q + 4 * hh]);
-          *reinterpret_cast<float4*>(&e0[4 * q]) = *reinterpret_cast<const float4*>(&rowstat[buf][2][8 * q + 4 * hh]);
-          *reinterpret_cast<float4*>(&e1[4 * q]) = *reinterpret_cast<const float4*>(&rowstat[buf][3][8 * q + 4 * hh]);
-        }
-        f32x16 mix;
+      for (int m = 1; m < 64; m <<= 1) dlam += __shfl_xor(dlam, m);
+      if (lane == 0) A.partial[((int64_t)(hv * per + u) * s.B + b) * A.parts + tile * 4 + wave] = dlam;
+      dlam = 0.0f;
+      ++u;
+      left = head_turns;
+      lam = uniform(s.lambda[hv * per + min(u, per - 1)]);
+    }
+  };
+  auto turn = [&](int i, Scores& now, Scores& old) __attribute__((always_inline)) {
+    constexpr int kSlots = 48;
+    const uint8_t* tn = &lds[i % kRing][0][0];
+    const uint8_t* to = &lds[(i + kRing - 1) % kRing][0][0];
+    const uint8_t* next = &lds[(i + 1) % kRing][0][0];
+    const float* stn = stat[i % kRing];
+    const float* old_st = stat[(i + kRing - 1) % kRing];
+    const float* next_st = stat[(i + 1) % kRing];
+    // (the gradients where only MFMAs reach them)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float a = __builtin_amdgcn_exp2f(__builtin_fmaf(p0[r], c, -l0[r]));
-          float d = __builtin_amdgcn_exp2f(__builtin_fmaf(p1[r], c, -l1[r]));
-          if (edge) {
-            const bool seen = valid && key <= row + 8 * (r >> 2) + 4 * hh + (r & 3) + sq.shift;
-            a = seen ? a : 0.0f;
-            d = seen ? d : 0.0f;
-          }
-          dlam = __builtin_fmaf(d, x[r], dlam);
-          mix[r] = __builtin_fmaf(-lam, d, a);
-          p0[r] = a * (x[r] - e0[r]);
-          p1[r] = -lam * d * (x[r] - e1[r]);
-        }
+    for (int d = 0; d < 4; ++d) {
+      asm volatile("" : "+a"(dv[d]), "+a"(dk[0][d]));
+      if (!kShared) asm volatile("" : "+a"(dk[kK - 1][d]));
+    }
+    hold_operands();
+    each<0, kSlots>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int j = slot.value;
+      if constexpr (j == kSlots - 8) {
+        copies_landed<0>();
+        copy_start(i + 2, i + 2);
+        slot_end();
+      }
+      if constexpr (j >= kSlots - 7) copy_part(j - (kSlots - 7));
+      const bf16x8 f = ring[j % kAhead];
+      if constexpr (j < 16) {
+        if constexpr (kShared || j % 2 == 0) score_a(now.s[j & 1], f, kf[0][j >> 1]);
+        else score(now.s[j & 1], f, kf[kK - 1][j >> 1]);
+      } else if constexpr (j < 24) {
+        if constexpr (kShared) score_a(now.x, f, vf[j - 16]);
+        else score(now.x, f, vf[j - 16]);
+      } else {
+        constexpr int w = (j - 24) % 3, d = ((j - 24) / 3) & 3, y = (j - 24) / 12;
+        const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(pw[w][4 * y], pw[w][4 * y + 1], pw[w][4 * y + 2], pw[w][4 * y + 3]));
+        if constexpr (w == 0) dv[d] = mfma(f, p, dv[d]);
+        else dk[kShared ? 0 : w - 1][d] = mfma(f, p, dk[kShared ? 0 : w - 1][d]);
+      }
+      constexpr int k = j + kAhead;
+      ring[j % kAhead] = k < kSlots ? fragment(k, tn, to) : fragment(k - kSlots, next, tn);
+      if constexpr (j < 24 && j % 3 == 0) finish(old, j / 3 * 2);
+      if constexpr (j >= 8 && j < 12) put(now.x, j - 8, quad(stn + kStatDelta0, j - 8));
+      if constexpr (j < 21 && j % 6 == 3) step = quad(old_st + kStatStep, j / 6 + 1);
+      if constexpr (j == 45) step = quad(stn + kStatStep, 0);
+      // the next turn's scores start from the rows' log sums
+      if constexpr (j >= 40 && j < 44) {
+        put(old.s[0], j - 40, quad(next_st + kStatLse0, j - 40));
+        put(old.s[1], j - 40, quad(next_st + kStatLse1, j - 40));
+      }
+      if constexpr (j >= 18) {  // the exponentials: 32 in 30 slots
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const bf16x8 fm = operand8(mix, y), f0 = operand8(p0, y), f1 = operand8(p1, y);
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const int at = 16 * y * kStride + 32 * d + tr;
-            dv[d] = mfma(column8(tg + at), fm, dv[d]);
-            dk[0][d] = mfma(column8(t0 + at), f0, dk[0][d]);
-            dk[kK - 1][d] = mfma(column8(t1 + at), f1, dk[kK - 1][d]);
-          }
+        for (int e = (j - 18) * 16 / 15; e < (j - 17) * 16 / 15; ++e) {
+          now.p[e & 1][e >> 1] = __builtin_amdgcn_exp2f(now.s[e & 1][e >> 1] * c);
+          pin(now.p[e & 1][e >> 1]);
         }
       }
-      if (more) store(buf ^ 1);
+      slot_end();
+    });
+    if (i > 0 && i <= turns) end_of_tile();
+    const int row = rt * kBwdRows;
+    if (wave_last_key >= sq.klen || wave_last_key > row + sq.shift || i >= turns) {
+      // rows below it do not see this key (past the last tile: none does)
+      const int limit = valid && i < turns ? key - sq.shift - row : kBwdRows;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (8 * (r >> 2) + 4 * hh + (r & 3) < limit) now.p[0][r] = now.p[1][r] = 0.0f;
+    }
+    if (++rt == end) rt = first;
+  };
+  if (turns > 0) {
+    copy(0, 0);
+    copy(0, kRing - 1);  // turn 0's products, of P = dS = 0
+    copies_landed<0>();
+    hold_operands();
+    all_landed();
+    copy(1, 1);
+    sb = Scores{};
+    step = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      put(sa.s[0], q, quad(stat[0] + kStatLse0, q));
+      put(sa.s[1], q, quad(stat[0] + kStatLse1, q));
     }
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) dlam += __shfl_xor(dlam, m);
-    if (lane == 0) A.partial[((int64_t)h * s.B + b) * A.parts + tile * 4 + wave] = dlam;
+    for (int j = 0; j < kAhead; ++j) ring[j] = fragment(j, &lds[0][0][0], nullptr);
+    for (int i = 0; i <= turns; i += 2) {
+      turn(i, sa, sb);
+      turn(i + 1, sb, sa);
+    }
+    copies_landed<0>();  // none is under way when the wave ends
+  } else if (lane < 1) {
+    for (int n = 0; n < per; ++n) A.partial[((int64_t)(hv * per + n) * s.B + b) * A.parts + tile * 4 + wave] = 0.0f;
   }
   if (key < s.M) {  // zero behind the sequence
     uint16_t* o = A.dv.p + b * A.dv.sb + hv * A.dv.sh + (int64_t)key * A.dv.sn + 4 * hh;
@@ -796,12 +1163,22 @@ __global__ __launch_bounds__(256, 1) void diff_dkv_kernel(DiffBwd A) {
   }
 }
 
-// dlambda of a head: its parts summed in one order, in 64 bits.
+// dlambda of a head: its parts and the rows' delta_1 summed in one order, in 64 bits.
 __global__ __launch_bounds__(256) void diff_dlambda_kernel(DiffBwd A) {
   __shared__ double sum[256];
-  const float* p = A.partial + (int64_t)blockIdx.x * A.s.B * A.parts;
+  const DiffShape& s = A.s;
+  const int h = blockIdx.x;
+  const float* p = A.partial + (int64_t)h * s.B * A.parts;
   double x = 0.0;
-  for (int64_t i = threadIdx.x; i < (int64_t)A.s.B * A.parts; i += 256) x += (double)p[i];
+  for (int64_t i = threadIdx.x; i < (int64_t)s.B * A.parts; i += 256) x += (double)p[i];
+  const int row_tiles = (s.N + kBwdRows - 1) / kBwdRows;
+  for (int b = 0; b < s.B; ++b) {
+    const float* st = A.stats + (int64_t)(b * s.H + h) * row_tiles * kStatFloats;
+    for (int i = threadIdx.x; i < row_tiles * kBwdRows; i += 256) {
+      const float* f = st + (int64_t)(i / kBwdRows) * kStatFloats + i % kBwdRows;
+      x -= (double)f[kStatDelta0] + (double)f[kStatStep];
+    }
+  }
   sum[threadIdx.x] = x;
   __syncthreads();
   for (int n = 128; n > 0; n >>= 1) {
@@ -843,9 +1220,9 @@ hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
   } else {
     const dim3 grid((unsigned)((int64_t)s.B * s.H * ((s.N + kDiffRows - 1) / kDiffRows) * p.nsplit));
     if (shared)
-      hipLaunchKernelGGL(diff_fwd_kernel<true>, grid, dim3(512), 0, stream, a, p.nsplit);
+      hipLaunchKernelGGL(diff_fwd_kernel<true>, grid, dim3(256), 0, stream, a, p.nsplit);
     else
-      hipLaunchKernelGGL(diff_fwd_kernel<false>, grid, dim3(512), 0, stream, a, p.nsplit);
+      hipLaunchKernelGGL(diff_fwd_kernel<false>, grid, dim3(256), 0, stream, a, p.nsplit);
   }
   if (p.nsplit > 1) {
     const int64_t rows = (int64_t)s.B * s.H * s.N;
@@ -855,7 +1232,7 @@ hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
 }
 
 size_t diff_bwd_bytes(const DiffShape& s, size_t* partial_at, int* parts) {
-  const size_t stats = ((size_t)s.B * 2 * s.H * s.N * sizeof(float2) + 255) & ~(size_t)255;
+  const size_t stats = (size_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows) * kStatFloats * sizeof(float);
   *partial_at = stats;
   *parts = 4 * ((s.M + kDiffRows - 1) / kDiffRows);
   return stats + (size_t)s.H * s.B * *parts * sizeof(float);
@@ -863,9 +1240,9 @@ size_t diff_bwd_bytes(const DiffShape& s, size_t* partial_at, int* parts) {
 
 hipError_t launch_diff_bwd(const DiffBwd& a, hipStream_t stream) {
   const DiffShape& s = a.s;
-  const int64_t rows = (int64_t)s.B * s.H * s.N;
+  const int64_t rows = (int64_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows) * kBwdRows;
   const bool shared = s.Hk == s.Hv;
-  hipLaunchKernelGGL(diff_stats_kernel, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(diff_stats_kernel, dim3((unsigned)(rows / 16)), dim3(256), 0, stream, a);
   const dim3 gq((unsigned)((int64_t)s.B * s.H * ((s.N + kDiffRows - 1) / kDiffRows)));
   const dim3 gk((unsigned)((int64_t)s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows)));
   if (shared) {

@@ -114,7 +114,7 @@ struct DiffBwd {
   const uint16_t* out2;
   const float* lse;
   float* dlambda;
-  float2* stats;   // [B][2H][N]
+  float* stats;    // [B][H][ceil(N / 32)][4][32]
   float* partial;  // [H][B][parts]
   int parts;
 };

@@ -161,6 +161,16 @@ def test_peaked_rows(own_keys):
     check(inputs(1, 2, 1, own_keys, 1, 4000, seed=6, boost=True), causal=True)
 
 
+@pytest.mark.parametrize("N", [1, 200])
+@pytest.mark.parametrize("own_keys", [False, True])
+def test_maxima_far_above_the_first_keys(own_keys, N):
+    """Keys late in the sequence whose scores are hundreds above the first tile's: more than a sum of exponentials held to that tile can hold."""
+    x = inputs(1, 2, 1, own_keys, N, 2000, seed=7)
+    x["k"][:, :, 1500:1503] *= 64
+    x["k"][:, :, 333] *= 24
+    check(x, causal=N == 1)
+
+
 @pytest.mark.parametrize("scale", [1e-3, 0.5, 3.0])
 def test_scales(scale):
     check(inputs(1, 2, 1, True, 70, 90, seed=8), scale=scale)

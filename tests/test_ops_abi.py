@@ -49,6 +49,7 @@ COMMON = [
     (dict(q_st=S(4 * 100 * 128, 100 * 128, 127)), -1, "q strides"),
     (dict(v_st=S(-8, 100 * 128, 128)), -1, "v strides"),
     (dict(k_st=S(1 << 41, 100 * 128, 128)), -1, "k strides"),
+    (dict(k_st=S(0, 100 * 128, 1 << 25)), -2, "between tokens"),
 ]
 
 
