@@ -308,7 +308,11 @@ size_t sol_diff_attn_fwd_workspace_bytes(int B, int H, int Hv, int N, int M, int
   if (B < 1 || H < 1 || Hv < 1 || N < 1 || M < 1 || H % Hv || D != sol::kHeadDim || N > SOL_MAX_TOKENS ||
       M > SOL_MAX_TOKENS || (int64_t)B * H * N > INT32_MAX)
     return 0;
-  return sol::diff_fwd_bytes(s);
+  // the larger of the two masks'
+  const size_t all = sol::diff_fwd_bytes(s);
+  s.causal = 1;
+  const size_t causal = sol::diff_fwd_bytes(s);
+  return all > causal ? all : causal;
 }
 
 size_t sol_diff_attn_bwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D) {
@@ -316,9 +320,10 @@ size_t sol_diff_attn_bwd_workspace_bytes(int B, int H, int Hv, int N, int M, int
   if (B < 1 || H < 1 || Hv < 1 || N < 1 || M < 1 || H % Hv || D != sol::kHeadDim || N > SOL_MAX_TOKENS ||
       M > SOL_MAX_TOKENS || (int64_t)B * H * N > INT32_MAX)
     return 0;
-  size_t at;
-  int parts;
-  return sol::diff_bwd_bytes(s, &at, &parts);
+  const size_t all = sol::diff_bwd_bytes(s, nullptr);
+  s.causal = 1;
+  const size_t causal = sol::diff_bwd_bytes(s, nullptr);
+  return all > causal ? all : causal;
 }
 
 int sol_diff_attn_fwd(const void* q, const sol_strides* q_strides, const void* k, const sol_strides* k_strides,
@@ -374,8 +379,8 @@ int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const v
   if (!aligned16(out2)) return fail(SOL_ERR_INVALID_ARG, "out2 must be 16-byte aligned");
   SOL_TRY(check_small("lse", lse, false));
   SOL_TRY(check_small("dlambda", dlambda, false));
-  size_t partial_at;
-  const size_t need = sol::diff_bwd_bytes(a.s, &partial_at, &a.parts);
+  a.stats = static_cast<float*>(workspace);
+  const size_t need = sol::diff_bwd_bytes(a.s, &a);
   SOL_TRY(check_workspace(workspace, workspace_bytes, need));
   in[5] = span("out2", out2, (uint64_t)B * H * N * D * 2);
   in[6] = span("lse", lse, (uint64_t)B * 2 * H * N * 4);
@@ -388,8 +393,6 @@ int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const v
   a.out2 = static_cast<const uint16_t*>(out2);
   a.lse = lse;
   a.dlambda = dlambda;
-  a.stats = static_cast<float*>(workspace);
-  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + partial_at);
   return done(sol::launch_diff_bwd(a, reinterpret_cast<hipStream_t>(stream)), "diff_attn_bwd");
 }
 

@@ -125,16 +125,40 @@ __device__ __forceinline__ float log2_sum(float m, float l, float c) {
   return l > 0.0f ? m * c + log2f(l) : -__builtin_inff();
 }
 
-// Partial results of split i of n: o fp32 [split][B][2H][N][128], then the
-// log2 sums [split][B][2H][N].
+// Results of pieces of the keys, to be joined: o fp32 [piece][map][row][128],
+// then the log2 sums [piece][map][row], for `rows` rows: those of the tiles that
+// are split (tile after tile), or, where the few-row kernel splits, all
+// [B][H][N].
 struct Parts {
   float* o;
   float* l;
-  int64_t rows;  // B 2H N
+  int64_t rows;
 };
-__device__ __forceinline__ Parts parts_of(float* ws, const DiffShape& s, int nsplit) {
-  const int64_t rows = (int64_t)s.B * 2 * s.H * s.N;
-  return {ws, ws + rows * nsplit * D, rows};
+__device__ __forceinline__ Parts parts_of(float* ws, int64_t rows, int pieces) {
+  return {ws, ws + rows * 2 * pieces * D, rows};
+}
+
+// The tile and piece of a workgroup: tiles [0, full) whole, the rest in pieces.
+struct Piece {
+  int tile, piece, pieces;
+};
+__device__ __forceinline__ Piece piece_of(int wg, int tiles, const DiffTiles& p) {
+  if (wg < p.full) return {xcd_local_id(wg, p.full), 0, 1};
+  const int id = xcd_local_id(wg - p.full, (tiles - p.full) * p.pieces);
+  return {p.full + id / p.pieces, id % p.pieces, p.pieces};
+}
+// A tile's place in the batch: tiles of kDiffRows rows, head after head (the
+// last rows of a head first: under a causal mask they are the longest).
+struct RowTile {
+  int b, h, row0;
+};
+__device__ __forceinline__ RowTile row_tile(int tile, const DiffShape& s) {
+  const int per_head = (s.N + kDiffRows - 1) / kDiffRows;
+  const int bh = tile / per_head;
+  return {bh / s.H, bh % s.H, (per_head - 1 - tile % per_head) * kDiffRows};
+}
+__host__ __device__ inline int row_tiles_of(const DiffShape& s) {
+  return s.B * s.H * ((s.N + kDiffRows - 1) / kDiffRows);
 }
 
 // ------------------------------------------------------------------- forward
@@ -169,7 +193,7 @@ __device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
 constexpr int kFwdKeys = 32;
 constexpr float kTooMuch = 1.2089258e24f;
 template <bool kShared>
-__global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, int nsplit) {
+__global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, DiffTiles plan) {
   constexpr int kTiles = kShared ? 2 : 3;  // K (of each map), V
   constexpr int kV = kTiles - 1;
   constexpr int kKFrags = kShared ? 8 : 16, kFrags = 8 + kKFrags, kAhead = 6, kHold = 8;
@@ -178,15 +202,10 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, int nsplit)
   lds_poison_done();
   const DiffShape& s = A.s;
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
-  const int tiles = (s.N + kDiffRows - 1) / kDiffRows;
-  int id = xcd_local_id(blockIdx.x, gridDim.x);
-  const int split = id % nsplit;
-  id /= nsplit;
-  const int tile = tiles - 1 - id % tiles;  // causal: the long rows first
-  id /= tiles;
-  const int h = id % s.H, b = id / s.H;
+  const Piece pc = piece_of(blockIdx.x, row_tiles_of(s), plan);
+  const RowTile rt = row_tile(pc.tile, s);
+  const int b = rt.b, h = rt.h, row0 = rt.row0;
   const Seq sq = sequence(s, b);
-  const int row0 = tile * kDiffRows;
   if (row0 >= sq.qlen) return;
   const int per = s.H / s.Hv, hv = h / per;
   const int row = row0 + 32 * wave + l32;
@@ -199,11 +218,10 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, int nsplit)
   load_row(qf[0], A.q.p + b * A.q.sb + 2 * h * A.q.sh + (int64_t)row * A.q.sn, valid, hh);
   load_row(qf[1], A.q.p + b * A.q.sb + (2 * h + 1) * A.q.sh + (int64_t)row * A.q.sn, valid, hh);
 
-  const int2 range = split_keys(sq.klen, split, nsplit, kDiffKeys);
   const int last = min(row + sq.shift, sq.klen - 1);  // of this lane's row
   const int last_row = min(row0 + kDiffRows, sq.qlen) - 1;
-  const int kend = min(range.y, min(last_row + sq.shift, sq.klen - 1) + 1);
-  const int turns = kend > range.x ? (kend - range.x + kFwdKeys - 1) / kFwdKeys : 0;
+  const int2 range = split_keys(max(min(last_row + sq.shift, sq.klen - 1) + 1, 0), pc.piece, pc.pieces, kFwdKeys);
+  const int turns = (range.y - range.x + kFwdKeys - 1) / kFwdKeys;
   const int all_to = min(row0 + 32 * wave + sq.shift, sq.klen - 1);  // every row of the wave sees these
 
   const uint32_t at0 = lds_address(&lds[0][0][0]) + wave * kRowBlock;
@@ -404,12 +422,12 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, int nsplit)
       for (int r = 0; r < 16; ++r) x[m].o[d][r] *= inv;
   }
   if (!valid) return;
-  const int64_t at = ((int64_t)(b * 2 * s.H + 2 * h)) * s.N + row;
-  if (nsplit > 1) {
-    const Parts p = parts_of(A.ws, s, nsplit);
+  if (pc.pieces > 1) {
+    const Parts p = parts_of(A.ws, (int64_t)(row_tiles_of(s) - plan.full) * kDiffRows, pc.pieces);
+    const int64_t pr = (int64_t)(pc.tile - plan.full) * kDiffRows + row - row0;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const int64_t am = split * p.rows + at + m * s.N;
+      const int64_t am = (2 * pc.piece + m) * p.rows + pr;
       float* o = p.o + am * D + 4 * hh;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -422,6 +440,7 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, int nsplit)
     return;
   }
   if (A.lse && hh == 0) {
+    const int64_t at = ((int64_t)(b * 2 * s.H + 2 * h)) * s.N + row;
     A.lse[at] = l2[0] * kLn2;
     A.lse[at + s.N] = l2[1] * kLn2;
   }
@@ -551,7 +570,7 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
     }
   }
   __syncthreads();
-  const Parts p = parts_of(A.ws, s, nsplit);
+  const Parts p = parts_of(A.ws, (int64_t)s.B * s.H * s.N, nsplit);
   // one pair of dims of one row a thread and turn
   for (int i = t; i < n_rows * (D / 2); i += 256) {
     const int r = i / (D / 2), d = 2 * (i % (D / 2));
@@ -581,7 +600,7 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
     if (nsplit > 1) {
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
-        const int64_t am = split * p.rows + at + m * s.N;
+        const int64_t am = (2 * split + m) * p.rows + ((int64_t)b * s.H + hr) * s.N + n;
         *reinterpret_cast<float2*>(p.o + am * D + d) = o[m];
         if (d == 0) p.l[am] = l2[m];
       }
@@ -599,29 +618,40 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
   }
 }
 
-// The splits' results joined: a wave takes a row of an output head, two dims a
+// The pieces' results joined: a wave takes a row of an output head, two dims a
 // lane, both maps.
-__global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, int nsplit) {
+template <bool kFew>
+__global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, DiffTiles plan) {
   const DiffShape& s = A.s;
+  const int64_t rows = kFew ? (int64_t)s.B * s.H * s.N : (int64_t)(row_tiles_of(s) - plan.full) * kDiffRows;
   const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= (int64_t)s.B * s.H * s.N) return;
+  if (i >= rows) return;
   const int lane = threadIdx.x & 63;
-  const int n = (int)(i % s.N);
-  const int bh = (int)(i / s.N), h = bh % s.H, b = bh / s.H;
+  int b, h, n;
+  if (kFew) {
+    n = (int)(i % s.N);
+    const int bh = (int)(i / s.N);
+    h = bh % s.H;
+    b = bh / s.H;
+  } else {
+    const RowTile rt = row_tile(plan.full + (int)(i / kDiffRows), s);
+    b = rt.b;
+    h = rt.h;
+    n = rt.row0 + (int)(i % kDiffRows);
+  }
   if (n >= sequence(s, b).qlen) return;
-  const Parts p = parts_of(A.ws, s, nsplit);
+  const Parts p = parts_of(A.ws, rows, plan.pieces);
   float2 o[2];
   float l2[2];
-  int64_t at = ((int64_t)(b * 2 * s.H + 2 * h)) * s.N + n;
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    const int64_t am = at + m * s.N;
     float top = kNoMax, sum = 0.0f;
-    for (int u = 0; u < nsplit; ++u) top = fmaxf(top, p.l[u * p.rows + am]);
+    for (int u = 0; u < plan.pieces; ++u) top = fmaxf(top, p.l[(2 * u + m) * rows + i]);
     o[m] = make_float2(0.0f, 0.0f);
-    for (int u = 0; u < nsplit; ++u) {
-      const float f = __builtin_amdgcn_exp2f(p.l[u * p.rows + am] - top);
-      const float2 x = *reinterpret_cast<const float2*>(p.o + (u * p.rows + am) * D + 2 * lane);
+    for (int u = 0; u < plan.pieces; ++u) {
+      const int64_t am = (2 * u + m) * rows + i;
+      const float f = __builtin_amdgcn_exp2f(p.l[am] - top);
+      const float2 x = *reinterpret_cast<const float2*>(p.o + am * D + 2 * lane);
       sum += f;
       o[m].x = __builtin_fmaf(f, x.x, o[m].x);
       o[m].y = __builtin_fmaf(f, x.y, o[m].y);
@@ -634,8 +664,9 @@ __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, int nsplit) {
   const float lam = s.lambda[h];
   *reinterpret_cast<uint32_t*>(A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)n * A.out.sn + 2 * lane) =
       pack_bf16x2(__builtin_fmaf(-lam, o[1].x, o[0].x), __builtin_fmaf(-lam, o[1].y, o[0].y));
-  if (A.out2) *reinterpret_cast<uint32_t*>(A.out2 + i * D + 2 * lane) = pack_bf16x2(o[1].x, o[1].y);
-  if (A.lse && lane < 2) A.lse[at + lane * s.N] = (lane ? l2[1] : l2[0]) * kLn2;
+  if (A.out2)
+    *reinterpret_cast<uint32_t*>(A.out2 + (((int64_t)b * s.H + h) * s.N + n) * D + 2 * lane) = pack_bf16x2(o[1].x, o[1].y);
+  if (A.lse && lane < 2) A.lse[((int64_t)(b * 2 * s.H + 2 * h) + lane) * s.N + n] = (lane ? l2[1] : l2[0]) * kLn2;
 }
 
 // ------------------------------------------------------------------ backward
@@ -656,14 +687,15 @@ constexpr int kBwdRows = 32;
 constexpr int kStatFloats = 4 * kBwdRows;
 enum { kStatLse0 = 0, kStatLse1 = kBwdRows, kStatDelta0 = 2 * kBwdRows, kStatStep = 3 * kBwdRows };
 
-__global__ __launch_bounds__(256) void diff_stats_kernel(DiffBwd A) {
+__global__ __launch_bounds__(16 * kBwdRows) void diff_stats_kernel(DiffBwd A) {
+  __shared__ float second[kBwdRows];  // delta_1 of the rows
+  lds_poison(second, sizeof(second));
+  lds_poison_done();
   const DiffShape& s = A.s;
   const int row_tiles = (s.N + kBwdRows - 1) / kBwdRows;
-  const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  if (i >= (int64_t)s.B * s.H * row_tiles * kBwdRows) return;
-  const int cc = threadIdx.x & 15;
-  const int n = (int)(i % (row_tiles * kBwdRows));
-  const int bh = (int)(i / (row_tiles * kBwdRows)), h = bh % s.H, b = bh / s.H;
+  const int r = threadIdx.x >> 4, cc = threadIdx.x & 15;
+  const int n = (int)(blockIdx.x % row_tiles) * kBwdRows + r;
+  const int bh = blockIdx.x / row_tiles, h = bh % s.H, b = bh / s.H;
   const bool valid = n < sequence(s, b).qlen;
   float d0 = 0.0f, d1 = 0.0f;
   if (valid) {
@@ -686,9 +718,16 @@ __global__ __launch_bounds__(256) void diff_stats_kernel(DiffBwd A) {
   if (cc < 2) {
     const float lse = valid ? A.lse[((int64_t)bh * 2 + cc) * s.N + n] : 0.0f;
     const bool some = valid && lse > -3e38f;
-    float* st = A.stats + ((int64_t)bh * row_tiles + n / kBwdRows) * kStatFloats + n % kBwdRows;
+    float* st = A.stats + (int64_t)blockIdx.x * kStatFloats + r;
     st[cc ? kStatLse1 : kStatLse0] = some ? -lse / s.scale : -__builtin_inff();
     st[cc ? kStatStep : kStatDelta0] = !some ? 0.0f : cc ? d0 - d1 : -d0;
+    if (cc) second[r] = some ? d1 : 0.0f;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float x = 0.0f;
+    for (int i = 0; i < kBwdRows; ++i) x += second[i];
+    A.delta[blockIdx.x] = x;
   }
 }
 
@@ -708,23 +747,17 @@ struct Scores {
 // wave over all the keys they see.
 constexpr int kDqKeys = 32;
 template <bool kShared>
-__global__ __launch_bounds__(256, 1) void diff_dq_kernel(DiffBwd A) {
+__device__ __forceinline__ void dq_of(const DiffBwd& A, uint8_t (*lds)[kShared ? 2 : 3][kTile32], int wg) {
   constexpr int kTiles = kShared ? 2 : 3;  // K (of each map), V
   constexpr int kV = kTiles - 1;
   constexpr int kAhead = 8;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing][kTiles][kTile32];
-  lds_poison(lds, sizeof(lds));
-  lds_poison_done();
   const DiffShape& s = A.s;
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
-  const int tiles = (s.N + kDiffRows - 1) / kDiffRows;
-  int id = xcd_local_id(blockIdx.x, gridDim.x);
-  const int tile = tiles - 1 - id % tiles;  // causal: the long rows first
-  id /= tiles;
-  const int h = id % s.H, b = id / s.H;
+  const Piece pc = piece_of(wg, row_tiles_of(s), A.plan);
+  const RowTile rt = row_tile(pc.tile, s);
+  const int b = rt.b, h = rt.h, row0 = rt.row0;
   const Seq sq = sequence(s, b);
   const int per = s.H / s.Hv, hv = h / per;
-  const int row0 = tile * kDiffRows;
   const int row = row0 + 32 * wave + l32;
   const bool valid = row < sq.qlen;
   const float c = s.scale * kLog2e, lam = s.lambda[h];
@@ -747,8 +780,9 @@ __global__ __launch_bounds__(256, 1) void diff_dq_kernel(DiffBwd A) {
 
   const int last = min(row + sq.shift, sq.klen - 1);
   const int last_row = min(row0 + kDiffRows, sq.qlen) - 1;
-  const int kend = row0 < sq.qlen ? min(last_row + sq.shift, sq.klen - 1) + 1 : 0;
-  const int turns = kend > 0 ? (kend + kDqKeys - 1) / kDqKeys : 0;
+  const int2 range = split_keys(row0 < sq.qlen ? max(min(last_row + sq.shift, sq.klen - 1) + 1, 0) : 0, pc.piece, pc.pieces,
+                                kDqKeys);
+  const int turns = (range.y - range.x + kDqKeys - 1) / kDqKeys;
   const int all_to = min(row0 + 32 * wave + sq.shift, sq.klen - 1);  // every row of the wave sees these
 
   const uint32_t at0 = lds_address(&lds[0][0][0]) + wave * kRowBlock;
@@ -760,7 +794,7 @@ __global__ __launch_bounds__(256, 1) void diff_dq_kernel(DiffBwd A) {
     const uint16_t *k, *v;
     int key;
     uint32_t to, ok, ov;
-  } cp_ = {k0 + (int64_t)0 * A.k.sn, v0 + (int64_t)0 * A.v.sn, 0, 0u, copy_offset(copy_row, A.k.sn, lane),
+  } cp_ = {k0 + (int64_t)range.x * A.k.sn, v0 + (int64_t)range.x * A.v.sn, range.x, 0u, copy_offset(copy_row, A.k.sn, lane),
            copy_offset(copy_row, A.v.sn, lane)};
   auto copy_start = [&](int i, int place) __attribute__((always_inline)) {
     const bool on = i > 0 && i < turns;
@@ -846,11 +880,12 @@ __global__ __launch_bounds__(256, 1) void diff_dq_kernel(DiffBwd A) {
       }
       slot_end();
     });
-    if (i * kDqKeys + kDqKeys - 1 > all_to || i >= turns) {
+    const int key = range.x + i * kDqKeys;
+    if (key + kDqKeys - 1 > all_to || i >= turns) {
       const int to_key = i < turns ? last : -1;  // (past the last tile: none)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (i * kDqKeys + 4 * hh + 8 * (r >> 2) + (r & 3) > to_key) now.p[0][r] = now.p[1][r] = 0.0f;
+        if (key + 4 * hh + 8 * (r >> 2) + (r & 3) > to_key) now.p[0][r] = now.p[1][r] = 0.0f;
     }
   };
   if (turns > 0) {
@@ -876,7 +911,18 @@ __global__ __launch_bounds__(256, 1) void diff_dq_kernel(DiffBwd A) {
     }
     copies_landed<0>();  // none is under way when the wave ends
   }
-  if (row < s.N) {  // zero behind the sequence
+  if (pc.pieces > 1) {
+    float* o = A.dq_parts +
+               (((int64_t)(pc.tile - A.plan.full) * pc.pieces + pc.piece) * 2 * kDiffRows + row - row0) * D + 4 * hh;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4*>(o + m * kDiffRows * D + 32 * d + 8 * q) =
+              make_float4(dq[m][d][4 * q], dq[m][d][4 * q + 1], dq[m][d][4 * q + 2], dq[m][d][4 * q + 3]);
+  } else if (row < s.N) {  // zero behind the sequence
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const float f = m ? -lam * s.scale : s.scale;
@@ -899,18 +945,15 @@ __global__ __launch_bounds__(256, 1) void diff_dq_kernel(DiffBwd A) {
 // (the rows of P_1 sum to 1; delta_1 comes from a rounded output, and that
 // rounding cancels here).
 template <bool kShared>
-__global__ __launch_bounds__(256, 1) void diff_dkv_kernel(DiffBwd A) {
+__device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile32], float (*stat)[kStatFloats], int wg,
+                                       int wgs) {
   constexpr int kK = kShared ? 1 : 2;
   constexpr int kAhead = kShared ? 6 : 4;  // (registers)
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing][3][kTile32];  // q of map 0, of map 1, dout
-  __shared__ __attribute__((aligned(1024))) float stat[kRing][kStatFloats];
-  lds_poison(lds, sizeof(lds));
-  lds_poison(stat, sizeof(stat));
-  lds_poison_done();
+  // lds: q of map 0, of map 1, dout
   const DiffShape& s = A.s;
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
   const int tiles = (s.M + kDiffRows - 1) / kDiffRows;
-  int id = xcd_local_id(blockIdx.x, gridDim.x);
+  int id = xcd_local_id(wg, wgs);
   const int tile = id % tiles;  // causal: the long columns first
   id /= tiles;
   const int hv = id % s.Hv, b = id / s.Hv;
@@ -1163,48 +1206,121 @@ __global__ __launch_bounds__(256, 1) void diff_dkv_kernel(DiffBwd A) {
   }
 }
 
-// dlambda of a head: its parts and the rows' delta_1 summed in one order, in 64 bits.
-__global__ __launch_bounds__(256) void diff_dlambda_kernel(DiffBwd A) {
+// Both in one launch, the keys' workgroups first: what either leaves of the last
+// round of the chip's 256 CUs the other fills.
+template <bool kShared>
+__global__ __launch_bounds__(256, 1) void diff_bwd_kernel(DiffBwd A, int key_wgs) {
+  struct Keys {
+    uint8_t tiles[kRing][3][kTile32];
+    float stat[kRing][kStatFloats];
+  };
+  struct Queries {
+    uint8_t tiles[kRing][kShared ? 2 : 3][kTile32];
+  };
+  union Lds {
+    Keys keys;
+    Queries rows;
+  };
+  __shared__ __attribute__((aligned(1024))) Lds lds;
+  lds_poison(&lds, sizeof(lds));
+  lds_poison_done();
+  if ((int)blockIdx.x < key_wgs)
+    dkv_of<kShared>(A, lds.keys.tiles, lds.keys.stat, blockIdx.x, key_wgs);
+  else
+    dq_of<kShared>(A, lds.rows.tiles, blockIdx.x - key_wgs);
+}
+
+// Workgroups 0 .. H - 1: dlambda of a head, its keys' parts and its rows'
+// delta_1 summed in one order, in 64 bits.  The others: dq of a tile that was
+// split, the pieces summed in order, 8 rows of both maps a workgroup.
+constexpr int kJoinRows = 8;
+__global__ __launch_bounds__(256) void diff_end_kernel(DiffBwd A) {
   __shared__ double sum[256];
+  lds_poison(sum, sizeof(sum));
+  lds_poison_done();
   const DiffShape& s = A.s;
-  const int h = blockIdx.x;
-  const float* p = A.partial + (int64_t)h * s.B * A.parts;
-  double x = 0.0;
-  for (int64_t i = threadIdx.x; i < (int64_t)s.B * A.parts; i += 256) x += (double)p[i];
-  const int row_tiles = (s.N + kBwdRows - 1) / kBwdRows;
-  for (int b = 0; b < s.B; ++b) {
-    const float* st = A.stats + (int64_t)(b * s.H + h) * row_tiles * kStatFloats;
-    for (int i = threadIdx.x; i < row_tiles * kBwdRows; i += 256) {
-      const float* f = st + (int64_t)(i / kBwdRows) * kStatFloats + i % kBwdRows;
-      x -= (double)f[kStatDelta0] + (double)f[kStatStep];
+  if ((int)blockIdx.x < s.H) {
+    const int h = blockIdx.x;
+    const float* p = A.partial + (int64_t)h * s.B * A.parts;
+    double x = 0.0;
+    for (int64_t i = threadIdx.x; i < (int64_t)s.B * A.parts; i += 256) x += (double)p[i];
+    const int row_tiles = (s.N + kBwdRows - 1) / kBwdRows;
+    for (int b = 0; b < s.B; ++b) {
+      const float* d = A.delta + (int64_t)(b * s.H + h) * row_tiles;
+      for (int i = threadIdx.x; i < row_tiles; i += 256) x += (double)d[i];
     }
-  }
-  sum[threadIdx.x] = x;
-  __syncthreads();
-  for (int n = 128; n > 0; n >>= 1) {
-    if ((int)threadIdx.x < n) sum[threadIdx.x] += sum[threadIdx.x + n];
+    sum[threadIdx.x] = x;
     __syncthreads();
+    for (int n = 128; n > 0; n >>= 1) {
+      if ((int)threadIdx.x < n) sum[threadIdx.x] += sum[threadIdx.x + n];
+      __syncthreads();
+    }
+    if (threadIdx.x == 0) A.dlambda[h] = (float)-sum[0];
+    return;
   }
-  if (threadIdx.x == 0) A.dlambda[blockIdx.x] = (float)-sum[0];
+  const int w = blockIdx.x - s.H, tile = w / (kDiffRows / kJoinRows);
+  const int m = threadIdx.x >> 7, r = w % (kDiffRows / kJoinRows) * kJoinRows + ((threadIdx.x >> 4) & 7), cc = threadIdx.x & 15;
+  const RowTile rt = row_tile(A.plan.full + tile, s);
+  const int row = rt.row0 + r;
+  if (row >= s.N) return;
+  const bool valid = row < sequence(s, rt.b).qlen;
+  float f[8] = {};
+  for (int u = 0; u < A.plan.pieces && valid; ++u) {
+    const float4* p = reinterpret_cast<const float4*>(
+        A.dq_parts + (((int64_t)tile * A.plan.pieces + u) * 2 * kDiffRows + m * kDiffRows + r) * D + 8 * cc);
+    const float4 x = p[0], y = p[1];
+    f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+    f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+  }
+  const float scale = m ? -s.lambda[rt.h] * s.scale : s.scale;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] *= scale;
+  *reinterpret_cast<uint4*>(A.dq.p + rt.b * A.dq.sb + (2 * rt.h + m) * A.dq.sh + (int64_t)row * A.dq.sn + 8 * cc) =
+      pack_bf16x8(f);
 }
 
 }  // namespace
 
+constexpr int kCus = 256;  // each holds one workgroup of the tile kernels
+
+// Tiles that leave part of the chip idle, in their last round or alone, are cut
+// along the keys so that their pieces fill it; a piece has 512 keys or more.
+// Under a causal mask tiles differ in length and the last ones are the
+// shortest: only a call of less than one round is cut.
+static DiffTiles cut_tiles(int tiles, int full, int cus, int M) {
+  const int rest = tiles - full;
+  int pieces = rest > 0 ? cus / rest : 1;
+  if (pieces > M / 512) pieces = M / 512;
+  if (pieces > 16) pieces = 16;
+  if (pieces < 2) return {tiles, 1};
+  return {full, pieces};
+}
+
 DiffPlan diff_plan(const DiffShape& s) {
   DiffPlan p;
   p.few = (int64_t)(s.H / s.Hv) * s.N <= kFewRows;
-  const int64_t wgs = p.few ? (int64_t)s.B * s.Hv : (int64_t)s.B * s.H * ((s.N + kDiffRows - 1) / kDiffRows);
-  // the chip's 256 CUs hold one workgroup each; a split has 512 keys or more
-  int64_t n = 256 / wgs;
-  const int64_t most = s.M / 512;
-  if (n > most) n = most;
-  p.nsplit = (int)(n < 1 ? 1 : n);
+  if (p.few) {
+    const int64_t wgs = (int64_t)s.B * s.Hv;
+    int64_t n = kCus / wgs;
+    const int64_t most = s.M / 512;
+    if (n > most) n = most;
+    p.tiles = {0, (int)(n < 1 ? 1 : n)};
+  } else {
+    const int tiles = row_tiles_of(s);
+    const int full = tiles / kCus * kCus;
+    p.tiles = s.causal && full ? DiffTiles{tiles, 1} : cut_tiles(tiles, full, kCus, s.M);
+  }
   return p;
+}
+
+static size_t join_rows(const DiffShape& s, const DiffPlan& p) {
+  if (p.tiles.pieces < 2) return 0;
+  return p.few ? (size_t)s.B * s.H * s.N : (size_t)(row_tiles_of(s) - p.tiles.full) * kDiffRows;
 }
 
 size_t diff_fwd_bytes(const DiffShape& s) {
   const DiffPlan p = diff_plan(s);
-  return p.nsplit > 1 ? (size_t)p.nsplit * s.B * 2 * s.H * s.N * (D + 1) * sizeof(float) : 0;
+  return join_rows(s, p) * p.tiles.pieces * 2 * (D + 1) * sizeof(float);
 }
 
 hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
@@ -1212,47 +1328,83 @@ hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
   const DiffPlan p = diff_plan(s);
   const bool shared = s.Hk == s.Hv;
   if (p.few) {
-    const dim3 grid((unsigned)((int64_t)s.B * s.Hv * p.nsplit));
+    const dim3 grid((unsigned)((int64_t)s.B * s.Hv * p.tiles.pieces));
     if (shared)
-      hipLaunchKernelGGL(diff_few_kernel<true>, grid, dim3(256), 0, stream, a, p.nsplit);
+      hipLaunchKernelGGL(diff_few_kernel<true>, grid, dim3(256), 0, stream, a, p.tiles.pieces);
     else
-      hipLaunchKernelGGL(diff_few_kernel<false>, grid, dim3(256), 0, stream, a, p.nsplit);
+      hipLaunchKernelGGL(diff_few_kernel<false>, grid, dim3(256), 0, stream, a, p.tiles.pieces);
   } else {
-    const dim3 grid((unsigned)((int64_t)s.B * s.H * ((s.N + kDiffRows - 1) / kDiffRows) * p.nsplit));
+    const dim3 grid((unsigned)(p.tiles.full + (row_tiles_of(s) - p.tiles.full) * p.tiles.pieces));
     if (shared)
-      hipLaunchKernelGGL(diff_fwd_kernel<true>, grid, dim3(256), 0, stream, a, p.nsplit);
+      hipLaunchKernelGGL(diff_fwd_kernel<true>, grid, dim3(256), 0, stream, a, p.tiles);
     else
-      hipLaunchKernelGGL(diff_fwd_kernel<false>, grid, dim3(256), 0, stream, a, p.nsplit);
+      hipLaunchKernelGGL(diff_fwd_kernel<false>, grid, dim3(256), 0, stream, a, p.tiles);
   }
-  if (p.nsplit > 1) {
-    const int64_t rows = (int64_t)s.B * s.H * s.N;
-    hipLaunchKernelGGL(diff_join_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, p.nsplit);
+  if (const size_t rows = join_rows(s, p)) {
+    const dim3 grid((unsigned)((rows + 3) / 4));
+    if (p.few)
+      hipLaunchKernelGGL(diff_join_kernel<true>, grid, dim3(256), 0, stream, a, p.tiles);
+    else
+      hipLaunchKernelGGL(diff_join_kernel<false>, grid, dim3(256), 0, stream, a, p.tiles);
   }
   return hipGetLastError();
 }
 
-size_t diff_bwd_bytes(const DiffShape& s, size_t* partial_at, int* parts) {
-  const size_t stats = (size_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows) * kStatFloats * sizeof(float);
-  *partial_at = stats;
-  *parts = 4 * ((s.M + kDiffRows - 1) / kDiffRows);
-  return stats + (size_t)s.H * s.B * *parts * sizeof(float);
+// The backward launch: the keys' workgroups, then the rows'.  A row tile takes
+// 5/6 of a key tile's time over the same length (40 MFMAs a 32 x 32 block
+// against 48), times the heads that share a value head; the row tiles that would
+// stand past the time that the chip needs for all of it at best are cut along
+// the keys.
+static DiffTiles bwd_tiles(const DiffShape& s) {
+  const int tiles = row_tiles_of(s);
+  const int64_t keys = (int64_t)s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows);
+  // in units of an MFMA slot of one 128 x 32 block
+  const int64_t key_cost = (int64_t)(s.H / s.Hv) * ((s.N + 31) / 32) * 48, row_cost = (int64_t)((s.M + 31) / 32) * 40;
+  const int64_t best = (keys * key_cost + tiles * row_cost) / kCus;  // a CU's time if nothing idled
+  const int64_t round = keys / kCus, more = keys % kCus;             // `more` CUs take round + 1 key tiles
+  const int64_t a = best - round * key_cost, b = a - key_cost;
+  int64_t full = (kCus - more) * (a > 0 ? a / row_cost : 0) + more * (b > 0 ? b / row_cost : 0);
+  if (full > tiles) full = tiles;
+  if (s.causal && keys + tiles >= kCus) return {tiles, 1};
+  // what is left goes to the CUs' remaining time, about rest row_cost in all
+  return cut_tiles(tiles, (int)full, kCus, s.M);
+}
+
+size_t diff_bwd_bytes(const DiffShape& s, DiffBwd* a) {
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const size_t row_tiles = (size_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows);
+  const int parts = 4 * ((s.M + kDiffRows - 1) / kDiffRows);
+  const DiffTiles plan = bwd_tiles(s);
+  size_t at[4] = {};
+  at[0] = up(row_tiles * kStatFloats * sizeof(float));
+  at[1] = up(at[0] + row_tiles * sizeof(float));
+  at[2] = up(at[1] + (size_t)s.H * s.B * parts * sizeof(float));
+  at[3] = at[2];
+  if (plan.pieces > 1)
+    at[3] += (size_t)(row_tiles_of(s) - plan.full) * plan.pieces * 2 * kDiffRows * D * sizeof(float);
+  if (a) {
+    char* ws = reinterpret_cast<char*>(a->stats);
+    a->delta = reinterpret_cast<float*>(ws + at[0]);
+    a->partial = reinterpret_cast<float*>(ws + at[1]);
+    a->dq_parts = reinterpret_cast<float*>(ws + at[2]);
+    a->parts = parts;
+    a->plan = plan;
+  }
+  return at[3];
 }
 
 hipError_t launch_diff_bwd(const DiffBwd& a, hipStream_t stream) {
   const DiffShape& s = a.s;
-  const int64_t rows = (int64_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows) * kBwdRows;
-  const bool shared = s.Hk == s.Hv;
-  hipLaunchKernelGGL(diff_stats_kernel, dim3((unsigned)(rows / 16)), dim3(256), 0, stream, a);
-  const dim3 gq((unsigned)((int64_t)s.B * s.H * ((s.N + kDiffRows - 1) / kDiffRows)));
-  const dim3 gk((unsigned)((int64_t)s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows)));
-  if (shared) {
-    hipLaunchKernelGGL(diff_dq_kernel<true>, gq, dim3(256), 0, stream, a);
-    hipLaunchKernelGGL(diff_dkv_kernel<true>, gk, dim3(256), 0, stream, a);
-  } else {
-    hipLaunchKernelGGL(diff_dq_kernel<false>, gq, dim3(256), 0, stream, a);
-    hipLaunchKernelGGL(diff_dkv_kernel<false>, gk, dim3(256), 0, stream, a);
-  }
-  hipLaunchKernelGGL(diff_dlambda_kernel, dim3((unsigned)s.H), dim3(256), 0, stream, a);
+  const unsigned row_tiles = (unsigned)((int64_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows));
+  hipLaunchKernelGGL(diff_stats_kernel, dim3(row_tiles), dim3(16 * kBwdRows), 0, stream, a);
+  const int keys = s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows);
+  const int rest = row_tiles_of(s) - a.plan.full;
+  const dim3 grid((unsigned)(keys + a.plan.full + rest * a.plan.pieces));
+  if (s.Hk == s.Hv)
+    hipLaunchKernelGGL(diff_bwd_kernel<true>, grid, dim3(256), 0, stream, a, keys);
+  else
+    hipLaunchKernelGGL(diff_bwd_kernel<false>, grid, dim3(256), 0, stream, a, keys);
+  hipLaunchKernelGGL(diff_end_kernel, dim3((unsigned)(s.H + rest * (kDiffRows / kJoinRows))), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

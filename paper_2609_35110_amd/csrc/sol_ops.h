@@ -89,12 +89,16 @@ struct DiffShape {
   const float* lambda;
 };
 
-// How a forward call runs: with so few rows that a group's fit one wave (few),
-// and over how many pieces of the keys (their results joined by a second
-// launch through the workspace).
+// Row tiles [0, full) whole, the others in `pieces` pieces of their keys, whose
+// results another launch joins through the workspace.
+struct DiffTiles {
+  int full, pieces;
+};
+// How a forward call runs: with so few rows that a group's fit one wave (few,
+// its workgroups all cut), or in row tiles.
 struct DiffPlan {
   bool few;
-  int nsplit;
+  DiffTiles tiles;
 };
 DiffPlan diff_plan(const DiffShape& s);
 size_t diff_fwd_bytes(const DiffShape& s);
@@ -114,12 +118,16 @@ struct DiffBwd {
   const uint16_t* out2;
   const float* lse;
   float* dlambda;
-  float* stats;    // [B][H][ceil(N / 32)][4][32]
+  float* stats;    // [B][H][ceil(N / 32)][4][32]: the workspace's start
+  float* delta;    // [B][H][ceil(N / 32)]
   float* partial;  // [H][B][parts]
+  float* dq_parts; // [row tile that is cut][piece][map][128][128]
   int parts;
+  DiffTiles plan;
 };
-// Workspace: the rows' stats, then dlambda's parts.
-size_t diff_bwd_bytes(const DiffShape& s, size_t* partial_at, int* parts);
+// Bytes of workspace; with a given, its sections and plan are filled in (from
+// a->stats on).
+size_t diff_bwd_bytes(const DiffShape& s, DiffBwd* a);
 hipError_t launch_diff_bwd(const DiffBwd& a, hipStream_t stream);
 
 }  // namespace sol
