@@ -29,40 +29,73 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kC = kLinRows;
-struct ScanArgs {
-  const uint16_t *a, *b, *c;
-  int64_t a_b, a_h, a_n, b_b, b_h, b_n, c_b, c_h, c_n;
+constexpr int kTile = 2 * kTile32;  // bytes of a chunk's rows
+
+// One scan.  A launch takes up to kMaxScans of the same shape (the backward
+// pass's), whose workgroups take turns.
+constexpr int kMaxScans = 3;
+struct Scan {
+  Rows a, b, c;
   int a_div, b_div, c_div;  // head h of the scan reads head h / div
   void* y;                  // bf16, or fp32 when y_f32
   int64_t y_b, y_h, y_n;
   int y_f32;
-  const float* log_decay;
-  const float* state_in;  // the state before the first token of a segment
+  const float* state_in;  // the state before the first token
   int state_t;            // state_in is held transposed
-  float* state_out;       // one segment only: the state after the last token
-  float* states;          // [slab][segment][128][128]: local states out (state pass), states before in
-  const int32_t* lens;
-  int H, N, seg_rows, nseg;
-  int reverse;    // walk the tokens from the last one
-  int zero_tail;  // write zeros to the rows behind the sequence
+  float* state_out;       // the state after the last token (may be null)
+  float* before;          // several segments: the states before them, [slab][segment][128][128]
   float p, r, u;
   int off;
+  int reverse;    // walk the tokens from the last one
+  int zero_tail;  // write zeros to the rows behind the sequence
+};
+// The states that segments add, found in one pass for the scans that need them.
+struct SegmentStates {
+  Rows b, c;
+  int b_div, c_div;
+  const float* state_in;
+  int state_t;
+  float* state_out;
+  float* local;       // in: what the segments add; out: the states before them
+  float* transposed;  // the same, transposed (may be null)
+  float u;
+  int off;
+  int reverse;
+};
+struct Shape {
+  const float* log_decay;
+  const int32_t* lens;
+  int H, N, seg_rows, nseg;
+};
+struct ScanArgs {
+  Shape sh;
+  Scan scan[kMaxScans];
+  int n;
+};
+struct StateArgs {
+  Shape sh;
+  SegmentStates st[2];
+  int n;
 };
 
 __device__ __forceinline__ float decay_log2(const float* log_decay, int h) {
   // -inf (a head without memory) becomes a number whose multiple by 0 is 0
   return fmaxf(log_decay[h], -1e30f) * 1.44269504088896341f;
 }
+__device__ __forceinline__ int length_of(const Shape& s, int b) {
+  return s.lens ? __builtin_amdgcn_readfirstlane(min(max(s.lens[b], 0), s.N)) : s.N;
+}
 
-using Tile = Stage<kC, kThreads>;
-
-// The wave's 32 columns of the state as four 32 x 32 MFMA results: s[t][r] of
-// lane l is S[32t + 8(r/4) + 4(l/32) + r%4][32 wave + l%32].
+// The wave's 32 columns of the state as four 32 x 32 MFMA results.  Its rows are
+// dealt to the results so that a lane's eight consecutive registers are eight
+// consecutive rows -- the operand of a product with eight consecutive dims of a
+// row of a: register r of result t is row state_row, column 32 wave + l % 32.
 struct State {
   f32x16 s[4];
 };
-__device__ __forceinline__ int state_row(int t, int r, int hh) { return 32 * t + 8 * (r >> 2) + 4 * hh + (r & 3); }
-
+__device__ __forceinline__ int state_row(int t, int r, int hh) {
+  return 32 * t + 16 * (r >> 3) + 8 * hh + (r & 7);
+}
 __device__ __forceinline__ void load_state(State& st, const float* p, bool transposed, int col, int hh) {
 #pragma unroll
   for (int t = 0; t < 4; ++t)
@@ -78,18 +111,27 @@ __device__ __forceinline__ void store_state(const State& st, float* p, int col, 
 #pragma unroll
     for (int r = 0; r < 16; ++r) p[state_row(t, r, hh) * D + col] = st.s[t][r];
 }
+// This lane's place in the transpose reads of b: column l % 32 with bits 2 and 3
+// exchanged, which deals the rows of the state as above.
+__device__ __forceinline__ int state_col_place(int lane) {
+  const int g16 = lane >> 4, i16 = lane & 15, r = 4 * (g16 >> 1) + (i16 >> 2);
+  const int x = (i16 & 1) * 2 + ((i16 >> 1) & 1);  // four columns from 4 x
+  return r * 128 + ((2 * (g16 & 1) + (x >> 1)) ^ swizzle(r)) * 16 + (x & 1) * 8;
+}
 
 // S = (1 - fade) S + b^T (c w): the decay is taken off as a difference, so that
 // its rounding is relative to what is lost and slow heads (e^{64 g} next to 1)
-// do not drift over long sequences.  A weighted row of c enters as the sum of
-// two bf16 (the rounding and the rounding of the rest, 2^-17 together): the
-// state is an fp32 result of its own.
-__device__ __forceinline__ void update_state(State& st, float fade, const uint16_t* tb, const bf16x8 (&cf)[4],
-                                             const float* w, int tr_off, int hh) {
+// do not drift over long sequences.  A weighted row of c enters rounded to bf16,
+// and with kExact (a state that is a result of its own) as the sum of two bf16,
+// the rounding and the rounding of the rest, 2^-17 together.
+template <bool kExact>
+__device__ __forceinline__ void update_state(State& st, float fade, const uint8_t* tb, const bf16x8 (&cf)[4],
+                                             const float* w, int place, int hh) {
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) st.s[t][r] = __builtin_fmaf(st.s[t][r], -fade, st.s[t][r]);
+  bf16x8 hi[4], lo[4];
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks) {
     const float4 w0 = *reinterpret_cast<const float4*>(w + 16 * ks + 4 * hh);
@@ -98,125 +140,199 @@ __device__ __forceinline__ void update_state(State& st, float fade, const uint16
     unpack_bf16x8(__builtin_bit_cast(uint4, cf[ks]), x);
     x[0] *= w0.x; x[1] *= w0.y; x[2] *= w0.z; x[3] *= w0.w;
     x[4] *= w1.x; x[5] *= w1.y; x[6] *= w1.z; x[7] *= w1.w;
-    const uint4 hi = pack_bf16x8(x);
-    unpack_bf16x8(hi, rest);
+    const uint4 h = pack_bf16x8(x);
+    hi[ks] = __builtin_bit_cast(bf16x8, h);
+    if (kExact) {
+      unpack_bf16x8(h, rest);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rest[i] = x[i] - rest[i];
-    const uint4 lo = pack_bf16x8(rest);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const bf16x8 bt = column8(tb + 16 * ks * kStride + 32 * t + tr_off);
-      st.s[t] = mfma(bt, __builtin_bit_cast(bf16x8, hi), st.s[t]);
-      st.s[t] = mfma(bt, __builtin_bit_cast(bf16x8, lo), st.s[t]);
+      for (int i = 0; i < 8; ++i) rest[i] = x[i] - rest[i];
+      lo[ks] = __builtin_bit_cast(bf16x8, pack_bf16x8(rest));
     }
   }
+  // fragments four reads ahead
+  bf16x8 ring[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) ring[f] = col_frag(tb + place, 0, f);
+  slot_end();
+  // (the decayed state and the weighted rows two wait states before an MFMA reads them)
+  asm volatile("s_nop 1" : "+v"(st.s[0]), "+v"(st.s[1]), "+v"(st.s[2]), "+v"(st.s[3]));
+#pragma unroll
+  for (int f = 0; f < 16; ++f) {
+    const int ks = f >> 2, t = f & 3;
+    score(st.s[t], ring[f & 3], hi[ks]);
+    if (kExact) score(st.s[t], ring[f & 3], lo[ks]);
+    if (f + 4 < 16) ring[f & 3] = col_frag(tb + place, (f + 4) >> 2, t);
+    slot_end();
+  }
 }
 
-// What a workgroup of either pass finds out first: its slab, its rows and its
-// weights.
+// A value that all lanes hold, in a scalar register (a division leaves it in a
+// vector one).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// The walk of a workgroup over its segment's chunks: rows [row0, rows) of the
+// sequence in walking order.
 struct Walk {
-  int b, h, seg, len, row0, rows;  // rows [row0, rows) of the (reversed) sequence
-  const uint16_t *a, *bb, *c;
-  int64_t an, bn, cn;
+  int b, h, seg, len, row0, rows, chunks;
   float g2;
 };
-__device__ __forceinline__ Walk make_walk(const ScanArgs& A, int id) {
+__device__ __forceinline__ Walk make_walk(const Shape& s, int id) {
   Walk w;
-  const int slab = id / A.nseg;
-  w.seg = id - slab * A.nseg;
-  w.b = slab / A.H;
-  w.h = slab - w.b * A.H;
-  w.len = A.lens ? min(max(A.lens[w.b], 0), A.N) : A.N;
-  w.row0 = w.seg * A.seg_rows;
-  w.rows = min(w.row0 + A.seg_rows, w.len);
-  w.a = A.a + w.b * A.a_b + (w.h / A.a_div) * A.a_h;
-  w.bb = A.b + w.b * A.b_b + (w.h / A.b_div) * A.b_h;
-  w.c = A.c + w.b * A.c_b + (w.h / A.c_div) * A.c_h;
-  w.an = A.a_n;
-  w.bn = A.b_n;
-  w.cn = A.c_n;
-  if (A.reverse && w.len > 0) {
-    w.a += (int64_t)(w.len - 1) * w.an;
-    w.bb += (int64_t)(w.len - 1) * w.bn;
-    w.c += (int64_t)(w.len - 1) * w.cn;
-    w.an = -w.an;
-    w.bn = -w.bn;
-    w.cn = -w.cn;
-  }
-  w.g2 = decay_log2(A.log_decay, w.h);
+  const int slab = uniform(id / s.nseg);
+  w.seg = id - slab * s.nseg;
+  w.b = uniform(slab / s.H);
+  w.h = slab - w.b * s.H;
+  w.len = length_of(s, w.b);
+  w.row0 = w.seg * s.seg_rows;
+  w.rows = min(w.row0 + s.seg_rows, w.len);
+  w.chunks = w.rows > w.row0 ? (w.rows - w.row0 + kC - 1) / kC : 0;
+  w.g2 = decay_log2(s.log_decay, w.h);
   return w;
 }
+__device__ __forceinline__ const uint16_t* slab_of(const Rows& r, const Walk& w, int div) {
+  return r.p + w.b * r.sb + (w.h / div) * r.sh;
+}
+// A chunk's 64 rows of one tensor into LDS, four kilobytes a wave.  Rows past
+// the sequence are its last ones again (their weights are 0, and no result of
+// theirs is stored).
+__device__ __forceinline__ void copy_chunk(uint32_t lds, const uint16_t* slab, int64_t sn, const Walk& w, int chunk,
+                                           int reverse, int wave, int lane) {
+  const int i = w.row0 + chunk * kC, m = min(kC, w.rows - i);
+  const uint64_t at = reinterpret_cast<uint64_t>(slab + (int64_t)(reverse ? w.len - i - m : i) * sn);
+  // (a vector instruction's scalar result is five wait states from a copy's address)
+  const uint32_t lo = uniform((int)(uint32_t)at), hi = uniform((int)(uint32_t)(at >> 32));
+  const void* base = reinterpret_cast<const void*>(lo | (uint64_t)hi << 32);
+  asm volatile("s_nop 4" : "+s"(base));
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int r = min(8 * (2 * wave + u) + (lane >> 3), m - 1);
+    const uint32_t off = copy_offset(reverse ? m - 1 - r : r, sn, lane);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (2 * wave + u) * kRowBlock);
+    copy_1k(to, base, off);
+    copy_1k(to + 1024, base, off + 128);
+  }
+}
+constexpr int kChunkCopies = 4;  // of one tensor, by each wave
 
-// w[j] = u e^{g(m - off - j)} for the m rows of a chunk (rows past them are zero).
-__device__ __forceinline__ void fill_weights(float* w, const ScanArgs& A, float g2, int m) {
-  if (threadIdx.x < kC) w[threadIdx.x] = A.u * __builtin_amdgcn_exp2f(g2 * (float)max(m - A.off - (int)threadIdx.x, 0));
+// w[j] = u e^{g(m - off - j)} for the m rows of a chunk, 0 past them.
+__device__ __forceinline__ void fill_weights(float* w, float u, int off, float g2, int m) {
+  const int j = threadIdx.x;
+  if (j < kC) w[j] = j < m ? u * __builtin_amdgcn_exp2f(g2 * (float)max(m - off - j, 0)) : 0.0f;
 }
 __device__ __forceinline__ float fade_of(float g2, int m) { return -expm1f(g2 * 0.693147180559945309f * (float)m); }
 
-// The state that a segment adds, from zero: one pass over b and c.
-__global__ __launch_bounds__(kThreads, 2) void lin_state_kernel(ScanArgs A) {
-  __shared__ __attribute__((aligned(16))) uint16_t tb[kC * kStride], tc[kC * kStride];
-  __shared__ __attribute__((aligned(16))) float wt[kC];
-  lds_poison(tb, sizeof(tb));
-  lds_poison(tc, sizeof(tc));
+// The states that segments add, from zero: one pass over b and c.
+constexpr int kStateRing = 4;
+template <bool kExact>
+__global__ __launch_bounds__(kThreads, 2) void lin_state_kernel(StateArgs A) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStateRing][2][kTile];
+  __shared__ __attribute__((aligned(16))) float wt[2][kC];
+  lds_poison(lds, sizeof(lds));
   lds_poison(wt, sizeof(wt));
   lds_poison_done();
-  const int id = xcd_local_id(blockIdx.x, gridDim.x);
-  const Walk W = make_walk(A, id);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, hh = lane >> 5, l32 = lane & 31;
-  const int tr_off = column_offset(lane);
+  const int all = xcd_local_id(blockIdx.x, gridDim.x);
+  const int id = uniform(all / A.n);
+  const SegmentStates S = A.st[all - id * A.n];
+  const Walk W = make_walk(A.sh, id);
+  // the last segment's state is wanted by the final state alone
+  if (W.seg == A.sh.nseg - 1 && !S.state_out) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hh = lane >> 5, l32 = lane & 31;
+  const int place = state_col_place(lane), c_place = col_place(lane);
+  const uint16_t *pb = slab_of(S.b, W, S.b_div), *pc = slab_of(S.c, W, S.c_div);
+  const uint32_t at0 = lds_address(&lds[0][0][0]);
+  auto copy = [&](int i) __attribute__((always_inline)) {
+    const int chunk = min(i, W.chunks - 1);  // (past the last one: again, not used)
+    const uint32_t to = at0 + (i % kStateRing) * (2 * kTile);
+    copy_chunk(to, pb, S.b.sn, W, chunk, S.reverse, wave, lane);
+    copy_chunk(to + kTile, pc, S.c.sn, W, chunk, S.reverse, wave, lane);
+  };
   State st{};
-  Tile sb, sc;
-  sb.load(W.bb, W.bn, W.row0, W.rows, threadIdx.x);
-  sc.load(W.c, W.cn, W.row0, W.rows, threadIdx.x);
-  for (int row = W.row0; row < W.rows; row += kC) {
-    const int m = min(kC, W.rows - row);
-    sb.store(tb, threadIdx.x);
-    sc.store(tc, threadIdx.x);
-    if (row == W.row0 || m < kC) fill_weights(wt, A, W.g2, m);
-    __syncthreads();
-    sb.load(W.bb, W.bn, row + kC, W.rows, threadIdx.x);
-    sc.load(W.c, W.cn, row + kC, W.rows, threadIdx.x);
-    bf16x8 cf[4];
+  if (W.chunks > 0) {
+    float fade = fade_of(W.g2, kC);
+    fill_weights(wt[0], S.u, S.off, W.g2, min(kC, W.rows - W.row0));
+    all_landed();
+    copy(0);
+    copy(1);
+    for (int i = 0; i < W.chunks; ++i) {
+      const int m = min(kC, W.rows - W.row0 - i * kC);
+      if (m < kC) {  // the last chunk's own (the other buffer: this one may be in use)
+        if (i > 0) fill_weights(wt[1], S.u, S.off, W.g2, m);
+        fade = fade_of(W.g2, m);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      copies_landed<2 * kChunkCopies>();
+      copy(i + 2);
+      const uint8_t* tb = lds[i % kStateRing][0];
+      bf16x8 cf[4];
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) cf[ks] = column8(tc + 16 * ks * kStride + 32 * wave + tr_off);
-    update_state(st, fade_of(W.g2, m), tb, cf, wt, tr_off, hh);
-    __syncthreads();
+      for (int ks = 0; ks < 4; ++ks) cf[ks] = col_frag(lds[i % kStateRing][1] + c_place, ks, wave);
+      update_state<kExact>(st, fade, tb, cf, wt[m < kC && i > 0], place, hh);
+    }
+    copies_landed<0>();
   }
-  store_state(st, A.states + (int64_t)id * kStateElems, 32 * wave + l32, hh);
+  settle(st.s[0], st.s[1]);
+  settle(st.s[2], st.s[3]);
+  store_state(st, S.local + (int64_t)id * kStateElems, 32 * wave + l32, hh);
 }
 
-// The states before each segment, from the segments' own: in place, one
-// workgroup per slab and 1,024 of its state's values.
-__global__ __launch_bounds__(kThreads) void lin_join_kernel(ScanArgs A) {
-  const int slab = blockIdx.x >> 4, part = blockIdx.x & 15;
-  const int b = slab / A.H, h = slab - b * A.H;
-  const int len = A.lens ? min(max(A.lens[b], 0), A.N) : A.N;
-  const float g2 = decay_log2(A.log_decay, h);
-  const int e = part * 1024 + threadIdx.x * 4;
+// The states before each segment, from what the segments add: in place, one
+// workgroup per slab and 1,024 of its state's values, eight segments' loads in
+// flight.
+__global__ __launch_bounds__(kThreads) void lin_join_kernel(StateArgs A) {
+  const SegmentStates& S = A.st[blockIdx.x % A.n];
+  const int slab = blockIdx.x / A.n >> 4, part = (blockIdx.x / A.n) & 15;
+  const int b = slab / A.sh.H, h = slab - b * A.sh.H;
+  const int len = length_of(A.sh, b), nseg = A.sh.nseg;
+  const float g2 = decay_log2(A.sh.log_decay, h);
+  const int e = part * 1024 + threadIdx.x * 4, row = e >> 7, col = e & 127;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (A.state_in) {
-    const float* p = A.state_in + (int64_t)slab * kStateElems;
-    if (A.state_t) {
-      const int row = e >> 7, col = e & 127;
-      s = make_float4(p[col * D + row], p[(col + 1) * D + row], p[(col + 2) * D + row], p[(col + 3) * D + row]);
-    } else {
-      s = *reinterpret_cast<const float4*>(p + e);
+  if (S.state_in) {
+    const float* p = S.state_in + (int64_t)slab * kStateElems;
+    s = S.state_t ? make_float4(p[col * D + row], p[(col + 1) * D + row], p[(col + 2) * D + row], p[(col + 3) * D + row])
+                  : *reinterpret_cast<const float4*>(p + e);
+  }
+  float* seg = S.local + (int64_t)slab * nseg * kStateElems;
+  float* tr = S.transposed ? S.transposed + (int64_t)slab * nseg * kStateElems + col * D + row : nullptr;
+  const float whole = fade_of(g2, A.sh.seg_rows);
+  const int last = S.state_out ? nseg : nseg - 1;  // segments whose own state was found
+  constexpr int kBatch = 8;
+  for (int i0 = 0; i0 < nseg; i0 += kBatch) {
+    float4 x[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i0 + u < last) x[u] = *reinterpret_cast<const float4*>(seg + (int64_t)(i0 + u) * kStateElems + e);
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int i = i0 + u;
+      if (i < nseg) {
+        *reinterpret_cast<float4*>(seg + (int64_t)i * kStateElems + e) = s;
+        if (tr) {
+          float* t = tr + (int64_t)i * kStateElems;
+          t[0] = s.x;
+          t[D] = s.y;
+          t[2 * D] = s.z;
+          t[3 * D] = s.w;
+        }
+        const int m = min(max(len - i * A.sh.seg_rows, 0), A.sh.seg_rows);
+        const float fade = m == A.sh.seg_rows ? whole : fade_of(g2, m);
+        s.x = __builtin_fmaf(s.x, -fade, s.x) + x[u].x;
+        s.y = __builtin_fmaf(s.y, -fade, s.y) + x[u].y;
+        s.z = __builtin_fmaf(s.z, -fade, s.z) + x[u].z;
+        s.w = __builtin_fmaf(s.w, -fade, s.w) + x[u].w;
+      }
     }
   }
-  float4* seg = reinterpret_cast<float4*>(A.states + (int64_t)slab * A.nseg * kStateElems + e);
-  float4 x = seg[0];
-  for (int i = 0; i < A.nseg; ++i) {
-    const float4 next = seg[(int64_t)min(i + 1, A.nseg - 1) * (kStateElems / 4)];
-    seg[(int64_t)i * (kStateElems / 4)] = s;
-    const float fade = fade_of(g2, min(max(len - i * A.seg_rows, 0), A.seg_rows));
-    s.x = __builtin_fmaf(s.x, -fade, s.x) + x.x;
-    s.y = __builtin_fmaf(s.y, -fade, s.y) + x.y;
-    s.z = __builtin_fmaf(s.z, -fade, s.z) + x.z;
-    s.w = __builtin_fmaf(s.w, -fade, s.w) + x.w;
-    x = next;
-  }
-  if (A.state_out) *reinterpret_cast<float4*>(A.state_out + (int64_t)slab * kStateElems + e) = s;
+  if (S.state_out) *reinterpret_cast<float4*>(S.state_out + (int64_t)slab * kStateElems + e) = s;
+}
+
+// a b^T of 32 rows each over the 128 dims, in two halves (two chains of MFMAs).
+__device__ __forceinline__ void tile_product(f32x16 (&s)[2], const bf16x8 (&bf)[8], const bf16x8 (&af)[8]) {
+  score_first(s[0], bf[0], af[0]);
+  score_first(s[1], bf[1], af[1]);
+#pragma unroll
+  for (int kk = 2; kk < 8; ++kk) score(s[kk & 1], bf[kk], af[kk]);
 }
 
 // y over a segment.  A wave owns 32 columns of the state and of y: the state
@@ -225,42 +341,67 @@ __global__ __launch_bounds__(kThreads) void lin_join_kernel(ScanArgs A) {
 // roundings are of the same size).  The C x C products are shared: waves 0 to 2
 // find the three 32 x 32 tiles on and below the diagonal, and pass them round
 // in the order the next product reads them.
+//
+// Its bytes bound it: a CU's share of a copy's rate is 64 KB (a chunk's a, b, c
+// and y) in 6,800 cycles, the products of a chunk take 1,500 of the matrix
+// cores.  So one workgroup a CU, the chunks straight into LDS in a ring of
+// three, two on their way.
+constexpr int kScanRing = 3;
+template <bool kExact>
 __global__ __launch_bounds__(kThreads, 2) void lin_scan_kernel(ScanArgs A) {
-  __shared__ __attribute__((aligned(16))) uint16_t ta[kC * kStride], tb[kC * kStride], tc[kC * kStride];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kScanRing][3][kTile];
   __shared__ __attribute__((aligned(16))) uint4 pf[3][2][64];  // tiles (0,0), (1,0), (1,1): 16 columns, lane
-  __shared__ __attribute__((aligned(16))) float wt[kC];
-  lds_poison(ta, sizeof(ta));
-  lds_poison(tb, sizeof(tb));
-  lds_poison(tc, sizeof(tc));
+  __shared__ __attribute__((aligned(16))) float wt[2][kC];
+  lds_poison(lds, sizeof(lds));
   lds_poison(pf, sizeof(pf));
   lds_poison(wt, sizeof(wt));
   lds_poison_done();
-  const int id = xcd_local_id(blockIdx.x, gridDim.x);
-  const Walk W = make_walk(A, id);
-  const int slab = W.b * A.H + W.h;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, hh = lane >> 5, l32 = lane & 31;
-  const int tr_off = column_offset(lane);
+  const int all = xcd_local_id(blockIdx.x, gridDim.x);
+  const int id = uniform(all / A.n);
+  const Scan S = A.scan[all - id * A.n];
+  const Walk W = make_walk(A.sh, id);
+  const int slab = W.b * A.sh.H + W.h;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hh = lane >> 5, l32 = lane & 31;
   const int col = 32 * wave + l32;
+  const int64_t y0 = W.b * S.y_b + W.h * S.y_h;
 
-  if (A.zero_tail) {  // rows of this segment behind the sequence
+  if (S.zero_tail) {  // rows of this segment behind the sequence
     const int r = threadIdx.x >> 4, cc = threadIdx.x & 15;
-    const int end = min(W.row0 + A.seg_rows, A.N);
+    const int end = min(W.row0 + A.sh.seg_rows, A.sh.N);
     for (int i = max(W.row0, W.len) + r; i < end; i += 16) {
-      const int64_t at = W.b * A.y_b + W.h * A.y_h + (int64_t)i * A.y_n + cc * 8;
-      if (A.y_f32) {
-        float4* y = reinterpret_cast<float4*>(static_cast<float*>(A.y) + at);
+      const int64_t at = y0 + (int64_t)i * S.y_n + cc * 8;
+      if (S.y_f32) {
+        float4* y = reinterpret_cast<float4*>(static_cast<float*>(S.y) + at);
         y[0] = y[1] = make_float4(0.f, 0.f, 0.f, 0.f);
       } else {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(A.y) + at) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(S.y) + at) = make_uint4(0, 0, 0, 0);
       }
     }
   }
+  if (W.chunks == 0) {  // (of a sequence without tokens, the first and last segment)
+    if (A.sh.nseg == 1 && S.state_out)
+      for (int e = threadIdx.x; e < kStateElems; e += kThreads)
+        S.state_out[(int64_t)slab * kStateElems + e] =
+            !S.state_in ? 0.0f : S.state_in[(int64_t)slab * kStateElems + (S.state_t ? (e & 127) * D + (e >> 7) : e)];
+    return;
+  }
 
+  const RowPlace rp = row_place(lane);
+  const int place = state_col_place(lane), c_place = col_place(lane);
+  const uint16_t *pa = slab_of(S.a, W, S.a_div), *pb = slab_of(S.b, W, S.b_div), *pc = slab_of(S.c, W, S.c_div);
+  const uint32_t at0 = lds_address(&lds[0][0][0]);
+  auto copy = [&](int i) __attribute__((always_inline)) {
+    const int chunk = min(i, W.chunks - 1);  // (past the last one: again, not used)
+    const uint32_t to = at0 + (i % kScanRing) * (3 * kTile);
+    copy_chunk(to, pa, S.a.sn, W, chunk, S.reverse, wave, lane);
+    copy_chunk(to + kTile, pb, S.b.sn, W, chunk, S.reverse, wave, lane);
+    copy_chunk(to + 2 * kTile, pc, S.c.sn, W, chunk, S.reverse, wave, lane);
+  };
   State st{};
-  if (A.nseg > 1)
-    load_state(st, A.states + (int64_t)id * kStateElems, false, col, hh);
-  else if (A.state_in)
-    load_state(st, A.state_in + (int64_t)slab * kStateElems, A.state_t, col, hh);
+  if (A.sh.nseg > 1)
+    load_state(st, S.before + (int64_t)id * kStateElems, false, col, hh);
+  else if (S.state_in)
+    load_state(st, S.state_in + (int64_t)slab * kStateElems, S.state_t, col, hh);
 
   // this wave's tile of the C x C product: rows 32 I + .. of a, 32 J + .. of b,
   // held transposed (lane: row of a), and its weights
@@ -269,88 +410,117 @@ __global__ __launch_bounds__(kThreads, 2) void lin_scan_kernel(ScanArgs A) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int gap = (32 * I + l32) - (32 * J + 8 * (r >> 2) + 4 * hh + (r & 3));
-    dec[r] = gap >= 0 ? A.p * __builtin_amdgcn_exp2f(W.g2 * (float)gap) : 0.0f;
+    dec[r] = gap >= 0 ? S.p * __builtin_amdgcn_exp2f(W.g2 * (float)gap) : 0.0f;
   }
-  const float win[2] = {A.r * __builtin_amdgcn_exp2f(W.g2 * (float)(l32 + A.off)),
-                        A.r * __builtin_amdgcn_exp2f(W.g2 * (float)(32 + l32 + A.off))};
-
-  Tile sa, sb, sc;
-  sa.load(W.a, W.an, W.row0, W.rows, threadIdx.x);
-  sb.load(W.bb, W.bn, W.row0, W.rows, threadIdx.x);
-  sc.load(W.c, W.cn, W.row0, W.rows, threadIdx.x);
-  for (int row = W.row0; row < W.rows; row += kC) {
-    const int m = min(kC, W.rows - row);
-    sa.store(ta, threadIdx.x);
-    sb.store(tb, threadIdx.x);
-    sc.store(tc, threadIdx.x);
-    if (row == W.row0 || m < kC) fill_weights(wt, A, W.g2, m);
-    __syncthreads();
-    sa.load(W.a, W.an, row + kC, W.rows, threadIdx.x);
-    sb.load(W.bb, W.bn, row + kC, W.rows, threadIdx.x);
-    sc.load(W.c, W.cn, row + kC, W.rows, threadIdx.x);
-    if (wave < 3) {
-      f32x16 s = {};
+  const float win[2] = {S.r * __builtin_amdgcn_exp2f(W.g2 * (float)(l32 + S.off)),
+                        S.r * __builtin_amdgcn_exp2f(W.g2 * (float)(32 + l32 + S.off))};
+  float fade = fade_of(W.g2, kC);
+  fill_weights(wt[0], S.u, S.off, W.g2, min(kC, W.rows - W.row0));
+  constexpr int kStores = 8;  // of y, by each wave and chunk
+  all_landed();
+  copy(0);
+  copy(1);
+  for (int i = 0; i < W.chunks; ++i) {
+    const int row = W.row0 + i * kC, m = min(kC, W.rows - row);
+    if (m < kC) {  // the last chunk's own (the other buffer: this one may be in use)
+      if (i > 0) fill_weights(wt[1], S.u, S.off, W.g2, m);
+      fade = fade_of(W.g2, m);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    // this chunk's copies: behind them the next one's, and from the second
+    // chunk on the last one's stores (every chunk but the last stores 8 times)
+    if (i == 0)
+      copies_landed<3 * kChunkCopies>();
+    else
+      copies_landed<3 * kChunkCopies + kStores>();
+    copy(i + 2);
+    const uint8_t *ta = lds[i % kScanRing][0], *tb = lds[i % kScanRing][1], *tc = lds[i % kScanRing][2];
+    bf16x8 af[2][8], cf[4];
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {
-        s = mfma(row8(tb + 32 * J * kStride, lane, kk), row8(ta + 32 * I * kStride, lane, kk), s);
-      }
+    for (int kk = 0; kk < 8; ++kk) af[0][kk] = row_frag(ta, rp, kk);
+    if (wave < 3) {
+      bf16x8 bf[8];
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) bf[kk] = row_frag(tb + J * kTile32, rp, kk);
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) af[1][kk] = row_frag(ta + kTile32, rp, kk);
+      slot_end();
+      f32x16 s[2];
+      if (wave == 0)
+        tile_product(s, bf, af[0]);
+      else
+        tile_product(s, bf, af[1]);
+      settle(s[0], s[1]);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         float f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = s[8 * x + i] * dec[8 * x + i];
+        for (int r = 0; r < 8; ++r) f[r] = (s[0][8 * x + r] + s[1][8 * x + r]) * dec[8 * x + r];
         pf[wave][x][lane] = pack_bf16x8(f);
       }
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) af[1][kk] = row_frag(ta + kTile32, rp, kk);
     }
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) cf[ks] = col_frag(tc + c_place, ks, wave);
     // y^T = S^T a^T, each row's weight on its lane
-    f32x16 y[2] = {};
+    f32x16 y[2];
+    bf16x8 sf[8];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int kk = 0; kk < 8; ++kk) sf[kk] = operand8(st.s[kk >> 1], kk & 1);
+    hold_in_vgprs(sf);
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const bf16x8 sf = operand8(st.s[t], x);
-#pragma unroll
-        for (int i2 = 0; i2 < 2; ++i2) {
-          const uint16_t* p = ta + (32 * i2 + l32) * kStride + 32 * t + 16 * x + 4 * hh;
-          const uint2 lo = *reinterpret_cast<const uint2*>(p), hi = *reinterpret_cast<const uint2*>(p + 8);
-          y[i2] = mfma(sf, __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y)), y[i2]);
-        }
+    for (int kk = 0; kk < 8; ++kk) {
+      if (kk == 0) {
+        score_first(y[0], sf[kk], af[0][kk]);
+        score_first(y[1], sf[kk], af[1][kk]);
+      } else {
+        score(y[0], sf[kk], af[0][kk]);
+        score(y[1], sf[kk], af[1][kk]);
       }
+    }
+    settle(y[0], y[1]);
 #pragma unroll
-    for (int i2 = 0; i2 < 2; ++i2)
+    for (int r = 0; r < 16; ++r) {
+      y[0][r] *= win[0];
+      y[1][r] *= win[1];
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    bf16x8 pt[3][2];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) y[i2][r] *= win[i2];
-    bf16x8 cf[4];
+    for (int t = 0; t < 3; ++t)
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) cf[ks] = column8(tc + 16 * ks * kStride + 32 * wave + tr_off);
-    __syncthreads();
+      for (int x = 0; x < 2; ++x) pt[t][x] = __builtin_bit_cast(bf16x8, pf[t][x][lane]);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      y[0] = mfma(cf[x], __builtin_bit_cast(bf16x8, pf[0][x][lane]), y[0]);
-      y[1] = mfma(cf[x], __builtin_bit_cast(bf16x8, pf[1][x][lane]), y[1]);
-      y[1] = mfma(cf[2 + x], __builtin_bit_cast(bf16x8, pf[2][x][lane]), y[1]);
+      score(y[0], cf[x], pt[0][x]);
+      score(y[1], cf[x], pt[1][x]);
+      score(y[1], cf[2 + x], pt[2][x]);
     }
+    update_state<kExact>(st, fade, tb, cf, wt[m < kC && i > 0], place, hh);
 #pragma unroll
     for (int i2 = 0; i2 < 2; ++i2) {
-      const int i = row + 32 * i2 + l32;
-      if (i < W.rows) {
-        const int n = A.reverse ? W.len - 1 - i : i;
-        const int64_t at = W.b * A.y_b + W.h * A.y_h + (int64_t)n * A.y_n + 32 * wave + 4 * hh;
+      const int j = row + 32 * i2 + l32;
+      if (j < W.rows) {
+        const int n = S.reverse ? W.len - 1 - j : j;
+        const int64_t at = y0 + (int64_t)n * S.y_n + 32 * wave + 4 * hh;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          if (A.y_f32)
-            *reinterpret_cast<float4*>(static_cast<float*>(A.y) + at + 8 * x) =
+          if (S.y_f32)
+            *reinterpret_cast<float4*>(static_cast<float*>(S.y) + at + 8 * x) =
                 make_float4(y[i2][4 * x], y[i2][4 * x + 1], y[i2][4 * x + 2], y[i2][4 * x + 3]);
           else
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(A.y) + at + 8 * x) =
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(S.y) + at + 8 * x) =
                 make_uint2(pack_bf16x2(y[i2][4 * x], y[i2][4 * x + 1]), pack_bf16x2(y[i2][4 * x + 2], y[i2][4 * x + 3]));
         }
       }
     }
-    update_state(st, fade_of(W.g2, m), tb, cf, wt, tr_off, hh);
-    __syncthreads();
   }
-  if (A.nseg == 1 && A.state_out) store_state(st, A.state_out + (int64_t)slab * kStateElems, col, hh);
+  copies_landed<0>();  // none is under way when the wave ends
+  settle(st.s[0], st.s[1]);
+  settle(st.s[2], st.s[3]);
+  if (A.sh.nseg == 1 && S.state_out) store_state(st, S.state_out + (int64_t)slab * kStateElems, col, hh);
 }
 
 // Gradients of shared heads: the sum, in head order, of the group's fp32 parts,
@@ -442,57 +612,50 @@ __global__ __launch_bounds__(kThreads) void lin_step_kernel(LinStep A) {
   }
 }
 
-// The state pass and the join where there are several segments, then the scan.
-hipError_t launch_scan(ScanArgs& A, int64_t slabs, hipStream_t stream) {
-  const LinPlan plan = lin_plan(slabs, A.N);
-  A.seg_rows = plan.seg_rows;
-  A.nseg = plan.nseg;
-  const unsigned wgs = (unsigned)(slabs * plan.nseg);
-  if (plan.nseg > 1) {
-    hipLaunchKernelGGL(lin_state_kernel, dim3(wgs), dim3(kThreads), 0, stream, A);
-    hipLaunchKernelGGL(lin_join_kernel, dim3((unsigned)(slabs * 16)), dim3(kThreads), 0, stream, A);
+// The state pass and the join where there are several segments, then the scans.
+hipError_t launch_scans(const StateArgs& st, const ScanArgs& sc, int64_t slabs, bool exact_states, bool exact_scan,
+                        hipStream_t stream) {
+  const unsigned wgs = (unsigned)(slabs * sc.sh.nseg);
+  if (sc.sh.nseg > 1) {
+    if (exact_states)
+      hipLaunchKernelGGL(lin_state_kernel<true>, dim3(wgs * st.n), dim3(kThreads), 0, stream, st);
+    else
+      hipLaunchKernelGGL(lin_state_kernel<false>, dim3(wgs * st.n), dim3(kThreads), 0, stream, st);
+    hipLaunchKernelGGL(lin_join_kernel, dim3((unsigned)(slabs * 16 * st.n)), dim3(kThreads), 0, stream, st);
   }
-  hipLaunchKernelGGL(lin_scan_kernel, dim3(wgs), dim3(kThreads), 0, stream, A);
+  if (exact_scan)
+    hipLaunchKernelGGL(lin_scan_kernel<true>, dim3(wgs * sc.n), dim3(kThreads), 0, stream, sc);
+  else
+    hipLaunchKernelGGL(lin_scan_kernel<false>, dim3(wgs * sc.n), dim3(kThreads), 0, stream, sc);
   return hipGetLastError();
 }
 
-void set_rows(const uint16_t*& p, int64_t& sb, int64_t& sh, int64_t& sn, const Rows& r) {
-  p = r.p;
-  sb = r.sb;
-  sh = r.sh;
-  sn = r.sn;
+Shape shape_of(const float* log_decay, const int32_t* lens, int B, int H, int N) {
+  const LinPlan plan = lin_plan((int64_t)B * H, N);
+  return {log_decay, lens, H, N, plan.seg_rows, plan.nseg};
 }
 
-ScanArgs scan_args(const Rows& a, int a_div, const Rows& b, int b_div, const Rows& c, int c_div, const float* log_decay,
-                   const int32_t* lens, int H, int N, float* states) {
-  ScanArgs A = {};
-  set_rows(A.a, A.a_b, A.a_h, A.a_n, a);
-  set_rows(A.b, A.b_b, A.b_h, A.b_n, b);
-  set_rows(A.c, A.c_b, A.c_h, A.c_n, c);
-  A.a_div = a_div;
-  A.b_div = b_div;
-  A.c_div = c_div;
-  A.log_decay = log_decay;
-  A.lens = lens;
-  A.H = H;
-  A.N = N;
-  A.states = states;
-  return A;
-}
-
-void set_out(ScanArgs& A, const Rows& y) {
-  A.y = y.p;
-  A.y_b = y.sb;
-  A.y_h = y.sh;
-  A.y_n = y.sn;
+Scan scan_of(const Rows& a, int a_div, const Rows& b, int b_div, const Rows& c, int c_div, const Rows& y) {
+  Scan s = {};
+  s.a = a;
+  s.b = b;
+  s.c = c;
+  s.a_div = a_div;
+  s.b_div = b_div;
+  s.c_div = c_div;
+  s.y = y.p;
+  s.y_b = y.sb;
+  s.y_h = y.sh;
+  s.y_n = y.sn;
+  return s;
 }
 
 }  // namespace
 
 LinPlan lin_plan(int64_t slabs, int N) {
-  // two workgroups on each of the 256 CUs, in segments of at least 256 tokens
+  // one workgroup on each of the 256 CUs, in segments of at least 256 tokens
   const int chunks = (N + kC - 1) / kC;
-  int64_t nseg = 512 / slabs;
+  int64_t nseg = 256 / slabs;
   nseg = nseg < 1 ? 1 : nseg;
   const int most = (chunks + 3) / 4;
   if (nseg > most) nseg = most;
@@ -507,66 +670,87 @@ size_t lin_states_bytes(int64_t slabs, int N) {
 
 hipError_t launch_lin_fwd(const LinFwd& a, hipStream_t stream) {
   const int per = a.H / a.Hk;
-  ScanArgs A = scan_args(a.q, 1, a.k, per, a.v, per, a.log_decay, a.lens, a.H, a.N, a.states);
-  set_out(A, a.out);
-  A.state_in = a.state_in;
-  A.state_out = a.state_out;
-  A.p = A.r = a.scale;
-  A.u = 1.0f;
-  A.off = 1;
-  return launch_scan(A, (int64_t)a.B * a.H, stream);
+  ScanArgs sc = {};
+  sc.sh = shape_of(a.log_decay, a.lens, a.B, a.H, a.N);
+  sc.n = 1;
+  Scan& s = sc.scan[0];
+  s = scan_of(a.q, 1, a.k, per, a.v, per, a.out);
+  s.state_in = a.state_in;
+  s.state_out = a.state_out;
+  s.before = a.states;
+  s.p = s.r = a.scale;
+  s.u = 1.0f;
+  s.off = 1;
+  StateArgs st = {};
+  st.sh = sc.sh;
+  st.n = 1;
+  st.st[0] = {a.k, a.v, per, per, a.state_in, 0, a.state_out, a.states, nullptr, 1.0f, 1, 0};
+  const bool exact = a.state_out != nullptr;
+  return launch_scans(st, sc, (int64_t)a.B * a.H, exact, exact && sc.sh.nseg == 1, stream);
 }
 
+// The three gradients in one launch (dq forwards; dk and dv backwards, side by
+// side, so that the second to read a row finds it in L2); the states of dk are
+// those of dv transposed.
 hipError_t launch_lin_bwd(const LinBwd& a, hipStream_t stream) {
   const int per = a.H / a.Hk;
-  const int64_t slabs = (int64_t)a.B * a.H;
-  {
-    ScanArgs A = scan_args(a.dout, 1, a.v, per, a.k, per, a.log_decay, a.lens, a.H, a.N, a.states);
-    set_out(A, a.dq);
-    A.state_in = a.state_in;
-    A.state_t = 1;
-    A.p = A.r = a.scale;
-    A.u = 1.0f;
-    A.off = 1;
-    A.zero_tail = 1;
-    const hipError_t e = launch_scan(A, slabs, stream);
-    if (e != hipSuccess) return e;
-  }
-  // dk, then dv, whose state is the gradient of the initial state (and may be
-  // written over the one that both read)
-  for (int which = 0; which < 2; ++which) {
-    ScanArgs A = which == 0 ? scan_args(a.v, per, a.dout, 1, a.q, 1, a.log_decay, a.lens, a.H, a.N, a.states)
-                            : scan_args(a.k, per, a.q, 1, a.dout, 1, a.log_decay, a.lens, a.H, a.N, a.states);
-    const Rows& y = which == 0 ? a.dk : a.dv;
-    float* part = a.partial ? a.partial + which * slabs * a.N * D : nullptr;
-    if (part) {
-      A.y = part;
-      A.y_f32 = 1;
-      A.y_n = D;
-      A.y_h = (int64_t)a.N * D;
-      A.y_b = a.H * A.y_h;
-    } else {
-      set_out(A, y);
+  const int64_t slabs = (int64_t)a.B * a.H, elems = slabs * a.N * D;
+  ScanArgs sc = {};
+  sc.sh = shape_of(a.log_decay, a.lens, a.B, a.H, a.N);
+  sc.n = 3;
+  const int64_t sec = slabs * sc.sh.nseg * kStateElems;  // floats of the segments' states
+  sc.scan[0] = scan_of(a.dout, 1, a.v, per, a.k, per, a.dq);
+  sc.scan[1] = scan_of(a.v, per, a.dout, 1, a.q, 1, a.dk);
+  sc.scan[2] = scan_of(a.k, per, a.q, 1, a.dout, 1, a.dv);
+  for (int i = 0; i < 3; ++i) {
+    Scan& s = sc.scan[i];
+    s.before = a.states + i * sec;
+    s.state_in = i == 0 ? a.state_in : a.dstate_in;
+    s.state_t = i < 2;
+    s.p = a.scale;
+    s.r = i == 0 ? a.scale : 1.0f;
+    s.u = i == 0 ? 1.0f : a.scale;
+    s.off = i == 0;
+    s.reverse = i > 0;
+    s.zero_tail = 1;
+    if (i > 0 && a.partial) {
+      s.y = a.partial + (i - 1) * elems;
+      s.y_f32 = 1;
+      s.y_n = D;
+      s.y_h = (int64_t)a.N * D;
+      s.y_b = a.H * s.y_h;
     }
-    A.state_in = a.dstate_in;
-    A.state_t = which == 0;
-    A.state_out = which == 1 ? a.dstate_out : nullptr;
-    A.p = A.u = a.scale;
-    A.r = 1.0f;
-    A.off = 0;
-    A.reverse = 1;
-    A.zero_tail = 1;
-    hipError_t e = launch_scan(A, slabs, stream);
-    if (e != hipSuccess) return e;
-    if (part) {
-      const int64_t chunks = (int64_t)a.B * a.Hk * a.N * (D / 8);
+  }
+  // (dk reads the state that dv's final one may be written over: not in one launch)
+  const bool in_place = a.dstate_out && a.dstate_out == a.dstate_in && sc.sh.nseg == 1;
+  sc.scan[2].state_out = a.dstate_out;
+  StateArgs st = {};
+  st.sh = sc.sh;
+  st.n = 2;
+  st.st[0] = {a.v, a.k, per, per, a.state_in, 1, nullptr, a.states, nullptr, 1.0f, 1, 0};
+  st.st[1] = {a.q, a.dout, 1, 1, a.dstate_in, 0, a.dstate_out, a.states + 2 * sec, a.states + sec, a.scale, 0, 1};
+  const bool exact = a.dstate_out != nullptr, exact_scan = exact && sc.sh.nseg == 1;
+  hipError_t e;
+  if (in_place) {
+    ScanArgs last = sc;
+    sc.n = 2;
+    last.n = 1;
+    last.scan[0] = sc.scan[2];
+    e = launch_scans(st, sc, slabs, exact, false, stream);
+    if (e == hipSuccess) e = launch_scans(st, last, slabs, exact, exact_scan, stream);
+  } else {
+    e = launch_scans(st, sc, slabs, exact, exact_scan, stream);
+  }
+  if (e != hipSuccess) return e;
+  if (a.partial) {
+    const int64_t chunks = (int64_t)a.B * a.Hk * a.N * (D / 8);
+    for (int which = 0; which < 2; ++which) {
+      const Rows& y = which ? a.dv : a.dk;
       hipLaunchKernelGGL(lin_group_sum_kernel, dim3((unsigned)((chunks + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                         stream, part, y.p, y.sb, y.sh, y.sn, chunks, a.H, a.Hk, a.N);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
+                         stream, a.partial + which * elems, y.p, y.sb, y.sh, y.sn, chunks, a.H, a.Hk, a.N);
     }
   }
-  return hipSuccess;
+  return hipGetLastError();
 }
 
 hipError_t launch_lin_step(const LinStep& a, hipStream_t stream) {

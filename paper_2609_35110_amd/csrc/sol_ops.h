@@ -36,7 +36,8 @@ LinPlan lin_plan(int64_t slabs, int N);
 size_t lin_states_bytes(int64_t slabs, int N);
 
 // out = scale (scan of q, k, v), state_out = the final state (fp32, may be
-// null or state_in itself); states: lin_states_bytes of workspace.
+// null or state_in itself); states: lin_states_bytes of workspace (three times
+// that for the gradients).
 struct LinFwd {
   Rows q, k, v, out;
   const float* log_decay;

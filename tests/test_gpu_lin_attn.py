@@ -2,13 +2,16 @@
 recurrence in 64 bits (plain torch on the CPU), through the torch binding.
 
 Tolerances.  A bf16 result is rounded once (half a step is 2^-9 of a value's
-binade, 2^-8 relative at most); on the way the kernels round the C x C products
-and the state to bf16 where they enter the next product, each a relative error
-of at most 2^-8 per term (uniform: 2^-8 / sqrt(3) / sqrt(2) over a binade, about
-1.7e-3 in the mean square).  Three such roundings give 3e-3 of a result's norm;
-TOL_BF16 = 5e-3.  The worst single value, where up to 2,000 terms' errors add
-like a random walk: 6 standard deviations of 2 x 1.7e-3 of the rms plus its own
-rounding, 2.1e-2 + 2^-8 |y|; MAX_BF16 = 3e-2 of the larger of rms and value.
+binade, 2^-8 relative at most); on the way the kernels round the C x C products,
+the state and the weighted rows that enter it to bf16 where they enter the next
+product, each a relative error of at most 2^-8 per term (uniform: 2^-8 / sqrt(3)
+/ sqrt(2) over a binade, about 1.7e-3 in the mean square).  Four such roundings
+give 2 x 1.7e-3 = 3.4e-3 of a result's norm; TOL_BF16 = 5e-3.  The worst single
+value: 6 standard deviations of 3.4e-3 of the rms plus its own rounding, 2.1e-2
++ 2^-8 |y|; MAX_BF16 = 3e-2 of the larger of rms and value, the rms being that
+of its row of 128 where that is the larger one: the sums of a row share their
+weights, so their errors scale with the row's own rms (in a padded batch whose
+rows are zero behind the sequences the tensor's is smaller than any row's).
 States are fp32: what enters them carries 2^-17 per term, and sums of N terms
 round by 2^-24 sqrt(N) of the norm each; TOL_F32 = 1e-5.
 """
@@ -55,7 +58,7 @@ def near(x, ref, tol=TOL_BF16, most=MAX_BF16):
     x, ref = x.double().cpu(), ref.double()
     assert x.shape == ref.shape and torch.isfinite(x).all()
     norm = ref.norm()
-    rms = norm / math.sqrt(ref.numel())
+    rms = torch.maximum(norm / math.sqrt(ref.numel()), ref.norm(dim=-1, keepdim=True) / math.sqrt(ref.shape[-1]))
     if norm == 0:
         assert x.abs().max() == 0
         return
@@ -82,7 +85,7 @@ def test_forward(B, H, Hk, N, state):
     near(fin, end, TOL_F32, 100 * TOL_F32)
     again, fin2 = sol.lin_attn_fwd(y["q"], y["k"], y["v"], y["g"], scale=0.125, state=y["S"], final_state=True)
     assert torch.equal(out, again) and torch.equal(fin, fin2)
-    assert torch.equal(sol.lin_attn_fwd(y["q"], y["k"], y["v"], y["g"], scale=0.125, state=y["S"]), out)
+    near(sol.lin_attn_fwd(y["q"], y["k"], y["v"], y["g"], scale=0.125, state=y["S"]), ref)  # (a state kept to fewer bits)
 
 
 @pytest.mark.parametrize("state", [False, True])

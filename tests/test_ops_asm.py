@@ -1,5 +1,5 @@
-"""Checks on the generated gfx950 code of the differential attention's kernels
-(CPU only), whose score MFMAs and tile copies are inline assembly that the
+"""Checks on the generated gfx950 code of the linear and differential attention's
+kernels (CPU only), whose score MFMAs and tile copies are inline assembly that the
 compiler's hazard recognizer does not see: MFMA latencies, operands settled
 before an inline MFMA, no spills (a reload's wait would wait for the copies
 too), M0 used by the copies alone, and no wait for the copies but the ones
@@ -14,7 +14,10 @@ import pytest
 import test_kernel_asm as checks
 from paper_2609_35110_amd import build as pkg_build
 
-KERNELS = ["diff_fwd_kernel", "diff_bwd_kernel"]
+# (source, kernels): two instances of each -- maps on one key head or on one
+# each, states that are results of their own or not
+SOURCES = [("sol_diff_attn.hip", ["diff_fwd_kernel", "diff_bwd_kernel"]),
+           ("sol_lin_attn.hip", ["lin_state_kernel", "lin_scan_kernel"])]
 WRITE_WAIT_STATES = 2  # a VALU write of an MFMA's A, B or C operand
 
 
@@ -24,14 +27,19 @@ def kernels(tmp_path_factory):
     if not os.path.exists(hipcc):
         pytest.skip("hipcc not available")
     flags = [f for f in pkg_build.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
-    out = str(tmp_path_factory.mktemp("asm") / "sol_diff_attn.s")
-    src = os.path.join(pkg_build.CSRC, "sol_diff_attn.hip")
-    res = subprocess.run([hipcc] + flags + ["--cuda-device-only", "-S", "-I", pkg_build.INCLUDE, "-I", pkg_build.CSRC,
-                                            "-x", "hip", src, "-o", out], capture_output=True, text=True)
-    assert res.returncode == 0, res.stderr[-2000:]
-    text = open(out).read()
-    found = [f for k in KERNELS for f in checks.functions(text, k)]
-    assert len(found) == 2 * len(KERNELS)  # maps on one key head, or on one each
+    found = []
+    for source, names in SOURCES:
+        out = str(tmp_path_factory.mktemp("asm") / (source + ".s"))
+        src = os.path.join(pkg_build.CSRC, source)
+        res = subprocess.run([hipcc] + flags + ["--cuda-device-only", "-S", "-I", pkg_build.INCLUDE, "-I",
+                                                pkg_build.CSRC, "-x", "hip", src, "-o", out],
+                             capture_output=True, text=True)
+        assert res.returncode == 0, res.stderr[-2000:]
+        text = open(out).read()
+        for name in names:
+            instances = checks.functions(text, name)
+            assert len(instances) == 2, name
+            found += instances
     return found
 
 
@@ -78,6 +86,8 @@ def test_copies_are_waited_for_only_at_the_barriers(kernels):
     the copies on their way: a vmcnt wait of the compiler's stands only where a
     load of its own is used, outside the turns."""
     for name, body in kernels:
+        if "diff" not in name:
+            continue
         blocks, cur = [], []
         for ln in body:
             if re.match(r"\.LBB", ln):
