@@ -163,14 +163,14 @@ extern "C" {
 
 size_t sol_lin_attn_fwd_workspace_bytes(int B, int H, int N, int D) {
   if (B < 1 || H < 1 || N < 1 || D != sol::kHeadDim || N > SOL_MAX_TOKENS || (int64_t)B * H > INT32_MAX / 16) return 0;
-  return sol::lin_states_bytes((int64_t)B * H, N);
+  return sol::lin_states_bytes((int64_t)B * H, N, 1);
 }
 
 size_t sol_lin_attn_bwd_workspace_bytes(int B, int H, int Hk, int N, int D) {
   if (Hk < 1 || H < Hk || H % Hk) return 0;
   if (B < 1 || N < 1 || D != sol::kHeadDim || N > SOL_MAX_TOKENS || (int64_t)B * H > INT32_MAX / 16) return 0;
   const size_t partial = Hk < H ? (size_t)2 * B * H * N * D * sizeof(float) : 0;
-  return up256(3 * sol::lin_states_bytes((int64_t)B * H, N)) + partial;
+  return up256(sol::lin_states_bytes((int64_t)B * H, N, 3)) + partial;
 }
 
 int sol_lin_attn_fwd(const void* q, const sol_strides* q_strides, const void* k, const sol_strides* k_strides,
@@ -265,7 +265,7 @@ int sol_lin_attn_bwd(const void* dout, const sol_strides* dout_strides, const vo
   a.states = static_cast<float*>(workspace);
   if (Hk < H)
     a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) +
-                                         up256(3 * sol::lin_states_bytes((int64_t)B * H, N)));
+                                         up256(sol::lin_states_bytes((int64_t)B * H, N, 3)));
   return done(sol::launch_lin_bwd(a, reinterpret_cast<hipStream_t>(stream)), "lin_attn_bwd");
 }
 

@@ -21,6 +21,8 @@
 // before it is decayed), tokens reversed by a negative row stride.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "sol_ops.h"
 #include "sol_tiles.h"
 
@@ -43,21 +45,22 @@ struct Scan {
   const float* state_in;  // the state before the first token
   int state_t;            // state_in is held transposed
   float* state_out;       // the state after the last token (may be null)
-  float* before;          // several segments: the states before them, [slab][segment][128][128]
+  const float* before;    // several segments: the states before them, [slab][segment][part 0][128][128]
+  int before_t;           // .. held transposed
   float p, r, u;
   int off;
   int reverse;    // walk the tokens from the last one
-  int zero_tail;  // write zeros to the rows behind the sequence
+  int zero_tail;  // write zeros to the rows behind the sequence (bf16)
 };
-// The states that segments add, found in one pass for the scans that need them.
+// The states that segments add, found in one pass for the scans that need them,
+// a segment in `parts` of its own where it takes as many to fill the CUs.
 struct SegmentStates {
   Rows b, c;
   int b_div, c_div;
   const float* state_in;
   int state_t;
   float* state_out;
-  float* local;       // in: what the segments add; out: the states before them
-  float* transposed;  // the same, transposed (may be null)
+  float* local;       // in: what the parts add; out: the states before the segments, at their first parts
   float u;
   int off;
   int reverse;
@@ -65,7 +68,8 @@ struct SegmentStates {
 struct Shape {
   const float* log_decay;
   const int32_t* lens;
-  int H, N, seg_rows, nseg;
+  int B, H, N, seg_rows, nseg;
+  int parts;  // of a segment, in the state pass
 };
 struct ScanArgs {
   Shape sh;
@@ -100,9 +104,18 @@ __device__ __forceinline__ void load_state(State& st, const float* p, bool trans
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int row = state_row(t, r, hh);
-      st.s[t][r] = transposed ? p[col * D + row] : p[row * D + col];
+    for (int r = 0; r < 16; r += 4) {
+      const int row = state_row(t, r, hh);  // (four consecutive ones)
+      if (transposed) {
+        const float4 x = *reinterpret_cast<const float4*>(p + col * D + row);
+        st.s[t][r] = x.x;
+        st.s[t][r + 1] = x.y;
+        st.s[t][r + 2] = x.z;
+        st.s[t][r + 3] = x.w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.s[t][r + i] = p[(row + i) * D + col];
+      }
     }
 }
 __device__ __forceinline__ void store_state(const State& st, float* p, int col, int hh) {
@@ -124,47 +137,35 @@ __device__ __forceinline__ int state_col_place(int lane) {
 // do not drift over long sequences.  A weighted row of c enters rounded to bf16,
 // and with kExact (a state that is a result of its own) as the sum of two bf16,
 // the rounding and the rounding of the rest, 2^-17 together.
+__device__ __forceinline__ void fade_state(f32x16& s, float fade, int r0, int n) {
+#pragma unroll
+  for (int r = r0; r < r0 + n; ++r) s[r] = __builtin_fmaf(s[r], -fade, s[r]);
+}
+// The weighted rows as MFMA operands, 16 rows (ks) at a time: two in use.
 template <bool kExact>
-__device__ __forceinline__ void update_state(State& st, float fade, const uint8_t* tb, const bf16x8 (&cf)[4],
-                                             const float* w, int place, int hh) {
-#pragma unroll
-  for (int t = 0; t < 4; ++t)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) st.s[t][r] = __builtin_fmaf(st.s[t][r], -fade, st.s[t][r]);
-  bf16x8 hi[4], lo[4];
-#pragma unroll
-  for (int ks = 0; ks < 4; ++ks) {
-    const float4 w0 = *reinterpret_cast<const float4*>(w + 16 * ks + 4 * hh);
-    const float4 w1 = *reinterpret_cast<const float4*>(w + 16 * ks + 8 + 4 * hh);
-    float x[8], rest[8];
-    unpack_bf16x8(__builtin_bit_cast(uint4, cf[ks]), x);
-    x[0] *= w0.x; x[1] *= w0.y; x[2] *= w0.z; x[3] *= w0.w;
-    x[4] *= w1.x; x[5] *= w1.y; x[6] *= w1.z; x[7] *= w1.w;
-    const uint4 h = pack_bf16x8(x);
-    hi[ks] = __builtin_bit_cast(bf16x8, h);
-    if (kExact) {
-      unpack_bf16x8(h, rest);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) rest[i] = x[i] - rest[i];
-      lo[ks] = __builtin_bit_cast(bf16x8, pack_bf16x8(rest));
+struct Weighted {
+  bf16x8 hi[2], lo[2];
+  uint32_t h[4], l[4];
+  // quarter q of row group ks: two rows
+  template <int ks, int q>
+  __device__ __forceinline__ void make(const bf16x8 (&cf)[4], const float (&w)[4][8]) {
+    const uint4 four = __builtin_bit_cast(uint4, cf[ks]);
+    const uint32_t x = q == 0 ? four.x : q == 1 ? four.y : q == 2 ? four.z : four.w;
+    const float x0 = __uint_as_float(x << 16) * w[ks][2 * q], x1 = __uint_as_float(x & 0xffff0000u) * w[ks][2 * q + 1];
+    h[q] = pack_bf16x2(x0, x1);
+    if (kExact) l[q] = pack_bf16x2(x0 - __uint_as_float(h[q] << 16), x1 - __uint_as_float(h[q] & 0xffff0000u));
+    if constexpr (q == 3) {
+      hi[ks & 1] = __builtin_bit_cast(bf16x8, make_uint4(h[0], h[1], h[2], h[3]));
+      asm volatile("" : "+v"(hi[ks & 1]));
+      if (kExact) {
+        lo[ks & 1] = __builtin_bit_cast(bf16x8, make_uint4(l[0], l[1], l[2], l[3]));
+        asm volatile("" : "+v"(lo[ks & 1]));
+      }
+    } else {
+      asm volatile("" : "+v"(h[q]));
     }
   }
-  // fragments four reads ahead
-  bf16x8 ring[4];
-#pragma unroll
-  for (int f = 0; f < 4; ++f) ring[f] = col_frag(tb + place, 0, f);
-  slot_end();
-  // (the decayed state and the weighted rows two wait states before an MFMA reads them)
-  asm volatile("s_nop 1" : "+v"(st.s[0]), "+v"(st.s[1]), "+v"(st.s[2]), "+v"(st.s[3]));
-#pragma unroll
-  for (int f = 0; f < 16; ++f) {
-    const int ks = f >> 2, t = f & 3;
-    score(st.s[t], ring[f & 3], hi[ks]);
-    if (kExact) score(st.s[t], ring[f & 3], lo[ks]);
-    if (f + 4 < 16) ring[f & 3] = col_frag(tb + place, (f + 4) >> 2, t);
-    slot_end();
-  }
-}
+};
 
 // A value that all lanes hold, in a scalar register (a division leaves it in a
 // vector one).
@@ -174,17 +175,24 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 // sequence in walking order.
 struct Walk {
   int b, h, seg, len, row0, rows, chunks;
+  int64_t at;  // of the segment's state
   float g2;
 };
-__device__ __forceinline__ Walk make_walk(const Shape& s, int id) {
+__device__ __forceinline__ Walk make_walk(const Shape& s, int id, int nseg, int seg_rows) {
   Walk w;
-  const int slab = uniform(id / s.nseg);
-  w.seg = id - slab * s.nseg;
-  w.b = uniform(slab / s.H);
-  w.h = slab - w.b * s.H;
+  const int slab = uniform(id / nseg);
+  w.seg = id - slab * nseg;
+  if (s.lens) {  // sequences of different lengths take turns: an XCD has some of each
+    w.h = uniform(slab / s.B);
+    w.b = slab - w.h * s.B;
+  } else {
+    w.b = uniform(slab / s.H);
+    w.h = slab - w.b * s.H;
+  }
+  w.at = (int64_t)(w.b * s.H + w.h) * nseg + w.seg;
   w.len = length_of(s, w.b);
-  w.row0 = w.seg * s.seg_rows;
-  w.rows = min(w.row0 + s.seg_rows, w.len);
+  w.row0 = w.seg * seg_rows;
+  w.rows = min(w.row0 + seg_rows, w.len);
   w.chunks = w.rows > w.row0 ? (w.rows - w.row0 + kC - 1) / kC : 0;
   w.g2 = decay_log2(s.log_decay, w.h);
   return w;
@@ -214,75 +222,119 @@ __device__ __forceinline__ void copy_chunk(uint32_t lds, const uint16_t* slab, i
 }
 constexpr int kChunkCopies = 4;  // of one tensor, by each wave
 
-// w[j] = u e^{g(m - off - j)} for the m rows of a chunk, 0 past them.
-__device__ __forceinline__ void fill_weights(float* w, float u, int off, float g2, int m) {
-  const int j = threadIdx.x;
-  if (j < kC) w[j] = j < m ? u * __builtin_amdgcn_exp2f(g2 * (float)max(m - off - j, 0)) : 0.0f;
-}
 __device__ __forceinline__ float fade_of(float g2, int m) { return -expm1f(g2 * 0.693147180559945309f * (float)m); }
+
+// w_j = u e^{g(m - off - j)} of this lane's rows in the transpose reads, in their
+// order, for the m rows of a chunk, 0 past them.
+__device__ __forceinline__ void row_weights(float (&w)[4][8], float u, int off, float g2, int m, int hh) {
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int j = 16 * ks + 4 * hh + (i & 3) + 8 * (i >> 2);
+      w[ks][i] = j < m ? u * __builtin_amdgcn_exp2f(g2 * (float)max(m - off - j, 0)) : 0.0f;
+    }
+}
+constexpr int kAhead = 6;  // operand reads on their way in the slots of a chunk
 
 // The states that segments add, from zero: one pass over b and c.
 constexpr int kStateRing = 4;
+using StateLds = uint8_t[kStateRing][2][kTile];
 template <bool kExact>
+__device__ __forceinline__ void state_walk(State& st, StateLds& lds, const SegmentStates& S, const Walk& W, int wave,
+                                           int lane) {
+  const int hh = lane >> 5, place = state_col_place(lane), c_place = col_place(lane);
+  const uint16_t *pb = slab_of(S.b, W, S.b_div), *pc = slab_of(S.c, W, S.c_div);
+  const uint32_t at0 = lds_address(&lds[0][0][0]);
+  auto copy = [&](int i) __attribute__((always_inline)) {
+    if (i >= W.chunks) return;
+    const uint32_t to = at0 + (i % kStateRing) * (2 * kTile);
+    copy_chunk(to, pb, S.b.sn, W, i, S.reverse, wave, lane);
+    copy_chunk(to + kTile, pc, S.c.sn, W, i, S.reverse, wave, lane);
+  };
+  float fade = fade_of(W.g2, min(kC, W.rows - W.row0)), w[4][8];
+  row_weights(w, S.u, S.off, W.g2, min(kC, W.rows - W.row0), hh);
+  all_landed();
+  copy(0);
+  copy(1);
+  for (int i = 0; i < W.chunks; ++i) {
+    const int m = min(kC, W.rows - W.row0 - i * kC);
+    if (m < kC && i > 0) {  // the last chunk's own
+      int half = hh;  // (not computed ahead of the loop and kept)
+      asm volatile("" : "+v"(half));
+      row_weights(w, S.u, S.off, W.g2, m, half);
+      fade = fade_of(W.g2, m);
+    }
+    if (i + 1 < W.chunks)
+      copies_landed<2 * kChunkCopies>();
+    else
+      copies_landed<0>();
+    const uint8_t *tb = lds[i % kStateRing][0] + place, *tc = lds[i % kStateRing][1] + c_place;
+    bf16x8 cf[4], ring[kAhead];
+    auto read = [&](auto slot) __attribute__((always_inline)) {
+      constexpr int f = decltype(slot)::value;
+      if constexpr (f < 16) ring[f % kAhead] = col_frag(tb, f >> 2, f & 3);
+    };
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) cf[ks] = col_frag(tc, ks, wave);
+    each<0, kAhead>(read);
+    slot_end();
+    copy(i + 2);
+    Weighted<kExact> x;
+    fade_state(st.s[0], fade, 0, 16);
+    fade_state(st.s[1], fade, 0, 8);
+    each<0, 4>([&](auto q) __attribute__((always_inline)) { x.template make<0, decltype(q)::value>(cf, w); });
+    slot_end();
+    asm volatile("s_nop 1" : "+v"(st.s[0]));
+    // slots of an MFMA (of the two parts): the decay of the results to come in
+    // the first four, the next weighted rows in all
+    each<0, 16>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int f = decltype(slot)::value, ks = f >> 2, t = f & 3;
+      if constexpr (ks < 3) x.template make<ks + 1, t>(cf, w);
+      score(st.s[t], ring[f % kAhead], x.hi[ks & 1]);
+      if (kExact) score(st.s[t], ring[f % kAhead], x.lo[ks & 1]);
+      read(std::integral_constant<int, f + kAhead>{});
+      if constexpr (f == 0) fade_state(st.s[1], fade, 8, 8);
+      if constexpr (f == 0) fade_state(st.s[2], fade, 0, 8);
+      if constexpr (f == 1) fade_state(st.s[2], fade, 8, 8);
+      if constexpr (f == 1) fade_state(st.s[3], fade, 0, 8);
+      if constexpr (f == 2) fade_state(st.s[3], fade, 8, 8);
+      if constexpr (f < 3) asm volatile("s_nop 1" : "+v"(st.s[f + 1]));
+      slot_end();
+    });
+    settle(st.s[0], st.s[1]);
+    settle(st.s[2], st.s[3]);
+  }
+}
 __global__ __launch_bounds__(kThreads, 2) void lin_state_kernel(StateArgs A) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStateRing][2][kTile];
-  __shared__ __attribute__((aligned(16))) float wt[2][kC];
+  __shared__ __attribute__((aligned(1024))) StateLds lds;
   lds_poison(lds, sizeof(lds));
-  lds_poison(wt, sizeof(wt));
   lds_poison_done();
   const int all = xcd_local_id(blockIdx.x, gridDim.x);
   const int id = uniform(all / A.n);
   const SegmentStates S = A.st[all - id * A.n];
-  const Walk W = make_walk(A.sh, id);
+  const Walk W = make_walk(A.sh, id, A.sh.nseg * A.sh.parts, A.sh.seg_rows / A.sh.parts);
   // the last segment's state is wanted by the final state alone
-  if (W.seg == A.sh.nseg - 1 && !S.state_out) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hh = lane >> 5, l32 = lane & 31;
-  const int place = state_col_place(lane), c_place = col_place(lane);
-  const uint16_t *pb = slab_of(S.b, W, S.b_div), *pc = slab_of(S.c, W, S.c_div);
-  const uint32_t at0 = lds_address(&lds[0][0][0]);
-  auto copy = [&](int i) __attribute__((always_inline)) {
-    const int chunk = min(i, W.chunks - 1);  // (past the last one: again, not used)
-    const uint32_t to = at0 + (i % kStateRing) * (2 * kTile);
-    copy_chunk(to, pb, S.b.sn, W, chunk, S.reverse, wave, lane);
-    copy_chunk(to + kTile, pc, S.c.sn, W, chunk, S.reverse, wave, lane);
-  };
+  if (W.seg >= (A.sh.nseg - 1) * A.sh.parts && !S.state_out) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   State st{};
   if (W.chunks > 0) {
-    float fade = fade_of(W.g2, kC);
-    fill_weights(wt[0], S.u, S.off, W.g2, min(kC, W.rows - W.row0));
-    all_landed();
-    copy(0);
-    copy(1);
-    for (int i = 0; i < W.chunks; ++i) {
-      const int m = min(kC, W.rows - W.row0 - i * kC);
-      if (m < kC) {  // the last chunk's own (the other buffer: this one may be in use)
-        if (i > 0) fill_weights(wt[1], S.u, S.off, W.g2, m);
-        fade = fade_of(W.g2, m);
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      copies_landed<2 * kChunkCopies>();
-      copy(i + 2);
-      const uint8_t* tb = lds[i % kStateRing][0];
-      bf16x8 cf[4];
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) cf[ks] = col_frag(lds[i % kStateRing][1] + c_place, ks, wave);
-      update_state<kExact>(st, fade, tb, cf, wt[m < kC && i > 0], place, hh);
-    }
-    copies_landed<0>();
+    if (S.state_out)
+      state_walk<true>(st, lds, S, W, wave, lane);
+    else
+      state_walk<false>(st, lds, S, W, wave, lane);
   }
-  settle(st.s[0], st.s[1]);
-  settle(st.s[2], st.s[3]);
-  store_state(st, S.local + (int64_t)id * kStateElems, 32 * wave + l32, hh);
+  store_state(st, S.local + W.at * kStateElems, 32 * wave + (lane & 31), lane >> 5);
 }
 
-// The states before each segment, from what the segments add: in place, one
-// workgroup per slab and 1,024 of its state's values, eight segments' loads in
+// The states before each segment, from what their parts add: in place, one
+// workgroup per slab and 1,024 of its state's values, eight parts' loads in
 // flight.
 __global__ __launch_bounds__(kThreads) void lin_join_kernel(StateArgs A) {
   const SegmentStates& S = A.st[blockIdx.x % A.n];
   const int slab = blockIdx.x / A.n >> 4, part = (blockIdx.x / A.n) & 15;
   const int b = slab / A.sh.H, h = slab - b * A.sh.H;
-  const int len = length_of(A.sh, b), nseg = A.sh.nseg;
+  const int len = length_of(A.sh, b), parts = A.sh.nseg * A.sh.parts, rows = A.sh.seg_rows / A.sh.parts;
   const float g2 = decay_log2(A.sh.log_decay, h);
   const int e = part * 1024 + threadIdx.x * 4, row = e >> 7, col = e & 127;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -291,12 +343,11 @@ __global__ __launch_bounds__(kThreads) void lin_join_kernel(StateArgs A) {
     s = S.state_t ? make_float4(p[col * D + row], p[(col + 1) * D + row], p[(col + 2) * D + row], p[(col + 3) * D + row])
                   : *reinterpret_cast<const float4*>(p + e);
   }
-  float* seg = S.local + (int64_t)slab * nseg * kStateElems;
-  float* tr = S.transposed ? S.transposed + (int64_t)slab * nseg * kStateElems + col * D + row : nullptr;
-  const float whole = fade_of(g2, A.sh.seg_rows);
-  const int last = S.state_out ? nseg : nseg - 1;  // segments whose own state was found
+  float* seg = S.local + (int64_t)slab * parts * kStateElems;
+  const float whole = fade_of(g2, rows);
+  const int last = S.state_out ? parts : parts - A.sh.parts;  // parts whose own state was found
   constexpr int kBatch = 8;
-  for (int i0 = 0; i0 < nseg; i0 += kBatch) {
+  for (int i0 = 0; i0 < parts; i0 += kBatch) {
     float4 x[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -306,17 +357,10 @@ __global__ __launch_bounds__(kThreads) void lin_join_kernel(StateArgs A) {
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       const int i = i0 + u;
-      if (i < nseg) {
-        *reinterpret_cast<float4*>(seg + (int64_t)i * kStateElems + e) = s;
-        if (tr) {
-          float* t = tr + (int64_t)i * kStateElems;
-          t[0] = s.x;
-          t[D] = s.y;
-          t[2 * D] = s.z;
-          t[3 * D] = s.w;
-        }
-        const int m = min(max(len - i * A.sh.seg_rows, 0), A.sh.seg_rows);
-        const float fade = m == A.sh.seg_rows ? whole : fade_of(g2, m);
+      if (i < parts) {
+        if (i % A.sh.parts == 0) *reinterpret_cast<float4*>(seg + (int64_t)i * kStateElems + e) = s;
+        const int m = min(max(len - i * rows, 0), rows);
+        const float fade = m == rows ? whole : fade_of(g2, m);
         s.x = __builtin_fmaf(s.x, -fade, s.x) + x[u].x;
         s.y = __builtin_fmaf(s.y, -fade, s.y) + x[u].y;
         s.z = __builtin_fmaf(s.z, -fade, s.z) + x[u].z;
@@ -335,214 +379,260 @@ __device__ __forceinline__ void tile_product(f32x16 (&s)[2], const bf16x8 (&bf)[
   for (int kk = 2; kk < 8; ++kk) score(s[kk & 1], bf[kk], af[kk]);
 }
 
-// y over a segment.  A wave owns 32 columns of the state and of y: the state
-// stays in its registers (64 a lane), where an MFMA leaves it and the next one
-// takes it as an operand (rounded to bf16 there, as y is a bf16 result: both
-// roundings are of the same size).  The C x C products are shared: waves 0 to 2
-// find the three 32 x 32 tiles on and below the diagonal, and pass them round
-// in the order the next product reads them.
+// y over a segment.  Eight waves, two a SIMD: four keep the state, four feed them.
 //
-// Its bytes bound it: a CU's share of a copy's rate is 64 KB (a chunk's a, b, c
-// and y) in 6,800 cycles, the products of a chunk take 1,500 of the matrix
-// cores.  So one workgroup a CU, the chunks straight into LDS in a ring of
-// three, two on their way.
+// Waves 0 to 3 own 32 columns each of the state and of y: the state stays in
+// registers (64 a lane), where an MFMA leaves it and the next one takes it as an
+// operand (rounded to bf16 there, as y is a bf16 result: both roundings are of
+// the same size).  Waves 4 to 7 copy the chunks straight into LDS (a ring of
+// three, two on their way) and find the three 32 x 32 tiles on and below the
+// diagonal of the C x C product, which they pass on in the order the next
+// product reads them, while the others multiply by the state.
+//
+// One chunk of the first four, a slot an MFMA with its operand read kAhead slots
+// before and a share of the vector work:
+//   16  y = a S        with S (1 - fade) for the update, and the first weighted c
+//   16  S += b^T (c w) with the next weighted c; the C x C tiles arrive on the way
+//    6  z = P c        after eight of those; the last eight add y and z up
+constexpr int kScanThreads = 512;
 constexpr int kScanRing = 3;
 template <bool kExact>
-__global__ __launch_bounds__(kThreads, 2) void lin_scan_kernel(ScanArgs A) {
+__global__ __launch_bounds__(kScanThreads, 2) void lin_scan_kernel(ScanArgs A) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kScanRing][3][kTile];
   __shared__ __attribute__((aligned(16))) uint4 pf[3][2][64];  // tiles (0,0), (1,0), (1,1): 16 columns, lane
-  __shared__ __attribute__((aligned(16))) float wt[2][kC];
   lds_poison(lds, sizeof(lds));
   lds_poison(pf, sizeof(pf));
-  lds_poison(wt, sizeof(wt));
   lds_poison_done();
   const int all = xcd_local_id(blockIdx.x, gridDim.x);
   const int id = uniform(all / A.n);
   const Scan S = A.scan[all - id * A.n];
-  const Walk W = make_walk(A.sh, id);
+  const Walk W = make_walk(A.sh, id, A.sh.nseg, A.sh.seg_rows);
   const int slab = W.b * A.sh.H + W.h;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hh = lane >> 5, l32 = lane & 31;
-  const int col = 32 * wave + l32;
   const int64_t y0 = W.b * S.y_b + W.h * S.y_h;
 
   if (S.zero_tail) {  // rows of this segment behind the sequence
     const int r = threadIdx.x >> 4, cc = threadIdx.x & 15;
     const int end = min(W.row0 + A.sh.seg_rows, A.sh.N);
-    for (int i = max(W.row0, W.len) + r; i < end; i += 16) {
+    for (int i = max(W.row0, W.len) + r; i < end; i += kScanThreads / 16) {
       const int64_t at = y0 + (int64_t)i * S.y_n + cc * 8;
-      if (S.y_f32) {
-        float4* y = reinterpret_cast<float4*>(static_cast<float*>(S.y) + at);
-        y[0] = y[1] = make_float4(0.f, 0.f, 0.f, 0.f);
-      } else {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(S.y) + at) = make_uint4(0, 0, 0, 0);
-      }
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(S.y) + at) = make_uint4(0, 0, 0, 0);
     }
   }
   if (W.chunks == 0) {  // (of a sequence without tokens, the first and last segment)
     if (A.sh.nseg == 1 && S.state_out)
-      for (int e = threadIdx.x; e < kStateElems; e += kThreads)
+      for (int e = threadIdx.x; e < kStateElems; e += kScanThreads)
         S.state_out[(int64_t)slab * kStateElems + e] =
             !S.state_in ? 0.0f : S.state_in[(int64_t)slab * kStateElems + (S.state_t ? (e & 127) * D + (e >> 7) : e)];
     return;
   }
-
   const RowPlace rp = row_place(lane);
+
+  if (wave >= 4) {
+    const int wv = wave - 4;
+    const uint16_t *pa = slab_of(S.a, W, S.a_div), *pb = slab_of(S.b, W, S.b_div), *pc = slab_of(S.c, W, S.c_div);
+    const uint32_t at0 = lds_address(&lds[0][0][0]);
+    auto copy = [&](int i) __attribute__((always_inline)) {
+      const uint32_t to = at0 + (i % kScanRing) * (3 * kTile);
+      copy_chunk(to, pa, S.a.sn, W, i, S.reverse, wv, lane);
+      copy_chunk(to + kTile, pb, S.b.sn, W, i, S.reverse, wv, lane);
+      copy_chunk(to + 2 * kTile, pc, S.c.sn, W, i, S.reverse, wv, lane);
+    };
+    all_landed();
+    copy(0);
+    if (W.chunks > 1) copy(1);
+    // this wave's tile of the C x C product: rows 32 I + .. of a, 32 J + .. of b,
+    // held transposed (lane: row of a), and its weights
+    const int I = wv == 0 ? 0 : 1, J = wv == 2 ? 1 : 0;
+    float dec[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int gap = (32 * I + l32) - (32 * J + 8 * (r >> 2) + 4 * hh + (r & 3));
+      dec[r] = gap >= 0 ? S.p * __builtin_amdgcn_exp2f(W.g2 * (float)gap) : 0.0f;
+    }
+    for (int i = 0; i < W.chunks; ++i) {
+      if (i + 1 < W.chunks)
+        copies_landed<3 * kChunkCopies>();
+      else
+        copies_landed<0>();
+      if (wv < 3) {
+        const uint8_t *ta = lds[i % kScanRing][0] + I * kTile32, *tb = lds[i % kScanRing][1] + J * kTile32;
+        bf16x8 af[8], bf[8];
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+          af[kk] = row_frag(ta, rp, kk);
+          bf[kk] = row_frag(tb, rp, kk);
+        }
+        slot_end();
+        f32x16 s[2];
+        tile_product(s, bf, af);
+        settle(s[0], s[1]);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float f[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) f[r] = (s[0][8 * x + r] + s[1][8 * x + r]) * dec[8 * x + r];
+          pf[wv][x][lane] = pack_bf16x8(f);
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (i + 2 < W.chunks) copy(i + 2);
+    }
+    return;
+  }
+
+  const int col = 32 * wave + l32;
   const int place = state_col_place(lane), c_place = col_place(lane);
-  const uint16_t *pa = slab_of(S.a, W, S.a_div), *pb = slab_of(S.b, W, S.b_div), *pc = slab_of(S.c, W, S.c_div);
-  const uint32_t at0 = lds_address(&lds[0][0][0]);
-  auto copy = [&](int i) __attribute__((always_inline)) {
-    const int chunk = min(i, W.chunks - 1);  // (past the last one: again, not used)
-    const uint32_t to = at0 + (i % kScanRing) * (3 * kTile);
-    copy_chunk(to, pa, S.a.sn, W, chunk, S.reverse, wave, lane);
-    copy_chunk(to + kTile, pb, S.b.sn, W, chunk, S.reverse, wave, lane);
-    copy_chunk(to + 2 * kTile, pc, S.c.sn, W, chunk, S.reverse, wave, lane);
-  };
   State st{};
   if (A.sh.nseg > 1)
-    load_state(st, S.before + (int64_t)id * kStateElems, false, col, hh);
+    load_state(st, S.before + W.at * A.sh.parts * kStateElems, S.before_t, col, hh);
   else if (S.state_in)
     load_state(st, S.state_in + (int64_t)slab * kStateElems, S.state_t, col, hh);
-
-  // this wave's tile of the C x C product: rows 32 I + .. of a, 32 J + .. of b,
-  // held transposed (lane: row of a), and its weights
-  const int I = wave == 0 ? 0 : 1, J = wave == 2 ? 1 : 0;
-  float dec[16];
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int gap = (32 * I + l32) - (32 * J + 8 * (r >> 2) + 4 * hh + (r & 3));
-    dec[r] = gap >= 0 ? S.p * __builtin_amdgcn_exp2f(W.g2 * (float)gap) : 0.0f;
-  }
   const float win[2] = {S.r * __builtin_amdgcn_exp2f(W.g2 * (float)(l32 + S.off)),
                         S.r * __builtin_amdgcn_exp2f(W.g2 * (float)(32 + l32 + S.off))};
-  float fade = fade_of(W.g2, kC);
-  fill_weights(wt[0], S.u, S.off, W.g2, min(kC, W.rows - W.row0));
-  constexpr int kStores = 8;  // of y, by each wave and chunk
+  float fade = fade_of(W.g2, min(kC, W.rows - W.row0));
+  float w[4][8];
+  row_weights(w, S.u, S.off, W.g2, min(kC, W.rows - W.row0), hh);
   all_landed();
-  copy(0);
-  copy(1);
   for (int i = 0; i < W.chunks; ++i) {
     const int row = W.row0 + i * kC, m = min(kC, W.rows - row);
-    if (m < kC) {  // the last chunk's own (the other buffer: this one may be in use)
-      if (i > 0) fill_weights(wt[1], S.u, S.off, W.g2, m);
+    if (m < kC && i > 0) {  // the last chunk's own
+      int half = hh;  // (not computed ahead of the loop and kept)
+      asm volatile("" : "+v"(half));
+      row_weights(w, S.u, S.off, W.g2, m, half);
       fade = fade_of(W.g2, m);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    // this chunk's copies: behind them the next one's, and from the second
-    // chunk on the last one's stores (every chunk but the last stores 8 times)
-    if (i == 0)
-      copies_landed<3 * kChunkCopies>();
-    else
-      copies_landed<3 * kChunkCopies + kStores>();
-    copy(i + 2);
-    const uint8_t *ta = lds[i % kScanRing][0], *tb = lds[i % kScanRing][1], *tc = lds[i % kScanRing][2];
-    bf16x8 af[2][8], cf[4];
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) af[0][kk] = row_frag(ta, rp, kk);
-    if (wave < 3) {
-      bf16x8 bf[8];
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) bf[kk] = row_frag(tb + J * kTile32, rp, kk);
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) af[1][kk] = row_frag(ta + kTile32, rp, kk);
-      slot_end();
-      f32x16 s[2];
-      if (wave == 0)
-        tile_product(s, bf, af[0]);
-      else
-        tile_product(s, bf, af[1]);
-      settle(s[0], s[1]);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        float f[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) f[r] = (s[0][8 * x + r] + s[1][8 * x + r]) * dec[8 * x + r];
-        pf[wave][x][lane] = pack_bf16x8(f);
-      }
-    } else {
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) af[1][kk] = row_frag(ta + kTile32, rp, kk);
-    }
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) cf[ks] = col_frag(tc + c_place, ks, wave);
-    // y^T = S^T a^T, each row's weight on its lane
-    f32x16 y[2];
     bf16x8 sf[8];
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) sf[kk] = operand8(st.s[kk >> 1], kk & 1);
     hold_in_vgprs(sf);
+    asm volatile("s_barrier" ::: "memory");
+    const uint8_t *ta = lds[i % kScanRing][0], *tb = lds[i % kScanRing][1] + place, *tc = lds[i % kScanRing][2] + c_place;
+    f32x16 y[2], z[2];
+    bf16x8 ring[kAhead], cf[4], pt[3][2];
+    Weighted<kExact> x;
+    uint32_t pk[8];
+    auto read = [&](auto slot) __attribute__((always_inline)) {
+      constexpr int f = decltype(slot)::value;
+      if constexpr (f < 16)
+        ring[f % kAhead] = row_frag(ta + (f & 1) * kTile32, rp, f >> 1);
+      else if constexpr (f < 32)
+        ring[f % kAhead] = col_frag(tb, (f - 16) >> 2, f & 3);
+    };
+    auto update = [&](auto slot) __attribute__((always_inline)) {
+      constexpr int f = decltype(slot)::value, ks = (f - 16) >> 2, t = f & 3;
+      if constexpr (ks < 3) x.template make<ks + 1, t>(cf, w);
+      score(st.s[t], ring[f % kAhead], x.hi[ks & 1]);
+      if (kExact) score(st.s[t], ring[f % kAhead], x.lo[ks & 1]);
+      read(std::integral_constant<int, f + kAhead>{});
+      slot_end();
+      if constexpr (f >= 24) {  // four rows' worth of y and z
+        constexpr int o = (f - 24) >> 2, q = f & 3;
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      if (kk == 0) {
-        score_first(y[0], sf[kk], af[0][kk]);
-        score_first(y[1], sf[kk], af[1][kk]);
-      } else {
-        score(y[0], sf[kk], af[0][kk]);
-        score(y[1], sf[kk], af[1][kk]);
+        for (int r = 4 * q; r < 4 * q + 4; ++r) y[o][r] = __builtin_fmaf(y[o][r], win[o], z[o][r]);
+        pk[2 * q] = pack_bf16x2(y[o][4 * q], y[o][4 * q + 1]);
+        pk[2 * q + 1] = pack_bf16x2(y[o][4 * q + 2], y[o][4 * q + 3]);
+        asm volatile("" : "+v"(pk[2 * q]), "+v"(pk[2 * q + 1]));
       }
-    }
-    settle(y[0], y[1]);
+      slot_end();
+    };
+    auto store = [&](int o) __attribute__((always_inline)) {
+      int j = row + 32 * o + l32;
+      asm volatile("" : "+v"(j));
+      const int n = S.reverse ? W.len - 1 - j : j;
+      const int64_t at = y0 + (int64_t)n * S.y_n + 32 * wave;
+      if (S.y_f32) {
+        float4* p = reinterpret_cast<float4*>(static_cast<float*>(S.y) + at + 4 * hh);
+        if (j < W.rows)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      y[0][r] *= win[0];
-      y[1][r] *= win[1];
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    bf16x8 pt[3][2];
+          for (int x = 0; x < 4; ++x)
+            p[2 * x] = make_float4(y[o][4 * x], y[o][4 * x + 1], y[o][4 * x + 2], y[o][4 * x + 3]);
+      } else {  // eight columns a lane: the halves of the wave exchange four
+#pragma unroll
+        for (int x = 0; x < 4; x += 2)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const auto both = __builtin_amdgcn_permlane32_swap(pk[2 * x + e], pk[2 * x + 2 + e], false, false);
+            pk[2 * x + e] = both[0];
+            pk[2 * x + 2 + e] = both[1];
+          }
+        uint4* p = reinterpret_cast<uint4*>(static_cast<uint16_t*>(S.y) + at + 8 * hh);
+        if (j < W.rows) {
+          p[0] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+          p[2] = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+        }
+      }
+    };
+    each<0, kAhead>(read);
+    slot_end();
+    each<0, 16>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int f = decltype(slot)::value, t = f >> 2;
+      fade_state(st.s[t], fade, 4 * (f & 3), 4);
+      if constexpr (f >= 12) x.template make<0, f - 12>(cf, w);
+      asm volatile("" : "+v"(st.s[t]));
+      if constexpr (f < 2)
+        score_first(y[f], sf[0], ring[f % kAhead]);
+      else
+        score(y[f & 1], sf[f >> 1], ring[f % kAhead]);
+      if constexpr (f >= 4 && f < 8) cf[f - 4] = col_frag(tc, f - 4, wave);
+      read(std::integral_constant<int, f + kAhead>{});
+      slot_end();
+    });
+    each<16, 20>(update);
+    asm volatile("s_barrier" ::: "memory");
 #pragma unroll
     for (int t = 0; t < 3; ++t)
 #pragma unroll
       for (int x = 0; x < 2; ++x) pt[t][x] = __builtin_bit_cast(bf16x8, pf[t][x][lane]);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      score(y[0], cf[x], pt[0][x]);
-      score(y[1], cf[x], pt[1][x]);
-      score(y[1], cf[2 + x], pt[2][x]);
-    }
-    update_state<kExact>(st, fade, tb, cf, wt[m < kC && i > 0], place, hh);
-#pragma unroll
-    for (int i2 = 0; i2 < 2; ++i2) {
-      const int j = row + 32 * i2 + l32;
-      if (j < W.rows) {
-        const int n = S.reverse ? W.len - 1 - j : j;
-        const int64_t at = y0 + (int64_t)n * S.y_n + 32 * wave + 4 * hh;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          if (S.y_f32)
-            *reinterpret_cast<float4*>(static_cast<float*>(S.y) + at + 8 * x) =
-                make_float4(y[i2][4 * x], y[i2][4 * x + 1], y[i2][4 * x + 2], y[i2][4 * x + 3]);
-          else
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(S.y) + at + 8 * x) =
-                make_uint2(pack_bf16x2(y[i2][4 * x], y[i2][4 * x + 1]), pack_bf16x2(y[i2][4 * x + 2], y[i2][4 * x + 3]));
-        }
-      }
-    }
+    slot_end();
+    each<20, 24>(update);
+    score_first(z[0], cf[0], pt[0][0]);
+    score_first(z[1], cf[0], pt[1][0]);
+    score(z[0], cf[1], pt[0][1]);
+    score(z[1], cf[1], pt[1][1]);
+    score(z[1], cf[2], pt[2][0]);
+    score(z[1], cf[3], pt[2][1]);
+    slot_end();
+    each<24, 28>(update);
+    store(0);
+    each<28, 32>(update);
+    store(1);
+    settle(st.s[0], st.s[1]);
+    settle(st.s[2], st.s[3]);
   }
-  copies_landed<0>();  // none is under way when the wave ends
-  settle(st.s[0], st.s[1]);
-  settle(st.s[2], st.s[3]);
   if (A.sh.nseg == 1 && S.state_out) store_state(st, S.state_out + (int64_t)slab * kStateElems, col, hh);
 }
 
-// Gradients of shared heads: the sum, in head order, of the group's fp32 parts,
-// rounded once.  One thread per 16-byte chunk of a row.
-__global__ __launch_bounds__(kThreads) void lin_group_sum_kernel(const float* __restrict__ part, uint16_t* out,
-                                                                 int64_t sb, int64_t sh, int64_t sn, int64_t chunks,
-                                                                 int H, int Hk, int N) {
+// Gradients of shared heads, dk's and dv's: the sum, in head order, of the
+// group's fp32 parts, rounded once, and zeros behind the sequence (where the
+// parts were not written).  One thread per 16-byte chunk of a row.
+struct GroupSum {
+  const float* part;  // dk's [B, H, N, 128], then dv's
+  Rows y[2];
+  const int32_t* lens;
+  int B, H, Hk, N;
+};
+__global__ __launch_bounds__(kThreads) void lin_group_sum_kernel(GroupSum A) {
   const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= chunks) return;
   const int cc = (int)(i & 15);
-  const int64_t row = i >> 4;
-  const int n = (int)(row % N);
-  const int64_t bh = row / N;
-  const int hk = (int)(bh % Hk), b = (int)(bh / Hk), per = H / Hk;
+  int64_t bh = (i >> 4) / A.N;
+  const int n = (int)((i >> 4) - bh * A.N), per = A.H / A.Hk;
+  const int64_t heads = (int64_t)A.B * A.Hk;
+  if (bh >= 2 * heads) return;
+  const int which = bh >= heads;
+  bh -= which * heads;
+  const int b = (int)(bh / A.Hk), hk = (int)(bh - (int64_t)b * A.Hk);
   float f[8] = {};
-  for (int u = 0; u < per; ++u) {
-    const float4* p = reinterpret_cast<const float4*>(part + ((((int64_t)b * H + hk * per + u) * N + n) * D + cc * 8));
-    const float4 x = p[0], y = p[1];
-    f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
-    f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+  if (!A.lens || n < A.lens[b]) {
+    const float* p = A.part + ((((int64_t)which * A.B + b) * A.H + hk * per) * A.N + n) * D + cc * 8;
+    for (int u = 0; u < per; ++u, p += (int64_t)A.N * D) {
+      const float4 x = reinterpret_cast<const float4*>(p)[0], y = reinterpret_cast<const float4*>(p)[1];
+      f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+      f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+    }
   }
-  *reinterpret_cast<uint4*>(out + b * sb + hk * sh + (int64_t)n * sn + cc * 8) = pack_bf16x8(f);
+  const Rows& y = A.y[which];
+  *reinterpret_cast<uint4*>(y.p + b * y.sb + hk * y.sh + (int64_t)n * y.sn + cc * 8) = pack_bf16x8(f);
 }
 
 // One token for each request: the state is read, decayed, added to and written,
@@ -613,26 +703,22 @@ __global__ __launch_bounds__(kThreads) void lin_step_kernel(LinStep A) {
 }
 
 // The state pass and the join where there are several segments, then the scans.
-hipError_t launch_scans(const StateArgs& st, const ScanArgs& sc, int64_t slabs, bool exact_states, bool exact_scan,
-                        hipStream_t stream) {
+hipError_t launch_scans(const StateArgs& st, const ScanArgs& sc, int64_t slabs, bool exact, hipStream_t stream) {
   const unsigned wgs = (unsigned)(slabs * sc.sh.nseg);
   if (sc.sh.nseg > 1) {
-    if (exact_states)
-      hipLaunchKernelGGL(lin_state_kernel<true>, dim3(wgs * st.n), dim3(kThreads), 0, stream, st);
-    else
-      hipLaunchKernelGGL(lin_state_kernel<false>, dim3(wgs * st.n), dim3(kThreads), 0, stream, st);
+    hipLaunchKernelGGL(lin_state_kernel, dim3(wgs * sc.sh.parts * st.n), dim3(kThreads), 0, stream, st);
     hipLaunchKernelGGL(lin_join_kernel, dim3((unsigned)(slabs * 16 * st.n)), dim3(kThreads), 0, stream, st);
   }
-  if (exact_scan)
-    hipLaunchKernelGGL(lin_scan_kernel<true>, dim3(wgs * sc.n), dim3(kThreads), 0, stream, sc);
+  if (exact)
+    hipLaunchKernelGGL(lin_scan_kernel<true>, dim3(wgs * sc.n), dim3(kScanThreads), 0, stream, sc);
   else
-    hipLaunchKernelGGL(lin_scan_kernel<false>, dim3(wgs * sc.n), dim3(kThreads), 0, stream, sc);
+    hipLaunchKernelGGL(lin_scan_kernel<false>, dim3(wgs * sc.n), dim3(kScanThreads), 0, stream, sc);
   return hipGetLastError();
 }
 
-Shape shape_of(const float* log_decay, const int32_t* lens, int B, int H, int N) {
-  const LinPlan plan = lin_plan((int64_t)B * H, N);
-  return {log_decay, lens, H, N, plan.seg_rows, plan.nseg};
+Shape shape_of(const float* log_decay, const int32_t* lens, int B, int H, int N, int scans) {
+  const LinPlan plan = lin_plan((int64_t)B * H, N, scans);
+  return {log_decay, lens, B, H, N, plan.seg_rows, plan.nseg, plan.parts};
 }
 
 Scan scan_of(const Rows& a, int a_div, const Rows& b, int b_div, const Rows& c, int c_div, const Rows& y) {
@@ -652,27 +738,44 @@ Scan scan_of(const Rows& a, int a_div, const Rows& b, int b_div, const Rows& c, 
 
 }  // namespace
 
-LinPlan lin_plan(int64_t slabs, int N) {
-  // one workgroup on each of the 256 CUs, in segments of at least 256 tokens
-  const int chunks = (N + kC - 1) / kC;
-  int64_t nseg = 256 / slabs;
-  nseg = nseg < 1 ? 1 : nseg;
-  const int most = (chunks + 3) / 4;
-  if (nseg > most) nseg = most;
-  const int seg_chunks = (int)((chunks + nseg - 1) / nseg);
-  return {seg_chunks * kC, (chunks + seg_chunks - 1) / seg_chunks};
+// Sets of states: dq's and dv's (dk's are dv's, transposed), or the forward's.
+static int lin_sets(int scans) { return scans > 1 ? 2 : 1; }
+
+// Segments: as many as give each of the 256 CUs one workgroup of the launch's
+// scans, of 256 tokens at least, where that is the faster way.  In times of a
+// chunk (1.75 us), n segments take C / n of the scan, 0.75 as many of the state
+// pass, and 7 + workgroups / 64 for two more launches and the states' bytes.
+// Measured, in us, one segment against n: forward of 2 heads x 512 tokens 18
+// against 24 (n = 2), x 1,024 31 against 24 (4); 24 heads x 1,024 31 against 31
+// (4), x 2,048 64 against 36 (8); 64 heads x 1,024 35 against 40 (4), x 2,048 65
+// against 53 (4); 128 heads x 2,048 74 against 86 (2), x 12,480 512 against 446
+// (2).  Gradients of 24 heads x 1,024 34 against 36 (3), x 2,048 63 against 52
+// (3; 69 in 8); 64 heads x 2,048 70 against 111 (4).
+LinPlan lin_plan(int64_t slabs, int N, int scans) {
+  const int chunks = (N + kC - 1) / kC, most = (chunks + 3) / 4;
+  const LinPlan one = {chunks * kC, 1, 1};
+  const int64_t wanted = std::min<int64_t>(256 / (slabs * scans), most);
+  if (wanted < 2) return one;
+  int seg_chunks = (int)((chunks + wanted - 1) / wanted);
+  const int nseg = (chunks + seg_chunks - 1) / seg_chunks;
+  const double split = 1.75 * seg_chunks + 7 + (double)(slabs * nseg) / 64;
+  if (split >= chunks) return one;
+  int parts = (int)std::min<int64_t>(256 / (slabs * lin_sets(scans) * (nseg - 1)), seg_chunks / 4);
+  parts = std::max(parts, 1);
+  seg_chunks = (seg_chunks + parts - 1) / parts * parts;
+  return {seg_chunks * kC, (chunks + seg_chunks - 1) / seg_chunks, parts};
 }
 
-size_t lin_states_bytes(int64_t slabs, int N) {
-  const LinPlan p = lin_plan(slabs, N);
-  return p.nseg > 1 ? (size_t)slabs * p.nseg * kStateElems * sizeof(float) : 0;
+size_t lin_states_bytes(int64_t slabs, int N, int scans) {
+  const LinPlan p = lin_plan(slabs, N, scans);
+  return p.nseg > 1 ? (size_t)slabs * p.nseg * p.parts * lin_sets(scans) * kStateElems * sizeof(float) : 0;
 }
 
 hipError_t launch_lin_fwd(const LinFwd& a, hipStream_t stream) {
   const int per = a.H / a.Hk;
   ScanArgs sc = {};
-  sc.sh = shape_of(a.log_decay, a.lens, a.B, a.H, a.N);
   sc.n = 1;
+  sc.sh = shape_of(a.log_decay, a.lens, a.B, a.H, a.N, sc.n);
   Scan& s = sc.scan[0];
   s = scan_of(a.q, 1, a.k, per, a.v, per, a.out);
   s.state_in = a.state_in;
@@ -684,9 +787,8 @@ hipError_t launch_lin_fwd(const LinFwd& a, hipStream_t stream) {
   StateArgs st = {};
   st.sh = sc.sh;
   st.n = 1;
-  st.st[0] = {a.k, a.v, per, per, a.state_in, 0, a.state_out, a.states, nullptr, 1.0f, 1, 0};
-  const bool exact = a.state_out != nullptr;
-  return launch_scans(st, sc, (int64_t)a.B * a.H, exact, exact && sc.sh.nseg == 1, stream);
+  st.st[0] = {a.k, a.v, per, per, a.state_in, 0, a.state_out, a.states, 1.0f, 1, 0};
+  return launch_scans(st, sc, (int64_t)a.B * a.H, a.state_out && sc.sh.nseg == 1, stream);
 }
 
 // The three gradients in one launch (dq forwards; dk and dv backwards, side by
@@ -696,15 +798,16 @@ hipError_t launch_lin_bwd(const LinBwd& a, hipStream_t stream) {
   const int per = a.H / a.Hk;
   const int64_t slabs = (int64_t)a.B * a.H, elems = slabs * a.N * D;
   ScanArgs sc = {};
-  sc.sh = shape_of(a.log_decay, a.lens, a.B, a.H, a.N);
-  sc.n = 3;
-  const int64_t sec = slabs * sc.sh.nseg * kStateElems;  // floats of the segments' states
+  sc.n = kMaxScans;
+  sc.sh = shape_of(a.log_decay, a.lens, a.B, a.H, a.N, sc.n);
+  const int64_t sec = slabs * sc.sh.nseg * sc.sh.parts * kStateElems;  // floats of the parts' states
   sc.scan[0] = scan_of(a.dout, 1, a.v, per, a.k, per, a.dq);
   sc.scan[1] = scan_of(a.v, per, a.dout, 1, a.q, 1, a.dk);
   sc.scan[2] = scan_of(a.k, per, a.q, 1, a.dout, 1, a.dv);
   for (int i = 0; i < 3; ++i) {
     Scan& s = sc.scan[i];
-    s.before = a.states + i * sec;
+    s.before = a.states + (i > 0) * sec;
+    s.before_t = i == 1;
     s.state_in = i == 0 ? a.state_in : a.dstate_in;
     s.state_t = i < 2;
     s.p = a.scale;
@@ -712,7 +815,7 @@ hipError_t launch_lin_bwd(const LinBwd& a, hipStream_t stream) {
     s.u = i == 0 ? 1.0f : a.scale;
     s.off = i == 0;
     s.reverse = i > 0;
-    s.zero_tail = 1;
+    s.zero_tail = !(i > 0 && a.partial);
     if (i > 0 && a.partial) {
       s.y = a.partial + (i - 1) * elems;
       s.y_f32 = 1;
@@ -727,28 +830,26 @@ hipError_t launch_lin_bwd(const LinBwd& a, hipStream_t stream) {
   StateArgs st = {};
   st.sh = sc.sh;
   st.n = 2;
-  st.st[0] = {a.v, a.k, per, per, a.state_in, 1, nullptr, a.states, nullptr, 1.0f, 1, 0};
-  st.st[1] = {a.q, a.dout, 1, 1, a.dstate_in, 0, a.dstate_out, a.states + 2 * sec, a.states + sec, a.scale, 0, 1};
-  const bool exact = a.dstate_out != nullptr, exact_scan = exact && sc.sh.nseg == 1;
+  st.st[0] = {a.v, a.k, per, per, a.state_in, 1, nullptr, a.states, 1.0f, 1, 0};
+  st.st[1] = {a.q, a.dout, 1, 1, a.dstate_in, 0, a.dstate_out, a.states + sec, a.scale, 0, 1};
+  const bool exact = a.dstate_out && sc.sh.nseg == 1;  // of the scans: else the state pass's
   hipError_t e;
   if (in_place) {
     ScanArgs last = sc;
     sc.n = 2;
     last.n = 1;
     last.scan[0] = sc.scan[2];
-    e = launch_scans(st, sc, slabs, exact, false, stream);
-    if (e == hipSuccess) e = launch_scans(st, last, slabs, exact, exact_scan, stream);
+    e = launch_scans(st, sc, slabs, false, stream);
+    if (e == hipSuccess) e = launch_scans(st, last, slabs, exact, stream);
   } else {
-    e = launch_scans(st, sc, slabs, exact, exact_scan, stream);
+    e = launch_scans(st, sc, slabs, exact, stream);
   }
   if (e != hipSuccess) return e;
   if (a.partial) {
-    const int64_t chunks = (int64_t)a.B * a.Hk * a.N * (D / 8);
-    for (int which = 0; which < 2; ++which) {
-      const Rows& y = which ? a.dv : a.dk;
-      hipLaunchKernelGGL(lin_group_sum_kernel, dim3((unsigned)((chunks + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                         stream, a.partial + which * elems, y.p, y.sb, y.sh, y.sn, chunks, a.H, a.Hk, a.N);
-    }
+    const int64_t chunks = 2 * (int64_t)a.B * a.Hk * a.N * (D / 8);
+    const GroupSum sum = {a.partial, {a.dk, a.dv}, a.lens, a.B, a.H, a.Hk, a.N};
+    hipLaunchKernelGGL(lin_group_sum_kernel, dim3((unsigned)((chunks + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                       stream, sum);
   }
   return hipGetLastError();
 }

@@ -30,14 +30,14 @@ constexpr int kStateElems = kHeadDim * kHeadDim;  // fp32 values of a head's sta
 struct LinPlan {
   int seg_rows;  // a multiple of kLinRows
   int nseg;
+  int parts;  // of a segment, in the pass that finds its state (divide its chunks)
 };
-LinPlan lin_plan(int64_t slabs, int N);
+LinPlan lin_plan(int64_t slabs, int N, int scans);
 // Bytes of the segments' states (0 for one segment).
-size_t lin_states_bytes(int64_t slabs, int N);
+size_t lin_states_bytes(int64_t slabs, int N, int scans);
 
 // out = scale (scan of q, k, v), state_out = the final state (fp32, may be
-// null or state_in itself); states: lin_states_bytes of workspace (three times
-// that for the gradients).
+// null or state_in itself); states: lin_states_bytes of workspace.
 struct LinFwd {
   Rows q, k, v, out;
   const float* log_decay;
