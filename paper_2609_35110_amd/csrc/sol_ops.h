@@ -101,7 +101,6 @@ struct DiffPlan {
   bool few;
   DiffTiles tiles;
 };
-DiffPlan diff_plan(const DiffShape& s);
 size_t diff_fwd_bytes(const DiffShape& s);
 
 struct DiffFwd {
