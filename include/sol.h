@@ -569,15 +569,16 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
  * new tokens at the end of a cache do.  A row that sees no key has out = 0.
  *
  * Scores and row sums are fp32; probabilities are rounded to bf16 for the
- * product with v.  Every call repeats bit for bit.  A call with few rows over
+ * product with v, which is divided by the sum of the rounded ones.  Every call repeats bit for bit.  A call with few rows over
  * many keys splits the keys over workgroups and joins them through the
  * workspace.
  *
  * sol_diff_attn_fwd: rows of out behind a sequence are left as they are.  For
- * training, out2 ([B][H][N][D] bf16, contiguous) receives the second map's own
- * output and lse ([B][2H][N] floats) the logarithm of each row's sum of
- * exponentials, -inf for a row that sees no key; both may be NULL, and both are
- * left as they are behind a sequence.
+ * training, out2 ([B][H][N][3][D] bf16, contiguous) receives the second map's
+ * own output, what its rounding to bf16 left of it, and what that of out left,
+ * and lse ([B][2H][N] floats) the logarithm of each row's sum of exponentials,
+ * -inf for a row that sees no key; both are NULL or neither, and both are left
+ * as they are behind a sequence.
  *
  * sol_diff_attn_bwd: from dout, the gradient of out, and the forward call's
  * out, out2 and lse: dq, dk, dv (bf16, zero behind a sequence; shared heads'

@@ -341,12 +341,13 @@ int sol_diff_attn_fwd(const void* q, const sol_strides* q_strides, const void* k
   SOL_TRY(take_rows("out", out, out_strides, B, H, N, true, &a.out, &outs[0]));
   if (!aligned16(out2)) return fail(SOL_ERR_INVALID_ARG, "out2 must be 16-byte aligned");
   SOL_TRY(check_small("lse", lse, true));
+  if (!out2 != !lse) return fail(SOL_ERR_INVALID_ARG, "out2 and lse are given together or not at all");
   const size_t need = sol::diff_fwd_bytes(a.s);
   SOL_TRY(check_workspace(workspace, workspace_bytes, need));
   in[3] = span("lambda", lambda, (uint64_t)H * 4);
   in[4] = span("q_lens", q_lens, (uint64_t)B * 4);
   in[5] = span("kv_lens", kv_lens, (uint64_t)B * 4);
-  outs[1] = span("out2", out2, (uint64_t)B * H * N * D * 2);
+  outs[1] = span("out2", out2, (uint64_t)B * H * N * D * 6);
   outs[2] = span("lse", lse, (uint64_t)B * 2 * H * N * 4);
   outs[3] = span("workspace", workspace, need);
   SOL_TRY(check_apart(in, 6, outs, 4));
@@ -382,7 +383,7 @@ int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const v
   a.stats = static_cast<float*>(workspace);
   const size_t need = sol::diff_bwd_bytes(a.s, &a);
   SOL_TRY(check_workspace(workspace, workspace_bytes, need));
-  in[5] = span("out2", out2, (uint64_t)B * H * N * D * 2);
+  in[5] = span("out2", out2, (uint64_t)B * H * N * D * 6);
   in[6] = span("lse", lse, (uint64_t)B * 2 * H * N * 4);
   in[7] = span("lambda", lambda, (uint64_t)H * 4);
   in[8] = span("q_lens", q_lens, (uint64_t)B * 4);

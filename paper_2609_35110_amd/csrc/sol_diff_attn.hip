@@ -47,13 +47,25 @@ __device__ __forceinline__ int2 split_keys(int klen, int i, int n, int tile) {
 // One map of 32 rows: a lane's row is lane % 32.
 struct MapRows {
   f32x16 o[4];  // O^T: dims 32t + 8(r/4) + 4(lane/32) + r%4
-  float m, l;   // maximum held to (raw scores), sum of this lane's half of the keys
+  float m;      // maximum held to (raw scores)
+  // Sums over this lane's half of the keys: of P as the product takes it, rounded,
+  // which O is divided by (a row that one key has most of gets that key's value
+  // whole, whatever its P's rounding), and of P before that for the log sum.
+  float l, exact;
 };
+// sum + the two values of a word
+__device__ __forceinline__ float add_bf16x2(uint32_t x, float sum) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
+}
+__device__ __forceinline__ float add_bf16x8(const bf16x8& p, float sum) {
+  const uint4 x = __builtin_bit_cast(uint4, p);
+  return add_bf16x2(x.x, add_bf16x2(x.y, add_bf16x2(x.z, add_bf16x2(x.w, sum))));
+}
 __device__ __forceinline__ void clear(MapRows& x) {
 #pragma unroll
   for (int t = 0; t < 4; ++t) x.o[t] = f32x16{};
   x.m = kNoMax;
-  x.l = 0.0f;
+  x.l = x.exact = 0.0f;
 }
 
 // Scores of 32 keys (rows of the result) for the wave's 32 rows.
@@ -86,6 +98,7 @@ __device__ __forceinline__ void raise_max(MapRows& x, const f32x16 (&s)[kBlocks]
     const float m = fmaxf(x.m, top);
     const float keep = __builtin_amdgcn_exp2f((x.m - m) * c);
     x.l *= keep;
+    x.exact *= keep;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -94,7 +107,7 @@ __device__ __forceinline__ void raise_max(MapRows& x, const f32x16 (&s)[kBlocks]
   }
 }
 
-// P of 32 keys in place of their scores, and its sum.
+// P of 32 keys in place of their scores, and its sum before any rounding.
 __device__ __forceinline__ void exponentials(MapRows& x, f32x16& s, float c) {
   const float mc = x.m * c;
   float a = 0.0f, b = 0.0f;
@@ -105,7 +118,7 @@ __device__ __forceinline__ void exponentials(MapRows& x, f32x16& s, float c) {
     a += s[r];
     b += s[r + 1];
   }
-  x.l += a + b;
+  x.exact += a + b;
 }
 
 // This lane's row of 8 operand registers.
@@ -122,22 +135,45 @@ __device__ __forceinline__ uint2 pack4(const f32x16& s, int x) {
   return make_uint2(pack_bf16x2(s[4 * x], s[4 * x + 1]), pack_bf16x2(s[4 * x + 2], s[4 * x + 3]));
 }
 
+// What rounding to bf16 left of values: what out2 holds beside the second map's
+// output, so that the gradients' sums dout . o_s start from 16 bits of o_s (in a
+// row that one key has most of they cancel against that key's dout . v).
+__device__ __forceinline__ uint32_t left2(float a, float b, uint32_t packed) {
+  return pack_bf16x2(a - __uint_as_float(packed << 16), b - __uint_as_float(packed & 0xffff0000u));
+}
+__device__ __forceinline__ uint2 left4(const f32x16& s, int x, uint2 packed) {
+  return make_uint2(left2(s[4 * x], s[4 * x + 1], packed.x), left2(s[4 * x + 2], s[4 * x + 3], packed.y));
+}
+// out and out2 of two dims from `d` of row (b, h, n).
+__device__ __forceinline__ void store_row2(const DiffFwd& A, int b, int h, int n, int d, float lam, const float2 (&o)[2]) {
+  const float2 y = make_float2(__builtin_fmaf(-lam, o[1].x, o[0].x), __builtin_fmaf(-lam, o[1].y, o[0].y));
+  const uint32_t w = pack_bf16x2(y.x, y.y);
+  *reinterpret_cast<uint32_t*>(A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)n * A.out.sn + d) = w;
+  if (A.out2) {
+    uint16_t* p = A.out2 + (((int64_t)b * A.s.H + h) * A.s.N + n) * (3 * D) + d;
+    const uint32_t w1 = pack_bf16x2(o[1].x, o[1].y);
+    *reinterpret_cast<uint32_t*>(p) = w1;
+    *reinterpret_cast<uint32_t*>(p + D) = left2(o[1].x, o[1].y, w1);
+    *reinterpret_cast<uint32_t*>(p + 2 * D) = left2(y.x, y.y, w);
+  }
+}
+
 // log2 of a row's sum of exponentials; -inf for a row without keys.
 __device__ __forceinline__ float log2_sum(float m, float l, float c) {
   return l > 0.0f ? m * c + log2f(l) : -__builtin_inff();
 }
 
 // Results of pieces of the keys, to be joined: o fp32 [piece][map][row][128],
-// then the log2 sums [piece][map][row], for `rows` rows: those of the tiles that
+// then the log2 of the sums that o was divided by, [piece][map][row], and of the
+// exact ones (for training), for `rows` rows: those of the tiles that
 // are split (tile after tile), or, where the few-row kernel splits, all
 // [B][H][N].
 struct Parts {
-  float* o;
-  float* l;
+  float *o, *l, *exact;
   int64_t rows;
 };
 __device__ __forceinline__ Parts parts_of(float* ws, int64_t rows, int pieces) {
-  return {ws, ws + rows * 2 * pieces * D, rows};
+  return {ws, ws + rows * 2 * pieces * D, ws + rows * 2 * pieces * (D + 1), rows};
 }
 
 // The tile and piece of a workgroup: tiles [0, full) whole, the rest in pieces.
@@ -205,7 +241,7 @@ __device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
 // found by a walk for scores alone.
 constexpr int kFwdKeys = 32;
 constexpr float kTooMuch = 1.2089258e24f;
-template <bool kShared>
+template <bool kShared, bool kTrain>
 __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, DiffTiles plan) {
   constexpr int kTiles = kShared ? 2 : 3;  // K (of each map), V
   constexpr int kV = kTiles - 1;
@@ -306,11 +342,13 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, DiffTiles p
   // exponential's result is not there at once)
   float e[2];
   auto take = [&](Tile& now, int m, int r) __attribute__((always_inline)) {  // rows r, r + 1
-    x[m].l += e[0];
+    if (kTrain) x[m].exact += e[0];
     now.pw[m][r >> 1] = pack_bf16x2(e[0], e[1]);
-    x[m].l += e[1];
+    if (kTrain) x[m].exact += e[1];
     pin(now.pw[m][r >> 1]);
+    x[m].l = add_bf16x2(now.pw[m][r >> 1], x[m].l);
     pin(x[m].l);
+    if (kTrain) pin(x[m].exact);
   };
   auto exponential = [&](Tile& now, int m, int r) __attribute__((always_inline)) {
     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(now.s[m][r], c, -mc[m]));
@@ -423,12 +461,13 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, DiffTiles p
     __syncthreads();
   }
 
-  float l2[2];
+  float l2[2], exact2[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     const float l = both_sum(x[m].l);
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     l2[m] = log2_sum(x[m].m, l, c);
+    if (kTrain) exact2[m] = log2_sum(x[m].m, both_sum(x[m].exact), c);
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -449,25 +488,32 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, DiffTiles p
           *reinterpret_cast<float4*>(o + 32 * d + 8 * q) = make_float4(
               x[m].o[d][4 * q], x[m].o[d][4 * q + 1], x[m].o[d][4 * q + 2], x[m].o[d][4 * q + 3]);
       if (hh == 0) p.l[am] = l2[m];
+      if (kTrain && hh == 0) p.exact[am] = exact2[m];
     }
     return;
   }
-  if (A.lse && hh == 0) {
+  if (kTrain && hh == 0) {
     const int64_t at = ((int64_t)(b * 2 * s.H + 2 * h)) * s.N + row;
-    A.lse[at] = l2[0] * kLn2;
-    A.lse[at + s.N] = l2[1] * kLn2;
+    A.lse[at] = exact2[0] * kLn2;
+    A.lse[at + s.N] = exact2[1] * kLn2;
   }
   const float lam = s.lambda[h];
   uint16_t* o = A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)row * A.out.sn + 4 * hh;
-  uint16_t* o2 = A.out2 ? A.out2 + (((int64_t)b * s.H + h) * s.N + row) * D + 4 * hh : nullptr;
+  uint16_t* o2 = A.out2 + (((int64_t)b * s.H + h) * s.N + row) * (3 * D) + 4 * hh;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      if (o2) *reinterpret_cast<uint2*>(o2 + 32 * d + 8 * q) = pack4(x[1].o[d], q);
 #pragma unroll
       for (int r = 4 * q; r < 4 * q + 4; ++r) x[0].o[d][r] = __builtin_fmaf(-lam, x[1].o[d][r], x[0].o[d][r]);
-      *reinterpret_cast<uint2*>(o + 32 * d + 8 * q) = pack4(x[0].o[d], q);
+      const uint2 y = pack4(x[0].o[d], q);
+      *reinterpret_cast<uint2*>(o + 32 * d + 8 * q) = y;
+      if (kTrain) {
+        const uint2 y1 = pack4(x[1].o[d], q);
+        *reinterpret_cast<uint2*>(o2 + 32 * d + 8 * q) = y1;
+        *reinterpret_cast<uint2*>(o2 + D + 32 * d + 8 * q) = left4(x[1].o[d], q, y1);
+        *reinterpret_cast<uint2*>(o2 + 2 * D + 32 * d + 8 * q) = left4(x[0].o[d], q, y);
+      }
     }
 }
 
@@ -485,7 +531,7 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
   constexpr int kRow = D + 4;
   struct Joined {
     float o[kWaves][2][kFewRows][kRow];
-    float m[kWaves][2][kFewRows], l[kWaves][2][kFewRows];
+    float m[kWaves][2][kFewRows], l[kWaves][2][kFewRows], exact[kWaves][2][kFewRows];
   };
   union Lds {
     uint16_t tiles[kWaves][(kKTiles + 1) * kTileElems];
@@ -554,6 +600,8 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
       const bf16x8 p0 = operand8(sc[0][0], y), p1 = operand8(sc[1][0], y);
+      x[0].l = add_bf16x8(p0, x[0].l);
+      x[1].l = add_bf16x8(p1, x[1].l);
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         const bf16x8 vf = column8(tv + 16 * y * kStride + 32 * d + tr);
@@ -568,7 +616,7 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
   __syncthreads();
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    const float l = both_sum(x[m].l);
+    const float l = both_sum(x[m].l), exact = both_sum(x[m].exact);
     if (l32 < n_rows) {
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -579,6 +627,7 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
       if (hh == 0) {
         lds.j.m[wave][m][l32] = x[m].m;
         lds.j.l[wave][m][l32] = l;
+        lds.j.exact[wave][m][l32] = exact;
       }
     }
   }
@@ -590,10 +639,10 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
     const int hr = hv * per + r / s.N, n = r % s.N;
     if (n >= sq.qlen) continue;
     float2 o[2];
-    float l2[2];
+    float l2[2], exact2[2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      float top = kNoMax, sum = 0.0f;
+      float top = kNoMax, sum = 0.0f, exact = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds.j.m[w][m][r]);
       o[m] = make_float2(0.0f, 0.0f);
@@ -601,6 +650,7 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
       for (int w = 0; w < kWaves; ++w) {
         const float f = __builtin_amdgcn_exp2f((lds.j.m[w][m][r] - top) * c);
         sum = __builtin_fmaf(f, lds.j.l[w][m][r], sum);
+        exact = __builtin_fmaf(f, lds.j.exact[w][m][r], exact);
         o[m].x = __builtin_fmaf(f, lds.j.o[w][m][r][d], o[m].x);
         o[m].y = __builtin_fmaf(f, lds.j.o[w][m][r][d + 1], o[m].y);
       }
@@ -608,6 +658,7 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
       o[m].x *= inv;
       o[m].y *= inv;
       l2[m] = log2_sum(top, sum, c);
+      exact2[m] = log2_sum(top, exact, c);
     }
     const int64_t at = ((int64_t)(b * 2 * s.H + 2 * hr)) * s.N + n;
     if (nsplit > 1) {
@@ -616,16 +667,13 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
         const int64_t am = (2 * split + m) * p.rows + ((int64_t)b * s.H + hr) * s.N + n;
         *reinterpret_cast<float2*>(p.o + am * D + d) = o[m];
         if (d == 0) p.l[am] = l2[m];
+        if (d == 0 && A.lse) p.exact[am] = exact2[m];
       }
     } else {
-      const float lam = s.lambda[hr];
-      *reinterpret_cast<uint32_t*>(A.out.p + b * A.out.sb + hr * A.out.sh + (int64_t)n * A.out.sn + d) =
-          pack_bf16x2(__builtin_fmaf(-lam, o[1].x, o[0].x), __builtin_fmaf(-lam, o[1].y, o[0].y));
-      if (A.out2)
-        *reinterpret_cast<uint32_t*>(A.out2 + (((int64_t)b * s.H + hr) * s.N + n) * D + d) = pack_bf16x2(o[1].x, o[1].y);
+      store_row2(A, b, hr, n, d, s.lambda[hr], o);
       if (A.lse && d == 0) {
-        A.lse[at] = l2[0] * kLn2;
-        A.lse[at + s.N] = l2[1] * kLn2;
+        A.lse[at] = exact2[0] * kLn2;
+        A.lse[at + s.N] = exact2[1] * kLn2;
       }
     }
   }
@@ -655,10 +703,10 @@ __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, DiffTiles pla
   if (n >= sequence(s, b).qlen) return;
   const Parts p = parts_of(A.ws, rows, plan.pieces);
   float2 o[2];
-  float l2[2];
+  float exact2[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    float top = kNoMax, sum = 0.0f;
+    float top = kNoMax, sum = 0.0f, exact = 0.0f;
     for (int u = 0; u < plan.pieces; ++u) top = fmaxf(top, p.l[(2 * u + m) * rows + i]);
     o[m] = make_float2(0.0f, 0.0f);
     for (int u = 0; u < plan.pieces; ++u) {
@@ -666,20 +714,17 @@ __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, DiffTiles pla
       const float f = __builtin_amdgcn_exp2f(p.l[am] - top);
       const float2 x = *reinterpret_cast<const float2*>(p.o + am * D + 2 * lane);
       sum += f;
+      if (A.lse) exact += __builtin_amdgcn_exp2f(p.exact[am] - top);
       o[m].x = __builtin_fmaf(f, x.x, o[m].x);
       o[m].y = __builtin_fmaf(f, x.y, o[m].y);
     }
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
     o[m].x *= inv;
     o[m].y *= inv;
-    l2[m] = sum > 0.0f ? top + log2f(sum) : -__builtin_inff();
+    exact2[m] = sum > 0.0f ? top + log2f(exact) : -__builtin_inff();
   }
-  const float lam = s.lambda[h];
-  *reinterpret_cast<uint32_t*>(A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)n * A.out.sn + 2 * lane) =
-      pack_bf16x2(__builtin_fmaf(-lam, o[1].x, o[0].x), __builtin_fmaf(-lam, o[1].y, o[0].y));
-  if (A.out2)
-    *reinterpret_cast<uint32_t*>(A.out2 + (((int64_t)b * s.H + h) * s.N + n) * D + 2 * lane) = pack_bf16x2(o[1].x, o[1].y);
-  if (A.lse && lane < 2) A.lse[((int64_t)(b * 2 * s.H + 2 * h) + lane) * s.N + n] = (lane ? l2[1] : l2[0]) * kLn2;
+  store_row2(A, b, h, n, 2 * lane, s.lambda[h], o);
+  if (A.lse && lane < 2) A.lse[((int64_t)(b * 2 * s.H + 2 * h) + lane) * s.N + n] = (lane ? exact2[1] : exact2[0]) * kLn2;
 }
 
 // ------------------------------------------------------------------ backward
@@ -712,10 +757,18 @@ __global__ __launch_bounds__(16 * kBwdRows) void diff_stats_kernel(DiffBwd A) {
   const bool valid = n < sequence(s, b).qlen;
   float d0 = 0.0f, d1 = 0.0f;
   if (valid) {
-    float o[8], o1[8], g[8];
-    unpack_bf16x8(*reinterpret_cast<const uint4*>(A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)n * A.out.sn + 8 * cc), o);
-    unpack_bf16x8(*reinterpret_cast<const uint4*>(A.out2 + ((int64_t)bh * s.N + n) * D + 8 * cc), o1);
-    unpack_bf16x8(*reinterpret_cast<const uint4*>(A.dout.p + b * A.dout.sb + h * A.dout.sh + (int64_t)n * A.dout.sn + 8 * cc), g);
+    float o[8], o1[8], g[8], left[8];
+    auto load = [](float (&f)[8], const uint16_t* p) { unpack_bf16x8(*reinterpret_cast<const uint4*>(p), f); };
+    load(o, A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)n * A.out.sn + 8 * cc);
+    load(g, A.dout.p + b * A.dout.sb + h * A.dout.sh + (int64_t)n * A.dout.sn + 8 * cc);
+    const uint16_t* p = A.out2 + ((int64_t)bh * s.N + n) * (3 * D) + 8 * cc;
+    load(o1, p);
+    load(left, p + D);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) o1[u] += left[u];
+    load(left, p + 2 * D);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) o[u] += left[u];
     const float lam = s.lambda[h];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -1338,7 +1391,7 @@ size_t diff_fwd_bytes(const DiffShape& s) {  // with lengths and without
   size_t most = 0;
   for (const bool ragged : {false, true}) {
     const DiffPlan p = diff_plan(s, ragged);
-    most = std::max(most, join_rows(s, p) * p.tiles.pieces * 2 * (D + 1) * sizeof(float));
+    most = std::max(most, join_rows(s, p) * p.tiles.pieces * 2 * (D + 2) * sizeof(float));
   }
   return most;
 }
@@ -1355,10 +1408,9 @@ hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
       hipLaunchKernelGGL(diff_few_kernel<false>, grid, dim3(256), 0, stream, a, p.tiles.pieces);
   } else {
     const dim3 grid((unsigned)(p.tiles.full + (row_tiles_of(s) - p.tiles.full) * p.tiles.pieces));
-    if (shared)
-      hipLaunchKernelGGL(diff_fwd_kernel<true>, grid, dim3(256), 0, stream, a, p.tiles);
-    else
-      hipLaunchKernelGGL(diff_fwd_kernel<false>, grid, dim3(256), 0, stream, a, p.tiles);
+    const auto kernel = a.lse ? (shared ? diff_fwd_kernel<true, true> : diff_fwd_kernel<false, true>)
+                              : (shared ? diff_fwd_kernel<true, false> : diff_fwd_kernel<false, false>);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, p.tiles);
   }
   if (const size_t rows = join_rows(s, p)) {
     const dim3 grid((unsigned)((rows + 3) / 4));

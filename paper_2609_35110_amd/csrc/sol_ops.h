@@ -106,8 +106,10 @@ size_t diff_fwd_bytes(const DiffShape& s);
 struct DiffFwd {
   DiffShape s;
   Rows q, k, v, out;
-  uint16_t* out2;  // second map's own output, [B][H][N][128], may be null
-  float* lse;      // [B][2H][N], may be null
+  // For the gradients (both null or neither): [B][H][N][3][128], the second map's
+  // own output, what its rounding left, and what that of out left; [B][2H][N].
+  uint16_t* out2;
+  float* lse;
   float* ws;
 };
 hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream);

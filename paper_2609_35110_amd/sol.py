@@ -955,7 +955,7 @@ def diff_attn_fwd(q, k, v, lam, scale=None, causal=False, q_lens=None, kv_lens=N
     op, os_ = _rows("out", out, dev, (B, H, N, D))
     out2 = lse = None
     if training:
-        out2 = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+        out2 = torch.empty((B, H, N, 3, D), dtype=torch.bfloat16, device=dev)
         lse = torch.empty((B, 2 * H, N), dtype=torch.float32, device=dev)
     if lam is None:
         raise ValueError("lam must be given")
@@ -991,7 +991,7 @@ def diff_attn_bwd(dout, q, k, v, lam, out, out2, lse, scale=None, causal=False, 
     ws, wp, wn = _scratch(workspace, sol_diff_attn_bwd_workspace_bytes(B, H, Hv, N, M, D), dev)
     (dq, dqp, dqs), (dk, dkp, dks), (dv, dvp, dvs) = grads
     _call(sol_diff_attn_bwd, dev, gp, gs, qp, qs, kp, ks, vp, vs, op, os_,
-          _device_array("out2", out2, dev, torch.bfloat16, (B, H, N, D)),
+          _device_array("out2", out2, dev, torch.bfloat16, (B, H, N, 3, D)),
           _device_array("lse", lse, dev, torch.float32, (B, 2 * H, N)),
           _device_array("lam", lam, dev, torch.float32, (H,)), dqp, dqs, dkp, dks, dvp, dvs, dlam.data_ptr(),
           _device_array("q_lens", q_lens, dev, torch.int32, (B,)),

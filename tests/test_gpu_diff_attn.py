@@ -10,11 +10,13 @@ rms and value, the rms being that of its row of 128 where that is the larger
 one: a row's 128 sums have the same weights, so their terms' errors scale with
 the row's own rms and not with the tensor's (of 400 keys with 1 % times 8, four
 take nearly all of dv: their rows' rms is sqrt(400 / 4) = 10 times the
-tensor's, and one standard deviation there, 10 x 2.4e-3, is most of 3e-2).  delta = dout . o is found from the stored outputs, each rounded
-to bf16 (half a step: 2^-9 of a value, in out and in out2), so a row's delta is
-off by at most 2^-9 sum |dout| (|o_s| + |out|), the same for all its keys; what
-that adds to dq and dk (it matters where few keys are seen, and X - delta
-cancels) is computed beside the reference and allowed on top.  lse: scores are
+tensor's, and one standard deviation there, 10 x 2.4e-3, is most of 3e-2).  delta = dout . o is found from the outputs of rounded P, divided
+by the sum of the rounded ones: off by sum_j e_j P_j (X_j - delta), e_j the
+roundings, so by at most 6 standard deviations, 6 x 1.7e-3 x
+sqrt(sum P^2 (X - delta)^2); and from outputs kept in two bf16 parts: 2^-16
+sum |dout| (|o_s| + |out|).  It is the same for all of a row's keys; what it adds
+to dq and dk (it matters where few keys are seen, and X - delta cancels) is
+computed beside the reference and allowed on top.  lse: scores are
 exact products summed in fp32 over 128 terms, 128 x 2^-24 x |score| at most and
 the final log: 1e-5 x the largest |score| + 1e-6.  dlam: an fp32 sum of terms
 P X, each within 1e-6: TOL_DLAM = 1e-5 of its terms' root of squares x sqrt of
@@ -86,7 +88,8 @@ def reference(x, scale=D ** -0.5, **kw):
     dk = keys(dS.transpose(-1, -2) @ q)
     dv = ((p[:, 0] - lam * p[:, 1]).transpose(-1, -2) @ do).reshape(B, Hv, H // Hv, M, D).sum(2)
     dlam = -(p[:, 1] * X).sum((0, 2, 3))
-    err = 2.0 ** -9 * (do.abs()[:, None] * (o.abs() + out.abs()[:, None])).sum(-1, keepdim=True) * w.abs()
+    err = 6 * 1.7e-3 * (p * (X[:, None] - delta)).norm(dim=-1, keepdim=True)
+    err = (err + 2.0 ** -16 * (do.abs()[:, None] * (o.abs() + out.abs()[:, None])).sum(-1, keepdim=True)) * w.abs()
     aq = (err * (p @ k).abs()).norm()
     ak = keys((p * err).transpose(-1, -2) @ q.abs()).norm()
     size = (p[:, 1] * X.abs()).sum((0, 2, 3))

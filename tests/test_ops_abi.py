@@ -184,6 +184,8 @@ def diff_fwd(**kw):
     (dict(out=at(3)), -1, "out overlaps v"),
     (dict(out2=at(5) + 8), -1, "out2 must be 16-byte"),
     (dict(out2=at(4)), -1, "out2 overlaps out"),
+    (dict(out2=None), -1, "out2 and lse are given together"),
+    (dict(lse=None), -1, "out2 and lse are given together"),
     (dict(lse=at(8) + 2), -1, "lse must be 4-byte"),
     (dict(lse=at(6)), -1, "lse overlaps lambda"),
     (dict(out_st=S(0, 100 * 128, 128)), -1, "rows of out overlap"),

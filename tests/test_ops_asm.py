@@ -38,7 +38,7 @@ def kernels(tmp_path_factory):
         text = open(out).read()
         for name in names:
             instances = checks.functions(text, name)
-            assert len(instances) == (1 if name == "lin_state_kernel" else 2), name
+            assert len(instances) == {"lin_state_kernel": 1, "diff_fwd_kernel": 4}.get(name, 2), name
             found += instances
     return found
 
