@@ -29,7 +29,7 @@
 namespace sol {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kScanThreads = 512;
 constexpr int kC = kLinRows;
 constexpr int kTile = 2 * kTile32;  // bytes of a chunk's rows
 
@@ -134,33 +134,29 @@ __device__ __forceinline__ int state_col_place(int lane) {
 
 // S = (1 - fade) S + b^T (c w): the decay is taken off as a difference, so that
 // its rounding is relative to what is lost and slow heads (e^{64 g} next to 1)
-// do not drift over long sequences.  A weighted row of c enters rounded to bf16,
-// and with kExact (a state that is a result of its own) as the sum of two bf16,
-// the rounding and the rounding of the rest, 2^-17 together.
+// do not drift over long sequences.  A weighted row of c enters as the sum of two
+// bf16, its rounding and the rounding of the rest, 2^-17 together.
 __device__ __forceinline__ void fade_state(f32x16& s, float fade, int r0, int n) {
 #pragma unroll
   for (int r = r0; r < r0 + n; ++r) s[r] = __builtin_fmaf(s[r], -fade, s[r]);
 }
 // The weighted rows as MFMA operands, 16 rows (ks) at a time: two in use.
-template <bool kExact>
 struct Weighted {
   bf16x8 hi[2], lo[2];
   uint32_t h[4], l[4];
   // quarter q of row group ks: two rows
-  template <int ks, int q>
-  __device__ __forceinline__ void make(const bf16x8 (&cf)[4], const float (&w)[4][8]) {
+  template <int ks, int q, int n>
+  __device__ __forceinline__ void make(const bf16x8 (&cf)[n], const float (&w)[n][8]) {
     const uint4 four = __builtin_bit_cast(uint4, cf[ks]);
     const uint32_t x = q == 0 ? four.x : q == 1 ? four.y : q == 2 ? four.z : four.w;
     const float x0 = __uint_as_float(x << 16) * w[ks][2 * q], x1 = __uint_as_float(x & 0xffff0000u) * w[ks][2 * q + 1];
     h[q] = pack_bf16x2(x0, x1);
-    if (kExact) l[q] = pack_bf16x2(x0 - __uint_as_float(h[q] << 16), x1 - __uint_as_float(h[q] & 0xffff0000u));
+    l[q] = pack_bf16x2(x0 - __uint_as_float(h[q] << 16), x1 - __uint_as_float(h[q] & 0xffff0000u));
     if constexpr (q == 3) {
       hi[ks & 1] = __builtin_bit_cast(bf16x8, make_uint4(h[0], h[1], h[2], h[3]));
       asm volatile("" : "+v"(hi[ks & 1]));
-      if (kExact) {
-        lo[ks & 1] = __builtin_bit_cast(bf16x8, make_uint4(l[0], l[1], l[2], l[3]));
-        asm volatile("" : "+v"(lo[ks & 1]));
-      }
+      lo[ks & 1] = __builtin_bit_cast(bf16x8, make_uint4(l[0], l[1], l[2], l[3]));
+      asm volatile("" : "+v"(lo[ks & 1]));
     } else {
       asm volatile("" : "+v"(h[q]));
     }
@@ -224,90 +220,27 @@ constexpr int kChunkCopies = 4;  // of one tensor, by each wave
 
 __device__ __forceinline__ float fade_of(float g2, int m) { return -expm1f(g2 * 0.693147180559945309f * (float)m); }
 
-// w_j = u e^{g(m - off - j)} of this lane's rows in the transpose reads, in their
-// order, for the m rows of a chunk, 0 past them.
-__device__ __forceinline__ void row_weights(float (&w)[4][8], float u, int off, float g2, int m, int hh) {
+// w_j = u e^{g(m - off - j)} of this lane's rows in the transpose reads from row
+// 16 ks0 on, in their order, for the m rows of a chunk, 0 past them.
+template <int n>
+__device__ __forceinline__ void row_weights(float (&w)[n][8], int ks0, float u, int off, float g2, int m, int hh) {
 #pragma unroll
-  for (int ks = 0; ks < 4; ++ks)
+  for (int ks = 0; ks < n; ++ks)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int j = 16 * ks + 4 * hh + (i & 3) + 8 * (i >> 2);
+      const int j = 16 * (ks0 + ks) + 4 * hh + (i & 3) + 8 * (i >> 2);
       w[ks][i] = j < m ? u * __builtin_amdgcn_exp2f(g2 * (float)max(m - off - j, 0)) : 0.0f;
     }
 }
 constexpr int kAhead = 6;  // operand reads on their way in the slots of a chunk
 
-// The states that segments add, from zero: one pass over b and c.
-constexpr int kStateRing = 4;
-using StateLds = uint8_t[kStateRing][2][kTile];
-template <bool kExact>
-__device__ __forceinline__ void state_walk(State& st, StateLds& lds, const SegmentStates& S, const Walk& W, int wave,
-                                           int lane) {
-  const int hh = lane >> 5, place = state_col_place(lane), c_place = col_place(lane);
-  const uint16_t *pb = slab_of(S.b, W, S.b_div), *pc = slab_of(S.c, W, S.c_div);
-  const uint32_t at0 = lds_address(&lds[0][0][0]);
-  auto copy = [&](int i) __attribute__((always_inline)) {
-    if (i >= W.chunks) return;
-    const uint32_t to = at0 + (i % kStateRing) * (2 * kTile);
-    copy_chunk(to, pb, S.b.sn, W, i, S.reverse, wave, lane);
-    copy_chunk(to + kTile, pc, S.c.sn, W, i, S.reverse, wave, lane);
-  };
-  float fade = fade_of(W.g2, min(kC, W.rows - W.row0)), w[4][8];
-  row_weights(w, S.u, S.off, W.g2, min(kC, W.rows - W.row0), hh);
-  all_landed();
-  copy(0);
-  copy(1);
-  for (int i = 0; i < W.chunks; ++i) {
-    const int m = min(kC, W.rows - W.row0 - i * kC);
-    if (m < kC && i > 0) {  // the last chunk's own
-      int half = hh;  // (not computed ahead of the loop and kept)
-      asm volatile("" : "+v"(half));
-      row_weights(w, S.u, S.off, W.g2, m, half);
-      fade = fade_of(W.g2, m);
-    }
-    if (i + 1 < W.chunks)
-      copies_landed<2 * kChunkCopies>();
-    else
-      copies_landed<0>();
-    const uint8_t *tb = lds[i % kStateRing][0] + place, *tc = lds[i % kStateRing][1] + c_place;
-    bf16x8 cf[4], ring[kAhead];
-    auto read = [&](auto slot) __attribute__((always_inline)) {
-      constexpr int f = decltype(slot)::value;
-      if constexpr (f < 16) ring[f % kAhead] = col_frag(tb, f >> 2, f & 3);
-    };
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) cf[ks] = col_frag(tc, ks, wave);
-    each<0, kAhead>(read);
-    slot_end();
-    copy(i + 2);
-    Weighted<kExact> x;
-    fade_state(st.s[0], fade, 0, 16);
-    fade_state(st.s[1], fade, 0, 8);
-    each<0, 4>([&](auto q) __attribute__((always_inline)) { x.template make<0, decltype(q)::value>(cf, w); });
-    slot_end();
-    asm volatile("s_nop 1" : "+v"(st.s[0]));
-    // slots of an MFMA (of the two parts): the decay of the results to come in
-    // the first four, the next weighted rows in all
-    each<0, 16>([&](auto slot) __attribute__((always_inline)) {
-      constexpr int f = decltype(slot)::value, ks = f >> 2, t = f & 3;
-      if constexpr (ks < 3) x.template make<ks + 1, t>(cf, w);
-      score(st.s[t], ring[f % kAhead], x.hi[ks & 1]);
-      if (kExact) score(st.s[t], ring[f % kAhead], x.lo[ks & 1]);
-      read(std::integral_constant<int, f + kAhead>{});
-      if constexpr (f == 0) fade_state(st.s[1], fade, 8, 8);
-      if constexpr (f == 0) fade_state(st.s[2], fade, 0, 8);
-      if constexpr (f == 1) fade_state(st.s[2], fade, 8, 8);
-      if constexpr (f == 1) fade_state(st.s[3], fade, 0, 8);
-      if constexpr (f == 2) fade_state(st.s[3], fade, 8, 8);
-      if constexpr (f < 3) asm volatile("s_nop 1" : "+v"(st.s[f + 1]));
-      slot_end();
-    });
-    settle(st.s[0], st.s[1]);
-    settle(st.s[2], st.s[3]);
-  }
-}
-__global__ __launch_bounds__(kThreads, 2) void lin_state_kernel(StateArgs A) {
-  __shared__ __attribute__((aligned(1024))) StateLds lds;
+// The states that segments add, from zero: one pass over b and c, 128 rows a
+// turn.  Eight waves, two a SIMD (one hides the other's waits): 32 columns of the
+// state and one half of the turn's rows each, the halves' states added up at the
+// end.
+constexpr int kStateRows = 2 * kC;
+__global__ __launch_bounds__(kScanThreads, 2) void lin_state_kernel(StateArgs A) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][2][kTile];  // ring of two; b, c; halves
   lds_poison(lds, sizeof(lds));
   lds_poison_done();
   const int all = xcd_local_id(blockIdx.x, gridDim.x);
@@ -316,15 +249,79 @@ __global__ __launch_bounds__(kThreads, 2) void lin_state_kernel(StateArgs A) {
   const Walk W = make_walk(A.sh, id, A.sh.nseg * A.sh.parts, A.sh.seg_rows / A.sh.parts);
   // the last segment's state is wanted by the final state alone
   if (W.seg >= (A.sh.nseg - 1) * A.sh.parts && !S.state_out) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hh = lane >> 5;
+  const int wc = wave & 3, half = wave >> 2;  // columns, rows
+  const int place = state_col_place(lane), c_place = col_place(lane);
+  // waves 0 to 3 copy b, 4 to 7 c (past the last 64 rows those again: weight 0)
+  const uint16_t* from = half ? slab_of(S.c, W, S.c_div) : slab_of(S.b, W, S.b_div);
+  const int64_t sn = half ? S.c.sn : S.b.sn;
+  const uint32_t at0 = lds_address(&lds[0][half][0][0]);
+  auto copy = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      copy_chunk(at0 + (i & 1) * (4 * kTile) + x * kTile, from, sn, W, min(2 * i + x, W.chunks - 1), S.reverse, wc, lane);
+  };
   State st{};
-  if (W.chunks > 0) {
-    if (S.state_out)
-      state_walk<true>(st, lds, S, W, wave, lane);
-    else
-      state_walk<false>(st, lds, S, W, wave, lane);
+  const int turns = (W.chunks + 1) / 2;
+  const int m0 = min(kStateRows, W.rows - W.row0);
+  float fade = fade_of(W.g2, m0), w[4][8];
+  row_weights(w, 4 * half, S.u, S.off, W.g2, m0, hh);
+  all_landed();
+  if (turns > 0) copy(0);
+  for (int i = 0; i < turns; ++i) {
+    const int m = min(kStateRows, W.rows - W.row0 - i * kStateRows);
+    if (m < kStateRows && i > 0) {  // the last turn's own
+      int h = hh;  // (not computed ahead of the loop and kept)
+      asm volatile("" : "+v"(h));
+      row_weights(w, 4 * half, S.u, S.off, W.g2, m, h);
+      fade = fade_of(W.g2, m);
+    }
+    copies_landed<0>();
+    const uint8_t *tb = lds[i & 1][0][half] + place, *tc = lds[i & 1][1][half] + c_place;
+    bf16x8 cf[4], ring[kAhead];
+    auto read = [&](auto slot) __attribute__((always_inline)) {
+      constexpr int f = decltype(slot)::value;
+      if constexpr (f < 16) ring[f % kAhead] = col_frag(tb, f >> 2, f & 3);
+    };
+    cf[0] = col_frag(tc, 0, wc);
+    each<0, kAhead>(read);
+#pragma unroll
+    for (int ks = 1; ks < 4; ++ks) cf[ks] = col_frag(tc, ks, wc);
+    slot_end();
+    if (i + 1 < turns) copy(i + 1);
+    Weighted x;
+    fade_state(st.s[0], fade, 0, 16);
+    each<0, 4>([&](auto q) __attribute__((always_inline)) { x.make<0, decltype(q)::value>(cf, w); });
+    slot_end();
+    asm volatile("s_nop 1" : "+v"(st.s[0]));
+    // slots of two MFMAs (the parts of c w): the next weighted rows, and in the
+    // first three the decay of the next result
+    each<0, 16>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int f = decltype(slot)::value, ks = f >> 2, t = f & 3;
+      if constexpr (ks < 3) x.make<ks + 1, t>(cf, w);
+      score(st.s[t], ring[f % kAhead], x.hi[ks & 1]);
+      score(st.s[t], ring[f % kAhead], x.lo[ks & 1]);
+      read(std::integral_constant<int, f + kAhead>{});
+      if constexpr (f < 3) {
+        fade_state(st.s[f + 1], fade, 0, 16);
+        asm volatile("s_nop 1" : "+v"(st.s[f + 1]));
+      }
+      slot_end();
+    });
+    settle(st.s[0], st.s[1]);
+    settle(st.s[2], st.s[3]);
   }
-  store_state(st, S.local + W.at * kStateElems, 32 * wave + (lane & 31), lane >> 5);
+  // the halves' sum
+  __syncthreads();
+  f32x16* other = reinterpret_cast<f32x16*>(&lds[0][0][0][0]) + wc * 256 + lane;
+  if (half)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) other[64 * t] = st.s[t];
+  __syncthreads();
+  if (half) return;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) st.s[t] += other[64 * t];
+  store_state(st, S.local + W.at * kStateElems, 32 * wc + (lane & 31), hh);
 }
 
 // The states before each segment, from what their parts add: in place, one
@@ -394,9 +391,7 @@ __device__ __forceinline__ void tile_product(f32x16 (&s)[2], const bf16x8 (&bf)[
 //   16  y = a S        with S (1 - fade) for the update, and the first weighted c
 //   16  S += b^T (c w) with the next weighted c; the C x C tiles arrive on the way
 //    6  z = P c        after eight of those; the last eight add y and z up
-constexpr int kScanThreads = 512;
 constexpr int kScanRing = 3;
-template <bool kExact>
 __global__ __launch_bounds__(kScanThreads, 2) void lin_scan_kernel(ScanArgs A) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kScanRing][3][kTile];
   __shared__ __attribute__((aligned(16))) uint4 pf[3][2][64];  // tiles (0,0), (1,0), (1,1): 16 columns, lane
@@ -492,14 +487,14 @@ __global__ __launch_bounds__(kScanThreads, 2) void lin_scan_kernel(ScanArgs A) {
                         S.r * __builtin_amdgcn_exp2f(W.g2 * (float)(32 + l32 + S.off))};
   float fade = fade_of(W.g2, min(kC, W.rows - W.row0));
   float w[4][8];
-  row_weights(w, S.u, S.off, W.g2, min(kC, W.rows - W.row0), hh);
+  row_weights(w, 0, S.u, S.off, W.g2, min(kC, W.rows - W.row0), hh);
   all_landed();
   for (int i = 0; i < W.chunks; ++i) {
     const int row = W.row0 + i * kC, m = min(kC, W.rows - row);
     if (m < kC && i > 0) {  // the last chunk's own
       int half = hh;  // (not computed ahead of the loop and kept)
       asm volatile("" : "+v"(half));
-      row_weights(w, S.u, S.off, W.g2, m, half);
+      row_weights(w, 0, S.u, S.off, W.g2, m, half);
       fade = fade_of(W.g2, m);
     }
     bf16x8 sf[8];
@@ -510,7 +505,7 @@ __global__ __launch_bounds__(kScanThreads, 2) void lin_scan_kernel(ScanArgs A) {
     const uint8_t *ta = lds[i % kScanRing][0], *tb = lds[i % kScanRing][1] + place, *tc = lds[i % kScanRing][2] + c_place;
     f32x16 y[2], z[2];
     bf16x8 ring[kAhead], cf[4], pt[3][2];
-    Weighted<kExact> x;
+    Weighted x;
     uint32_t pk[8];
     auto read = [&](auto slot) __attribute__((always_inline)) {
       constexpr int f = decltype(slot)::value;
@@ -521,9 +516,9 @@ __global__ __launch_bounds__(kScanThreads, 2) void lin_scan_kernel(ScanArgs A) {
     };
     auto update = [&](auto slot) __attribute__((always_inline)) {
       constexpr int f = decltype(slot)::value, ks = (f - 16) >> 2, t = f & 3;
-      if constexpr (ks < 3) x.template make<ks + 1, t>(cf, w);
+      if constexpr (ks < 3) x.make<ks + 1, t>(cf, w);
       score(st.s[t], ring[f % kAhead], x.hi[ks & 1]);
-      if (kExact) score(st.s[t], ring[f % kAhead], x.lo[ks & 1]);
+      score(st.s[t], ring[f % kAhead], x.lo[ks & 1]);
       read(std::integral_constant<int, f + kAhead>{});
       slot_end();
       if constexpr (f >= 24) {  // four rows' worth of y and z
@@ -568,7 +563,7 @@ __global__ __launch_bounds__(kScanThreads, 2) void lin_scan_kernel(ScanArgs A) {
     each<0, 16>([&](auto slot) __attribute__((always_inline)) {
       constexpr int f = decltype(slot)::value, t = f >> 2;
       fade_state(st.s[t], fade, 4 * (f & 3), 4);
-      if constexpr (f >= 12) x.template make<0, f - 12>(cf, w);
+      if constexpr (f >= 12) x.make<0, f - 12>(cf, w);
       asm volatile("" : "+v"(st.s[t]));
       if constexpr (f < 2)
         score_first(y[f], sf[0], ring[f % kAhead]);
@@ -703,16 +698,13 @@ __global__ __launch_bounds__(kThreads) void lin_step_kernel(LinStep A) {
 }
 
 // The state pass and the join where there are several segments, then the scans.
-hipError_t launch_scans(const StateArgs& st, const ScanArgs& sc, int64_t slabs, bool exact, hipStream_t stream) {
+hipError_t launch_scans(const StateArgs& st, const ScanArgs& sc, int64_t slabs, hipStream_t stream) {
   const unsigned wgs = (unsigned)(slabs * sc.sh.nseg);
   if (sc.sh.nseg > 1) {
-    hipLaunchKernelGGL(lin_state_kernel, dim3(wgs * sc.sh.parts * st.n), dim3(kThreads), 0, stream, st);
+    hipLaunchKernelGGL(lin_state_kernel, dim3(wgs * sc.sh.parts * st.n), dim3(kScanThreads), 0, stream, st);
     hipLaunchKernelGGL(lin_join_kernel, dim3((unsigned)(slabs * 16 * st.n)), dim3(kThreads), 0, stream, st);
   }
-  if (exact)
-    hipLaunchKernelGGL(lin_scan_kernel<true>, dim3(wgs * sc.n), dim3(kScanThreads), 0, stream, sc);
-  else
-    hipLaunchKernelGGL(lin_scan_kernel<false>, dim3(wgs * sc.n), dim3(kScanThreads), 0, stream, sc);
+  hipLaunchKernelGGL(lin_scan_kernel, dim3(wgs * sc.n), dim3(kScanThreads), 0, stream, sc);
   return hipGetLastError();
 }
 
@@ -788,7 +780,7 @@ hipError_t launch_lin_fwd(const LinFwd& a, hipStream_t stream) {
   st.sh = sc.sh;
   st.n = 1;
   st.st[0] = {a.k, a.v, per, per, a.state_in, 0, a.state_out, a.states, 1.0f, 1, 0};
-  return launch_scans(st, sc, (int64_t)a.B * a.H, a.state_out && sc.sh.nseg == 1, stream);
+  return launch_scans(st, sc, (int64_t)a.B * a.H, stream);
 }
 
 // The three gradients in one launch (dq forwards; dk and dv backwards, side by
@@ -832,17 +824,16 @@ hipError_t launch_lin_bwd(const LinBwd& a, hipStream_t stream) {
   st.n = 2;
   st.st[0] = {a.v, a.k, per, per, a.state_in, 1, nullptr, a.states, 1.0f, 1, 0};
   st.st[1] = {a.q, a.dout, 1, 1, a.dstate_in, 0, a.dstate_out, a.states + sec, a.scale, 0, 1};
-  const bool exact = a.dstate_out && sc.sh.nseg == 1;  // of the scans: else the state pass's
   hipError_t e;
   if (in_place) {
     ScanArgs last = sc;
     sc.n = 2;
     last.n = 1;
     last.scan[0] = sc.scan[2];
-    e = launch_scans(st, sc, slabs, false, stream);
-    if (e == hipSuccess) e = launch_scans(st, last, slabs, exact, stream);
+    e = launch_scans(st, sc, slabs, stream);
+    if (e == hipSuccess) e = launch_scans(st, last, slabs, stream);
   } else {
-    e = launch_scans(st, sc, slabs, exact, stream);
+    e = launch_scans(st, sc, slabs, stream);
   }
   if (e != hipSuccess) return e;
   if (a.partial) {
