@@ -520,7 +520,8 @@ int sol_attn_fwd_records(const void* rec, const void* k_prep, const void* v_prep
  * workspace: sol_lin_attn_fwd_workspace_bytes / _bwd_workspace_bytes bytes of
  * device memory (0: none is needed and NULL is taken), 16-byte aligned, not
  * overlapping any tensor; its contents are scratch.  Those return 0 for
- * invalid sizes too.  D = 128; 1 <= N <= SOL_MAX_TOKENS.
+ * invalid sizes too.  D = 128; 1 <= N <= SOL_MAX_TOKENS; B*H and R*H <= 2^21,
+ * B*Hk*N <= 2^26 for the gradients of shared heads.
  */
 typedef struct sol_strides {
   int64_t b, h, n;

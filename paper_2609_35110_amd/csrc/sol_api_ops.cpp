@@ -127,10 +127,12 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
     if (st_ != SOL_OK) return st_;    \
   } while (0)
 
-// Workgroups of a linear pass, each launch a 1D grid: 16 a slab at least (the
-// join) and the segments, at most 512 or one a slab.
-int check_lin_grid(int64_t slabs) {
-  if (slabs > INT32_MAX / 16) return fail(SOL_ERR_UNSUPPORTED, "B*H too large");
+// (b, h) slabs of a linear call.  A launch is a 1D grid of fewer than 2^32
+// threads: three scans of 512 a slab, or four workgroups of 256 a request and
+// head; segments add to a call of few slabs only.
+constexpr int64_t kMaxSlabs = (int64_t)1 << 21;
+int check_slabs(const char* what, int64_t slabs) {
+  if (slabs > kMaxSlabs) return fail(SOL_ERR_UNSUPPORTED, "%s too large (at most 2^21)", what);
   return SOL_OK;
 }
 
@@ -162,13 +164,13 @@ constexpr uint64_t kStateBytes = (uint64_t)sol::kStateElems * sizeof(float);
 extern "C" {
 
 size_t sol_lin_attn_fwd_workspace_bytes(int B, int H, int N, int D) {
-  if (B < 1 || H < 1 || N < 1 || D != sol::kHeadDim || N > SOL_MAX_TOKENS || (int64_t)B * H > INT32_MAX / 16) return 0;
+  if (B < 1 || H < 1 || N < 1 || D != sol::kHeadDim || N > SOL_MAX_TOKENS || (int64_t)B * H > kMaxSlabs) return 0;
   return sol::lin_states_bytes((int64_t)B * H, N, 1);
 }
 
 size_t sol_lin_attn_bwd_workspace_bytes(int B, int H, int Hk, int N, int D) {
   if (Hk < 1 || H < Hk || H % Hk) return 0;
-  if (B < 1 || N < 1 || D != sol::kHeadDim || N > SOL_MAX_TOKENS || (int64_t)B * H > INT32_MAX / 16) return 0;
+  if (B < 1 || N < 1 || D != sol::kHeadDim || N > SOL_MAX_TOKENS || (int64_t)B * H > kMaxSlabs) return 0;
   const size_t partial = Hk < H ? (size_t)2 * B * H * N * D * sizeof(float) : 0;
   return up256(sol::lin_states_bytes((int64_t)B * H, N, 3)) + partial;
 }
@@ -178,7 +180,7 @@ int sol_lin_attn_fwd(const void* q, const sol_strides* q_strides, const void* k,
                      const float* log_decay, const float* state_in, float* state_out, const int32_t* lens, int B, int H,
                      int Hk, int N, int D, float scale, void* workspace, size_t workspace_bytes, sol_stream_t stream) {
   SOL_TRY(check_heads(B, H, Hk, N, D));
-  SOL_TRY(check_lin_grid((int64_t)B * H));
+  SOL_TRY(check_slabs("B*H", (int64_t)B * H));
   sol::LinFwd a = {};
   Span in[6], outs[3];
   SOL_TRY(take_rows("q", q, q_strides, B, H, N, false, &a.q, &in[0]));
@@ -224,9 +226,9 @@ int sol_lin_attn_bwd(const void* dout, const sol_strides* dout_strides, const vo
                      const float* dstate_out, float* dstate_in, const int32_t* lens, int B, int H, int Hk, int N, int D,
                      float scale, void* workspace, size_t workspace_bytes, sol_stream_t stream) {
   SOL_TRY(check_heads(B, H, Hk, N, D));
-  SOL_TRY(check_lin_grid((int64_t)B * H));
-  // the shared heads' sum runs one thread per 16-byte chunk
-  if ((int64_t)B * Hk * N > (int64_t)INT32_MAX * 8) return fail(SOL_ERR_UNSUPPORTED, "B*Hk*N too large");
+  SOL_TRY(check_slabs("B*H", (int64_t)B * H));
+  // the shared heads' sum runs one thread per 16-byte chunk of dk and dv
+  if (Hk < H && (int64_t)B * Hk * N > ((int64_t)1 << 26)) return fail(SOL_ERR_UNSUPPORTED, "B*Hk*N too large");
   sol::LinBwd a = {};
   Span in[8], outs[5];
   SOL_TRY(take_rows("dout", dout, dout_strides, B, H, N, false, &a.dout, &in[0]));
@@ -274,7 +276,7 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
                       const float* log_decay, float* state, const int32_t* slots, int R, int H, int Hk, int n_slots,
                       int D, float scale, sol_stream_t stream) {
   SOL_TRY(check_heads(R, H, Hk, 1, D));
-  if ((int64_t)R * H > INT32_MAX / 4) return fail(SOL_ERR_UNSUPPORTED, "R*H too large");
+  SOL_TRY(check_slabs("R*H", (int64_t)R * H));
   if (n_slots < 1) return fail(SOL_ERR_INVALID_ARG, "n_slots must be >= 1 (got %d)", n_slots);
   if (!slots && R > n_slots) return fail(SOL_ERR_INVALID_ARG, "%d requests without slots, a pool of %d", R, n_slots);
   sol::LinStep a = {};

@@ -39,6 +39,7 @@ COMMON = [
     (dict(D=64), -2, "head dim"),
     (dict(N=(1 << 23) + 1), -2, "exceeds"),
     (dict(B=1 << 20, H=1 << 10, Hk=1), -2, "too large"),
+    (dict(B=(1 << 20) + 1, H=2, Hk=1), -2, "B*H too large"),
     (dict(scale=float("nan")), -1, "scale"),
     (dict(scale=float("inf")), -1, "scale"),
     (dict(q=None), -1, "q must not be NULL"),
@@ -122,6 +123,7 @@ def step(**kw):
     (dict(Hk=3), -1, "multiple"),
     (dict(D=64), -2, "head dim"),
     (dict(B=1 << 21, H=1 << 10, Hk=1), -2, "too large"),
+    (dict(B=(1 << 20) + 1, H=2, Hk=1), -2, "R*H too large"),
     (dict(n_slots=0), -1, "n_slots"),
     (dict(slots=None, B=4), -1, "without slots"),
     (dict(slots=at(7) + 2), -1, "slots must be 4-byte"),
