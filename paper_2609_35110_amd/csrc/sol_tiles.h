@@ -115,6 +115,8 @@ __device__ __forceinline__ bf16x8 col_frag(const uint8_t* p, int y, int d) {
 __device__ __forceinline__ uint32_t copy_offset(int row, int64_t sn, int lane) {
   return (uint32_t)(row * sn * 2) + ((lane & 7) ^ swizzle(lane >> 3)) * 16;
 }
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // M0 is a reserved register
 __device__ __forceinline__ void copy_1k(uint32_t lds, const void* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
@@ -128,6 +130,7 @@ __device__ __forceinline__ void copy_256(uint32_t lds, const void* base, uint32_
                : "s"(lds), "v"(off), "s"(base)
                : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // This wave's copies but the last kLeft are in LDS, and every wave's once all
 // have passed.
 template <int kLeft>

@@ -822,7 +822,7 @@ def _scratch(workspace, nbytes, dev):
 def _call(entry, dev, *args):
     """entry(*args, stream), on the tensors' device and its current stream."""
     i = dev.index
-    if i == torch.cuda.current_device():
+    if i == torch._C._cuda_getDevice():
         check(entry(*args, torch._C._cuda_getCurrentRawStream(i)))
     else:
         with torch.cuda.device(dev):
