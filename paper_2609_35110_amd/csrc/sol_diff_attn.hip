@@ -200,35 +200,50 @@ __device__ __forceinline__ Parts parts_of(float* ws, int64_t rows, int pieces) {
   return {ws, ws + rows * 2 * pieces * D, ws + rows * 2 * pieces * (D + 1), rows};
 }
 
+// Tiles of 128 rows (keys) of the batch's slabs, `heads` per sequence, in the
+// order that workgroups take them, a run of consecutive ones to an XCD:
+//  - slab after slab, sequence after sequence;
+//  - where lengths differ, head after head, so that every XCD has some of each
+//    sequence (4 sequences of 2,047 to 511 rows, 16 heads: forward 227 -> 142 us,
+//    gradients 729 -> 421);
+//  - by rank under a causal mask, the longest tiles of all slabs first, every
+//    eighth to an XCD, so that the short ones fill what the long ones leave
+//    (12,480 rows x 3 heads: forward 413 -> 298 us, gradients 890 -> 667; 4,096 x
+//    24: 241 -> 220, 628 -> 612).  Not where lengths differ and an XCD has two
+//    slabs or more: there one head at a time in its L2 is worth more (4,097 and
+//    2,048 rows x 8 heads: 113 us head after head, 136 by rank).
+__host__ __device__ inline bool by_rank(const DiffShape& s, int heads) {
+  return s.causal && (!(s.q_lens || s.kv_lens) || s.B * heads < 16);
+}
+struct SlabTile {
+  int b, h, rank;
+};
+__device__ __forceinline__ SlabTile slab_tile(int i, int per_slab, int heads, const DiffShape& s) {
+  if (by_rank(s, heads)) {
+    const int slabs = s.B * heads, rank = i / slabs, slab = i - rank * slabs;
+    return {slab / heads, slab % heads, rank};
+  }
+  const int slab = i / per_slab, rank = i - slab * per_slab;
+  if (s.q_lens || s.kv_lens) return {slab % s.B, slab / s.B, rank};
+  return {slab / heads, slab % heads, rank};
+}
 // The tile and piece of a workgroup: tiles [0, full) whole, the rest in pieces.
 struct Piece {
   int tile, piece, pieces;
 };
-__device__ __forceinline__ Piece piece_of(int wg, int tiles, const DiffTiles& p) {
-  if (wg < p.full) return {xcd_local_id(wg, p.full), 0, 1};
-  const int id = xcd_local_id(wg - p.full, (tiles - p.full) * p.pieces);
+__device__ __forceinline__ Piece piece_of(int wg, int tiles, const DiffTiles& p, bool by_rank) {
+  if (wg < p.full) return {by_rank ? wg : xcd_local_id(wg, p.full), 0, 1};
+  const int id = by_rank ? wg - p.full : xcd_local_id(wg - p.full, (tiles - p.full) * p.pieces);
   return {p.full + id / p.pieces, id % p.pieces, p.pieces};
 }
-// Slab i of the batch's `heads` per sequence: sequence after sequence, or, where
-// their lengths differ, head after head, so that every XCD (they take runs of
-// consecutive workgroups) has some of each sequence (4 sequences of 2,047 to 511
-// rows, 16 heads: forward 227 -> 142 us, gradients 729 -> 421).
-struct Slab {
-  int b, h;
-};
-__device__ __forceinline__ Slab slab_at(int i, int heads, const DiffShape& s) {
-  if (s.q_lens || s.kv_lens) return {i % s.B, i / s.B};
-  return {i / heads, i % heads};
-}
-// A tile's place in the batch: tiles of kDiffRows rows, slab after slab (the
-// last rows of a head first: under a causal mask they are the longest).
+// The row tiles: a head's last rows first (under a causal mask the longest).
 struct RowTile {
   int b, h, row0;
 };
 __device__ __forceinline__ RowTile row_tile(int tile, const DiffShape& s) {
   const int per_head = (s.N + kDiffRows - 1) / kDiffRows;
-  const Slab at = slab_at(tile / per_head, s.H, s);
-  return {at.b, at.h, (per_head - 1 - tile % per_head) * kDiffRows};
+  const SlabTile at = slab_tile(tile, per_head, s.H, s);
+  return {at.b, at.h, (per_head - 1 - at.rank) * kDiffRows};
 }
 __host__ __device__ inline int row_tiles_of(const DiffShape& s) {
   return s.B * s.H * ((s.N + kDiffRows - 1) / kDiffRows);
@@ -275,7 +290,7 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, DiffTiles p
   lds_poison_done();
   const DiffShape& s = A.s;
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
-  const Piece pc = piece_of(blockIdx.x, row_tiles_of(s), plan);
+  const Piece pc = piece_of(blockIdx.x, row_tiles_of(s), plan, by_rank(s, s.H));
   const RowTile rt = row_tile(pc.tile, s);
   const int b = rt.b, h = rt.h, row0 = rt.row0;
   const Seq sq = sequence(s, b);
@@ -842,7 +857,7 @@ __device__ __forceinline__ void dq_of(const DiffBwd& A, uint8_t (*lds)[kShared ?
   constexpr int kAhead = 8;
   const DiffShape& s = A.s;
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
-  const Piece pc = piece_of(wg, row_tiles_of(s), A.plan);
+  const Piece pc = piece_of(wg, row_tiles_of(s), A.plan, by_rank(s, s.H));
   const RowTile rt = row_tile(pc.tile, s);
   const int b = rt.b, h = rt.h, row0 = rt.row0;
   const Seq sq = sequence(s, b);
@@ -1042,10 +1057,8 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
   const DiffShape& s = A.s;
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
   const int tiles = (s.M + kDiffRows - 1) / kDiffRows;
-  const int id = xcd_local_id(wg, wgs);
-  const int tile = id % tiles;  // causal: the long columns first
-  const Slab at = slab_at(id / tiles, s.Hv, s);
-  const int hv = at.h, b = at.b;
+  const SlabTile at = slab_tile(by_rank(s, s.Hv) ? wg : xcd_local_id(wg, wgs), tiles, s.Hv, s);
+  const int hv = at.h, b = at.b, tile = at.rank;  // causal: the first keys have the long columns
   const Seq sq = sequence(s, b);
   const int per = s.H / s.Hv;
   const int key0 = tile * kDiffRows;
