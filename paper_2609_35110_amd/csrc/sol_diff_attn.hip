@@ -1058,10 +1058,11 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
   const DiffShape& s = A.s;
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
   const int tiles = (s.M + kDiffRows - 1) / kDiffRows;
-  const SlabTile at = slab_tile(by_rank(s, s.Hv) ? wg : xcd_local_id(wg, wgs), tiles, s.Hv, s);
+  const int id = by_rank(s, s.Hv) ? wg : xcd_local_id(wg, wgs), piece = id % A.key_pieces;
+  const SlabTile at = slab_tile(id / A.key_pieces, tiles, s.Hv, s);
   const int hv = at.h, b = at.b, tile = at.rank;  // causal: the first keys have the long columns
   const Seq sq = sequence(s, b);
-  const int per = s.H / s.Hv;
+  const int per = s.H / s.Hv / A.key_pieces, h0 = (hv * A.key_pieces + piece) * per;  // the piece's query heads
   const int key0 = tile * kDiffRows;
   const int key = key0 + 32 * wave + l32;
   const bool valid = key < sq.klen;
@@ -1083,9 +1084,9 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
   const uint32_t at0 = lds_address(&lds[0][0][0]) + wave * kRowBlock;
   const uint32_t stat0 = lds_address(&stat[0][0]) + (wave & 1) * 256;
   const int copy_row = 8 * wave + (lane >> 3);
-  const uint16_t* qh = A.q.p + b * A.q.sb + 2 * (int64_t)hv * per * A.q.sh;
-  const uint16_t* gh = A.dout.p + b * A.dout.sb + (int64_t)hv * per * A.dout.sh;
-  const float* sth = A.stats + (int64_t)(b * s.H + hv * per) * row_tiles * kStatFloats + (wave & 1) * 64;
+  const uint16_t* qh = A.q.p + b * A.q.sb + 2 * (int64_t)h0 * A.q.sh;
+  const uint16_t* gh = A.dout.p + b * A.dout.sb + (int64_t)h0 * A.dout.sh;
+  const float* sth = A.stats + (int64_t)(b * s.H + h0) * row_tiles * kStatFloats + (wave & 1) * 64;
   // Tile after tile (head after head) into the ring, one kilobyte at a time; past
   // the last tile it comes again, and is not used.
   constexpr int kCopies = 7;
@@ -1143,7 +1144,7 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
   const int cp = col_place(lane);
   int u = 0, left = head_turns;  // of the last tile: its head, and the tiles of that head from it on
   int rt = first;                // row tile of the turn's scores
-  float lam = uniform(s.lambda[hv * per]);
+  float lam = uniform(s.lambda[h0]);
   // of the keys' operands, the first map's beside the gradients, and V's where
   // there is room; the second map's beside the scores
   auto hold_operands = [&]() __attribute__((always_inline)) {
@@ -1188,11 +1189,11 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
     if (--left == 0) {
 #pragma unroll
       for (int m = 1; m < 64; m <<= 1) dlam += __shfl_xor(dlam, m);
-      if (lane == 0) A.partial[((int64_t)(hv * per + u) * s.B + b) * A.parts + tile * 4 + wave] = dlam;
+      if (lane == 0) A.partial[((int64_t)(h0 + u) * s.B + b) * A.parts + tile * 4 + wave] = dlam;
       dlam = 0.0f;
       ++u;
       left = head_turns;
-      lam = uniform(s.lambda[hv * per + min(u, per - 1)]);
+      lam = uniform(s.lambda[h0 + min(u, per - 1)]);
     }
   };
   auto turn = [&](int i, Scores& now, Scores& old) __attribute__((always_inline)) {
@@ -1284,7 +1285,22 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
     }
     copies_landed<0>();  // none is under way when the wave ends
   } else if (lane < 1) {
-    for (int n = 0; n < per; ++n) A.partial[((int64_t)(hv * per + n) * s.B + b) * A.parts + tile * 4 + wave] = 0.0f;
+    for (int n = 0; n < per; ++n) A.partial[((int64_t)(h0 + n) * s.B + b) * A.parts + tile * 4 + wave] = 0.0f;
+  }
+  if (A.key_pieces > 1) {
+    float* o = A.dkv_parts +
+               (((((int64_t)b * s.Hv + hv) * tiles + tile) * A.key_pieces + piece) * 3 * kDiffRows + key - key0) * D + 4 * hh;
+#pragma unroll
+    for (int m = 0; m < 1 + kK; ++m)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x16& x = m ? dk[m - 1][d] : dv[d];
+          *reinterpret_cast<float4*>(o + m * kDiffRows * D + 32 * d + 8 * q) =
+              make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+        }
+    return;
   }
   // zero behind the sequence
   uint8_t* mine = reinterpret_cast<uint8_t*>(lds) + wave * kOutBytes;
@@ -1356,6 +1372,29 @@ __global__ __launch_bounds__(256) void diff_end_kernel(DiffBwd A) {
       __syncthreads();
     }
     if (threadIdx.x == 0) A.dlambda[h] = (float)-sum[0];
+    return;
+  }
+  const int dq_blocks = (row_tiles_of(s) - A.plan.full) * (kDiffRows / kJoinRows);
+  if ((int)blockIdx.x - s.H >= dq_blocks) {  // 16 rows of dv or of a map's dk, from the pieces' sums
+    const int tiles = (s.M + kDiffRows - 1) / kDiffRows, per_tile = kDiffRows / 16, grads = s.Hk == s.Hv ? 2 : 3;
+    const int w = blockIdx.x - s.H - dq_blocks, m = w % grads, id = w / grads / per_tile;
+    const int r = w / grads % per_tile * 16 + (threadIdx.x >> 4), cc = threadIdx.x & 15;
+    const int key = id % tiles * kDiffRows + r, bh = id / tiles, b = bh / s.Hv, hv = bh - b * s.Hv;
+    if (key >= s.M) return;
+    const bool valid = key < sequence(s, b).klen;
+    float f[8] = {};
+    for (int u = 0; u < A.key_pieces && valid; ++u) {
+      const float4* p = reinterpret_cast<const float4*>(
+          A.dkv_parts + ((((int64_t)id * A.key_pieces + u) * 3 + m) * kDiffRows + r) * D + 8 * cc);
+      const float4 x = p[0], y = p[1];
+      f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+      f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] *= m ? s.scale : 1.0f;
+    const Rows& y = m ? A.dk : A.dv;
+    const int head = m == 0 ? hv : grads == 2 ? hv : 2 * hv + m - 1;
+    *reinterpret_cast<uint4*>(y.p + b * y.sb + head * y.sh + (int64_t)key * y.sn + 8 * cc) = pack_bf16x8(f);
     return;
   }
   const int w = blockIdx.x - s.H, tile = w / (kDiffRows / kJoinRows);
@@ -1472,11 +1511,38 @@ hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
 // against 48), times the heads that share a value head; the row tiles that would
 // stand past the time that the chip needs for all of it at best are cut along
 // the keys.
-static DiffTiles bwd_tiles(const DiffShape& s) {
+struct BwdCost {
+  int64_t keys, key, row;  // key tiles; a key tile's time, a row tile's, in slots of an MFMA (0.025 us)
+};
+static BwdCost bwd_cost(const DiffShape& s) {
+  return {(int64_t)s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows), (int64_t)(s.H / s.Hv) * ((s.N + 31) / 32) * 48,
+          (int64_t)((s.M + 31) / 32) * 40};
+}
+// A key tile walks the rows of all the query heads that share it.  Where that
+// takes longer than the chip needs for everything, its heads go to several
+// workgroups, if that saves more than their sums' way through the workspace
+// costs: gradients of 2,000 rows and keys, 16 heads on 2, 686 -> 216 us, 500 rows,
+// 8 heads on 1, 186 -> 45; 2,047, 4 x 16 heads on 4, stay whole (755).
+static int key_pieces(const DiffShape& s) {
+  const BwdCost c = bwd_cost(s);
+  const double part = s.causal ? 1.0 - 0.5 * std::min(s.N, s.M) / s.M : 1.0;  // of all pairs that are seen
+  const double fair = part * (double)(c.keys * c.key + row_tiles_of(s) * c.row) / kCus;
+  double least = std::max((double)c.key, fair);
+  int pieces = 1;
+  for (int p = 2; p <= s.H / s.Hv; ++p) {
+    if (s.H / s.Hv % p) continue;
+    const double time = std::max((double)c.key / p, fair) + 400 + 4.0 * c.keys * p;
+    if (time < least) {
+      least = time;
+      pieces = p;
+    }
+  }
+  return pieces;
+}
+static DiffTiles bwd_tiles(const DiffShape& s, int pieces) {
   const int tiles = row_tiles_of(s);
-  const int64_t keys = (int64_t)s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows);
-  // in units of an MFMA slot of one 128 x 32 block
-  const int64_t key_cost = (int64_t)(s.H / s.Hv) * ((s.N + 31) / 32) * 48, row_cost = (int64_t)((s.M + 31) / 32) * 40;
+  const BwdCost c = bwd_cost(s);
+  const int64_t keys = c.keys * pieces, key_cost = c.key / pieces, row_cost = c.row;
   const int64_t best = (keys * key_cost + tiles * row_cost) / kCus;  // a CU's time if nothing idled
   const int64_t round = keys / kCus, more = keys % kCus;             // `more` CUs take round + 1 key tiles
   const int64_t a = best - round * key_cost, b = a - key_cost;
@@ -1491,37 +1557,44 @@ size_t diff_bwd_bytes(const DiffShape& s, DiffBwd* a) {
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t row_tiles = (size_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows);
   const int parts = 4 * ((s.M + kDiffRows - 1) / kDiffRows);
-  const DiffTiles plan = bwd_tiles(s);
-  size_t at[4] = {};
+  const int pieces = key_pieces(s);
+  const DiffTiles plan = bwd_tiles(s, pieces);
+  size_t at[5] = {};
   at[0] = up(row_tiles * kStatFloats * sizeof(float));
   at[1] = up(at[0] + row_tiles * sizeof(float));
   at[2] = up(at[1] + (size_t)s.H * s.B * parts * sizeof(float));
   at[3] = at[2];
   if (plan.pieces > 1)
     at[3] += (size_t)(row_tiles_of(s) - plan.full) * plan.pieces * 2 * kDiffRows * D * sizeof(float);
+  at[4] = at[3];
+  if (pieces > 1) at[4] += (size_t)bwd_cost(s).keys * pieces * 3 * kDiffRows * D * sizeof(float);
   if (a) {
     char* ws = reinterpret_cast<char*>(a->stats);
     a->delta = reinterpret_cast<float*>(ws + at[0]);
     a->partial = reinterpret_cast<float*>(ws + at[1]);
     a->dq_parts = reinterpret_cast<float*>(ws + at[2]);
+    a->dkv_parts = reinterpret_cast<float*>(ws + at[3]);
+    a->key_pieces = pieces;
     a->parts = parts;
     a->plan = plan;
   }
-  return at[3];
+  return at[4];
 }
 
 hipError_t launch_diff_bwd(const DiffBwd& a, hipStream_t stream) {
   const DiffShape& s = a.s;
   const unsigned row_tiles = (unsigned)((int64_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows));
   hipLaunchKernelGGL(diff_stats_kernel, dim3(row_tiles), dim3(16 * kBwdRows), 0, stream, a);
-  const int keys = s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows);
+  const int key_tiles = s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows), keys = key_tiles * a.key_pieces;
   const int rest = row_tiles_of(s) - a.plan.full;
   const dim3 grid((unsigned)(keys + a.plan.full + rest * a.plan.pieces));
   if (s.Hk == s.Hv)
     hipLaunchKernelGGL(diff_bwd_kernel<true>, grid, dim3(256), 0, stream, a, keys);
   else
     hipLaunchKernelGGL(diff_bwd_kernel<false>, grid, dim3(256), 0, stream, a, keys);
-  hipLaunchKernelGGL(diff_end_kernel, dim3((unsigned)(s.H + rest * (kDiffRows / kJoinRows))), dim3(256), 0, stream, a);
+  const int dkv_blocks = a.key_pieces > 1 ? key_tiles * (kDiffRows / 16) * (s.Hk == s.Hv ? 2 : 3) : 0;
+  hipLaunchKernelGGL(diff_end_kernel, dim3((unsigned)(s.H + rest * (kDiffRows / kJoinRows) + dkv_blocks)), dim3(256), 0,
+                     stream, a);
   return hipGetLastError();
 }
 

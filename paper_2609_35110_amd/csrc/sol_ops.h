@@ -126,6 +126,8 @@ struct DiffBwd {
   float* dq_parts; // [row tile that is cut][piece][map][128][128]
   int parts;
   DiffTiles plan;
+  int key_pieces;    // of a key tile's query heads (divides H / Hv)
+  float* dkv_parts;  // [key tile][piece][dv, dk of each map][128][128], several pieces
 };
 // Bytes of workspace; with a given, its sections and plan are filled in (from
 // a->stats on).

@@ -158,6 +158,17 @@ def test_few_rows_over_many_keys(B, H, Hv, own_keys, N, M):
     check(inputs(B, H, Hv, own_keys, N, M, seed=M), causal=True)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,Hv,own_keys,N,M", [(6, 1, False, 700, 130), (4, 1, True, 900, 1), (8, 2, True, 333, 333),
+                                               (3, 1, False, 1500, 260)])
+def test_query_heads_of_a_key_tile_in_pieces(H, Hv, own_keys, N, M, causal):
+    """Few keys under many rows of several heads: the heads' sums of dk and dv are joined."""
+    x = inputs(2, H, Hv, own_keys, N, M, seed=5)
+    check(x, causal=causal)
+    check(x, causal=causal, q_lens=torch.tensor([N, N // 3], dtype=torch.int32),
+          kv_lens=torch.tensor([M // 2, M], dtype=torch.int32))
+
+
 @pytest.mark.parametrize("own_keys", [False, True])
 def test_peaked_rows(own_keys):
     """1 % of the keys times 8: scores of 90 and more, maxima that come late."""
