@@ -1058,11 +1058,12 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
   const DiffShape& s = A.s;
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
   const int tiles = (s.M + kDiffRows - 1) / kDiffRows;
-  const int id = by_rank(s, s.Hv) ? wg : xcd_local_id(wg, wgs), piece = id % A.key_pieces;
-  const SlabTile at = slab_tile(id / A.key_pieces, tiles, s.Hv, s);
+  const int id = by_rank(s, s.Hv) ? wg : xcd_local_id(wg, wgs), pieces = A.head_pieces * A.row_pieces;
+  const SlabTile at = slab_tile(id / pieces, tiles, s.Hv, s);
+  const int piece = id % pieces, row_piece = piece % A.row_pieces;
   const int hv = at.h, b = at.b, tile = at.rank;  // causal: the first keys have the long columns
   const Seq sq = sequence(s, b);
-  const int per = s.H / s.Hv / A.key_pieces, h0 = (hv * A.key_pieces + piece) * per;  // the piece's query heads
+  const int per = s.H / s.Hv / A.head_pieces, h0 = (hv * A.head_pieces + piece / A.row_pieces) * per;  // the piece's heads
   const int key0 = tile * kDiffRows;
   const int key = key0 + 32 * wave + l32;
   const bool valid = key < sq.klen;
@@ -1075,8 +1076,10 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
   load_row(vf, A.v.p + b * A.v.sb + hv * A.v.sh + (int64_t)key * A.v.sn, valid, hh);
 
   // the tiles of rows that see any key of this workgroup, head after head
-  const int first = key0 < sq.klen ? min(max(key0 - sq.shift, 0), sq.qlen) / kBwdRows : 0;
-  const int end = key0 < sq.klen ? (sq.qlen + kBwdRows - 1) / kBwdRows : 0;
+  const int sees = key0 < sq.klen ? min(max(key0 - sq.shift, 0), sq.qlen) / kBwdRows : 0;
+  const int all = key0 < sq.klen ? max((sq.qlen + kBwdRows - 1) / kBwdRows - sees, 0) : 0;
+  const int first = sees + (int)((int64_t)all * row_piece / A.row_pieces);
+  const int end = sees + (int)((int64_t)all * (row_piece + 1) / A.row_pieces);
   const int head_turns = max(end - first, 0), turns = head_turns * per;
   const int row_tiles = (s.N + kBwdRows - 1) / kBwdRows;
   const int wave_last_key = key0 + 32 * wave + 31;
@@ -1189,7 +1192,7 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
     if (--left == 0) {
 #pragma unroll
       for (int m = 1; m < 64; m <<= 1) dlam += __shfl_xor(dlam, m);
-      if (lane == 0) A.partial[((int64_t)(h0 + u) * s.B + b) * A.parts + tile * 4 + wave] = dlam;
+      if (lane == 0) A.partial[((int64_t)(h0 + u) * s.B + b) * A.parts + (tile * A.row_pieces + row_piece) * 4 + wave] = dlam;
       dlam = 0.0f;
       ++u;
       left = head_turns;
@@ -1285,11 +1288,11 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
     }
     copies_landed<0>();  // none is under way when the wave ends
   } else if (lane < 1) {
-    for (int n = 0; n < per; ++n) A.partial[((int64_t)(h0 + n) * s.B + b) * A.parts + tile * 4 + wave] = 0.0f;
+    for (int n = 0; n < per; ++n) A.partial[((int64_t)(h0 + n) * s.B + b) * A.parts + (tile * A.row_pieces + row_piece) * 4 + wave] = 0.0f;
   }
-  if (A.key_pieces > 1) {
+  if (pieces > 1) {
     float* o = A.dkv_parts +
-               (((((int64_t)b * s.Hv + hv) * tiles + tile) * A.key_pieces + piece) * 3 * kDiffRows + key - key0) * D + 4 * hh;
+               (((((int64_t)b * s.Hv + hv) * tiles + tile) * pieces + piece) * 3 * kDiffRows + key - key0) * D + 4 * hh;
 #pragma unroll
     for (int m = 0; m < 1 + kK; ++m)
 #pragma unroll
@@ -1383,9 +1386,10 @@ __global__ __launch_bounds__(256) void diff_end_kernel(DiffBwd A) {
     if (key >= s.M) return;
     const bool valid = key < sequence(s, b).klen;
     float f[8] = {};
-    for (int u = 0; u < A.key_pieces && valid; ++u) {
+    const int pieces = A.head_pieces * A.row_pieces;
+    for (int u = 0; u < pieces && valid; ++u) {
       const float4* p = reinterpret_cast<const float4*>(
-          A.dkv_parts + ((((int64_t)id * A.key_pieces + u) * 3 + m) * kDiffRows + r) * D + 8 * cc);
+          A.dkv_parts + ((((int64_t)id * pieces + u) * 3 + m) * kDiffRows + r) * D + 8 * cc);
       const float4 x = p[0], y = p[1];
       f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
       f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
@@ -1519,25 +1523,34 @@ static BwdCost bwd_cost(const DiffShape& s) {
           (int64_t)((s.M + 31) / 32) * 40};
 }
 // A key tile walks the rows of all the query heads that share it.  Where that
-// takes longer than the chip needs for everything, its heads go to several
-// workgroups, if that saves more than their sums' way through the workspace
-// costs: gradients of 2,000 rows and keys, 16 heads on 2, 686 -> 216 us, 500 rows,
-// 8 heads on 1, 186 -> 45; 2,047, 4 x 16 heads on 4, stay whole (755).
-static int key_pieces(const DiffShape& s) {
+// takes longer than the chip needs for everything, its heads and then their rows
+// (256 or more) go to several workgroups, if that saves more than their sums' way
+// through the workspace costs: gradients of 2,000 rows and keys, 16 heads on 2,
+// 686 -> 216 us, 500 rows, 8 heads on 1, 186 -> 45, 10,000 rows of one head over
+// 100 keys 415 -> 49; causal 5,000 x 5 heads (236, 271 in two) and 2,047, 4 x 16 on 4,
+// stay whole (755).
+struct KeyPieces {
+  int heads, rows;
+  int all() const { return heads * rows; }
+};
+static KeyPieces key_pieces(const DiffShape& s) {
   const BwdCost c = bwd_cost(s);
   const double part = s.causal ? 1.0 - 0.5 * std::min(s.N, s.M) / s.M : 1.0;  // of all pairs that are seen
   const double fair = part * (double)(c.keys * c.key + row_tiles_of(s) * c.row) / kCus;
-  double least = std::max((double)c.key, fair);
-  int pieces = 1;
-  for (int p = 2; p <= s.H / s.Hv; ++p) {
-    if (s.H / s.Hv % p) continue;
-    const double time = std::max((double)c.key / p, fair) + 400 + 4.0 * c.keys * p;
-    if (time < least) {
-      least = time;
-      pieces = p;
+  const int per = s.H / s.Hv;
+  KeyPieces least = {1, 1};
+  double time = std::max((double)c.key, fair);
+  auto consider = [&](KeyPieces p) {
+    const double t = std::max((double)c.key / p.all(), fair) + 600 + 6.0 * c.keys * p.all();
+    if (t < time) {
+      time = t;
+      least = p;
     }
-  }
-  return pieces;
+  };
+  for (int p = 2; p <= per; ++p)
+    if (per % p == 0) consider({p, 1});
+  for (int p = 2; p <= std::min(16, s.N / 256); ++p) consider({per, p});
+  return least;
 }
 static DiffTiles bwd_tiles(const DiffShape& s, int pieces) {
   const int tiles = row_tiles_of(s);
@@ -1556,9 +1569,9 @@ static DiffTiles bwd_tiles(const DiffShape& s, int pieces) {
 size_t diff_bwd_bytes(const DiffShape& s, DiffBwd* a) {
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t row_tiles = (size_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows);
-  const int parts = 4 * ((s.M + kDiffRows - 1) / kDiffRows);
-  const int pieces = key_pieces(s);
-  const DiffTiles plan = bwd_tiles(s, pieces);
+  const KeyPieces pieces = key_pieces(s);
+  const DiffTiles plan = bwd_tiles(s, pieces.all());
+  const int parts = 4 * ((s.M + kDiffRows - 1) / kDiffRows) * pieces.rows;
   size_t at[5] = {};
   at[0] = up(row_tiles * kStatFloats * sizeof(float));
   at[1] = up(at[0] + row_tiles * sizeof(float));
@@ -1567,14 +1580,15 @@ size_t diff_bwd_bytes(const DiffShape& s, DiffBwd* a) {
   if (plan.pieces > 1)
     at[3] += (size_t)(row_tiles_of(s) - plan.full) * plan.pieces * 2 * kDiffRows * D * sizeof(float);
   at[4] = at[3];
-  if (pieces > 1) at[4] += (size_t)bwd_cost(s).keys * pieces * 3 * kDiffRows * D * sizeof(float);
+  if (pieces.all() > 1) at[4] += (size_t)bwd_cost(s).keys * pieces.all() * 3 * kDiffRows * D * sizeof(float);
   if (a) {
     char* ws = reinterpret_cast<char*>(a->stats);
     a->delta = reinterpret_cast<float*>(ws + at[0]);
     a->partial = reinterpret_cast<float*>(ws + at[1]);
     a->dq_parts = reinterpret_cast<float*>(ws + at[2]);
     a->dkv_parts = reinterpret_cast<float*>(ws + at[3]);
-    a->key_pieces = pieces;
+    a->head_pieces = pieces.heads;
+    a->row_pieces = pieces.rows;
     a->parts = parts;
     a->plan = plan;
   }
@@ -1585,14 +1599,14 @@ hipError_t launch_diff_bwd(const DiffBwd& a, hipStream_t stream) {
   const DiffShape& s = a.s;
   const unsigned row_tiles = (unsigned)((int64_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows));
   hipLaunchKernelGGL(diff_stats_kernel, dim3(row_tiles), dim3(16 * kBwdRows), 0, stream, a);
-  const int key_tiles = s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows), keys = key_tiles * a.key_pieces;
+  const int key_tiles = s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows), keys = key_tiles * a.head_pieces * a.row_pieces;
   const int rest = row_tiles_of(s) - a.plan.full;
   const dim3 grid((unsigned)(keys + a.plan.full + rest * a.plan.pieces));
   if (s.Hk == s.Hv)
     hipLaunchKernelGGL(diff_bwd_kernel<true>, grid, dim3(256), 0, stream, a, keys);
   else
     hipLaunchKernelGGL(diff_bwd_kernel<false>, grid, dim3(256), 0, stream, a, keys);
-  const int dkv_blocks = a.key_pieces > 1 ? key_tiles * (kDiffRows / 16) * (s.Hk == s.Hv ? 2 : 3) : 0;
+  const int dkv_blocks = keys > key_tiles ? key_tiles * (kDiffRows / 16) * (s.Hk == s.Hv ? 2 : 3) : 0;
   hipLaunchKernelGGL(diff_end_kernel, dim3((unsigned)(s.H + rest * (kDiffRows / kJoinRows) + dkv_blocks)), dim3(256), 0,
                      stream, a);
   return hipGetLastError();

@@ -122,11 +122,13 @@ struct DiffBwd {
   float* dlambda;
   float* stats;    // [B][H][ceil(N / 32)][4][32]: the workspace's start
   float* delta;    // [B][H][ceil(N / 32)]
-  float* partial;  // [H][B][parts]
+  float* partial;  // [H][B][parts], parts 4 a key tile and row piece
   float* dq_parts; // [row tile that is cut][piece][map][128][128]
   int parts;
   DiffTiles plan;
-  int key_pieces;    // of a key tile's query heads (divides H / Hv)
+  // A key tile's query heads and their rows in head_pieces x row_pieces workgroups
+  // (head_pieces divides H / Hv, and is that where row_pieces > 1).
+  int head_pieces, row_pieces;
   float* dkv_parts;  // [key tile][piece][dv, dk of each map][128][128], several pieces
 };
 // Bytes of workspace; with a given, its sections and plan are filled in (from

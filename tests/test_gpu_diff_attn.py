@@ -160,9 +160,10 @@ def test_few_rows_over_many_keys(B, H, Hv, own_keys, N, M):
 
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("H,Hv,own_keys,N,M", [(6, 1, False, 700, 130), (4, 1, True, 900, 1), (8, 2, True, 333, 333),
-                                               (3, 1, False, 1500, 260)])
-def test_query_heads_of_a_key_tile_in_pieces(H, Hv, own_keys, N, M, causal):
-    """Few keys under many rows of several heads: the heads' sums of dk and dv are joined."""
+                                               (3, 1, False, 1500, 260), (1, 1, True, 2600, 150),
+                                               (2, 1, False, 1300, 40)])
+def test_rows_and_heads_of_a_key_tile_in_pieces(H, Hv, own_keys, N, M, causal):
+    """Few keys under many rows, of several heads: sums of dk and dv are joined."""
     x = inputs(2, H, Hv, own_keys, N, M, seed=5)
     check(x, causal=causal)
     check(x, causal=causal, q_lens=torch.tensor([N, N // 3], dtype=torch.int32),
