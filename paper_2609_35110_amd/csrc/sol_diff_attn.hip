@@ -1534,11 +1534,17 @@ hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
 // stand past the time that the chip needs for all of it at best are cut along
 // the keys.
 struct BwdCost {
-  int64_t keys, key, row;  // key tiles; a key tile's time, a row tile's, in slots of an MFMA (0.025 us)
+  // key tiles; a key tile's time, a row tile's (the longest's under a causal mask),
+  // in slots of an MFMA (0.025 us)
+  int64_t keys, key, row;
+  double fair;  // a CU's time for everything if nothing idled
 };
 static BwdCost bwd_cost(const DiffShape& s) {
-  return {(int64_t)s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows), (int64_t)(s.H / s.Hv) * ((s.N + 31) / 32) * 48,
-          (int64_t)((s.M + 31) / 32) * 40};
+  BwdCost c = {(int64_t)s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows), (int64_t)(s.H / s.Hv) * ((s.N + 31) / 32) * 48,
+               (int64_t)((s.M + 31) / 32) * 40, 0.0};
+  const double seen = s.causal ? 1.0 - 0.5 * std::min(s.N, s.M) / s.M : 1.0;  // of all pairs
+  c.fair = seen * (double)(c.keys * c.key + row_tiles_of(s) * c.row) / kCus;
+  return c;
 }
 // A key tile walks the rows of all the query heads that share it.  Where that
 // takes longer than the chip needs for everything, its heads and then their rows
@@ -1553,8 +1559,7 @@ struct KeyPieces {
 };
 static KeyPieces key_pieces(const DiffShape& s) {
   const BwdCost c = bwd_cost(s);
-  const double part = s.causal ? 1.0 - 0.5 * std::min(s.N, s.M) / s.M : 1.0;  // of all pairs that are seen
-  const double fair = part * (double)(c.keys * c.key + row_tiles_of(s) * c.row) / kCus;
+  const double fair = c.fair;
   const int per = s.H / s.Hv;
   KeyPieces least = {1, 1};
   double time = std::max((double)c.key, fair);
@@ -1574,12 +1579,26 @@ static DiffTiles bwd_tiles(const DiffShape& s, int pieces) {
   const int tiles = row_tiles_of(s);
   const BwdCost c = bwd_cost(s);
   const int64_t keys = c.keys * pieces, key_cost = c.key / pieces, row_cost = c.row;
-  const int64_t best = (keys * key_cost + tiles * row_cost) / kCus;  // a CU's time if nothing idled
+  if (s.causal) {
+    // the longest row tiles cut where they would outlast the rest, if that saves
+    // more than the pieces' way through the workspace costs (one head of 12,480
+    // rows 443 us uncut, 278 cut)
+    double time = std::max((double)row_cost, c.fair);
+    int cut = 1;
+    for (int p = 2; p <= std::min(16, s.M / 512); ++p) {
+      const double t = std::max((double)row_cost / p, c.fair) + 600 + 2.6 * tiles * p;
+      if (t < time) {
+        time = t;
+        cut = p;
+      }
+    }
+    return cut_tiles(tiles, 0, cut, s.M);
+  }
+  const int64_t best = (keys * key_cost + tiles * row_cost) / kCus;
   const int64_t round = keys / kCus, more = keys % kCus;             // `more` CUs take round + 1 key tiles
   const int64_t a = best - round * key_cost, b = a - key_cost;
   int64_t full = (kCus - more) * (a > 0 ? a / row_cost : 0) + more * (b > 0 ? b / row_cost : 0);
   if (full > tiles) full = tiles;
-  if (s.causal && keys + tiles >= kCus) return {tiles, 1};
   // what is left goes to the CUs' remaining time, about rest row_cost in all
   return cut_tiles(tiles, (int)full, filling(tiles, (int)full), s.M);
 }
