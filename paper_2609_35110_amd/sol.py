@@ -944,7 +944,8 @@ def diff_attn_fwd(q, k, v, lam, scale=None, causal=False, q_lens=None, kv_lens=N
     kv_lens int32 [B] on the device (None: all); causal: row i sees keys up to
     i + kv_len - q_len.  Rows of out behind a sequence are not written.
     Returns out, or with training (out, out2, lse), which diff_attn_bwd takes:
-    the second map's own output and the rows' log sums, float32 [B, 2H, N]."""
+    out2 bf16 [B, H, N, 3, D], the second map's own output, what its rounding
+    left and what that of out left, and the rows' log sums, float32 [B, 2H, N]."""
     B, H, Hv, Hk, N, M, D = _diff_shape(q, k, v)
     dev = q.device
     qp, qs = _rows("q", q)
