@@ -566,9 +566,14 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, DiffTiles p
   }
 }
 
+// Groups of rows of one value head's heads in the few-row kernel.
+__host__ __device__ inline int few_groups(const DiffShape& s) {
+  return (int)(((int64_t)(s.H / s.Hv) * s.N + kFewRows - 1) / kFewRows);
+}
 // Few rows over many keys (a token or some drafted ones over a cache): the rows
 // of all heads that share a value head -- row r is token r % N of head
-// hv per + r / N -- fit one wave's 32.  The keys' bytes bound it, so each wave
+// hv per + r / N -- in groups of one wave's 32, a workgroup each (the tile kernel
+// would give every head a tile of 128).  The keys' bytes bound it, so each wave
 // of the workgroup walks every fourth block of 32 keys with both maps on its
 // own, through LDS of its own (no barriers), the next block's bytes in flight
 // in its registers; the four waves' rows are joined at the end.  5.9 TB/s over
@@ -592,14 +597,18 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
   lds_poison_done();
   const DiffShape& s = A.s;
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63, hh = lane >> 5, l32 = lane & 31;
-  int id = blockIdx.x;  // in the grid's order, one after the other over the XCDs: no two read the same keys
+  // (sequence, value head, piece of the keys) after another over the XCDs, but the
+  // groups of rows that read the same keys on one, side by side
+  const int per = s.H / s.Hv, groups = few_groups(s);
+  int id = blockIdx.x / (8 * groups) * 8 + blockIdx.x % 8;
+  const int row_base = blockIdx.x / 8 % groups * kFewRows, n_rows = min(per * s.N - row_base, kFewRows);
+  if (id >= s.B * s.Hv * nsplit) return;
   const int split = id % nsplit;
   id /= nsplit;
   const int hv = id % s.Hv, b = id / s.Hv;
-  const int per = s.H / s.Hv, n_rows = per * s.N;
   const Seq sq = sequence(s, b);
   const float c = s.scale * kLog2e;
-  const int my = min(l32, n_rows - 1);
+  const int my = row_base + min(l32, n_rows - 1);
   const int h = hv * per + my / s.N, row = my % s.N;
   const bool valid = l32 < n_rows && row < sq.qlen;
   const int last = min(row + sq.shift, sq.klen - 1);
@@ -686,7 +695,7 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
   // one pair of dims of one row a thread and turn
   for (int i = t; i < n_rows * (D / 2); i += 256) {
     const int r = i / (D / 2), d = 2 * (i % (D / 2));
-    const int hr = hv * per + r / s.N, n = r % s.N;
+    const int hr = hv * per + (row_base + r) / s.N, n = (row_base + r) % s.N;
     if (n >= sq.qlen) continue;
     float2 o[2];
     float l2[2], exact2[2];
@@ -758,8 +767,11 @@ __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, DiffTiles pla
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     float top = kNoMax, sum = 0.0f, exact = 0.0f;
+    // (loads of eight pieces at a time)
+#pragma unroll 8
     for (int u = 0; u < plan.pieces; ++u) top = fmaxf(top, p.l[(2 * u + m) * rows + i]);
     o[m] = make_float2(0.0f, 0.0f);
+#pragma unroll 8
     for (int u = 0; u < plan.pieces; ++u) {
       const int64_t am = (2 * u + m) * rows + i;
       const float f = __builtin_amdgcn_exp2f(p.l[am] - top);
@@ -1455,13 +1467,16 @@ static int filling(int tiles, int full) { return tiles > full ? kCus / (tiles - 
 
 static DiffPlan diff_plan(const DiffShape& s, bool ragged) {
   DiffPlan p;
-  p.few = (int64_t)(s.H / s.Hv) * s.N <= kFewRows;
+  // (a row group's 128 keys take 4 us here, a tile's 3.7 in the tile kernel: where
+  // groups are fewer than heads.  3 heads x 17 rows over 20,000 keys, 8 key heads, 56
+  // us here and 74 there, 40 x 1 over 20,000 62 and 95, 8 x 40 60 and 58)
+  p.few = few_groups(s) == 1 || (few_groups(s) < s.H / s.Hv && s.N <= kDiffRows);
   if (p.few) {
     // one workgroup a CU, where lengths may differ two, half as long: 32
     // caches of 256 to 8,192 keys, 8 heads, took 141 us uncut, 107 in halves,
     // 114 in thirds (the join with it); equal ones gain nothing from it
-    const int64_t wgs = (int64_t)s.B * s.Hv;
-    int64_t n = (ragged ? 2 : 1) * kCus / wgs;
+    const int64_t wgs = (int64_t)s.B * s.Hv * few_groups(s);
+    int64_t n = (ragged && s.B > 1 && few_groups(s) == 1 ? 2 : 1) * kCus / wgs;
     const int64_t most = s.M / 512;
     if (n > most) n = most;
     p.tiles = {0, (int)(n < 1 ? 1 : n)};
@@ -1507,7 +1522,8 @@ hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
   const DiffPlan p = diff_plan(s, s.kv_lens != nullptr);
   const bool shared = s.Hk == s.Hv;
   if (p.few) {
-    const dim3 grid((unsigned)((int64_t)s.B * s.Hv * p.tiles.pieces));
+    const int64_t units = (int64_t)s.B * s.Hv * p.tiles.pieces;
+    const dim3 grid((unsigned)((units + 7) / 8 * 8 * few_groups(s)));
     if (shared)
       hipLaunchKernelGGL(diff_few_kernel<true>, grid, dim3(256), 0, stream, a, p.tiles.pieces);
     else

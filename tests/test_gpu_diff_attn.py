@@ -151,11 +151,14 @@ def test_against_definition(B, H, Hv, N, M, own_keys, causal):
 
 @pytest.mark.parametrize("B,H,Hv,own_keys,N,M", [(1, 1, 1, True, 1, 5000), (1, 6, 2, False, 1, 2100), (2, 4, 1, True, 8, 1100),
                                                  (1, 8, 1, False, 4, 1024), (1, 2, 1, True, 17, 2048),
-                                                 (1, 1, 1, True, 40, 2900), (1, 2, 2, False, 150, 2500)])
+                                                 (1, 1, 1, True, 40, 2900), (1, 2, 2, False, 150, 2500),
+                                                 (1, 6, 2, False, 17, 1100), (2, 36, 1, True, 1, 2100),
+                                                 (1, 3, 1, True, 40, 1500), (1, 1, 1, False, 90, 2000)])
 def test_few_rows_over_many_keys(B, H, Hv, own_keys, N, M):
     """Tokens at the end of a cache: the keys are split and joined."""
     assert sol.sol_diff_attn_fwd_workspace_bytes(B, H, Hv, N, M, D) > 0  # it is this path
     check(inputs(B, H, Hv, own_keys, N, M, seed=M), causal=True)
+    check(inputs(B, H, Hv, own_keys, N, M, seed=M), causal=True, kv_lens=torch.arange(B, dtype=torch.int32) * 99 + M // 2)
 
 
 @pytest.mark.parametrize("causal", [False, True])
