@@ -739,13 +739,20 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
 }
 
 // The pieces' results joined: a wave takes a row of an output head, two dims a
-// lane, both maps.  Bound by its bytes and, of few rows, by latency: 5 to 13 us in
+// lane, both maps; of few rows, which have many pieces, four waves do.  Bound by its bytes and, of few rows, by latency: 5 to 13 us in
 // the calls above.
 template <bool kFew>
 __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, DiffTiles plan) {
+  __shared__ float2 of[kFew ? 8 : 1][64];
+  __shared__ float sums[kFew ? 8 : 1][3];
+  lds_poison(of, sizeof(of));
+  lds_poison(sums, sizeof(sums));
+  lds_poison_done();
   const DiffShape& s = A.s;
   const int64_t rows = kFew ? (int64_t)s.B * s.H * s.N : (int64_t)(row_tiles_of(s) - plan.full) * kDiffRows;
-  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int kStep = kFew ? 4 : 1;  // pieces: every fourth a wave, or all
+  const int wave = threadIdx.x >> 6;
+  const int64_t i = kFew ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   if (i >= rows) return;
   const int lane = threadIdx.x & 63;
   int b, h, n;
@@ -769,10 +776,10 @@ __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, DiffTiles pla
     float top = kNoMax, sum = 0.0f, exact = 0.0f;
     // (loads of eight pieces at a time)
 #pragma unroll 8
-    for (int u = 0; u < plan.pieces; ++u) top = fmaxf(top, p.l[(2 * u + m) * rows + i]);
+    for (int u = kFew ? wave : 0; u < plan.pieces; u += kStep) top = fmaxf(top, p.l[(2 * u + m) * rows + i]);
     o[m] = make_float2(0.0f, 0.0f);
 #pragma unroll 8
-    for (int u = 0; u < plan.pieces; ++u) {
+    for (int u = kFew ? wave : 0; u < plan.pieces; u += kStep) {
       const int64_t am = (2 * u + m) * rows + i;
       const float f = __builtin_amdgcn_exp2f(p.l[am] - top);
       const float2 x = *reinterpret_cast<const float2*>(p.o + am * D + 2 * lane);
@@ -781,11 +788,29 @@ __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, DiffTiles pla
       o[m].x = __builtin_fmaf(f, x.x, o[m].x);
       o[m].y = __builtin_fmaf(f, x.y, o[m].y);
     }
+    if (kFew) {  // the four waves' parts
+      const int at = wave * 2 + m;
+      of[at][lane] = o[m];
+      if (lane == 0) sums[at][0] = top, sums[at][1] = sum, sums[at][2] = exact;
+      __syncthreads();
+      top = fmaxf(fmaxf(sums[m][0], sums[2 + m][0]), fmaxf(sums[4 + m][0], sums[6 + m][0]));
+      sum = exact = 0.0f;
+      o[m] = make_float2(0.0f, 0.0f);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(sums[2 * w + m][0] - top);
+        sum = __builtin_fmaf(f, sums[2 * w + m][1], sum);
+        exact = __builtin_fmaf(f, sums[2 * w + m][2], exact);
+        o[m].x = __builtin_fmaf(f, of[2 * w + m][lane].x, o[m].x);
+        o[m].y = __builtin_fmaf(f, of[2 * w + m][lane].y, o[m].y);
+      }
+    }
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
     o[m].x *= inv;
     o[m].y *= inv;
     exact2[m] = sum > 0.0f ? top + log2f(exact) : -__builtin_inff();
   }
+  if (kFew && wave) return;
   store_row2(A, b, h, n, 2 * lane, s.lambda[h], o);
   if (A.lse && lane < 2) A.lse[((int64_t)(b * 2 * s.H + 2 * h) + lane) * s.N + n] = (lane ? exact2[1] : exact2[0]) * kLn2;
 }
@@ -1535,7 +1560,7 @@ hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, p.tiles);
   }
   if (const size_t rows = join_rows(s, p)) {
-    const dim3 grid((unsigned)((rows + 3) / 4));
+    const dim3 grid((unsigned)(p.few ? rows : (rows + 3) / 4));
     if (p.few)
       hipLaunchKernelGGL(diff_join_kernel<true>, grid, dim3(256), 0, stream, a, p.tiles);
     else
