@@ -1497,13 +1497,15 @@ static DiffPlan diff_plan(const DiffShape& s, bool ragged) {
   // us here and 74 there, 40 x 1 over 20,000 62 and 95, 8 x 40 60 and 58)
   p.few = few_groups(s) == 1 || (few_groups(s) < s.H / s.Hv && s.N <= kDiffRows);
   if (p.few) {
-    // one workgroup a CU, where lengths may differ two, half as long: 32
-    // caches of 256 to 8,192 keys, 8 heads, took 141 us uncut, 107 in halves,
-    // 114 in thirds (the join with it); equal ones gain nothing from it
+    // One workgroup a CU, of 128 keys or more (one row over 600 keys 20 us in one
+    // piece, 15 in 4; 5,000 keys 26 in 9, 19 in 39).  Where lengths may differ two,
+    // half as long, of 512 or more: 32 caches of 256 to 8,192 keys, 8 heads, took
+    // 141 us uncut, 107 in halves, 114 in thirds (the join with it); equal ones gain
+    // nothing from it.
     const int64_t wgs = (int64_t)s.B * s.Hv * few_groups(s);
-    int64_t n = (ragged && s.B > 1 && few_groups(s) == 1 ? 2 : 1) * kCus / wgs;
-    const int64_t most = s.M / 512;
-    if (n > most) n = most;
+    int64_t n = kCus / wgs;
+    if (ragged && s.B > 1 && few_groups(s) == 1) n = std::max(n, std::min<int64_t>(2 * kCus / wgs, s.M / 512));
+    n = std::min<int64_t>(n, s.M / 128);
     p.tiles = {0, (int)(n < 1 ? 1 : n)};
   } else {
     const int tiles = row_tiles_of(s);
