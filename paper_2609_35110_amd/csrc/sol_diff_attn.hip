@@ -1492,10 +1492,11 @@ static int filling(int tiles, int full) { return tiles > full ? kCus / (tiles - 
 
 static DiffPlan diff_plan(const DiffShape& s, bool ragged) {
   DiffPlan p;
-  // (a row group's 128 keys take 4 us here, a tile's 3.7 in the tile kernel: where
-  // groups are fewer than heads.  3 heads x 17 rows over 20,000 keys, 8 key heads, 56
-  // us here and 74 there, 40 x 1 over 20,000 62 and 95, 8 x 40 60 and 58)
-  p.few = few_groups(s) == 1 || (few_groups(s) < s.H / s.Hv && s.N <= kDiffRows);
+  // A row group's 128 keys take 4 us in the few-row kernel, a tile's 3.7 in the tile
+  // kernel: there where groups are no more than heads.  24 heads on 8, 17 rows,
+  // 20,000 keys 44 us there, 74 in tiles; 40 on 1, one row 29, 95; 16 on 8, 4 x 17
+  // rows, 6,000 keys 47, 62; 2 on 1, 30 rows, 40 keys 13, 11.
+  p.few = few_groups(s) == 1 || (few_groups(s) <= s.H / s.Hv && s.N <= kDiffRows && s.M >= 512);
   if (p.few) {
     // One workgroup a CU, of 128 keys or more (one row over 600 keys 20 us in one
     // piece, 15 in 4; 5,000 keys 26 in 9, 19 in 39).  Where lengths may differ two,
