@@ -1614,7 +1614,7 @@ static KeyPieces key_pieces(const DiffShape& s) {
       least = p;
     }
   };
-  for (int p = 2; p <= per; ++p)
+  for (int p = 2; p <= std::min(per, kCus); ++p)
     if (per % p == 0) consider({p, 1});
   for (int p = 2; p <= std::min(16, s.N / 256); ++p) consider({per, p});
   return least;
