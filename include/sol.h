@@ -489,14 +489,17 @@ int sol_attn_fwd_records(const void* rec, const void* k_prep, const void* v_prep
  * D values contiguous; a NULL strides pointer means contiguous
  * [B][heads][N][D].  Strides are multiples of 8 elements (n: at most 2^24), at
  * least 0 for inputs (0 broadcasts) and such that rows do not meet for
- * outputs; pointers are 16-byte aligned.  An output may not overlap the span of an input or of
- * another output.  log_decay: H floats, <= 0 (-inf: a head without memory).
+ * outputs; pointers are 16-byte aligned.  An output may not overlap the span of
+ * an input or of another output.  log_decay: H floats, <= 0 (-inf: a head
+ * without memory).
  * States: float [B][H][D][D], row = the dim of k, column = the dim of v.  lens:
  * B int32 on the device, or NULL (all N): sequence b has its first lens[b]
  * tokens (taken into 0..N); no token behind them is read.
  *
- * Products run in bf16 with fp32 accumulation; the states are fp32, and what
- * enters them keeps 16 bits or more.  Every call repeats bit for bit.
+ * Products run in bf16 with fp32 accumulation.  The states are fp32, and what
+ * enters them keeps 16 bits or more; where a chunk's rows are multiplied by one
+ * it is rounded to bf16 (sol_lin_attn_step: it is not).  Every call repeats bit
+ * for bit.
  *
  * sol_lin_attn_fwd: out for all tokens.  state_in: the state before the first
  * token (NULL: zero); state_out: receives the one after the last (NULL: not
@@ -570,9 +573,9 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
  * new tokens at the end of a cache do.  A row that sees no key has out = 0.
  *
  * Scores and row sums are fp32; probabilities are rounded to bf16 for the
- * product with v, which is divided by the sum of the rounded ones.  Every call repeats bit for bit.  A call with few rows over
- * many keys splits the keys over workgroups and joins them through the
- * workspace.
+ * product with v, which is divided by the sum of the rounded ones.  Every call
+ * repeats bit for bit.  A call with few rows over many keys splits the keys over
+ * workgroups and joins them through the workspace.
  *
  * sol_diff_attn_fwd: rows of out behind a sequence are left as they are.  For
  * training, out2 ([B][H][N][3][D] bf16, contiguous) receives the second map's
