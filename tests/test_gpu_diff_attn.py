@@ -162,6 +162,17 @@ def test_few_rows_over_many_keys(B, H, Hv, own_keys, N, M):
 
 
 @pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B,H,own_keys,N", [(1, 1, True, 2300), (1, 2, False, 1900), (2, 1, True, 1700)])
+def test_one_head_over_the_whole_chip(B, H, own_keys, N, causal):
+    """Few tiles: rows' keys and keys' rows are cut, forwards and backwards, and joined."""
+    x = inputs(B, H, H, own_keys, N, N, seed=N)
+    check(x, causal=causal)
+    if B > 1:
+        n = torch.tensor([N - 1, N // 2 + 3], dtype=torch.int32)
+        check(x, causal=causal, q_lens=n, kv_lens=n)
+
+
+@pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("H,Hv,own_keys,N,M", [(6, 1, False, 700, 130), (4, 1, True, 900, 1), (8, 2, True, 333, 333),
                                                (3, 1, False, 1500, 260), (1, 1, True, 2600, 150),
                                                (2, 1, False, 1300, 40)])

@@ -108,6 +108,29 @@ def test_backward(B, H, Hk, N, state):
     assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
+@pytest.mark.parametrize("ragged", [False, True])
+def test_segments_whose_states_are_found_in_parts(ragged):
+    """24 slabs of 27 chunks: three segments, the pass for their states in halves of them; one head compared."""
+    B, H, N, h = 2, 12, 1700, 5
+    x = inputs(B, H, H, N, seed=3)
+    assert sol.sol_lin_attn_bwd_workspace_bytes(B, H, H, N, D) == B * H * 3 * 2 * 2 * D * D * 4  # segments, parts, sets
+    lens = torch.tensor([N - 1, 1111], dtype=torch.int32) if ragged else None
+    leaves = [x[n][:, h:h + 1].double().requires_grad_(True) for n in "qkvS"]
+    out, end = recurrence(*leaves[:3], x["g"][h:h + 1], 0.125, leaves[3], lens)
+    rows = torch.ones(B, N) if lens is None else (torch.arange(N) < lens[:, None]).float()
+    do = x["do"].double() * rows[:, None, :, None]
+    ((out * do[:, h:h + 1]).sum() + (end * x["dS"][:, h:h + 1].double()).sum()).backward()
+    y = dev(x)
+    n = None if lens is None else lens.cuda()
+    got = sol.lin_attn_bwd(y["do"], y["q"], y["k"], y["v"], y["g"], scale=0.125, state=y["S"], dfinal_state=y["dS"], lens=n)
+    for a, b in zip(got[:3], leaves):
+        near(a[:, h:h + 1], b.grad)
+    near(got[3][:, h:h + 1], leaves[3].grad, TOL_F32, 100 * TOL_F32)
+    out2, end2 = sol.lin_attn_fwd(y["q"], y["k"], y["v"], y["g"], scale=0.125, state=y["S"], final_state=True, lens=n)
+    near(end2[:, h:h + 1], end.detach(), TOL_F32, 100 * TOL_F32)
+    near(out2[:, h:h + 1].cpu() * rows[:, None, :, None], out.detach() * rows[:, None, :, None])
+
+
 def test_backward_against_differences():
     """A step along random directions of q, k, v and the state, in the 64-bit recurrence, against the kernel's gradients."""
     x = inputs(1, 2, 1, 70, seed=3)
