@@ -518,7 +518,9 @@ int sol_attn_fwd_records(const void* rec, const void* k_prep, const void* v_prep
  * request, or NULL (request r has slot r, R <= n_slots).  A request whose slot
  * is negative is an empty place of the batch: its out is zero.  One whose slot
  * is past the pool, or is an earlier request's of the same call, gets NaN and
- * leaves the pool alone.
+ * leaves the pool alone.  A state decays by what a token takes off it, rounded
+ * once: by nothing where that is less than half of a value's last bit
+ * (g > -2^-25).
  *
  * workspace: sol_lin_attn_fwd_workspace_bytes / _bwd_workspace_bytes bytes of
  * device memory (0: none is needed and NULL is taken), 16-byte aligned, not
