@@ -136,8 +136,14 @@ int check_slabs(const char* what, int64_t slabs) {
   return SOL_OK;
 }
 
-// The shape of a differential call.
-int check_diff(const sol::DiffShape& s, int D) {
+// The sum of shared heads' gradients runs one thread per 16-byte chunk of dk and dv.
+int check_group_sum(int B, int H, int Hk, int N) {
+  if (Hk < H && (int64_t)B * Hk * N > ((int64_t)1 << 26)) return fail(SOL_ERR_UNSUPPORTED, "B*Hk*N too large");
+  return SOL_OK;
+}
+
+// The sizes of a differential call.
+int check_diff_sizes(const sol::DiffShape& s, int D) {
   if (s.B < 1 || s.H < 1 || s.Hv < 1 || s.N < 1 || s.M < 1)
     return fail(SOL_ERR_INVALID_ARG, "B, H, Hv, N, M must be >= 1 (got %d, %d, %d, %d, %d)", s.B, s.H, s.Hv, s.N, s.M);
   if (s.H % s.Hv) return fail(SOL_ERR_INVALID_ARG, "H = %d is not a multiple of Hv = %d", s.H, s.Hv);
@@ -146,10 +152,13 @@ int check_diff(const sol::DiffShape& s, int D) {
   if (D != sol::kHeadDim) return fail(SOL_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", D);
   if (s.N > SOL_MAX_TOKENS || s.M > SOL_MAX_TOKENS)
     return fail(SOL_ERR_UNSUPPORTED, "N=%d or M=%d exceeds %d", s.N, s.M, SOL_MAX_TOKENS);
-  // rows and keys stay below 2^31 (16 and more of each to a workgroup, times
-  // the splits of the few-row calls, at most 256)
+  // rows and keys are counted in 31 bits
   if ((int64_t)s.B * s.H > (1 << 22) || (int64_t)s.B * s.H * s.N > INT32_MAX || (int64_t)s.B * s.Hv * s.M > INT32_MAX)
     return fail(SOL_ERR_UNSUPPORTED, "B*H, B*H*N or B*Hv*M too large");
+  return SOL_OK;
+}
+int check_diff(const sol::DiffShape& s, int D) {
+  SOL_TRY(check_diff_sizes(s, D));
   if (!std::isfinite(s.scale) || !(s.scale > 0.0f)) return fail(SOL_ERR_INVALID_ARG, "scale must be finite and > 0");
   SOL_TRY(check_small("lambda", s.lambda, false));
   SOL_TRY(check_small("q_lens", s.q_lens, true));
@@ -164,13 +173,14 @@ constexpr uint64_t kStateBytes = (uint64_t)sol::kStateElems * sizeof(float);
 extern "C" {
 
 size_t sol_lin_attn_fwd_workspace_bytes(int B, int H, int N, int D) {
-  if (B < 1 || H < 1 || N < 1 || D != sol::kHeadDim || N > SOL_MAX_TOKENS || (int64_t)B * H > kMaxSlabs) return 0;
+  if (check_heads(B, H, H, N, D) != SOL_OK || check_slabs("B*H", (int64_t)B * H) != SOL_OK) return 0;
   return sol::lin_states_bytes((int64_t)B * H, N, 1);
 }
 
 size_t sol_lin_attn_bwd_workspace_bytes(int B, int H, int Hk, int N, int D) {
-  if (Hk < 1 || H < Hk || H % Hk) return 0;
-  if (B < 1 || N < 1 || D != sol::kHeadDim || N > SOL_MAX_TOKENS || (int64_t)B * H > kMaxSlabs) return 0;
+  if (check_heads(B, H, Hk, N, D) != SOL_OK || check_slabs("B*H", (int64_t)B * H) != SOL_OK ||
+      check_group_sum(B, H, Hk, N) != SOL_OK)
+    return 0;
   const size_t partial = Hk < H ? (size_t)2 * B * H * N * D * sizeof(float) : 0;
   return up256(sol::lin_states_bytes((int64_t)B * H, N, 3)) + partial;
 }
@@ -227,8 +237,7 @@ int sol_lin_attn_bwd(const void* dout, const sol_strides* dout_strides, const vo
                      float scale, void* workspace, size_t workspace_bytes, sol_stream_t stream) {
   SOL_TRY(check_heads(B, H, Hk, N, D));
   SOL_TRY(check_slabs("B*H", (int64_t)B * H));
-  // the shared heads' sum runs one thread per 16-byte chunk of dk and dv
-  if (Hk < H && (int64_t)B * Hk * N > ((int64_t)1 << 26)) return fail(SOL_ERR_UNSUPPORTED, "B*Hk*N too large");
+  SOL_TRY(check_group_sum(B, H, Hk, N));
   sol::LinBwd a = {};
   Span in[8], outs[5];
   SOL_TRY(take_rows("dout", dout, dout_strides, B, H, N, false, &a.dout, &in[0]));
@@ -307,9 +316,7 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
 
 size_t sol_diff_attn_fwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D) {
   sol::DiffShape s = {B, H, Hv, Hv, N, M, 1.0f, 0, nullptr, nullptr, nullptr};
-  if (B < 1 || H < 1 || Hv < 1 || N < 1 || M < 1 || H % Hv || D != sol::kHeadDim || N > SOL_MAX_TOKENS ||
-      M > SOL_MAX_TOKENS || (int64_t)B * H * N > INT32_MAX)
-    return 0;
+  if (check_diff_sizes(s, D) != SOL_OK) return 0;
   // the larger of the two masks'
   const size_t all = sol::diff_fwd_bytes(s);
   s.causal = 1;
@@ -319,9 +326,7 @@ size_t sol_diff_attn_fwd_workspace_bytes(int B, int H, int Hv, int N, int M, int
 
 size_t sol_diff_attn_bwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D) {
   sol::DiffShape s = {B, H, Hv, Hv, N, M, 1.0f, 0, nullptr, nullptr, nullptr};
-  if (B < 1 || H < 1 || Hv < 1 || N < 1 || M < 1 || H % Hv || D != sol::kHeadDim || N > SOL_MAX_TOKENS ||
-      M > SOL_MAX_TOKENS || (int64_t)B * H * N > INT32_MAX)
-    return 0;
+  if (check_diff_sizes(s, D) != SOL_OK) return 0;
   const size_t all = sol::diff_bwd_bytes(s, nullptr);
   s.causal = 1;
   const size_t causal = sol::diff_bwd_bytes(s, nullptr);
