@@ -594,7 +594,9 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
  * device memory (0: none is needed and NULL is taken), 16-byte aligned, not
  * overlapping any tensor; its contents are scratch.  Those return 0 for
  * invalid sizes too.  D = 128; 1 <= N, M <= SOL_MAX_TOKENS; B*H <= 2^22,
- * B*H*N and B*Hv*M < 2^31.
+ * B*H*N and B*Hv*M < 2^31, and no launch of 2^32 threads (forward 256 for 128 rows
+ * of a head, backward 512 for 32): B*H*N and B*Hv*M <= 2^25 with B*H <= 2^20 are
+ * always taken.
  */
 size_t sol_diff_attn_fwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D);
 size_t sol_diff_attn_bwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D);

@@ -157,6 +157,11 @@ int check_diff_sizes(const sol::DiffShape& s, int D) {
     return fail(SOL_ERR_UNSUPPORTED, "B*H, B*H*N or B*Hv*M too large");
   return SOL_OK;
 }
+int check_launch(size_t need) {
+  if (need == sol::kTooLarge)
+    return fail(SOL_ERR_UNSUPPORTED, "B, H, N, M too large together (a launch of 2^32 threads or more)");
+  return SOL_OK;
+}
 int check_diff(const sol::DiffShape& s, int D) {
   SOL_TRY(check_diff_sizes(s, D));
   if (!std::isfinite(s.scale) || !(s.scale > 0.0f)) return fail(SOL_ERR_INVALID_ARG, "scale must be finite and > 0");
@@ -321,7 +326,8 @@ size_t sol_diff_attn_fwd_workspace_bytes(int B, int H, int Hv, int N, int M, int
   const size_t all = sol::diff_fwd_bytes(s);
   s.causal = 1;
   const size_t causal = sol::diff_fwd_bytes(s);
-  return all > causal ? all : causal;
+  const size_t most = all > causal ? all : causal;
+  return check_launch(most) == SOL_OK ? most : 0;
 }
 
 size_t sol_diff_attn_bwd_workspace_bytes(int B, int H, int Hv, int N, int M, int D) {
@@ -330,7 +336,8 @@ size_t sol_diff_attn_bwd_workspace_bytes(int B, int H, int Hv, int N, int M, int
   const size_t all = sol::diff_bwd_bytes(s, nullptr);
   s.causal = 1;
   const size_t causal = sol::diff_bwd_bytes(s, nullptr);
-  return all > causal ? all : causal;
+  const size_t most = all > causal ? all : causal;
+  return check_launch(most) == SOL_OK ? most : 0;
 }
 
 int sol_diff_attn_fwd(const void* q, const sol_strides* q_strides, const void* k, const sol_strides* k_strides,
@@ -350,6 +357,7 @@ int sol_diff_attn_fwd(const void* q, const sol_strides* q_strides, const void* k
   SOL_TRY(check_small("lse", lse, true));
   if (!out2 != !lse) return fail(SOL_ERR_INVALID_ARG, "out2 and lse are given together or not at all");
   const size_t need = sol::diff_fwd_bytes(a.s);
+  SOL_TRY(check_launch(need));
   SOL_TRY(check_workspace(workspace, workspace_bytes, need));
   in[3] = span("lambda", lambda, (uint64_t)H * 4);
   in[4] = span("q_lens", q_lens, (uint64_t)B * 4);
@@ -389,6 +397,7 @@ int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const v
   SOL_TRY(check_small("dlambda", dlambda, false));
   a.stats = static_cast<float*>(workspace);
   const size_t need = sol::diff_bwd_bytes(a.s, &a);
+  SOL_TRY(check_launch(need));
   SOL_TRY(check_workspace(workspace, workspace_bytes, need));
   in[5] = span("out2", out2, (uint64_t)B * H * N * D * 6);
   in[6] = span("lse", lse, (uint64_t)B * 2 * H * N * 4);

@@ -1536,10 +1536,20 @@ static size_t join_rows(const DiffShape& s, const DiffPlan& p) {
   return p.few ? (size_t)s.B * s.H * s.N : (size_t)(row_tiles_of(s) - p.tiles.full) * kDiffRows;
 }
 
+// A launch is a 1D grid of fewer than 2^32 threads.
+static bool fits(int64_t workgroups, int threads) { return workgroups < ((int64_t)1 << 32) / threads; }
+
+// Workgroups of the forward kernels (those of the join are fewer than 2^19).
+static int64_t fwd_workgroups(const DiffShape& s, const DiffPlan& p) {
+  if (p.few) return ((int64_t)s.B * s.Hv * p.tiles.pieces + 7) / 8 * 8 * few_groups(s);
+  return p.tiles.full + (int64_t)(row_tiles_of(s) - p.tiles.full) * p.tiles.pieces;
+}
+
 size_t diff_fwd_bytes(const DiffShape& s) {  // with lengths and without
   size_t most = 0;
   for (const bool ragged : {false, true}) {
     const DiffPlan p = diff_plan(s, ragged);
+    if (!fits(fwd_workgroups(s, p), 256)) return kTooLarge;
     most = std::max(most, join_rows(s, p) * p.tiles.pieces * 2 * (D + 2) * sizeof(float));
   }
   return most;
@@ -1549,25 +1559,23 @@ hipError_t launch_diff_fwd(const DiffFwd& a, hipStream_t stream) {
   const DiffShape& s = a.s;
   const DiffPlan p = diff_plan(s, s.kv_lens != nullptr);
   const bool shared = s.Hk == s.Hv;
+  const dim3 grid((unsigned)fwd_workgroups(s, p));
   if (p.few) {
-    const int64_t units = (int64_t)s.B * s.Hv * p.tiles.pieces;
-    const dim3 grid((unsigned)((units + 7) / 8 * 8 * few_groups(s)));
     if (shared)
       hipLaunchKernelGGL(diff_few_kernel<true>, grid, dim3(256), 0, stream, a, p.tiles.pieces);
     else
       hipLaunchKernelGGL(diff_few_kernel<false>, grid, dim3(256), 0, stream, a, p.tiles.pieces);
   } else {
-    const dim3 grid((unsigned)(p.tiles.full + (row_tiles_of(s) - p.tiles.full) * p.tiles.pieces));
     const auto kernel = a.lse ? (shared ? diff_fwd_kernel<true, true> : diff_fwd_kernel<false, true>)
                               : (shared ? diff_fwd_kernel<true, false> : diff_fwd_kernel<false, false>);
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, p.tiles);
   }
   if (const size_t rows = join_rows(s, p)) {
-    const dim3 grid((unsigned)(p.few ? rows : (rows + 3) / 4));
+    const dim3 joins((unsigned)(p.few ? rows : (rows + 3) / 4));
     if (p.few)
-      hipLaunchKernelGGL(diff_join_kernel<true>, grid, dim3(256), 0, stream, a, p.tiles);
+      hipLaunchKernelGGL(diff_join_kernel<true>, joins, dim3(256), 0, stream, a, p.tiles);
     else
-      hipLaunchKernelGGL(diff_join_kernel<false>, grid, dim3(256), 0, stream, a, p.tiles);
+      hipLaunchKernelGGL(diff_join_kernel<false>, joins, dim3(256), 0, stream, a, p.tiles);
   }
   return hipGetLastError();
 }
@@ -1647,11 +1655,29 @@ static DiffTiles bwd_tiles(const DiffShape& s, int pieces) {
   return cut_tiles(tiles, (int)full, filling(tiles, (int)full), s.M);
 }
 
+// Workgroups of the backward launches: the rows' statistics, both walks (the keys'
+// first), the end.
+struct BwdGrids {
+  int64_t stats, keys, walks, end;
+};
+static BwdGrids bwd_grids(const DiffShape& s, const KeyPieces& pieces, const DiffTiles& plan) {
+  const int64_t key_tiles = bwd_cost(s).keys, rest = row_tiles_of(s) - plan.full;
+  BwdGrids g;
+  g.stats = (int64_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows);
+  g.keys = key_tiles * pieces.all();
+  g.walks = g.keys + plan.full + rest * plan.pieces;
+  g.end = s.H + rest * (kDiffRows / kJoinRows);
+  if (pieces.all() > 1) g.end += key_tiles * (kDiffRows / 16) * (s.Hk == s.Hv ? 2 : 3);
+  return g;
+}
+
 size_t diff_bwd_bytes(const DiffShape& s, DiffBwd* a) {
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t row_tiles = (size_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows);
   const KeyPieces pieces = key_pieces(s);
   const DiffTiles plan = bwd_tiles(s, pieces.all());
+  const BwdGrids g = bwd_grids(s, pieces, plan);
+  if (!fits(g.stats, 16 * kBwdRows) || !fits(g.walks, 256) || !fits(g.end, 256)) return kTooLarge;
   const int parts = 4 * ((s.M + kDiffRows - 1) / kDiffRows) * pieces.rows;
   size_t at[5] = {};
   at[0] = up(row_tiles * kStatFloats * sizeof(float));
@@ -1678,18 +1704,14 @@ size_t diff_bwd_bytes(const DiffShape& s, DiffBwd* a) {
 
 hipError_t launch_diff_bwd(const DiffBwd& a, hipStream_t stream) {
   const DiffShape& s = a.s;
-  const unsigned row_tiles = (unsigned)((int64_t)s.B * s.H * ((s.N + kBwdRows - 1) / kBwdRows));
-  hipLaunchKernelGGL(diff_stats_kernel, dim3(row_tiles), dim3(16 * kBwdRows), 0, stream, a);
-  const int key_tiles = s.B * s.Hv * ((s.M + kDiffRows - 1) / kDiffRows), keys = key_tiles * a.head_pieces * a.row_pieces;
-  const int rest = row_tiles_of(s) - a.plan.full;
-  const dim3 grid((unsigned)(keys + a.plan.full + rest * a.plan.pieces));
+  const BwdGrids g = bwd_grids(s, {a.head_pieces, a.row_pieces}, a.plan);
+  hipLaunchKernelGGL(diff_stats_kernel, dim3((unsigned)g.stats), dim3(16 * kBwdRows), 0, stream, a);
+  const dim3 walks((unsigned)g.walks);
   if (s.Hk == s.Hv)
-    hipLaunchKernelGGL(diff_bwd_kernel<true>, grid, dim3(256), 0, stream, a, keys);
+    hipLaunchKernelGGL(diff_bwd_kernel<true>, walks, dim3(256), 0, stream, a, (int)g.keys);
   else
-    hipLaunchKernelGGL(diff_bwd_kernel<false>, grid, dim3(256), 0, stream, a, keys);
-  const int dkv_blocks = keys > key_tiles ? key_tiles * (kDiffRows / 16) * (s.Hk == s.Hv ? 2 : 3) : 0;
-  hipLaunchKernelGGL(diff_end_kernel, dim3((unsigned)(s.H + rest * (kDiffRows / kJoinRows) + dkv_blocks)), dim3(256), 0,
-                     stream, a);
+    hipLaunchKernelGGL(diff_bwd_kernel<false>, walks, dim3(256), 0, stream, a, (int)g.keys);
+  hipLaunchKernelGGL(diff_end_kernel, dim3((unsigned)g.end), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

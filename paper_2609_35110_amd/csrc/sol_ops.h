@@ -80,6 +80,9 @@ constexpr int kDiffRows = 128;  // query rows of a workgroup
 constexpr int kDiffKeys = 64;   // keys of a tile
 constexpr int kFewRows = 32;    // (head of a group, token) rows of the few-row kernel
 
+// In place of a call's workspace: its launches would have 2^32 threads or more.
+constexpr size_t kTooLarge = ~(size_t)0;
+
 // What both directions share.  Hk is Hv (both maps read one key head) or 2 Hv.
 struct DiffShape {
   int B, H, Hv, Hk, N, M;
@@ -101,7 +104,7 @@ struct DiffPlan {
   bool few;
   DiffTiles tiles;
 };
-size_t diff_fwd_bytes(const DiffShape& s);
+size_t diff_fwd_bytes(const DiffShape& s);  // (or kTooLarge)
 
 struct DiffFwd {
   DiffShape s;
@@ -131,8 +134,8 @@ struct DiffBwd {
   int head_pieces, row_pieces;
   float* dkv_parts;  // [key tile][piece][dv, dk of each map][128][128], several pieces
 };
-// Bytes of workspace; with a given, its sections and plan are filled in (from
-// a->stats on).
+// Bytes of workspace, or kTooLarge; with a given, its sections and plan are filled
+// in (from a->stats on).
 size_t diff_bwd_bytes(const DiffShape& s, DiffBwd* a);
 hipError_t launch_diff_bwd(const DiffBwd& a, hipStream_t stream);
 

@@ -1,11 +1,52 @@
-"""What the linear and differential attention's workspace queries answer for sizes
-that the calls refuse, without a GPU."""
+"""Sizes that the linear and differential attention refuse by name, and what the
+workspace queries answer for them, without a GPU (the pointers are never read)."""
 import pytest
 
 from paper_2609_35110_amd import sol
-from test_ops_abi import L  # noqa: F401 (the library is built)
+from test_ops_abi import L, diff_bwd, diff_fwd, refused  # noqa: F401 (L: the library is built)
 
 K = 1 << 10
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=2 * K, H=2 * K, Hv=1, Hk=1, N=511, M=1),            # 2^24 row tiles of 256 threads
+    dict(B=2 * K, H=2 * K, Hv=1, Hk=2, N=500, M=1, causal=0),
+    dict(B=1, H=4 * K * K, Hv=1, Hk=1, N=32, M=512),           # few rows: 2^22 groups on each of eight XCDs
+])
+def test_forward_grids_past_a_launch(kw):
+    refused(-2, "too large", diff_fwd(**kw))
+    shape = (kw["B"], kw["H"], kw["Hv"], kw["N"], kw["M"], 128)
+    assert sol.sol_diff_attn_fwd_workspace_bytes(*shape) == 0
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=2 * K, H=2 * K, Hv=1, Hk=1, N=33, M=1),             # 2^23 groups of 32 rows, 512 threads each
+    dict(B=1, H=4 * K * K, Hv=1, Hk=2, N=100, M=1, causal=0),
+    dict(B=4 * K, H=K, Hv=K, Hk=K, N=1, M=511),                # 2^24 key tiles
+    dict(B=1, H=K * 512 - 1, Hv=1, Hk=1, N=512, M=2560),       # a prime number of heads on one: pieces of key tiles
+])
+def test_backward_grids_past_a_launch(kw):
+    refused(-2, "too large", diff_bwd(**kw))
+    shape = (kw["B"], kw["H"], kw["Hv"], kw["N"], kw["M"], 128)
+    assert sol.sol_diff_attn_bwd_workspace_bytes(*shape) == 0
+
+
+def test_grids_within_a_launch_are_taken():
+    """Sizes just below: these get past the sizes (and find that the made-up tensors overlap)."""
+    refused(-1, "overlaps", diff_fwd(B=2 * K, H=2 * K, Hv=1, Hk=1, N=384, M=1))
+    refused(-1, "workspace needs", diff_bwd(B=2 * K, H=2 * K - 1, Hv=1, Hk=1, N=64, M=1))
+    assert sol.sol_diff_attn_bwd_workspace_bytes(2 * K, 2 * K - 1, 1, 64, 1, 128) > 0
+
+
+@pytest.mark.parametrize("B,H,Hv,N,M", [(1, K * K, 1, 32, 32 * K * K // 4), (K, K, K, 32, 32), (1, 65521, 1, 512, 8 * K * K),
+                                         (1, 40, 40, 111600, 111600), (4, 1, 1, 8 * K * K, 8 * K * K), (1, 4, 4, 1, 8 * K * K),
+                                         (1, 127, 1, 256 * K, 1), (1, 64, 1, 512 * K, 100), (1, K * K, 1, 1, 1)])
+def test_sizes_that_are_always_taken(B, H, Hv, N, M):
+    assert B * H * N <= 1 << 25 and B * Hv * M <= 1 << 25 and B * H <= 1 << 20
+    assert sol.sol_diff_attn_bwd_workspace_bytes(B, H, Hv, N, M, 128) > 0
+    refused(-1, "workspace", diff_bwd(B=B, H=H, Hv=Hv, Hk=Hv, N=N, M=M, ws=None))
+    shape = dict(B=B, H=H, Hv=Hv, Hk=Hv, N=N, M=M)
+    assert diff_fwd(**shape) == -1 and "too large" not in sol.sol_last_error()
 
 
 @pytest.mark.parametrize("query", [sol.sol_diff_attn_fwd_workspace_bytes, sol.sol_diff_attn_bwd_workspace_bytes])
