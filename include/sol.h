@@ -489,9 +489,10 @@ int sol_attn_fwd_records(const void* rec, const void* k_prep, const void* v_prep
  * D values contiguous; a NULL strides pointer means contiguous
  * [B][heads][N][D].  Strides are multiples of 8 elements (n: at most 2^24), at
  * least 0 for inputs (0 broadcasts) and such that rows do not meet for
- * outputs; pointers are 16-byte aligned.  An output may not overlap the span of
- * an input or of another output.  log_decay: H floats, <= 0 (-inf: a head
- * without memory).
+ * outputs; pointers are 16-byte aligned.  No row of an output may meet one of
+ * another tensor: their spans lie apart, or the rows side by side in one buffer
+ * (a packed [B][N][3][H][D]: modulo some stride of theirs each tensor keeps to its
+ * own part).  log_decay: H floats, <= 0 (-inf: a head without memory).
  * States: float [B][H][D][D], row = the dim of k, column = the dim of v.  lens:
  * B int32 on the device, or NULL (all N): sequence b has its first lens[b]
  * tokens (taken into 0..N); no token behind them is read.

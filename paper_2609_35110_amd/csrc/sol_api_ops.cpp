@@ -27,14 +27,47 @@ int done(hipError_t e, const char* what) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// A piece of memory that a call reads or writes.
+// A piece of memory that a call reads or writes: all of its bytes, or rows of D
+// elements in it (strides s and counts n, in elements).
 struct Span {
   const char* name;
   uintptr_t at;
   uint64_t bytes;
+  bool rows;
+  int64_t s[3], n[3];
 };
-bool meet(const Span& x, const Span& y) { return x.bytes && y.bytes && x.at < y.at + y.bytes && y.at < x.at + x.bytes; }
-Span span(const char* name, const void* p, uint64_t bytes) { return {name, reinterpret_cast<uintptr_t>(p), p ? bytes : 0}; }
+Span span(const char* name, const void* p, uint64_t bytes) {
+  return {name, reinterpret_cast<uintptr_t>(p), p ? bytes : 0, false, {}, {}};
+}
+// What rows cover of every `period` elements from their first on, 0 where that is
+// no bound: the strides that are no multiple of it are to stay within one.
+int64_t covered(const Span& x, int64_t period) {
+  int64_t last = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (x.n[i] == 1 || x.s[i] % period == 0) continue;
+    if (x.s[i] > period || x.n[i] - 1 > period / x.s[i]) return 0;
+    last += (x.n[i] - 1) * x.s[i];
+  }
+  return last + sol::kHeadDim <= period ? last + sol::kHeadDim : 0;
+}
+// Rows side by side in one buffer, as of a packed q, k and v: seen modulo a stride
+// of either, neither's part of a period meets the other's.
+bool side_by_side(const Span& x, const Span& y) {
+  if (!x.rows || !y.rows) return false;
+  for (int i = 0; i < 6; ++i) {
+    const int64_t period = i < 3 ? x.s[i] : y.s[i - 3];
+    if ((i < 3 ? x.n[i] : y.n[i - 3]) == 1 || period == 0) continue;
+    const int64_t cx = covered(x, period), cy = covered(y, period);
+    if (!cx || !cy) continue;
+    int64_t from = (static_cast<int64_t>(y.at - x.at) / 2) % period;  // (both are 16-byte aligned)
+    if (from < 0) from += period;
+    if (from >= cx && from + cy <= period) return true;
+  }
+  return false;
+}
+bool meet(const Span& x, const Span& y) {
+  return x.bytes && y.bytes && x.at < y.at + y.bytes && y.at < x.at + x.bytes && !side_by_side(x, y);
+}
 
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
 // Elements between tokens: the kernels' copies address the rows of a tile by 32-bit byte offsets.
@@ -80,7 +113,7 @@ int take_rows(const char* name, const void* p, const sol_strides* st, int B, int
   rows->sb = B == 1 ? 0 : s[0];
   rows->sh = H == 1 ? 0 : s[1];
   rows->sn = N == 1 ? 0 : s[2];
-  *sp = span(name, p, (last + D) * 2);
+  *sp = {name, reinterpret_cast<uintptr_t>(p), (last + D) * 2, true, {s[0], s[1], s[2]}, {n[0], n[1], n[2]}};
   return SOL_OK;
 }
 
