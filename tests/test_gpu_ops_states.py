@@ -40,3 +40,34 @@ def test_slow_heads_keep_their_rate_token_by_token(tokens):
     off = ((chunked.double() - ref) * kept).sum((0, 2, 3)) / (kept * kept).sum((0, 2, 3))
     print("prompt off by", off.tolist())
     assert (off.abs() <= 2e-5).all()
+
+
+def inputs(B, H, Hk, N, seed):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    return {"do": r(B, H, N, D).bfloat16(), "q": r(B, H, N, D).bfloat16(), "k": r(B, Hk, N, D).bfloat16(),
+            "v": r(B, Hk, N, D).bfloat16(), "rate": -torch.exp2(-1.0 - 10.0 * torch.rand(H, generator=g)),
+            "S": r(B, H, D, D), "dS": r(B, H, D, D)}
+
+
+def backward(x, lens=None, **kw):
+    y = {n: t.cuda() for n, t in x.items()}
+    return sol.lin_attn_bwd(y["do"], y["q"], y["k"], y["v"], y["rate"], state=y["S"], dfinal_state=kw.pop("dS", y["dS"]),
+                            lens=lens, **kw)
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("B,H,Hk,N", [(2, 2, 2, 65), (3, 2, 1, 64), (2, 4, 2, 1), (2, 1, 1, 2500), (2, 12, 12, 1700)])
+def test_state_gradient_in_place(B, H, Hk, N, ragged):
+    """dstate written over dfinal_state: the bits of a call with a tensor of its own,
+    in one segment (whose dk reads what dv's walk ends by overwriting) and in several
+    (whose states are joined over it), sequences without tokens among them."""
+    x = inputs(B, H, Hk, N, seed=N)
+    lens = torch.tensor([0, N, N // 2][:B], dtype=torch.int32, device="cuda") if ragged else None
+    want = backward(x, lens)
+    dS = x["dS"].cuda()
+    got = backward(x, lens, dS=dS, dstate=dS)
+    assert got[3] is dS
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    if ragged:
+        assert torch.equal(dS[0].cpu(), x["dS"][0])  # no token: the gradient passes
