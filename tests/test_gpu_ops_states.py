@@ -42,6 +42,19 @@ def test_slow_heads_keep_their_rate_token_by_token(tokens):
     assert (off.abs() <= 2e-5).all()
 
 
+def recurrence(q, k, v, rate, scale, state, lens):
+    """out and the final states in 64 bits, token by token (lens: on the CPU)."""
+    H = q.shape[1]
+    k, v = (x.repeat_interleave(H // x.shape[1], dim=1) for x in (k, v))
+    a = torch.exp(rate.double())[None, :, None, None]
+    out = []
+    for t in range(q.shape[2]):
+        new = a * state + k[:, :, t, :, None] * v[:, :, t, None, :]
+        state = torch.where((t < lens)[:, None, None, None], new, state)
+        out.append(scale * (q[:, :, t, None, :] @ new)[:, :, 0])
+    return torch.stack(out, 2), state
+
+
 def inputs(B, H, Hk, N, seed):
     g = torch.Generator().manual_seed(seed)
     r = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
@@ -71,3 +84,35 @@ def test_state_gradient_in_place(B, H, Hk, N, ragged):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     if ragged:
         assert torch.equal(dS[0].cpu(), x["dS"][0])  # no token: the gradient passes
+
+
+@pytest.mark.parametrize("N", [1, 63, 600])
+@pytest.mark.parametrize("rate", [0.0, -1e-6, -60.0, -float("inf")])
+def test_gradients_of_decays_at_the_ends(rate, N):
+    """No decay, one next to it, heads without memory: the gradients of the 64-bit
+    recurrence.
+
+    As for other decays, dq, dk and dv are rounded once and have at most three
+    roundings of their operands before (the chunk's product, the state, the row of a
+    state's gradient), 2^-8 / sqrt(3) / sqrt(2) = 1.6e-3 each in the mean square of
+    terms of either sign: 2 x 1.6e-3 = 3.2e-3 of the norm; 5e-3, and six standard
+    deviations of a single value against the rms of its row or the tensor's, and its
+    own rounding: 6 x 3.2e-3 + 2^-8 < 3e-2.  dstate: fp32, terms in two bf16 parts
+    (2^-17), sums of 600: 1e-5."""
+    x = inputs(2, 2, 2, N, seed=N + 1)
+    x["rate"] = torch.tensor([rate, -0.3])
+    lens = torch.tensor([N, N // 2], dtype=torch.int32)
+    leaf = {n: x[n].double().requires_grad_(True) for n in ("q", "k", "v", "S")}
+    out, end = recurrence(leaf["q"], leaf["k"], leaf["v"], x["rate"], D ** -0.5, leaf["S"], lens)
+    rows = (torch.arange(N) < lens[:, None])[:, None, :, None]
+    ((out * rows * x["do"].double()).sum() + (end * x["dS"].double()).sum()).backward()
+    got = backward(x, lens.cuda())
+    for name, a in zip(("q", "k", "v", "S"), got):
+        ref, a = leaf[name].grad, a.double().cpu()
+        tol, most = (1e-5, 1e-3) if name == "S" else (5e-3, 3e-2)
+        assert torch.isfinite(a).all()
+        for h in range(2):  # each head against its own norm
+            r, d = ref[:, h], (a - ref)[:, h]
+            assert d.norm() <= tol * r.norm(), (name, h)
+            rms = torch.maximum(r.norm() / r.numel() ** 0.5, r.norm(dim=-1, keepdim=True) / D ** 0.5)
+            assert (d.abs() <= most * torch.maximum(rms, r.abs())).all(), (name, h)
