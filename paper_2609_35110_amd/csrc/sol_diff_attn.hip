@@ -1490,7 +1490,7 @@ static DiffTiles cut_tiles(int tiles, int full, int pieces, int M) {
 // Pieces of the last tiles, which leave part of the chip idle, that fill it.
 static int filling(int tiles, int full) { return tiles > full ? kCus / (tiles - full) : 1; }
 
-static DiffPlan diff_plan(const DiffShape& s, bool ragged) {
+DiffPlan diff_plan(const DiffShape& s, bool ragged) {
   DiffPlan p;
   // A row group's 128 keys take 4 us in the few-row kernel, a tile's 3.7 in the tile
   // kernel: there where groups are no more than heads.  24 heads on 8, 17 rows,

@@ -104,6 +104,7 @@ struct DiffPlan {
   bool few;
   DiffTiles tiles;
 };
+DiffPlan diff_plan(const DiffShape& s, bool ragged);  // ragged: with kv_lens
 size_t diff_fwd_bytes(const DiffShape& s);  // (or kTooLarge)
 
 struct DiffFwd {
