@@ -282,8 +282,8 @@ __device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
 // A row is held to the maximum of its first tile: P and the sums have 8 exponent
 // bits, so scores far above it cost no precision, and most rows' stay within a
 // few binades.  A row whose P add up to more than 2^80 (55 above it in the
-// exponent) has its workgroup walk the keys again, held to the rows' own maxima,
-// found by a walk for scores alone.
+// exponent), or whose products with the values leave fp32, has its workgroup walk the
+// keys again, held to the rows' own maxima, found by a walk for scores alone.
 //
 // 12,480 rows x 24 heads: 3.28 ms, 1,165 TFLOP/s, 90 % of a large bf16 product's
 // rate here; the matrix cores are busy 60 % of the cycles at 1.7 GHz, which the
@@ -479,6 +479,18 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, DiffTiles p
       x[m].m = fmaxf(x[m].m, both_max(top));
     }
   };
+  // Large values under P that pass 1 may leave fp32 with sums that stay below 2^80:
+  // looked for in waves where a row's P add up to more than its keys could at 1.
+  auto not_finite = [&]() __attribute__((always_inline)) {
+    if (!__any(x[0].l > (float)SOL_MAX_TOKENS || x[1].l > (float)SOL_MAX_TOKENS)) return false;
+    uint32_t top = 0;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        top = max(top, max(__float_as_uint(x[0].o[d][r]) & 0x7fffffffu, __float_as_uint(x[1].o[d][r]) & 0x7fffffffu));
+    return top >= 0x7f800000u;
+  };
   for (int attempt = 0; turns > 0; ++attempt) {
     copy(0, 0);
     copy(0, kRing - 1);  // turn 0's products, of P = 0
@@ -498,7 +510,7 @@ __global__ __launch_bounds__(256, 1) void diff_fwd_kernel(DiffFwd A, DiffTiles p
       turn(i + 1, tb, ta);
     }
     copies_landed<0>();  // none is under way when the wave ends
-    if (attempt || !__syncthreads_or(!(x[0].l < kTooMuch && x[1].l < kTooMuch))) break;
+    if (attempt || !__syncthreads_or(!(x[0].l < kTooMuch && x[1].l < kTooMuch) || not_finite())) break;
     clear(x[0]);
     clear(x[1]);
     for (int i = 0; i < turns; ++i) {
