@@ -497,6 +497,10 @@ int sol_attn_fwd_records(const void* rec, const void* k_prep, const void* v_prep
  * B int32 on the device, or NULL (all N): sequence b has its first lens[b]
  * tokens (taken into 0..N); no token behind them is read.
  *
+ * Values are finite where they are read.  One that is not (in q, k, v, dout or a
+ * state) may make NaN of any result of its sequence and its head, or of the heads
+ * that share its key head, those of earlier tokens too, but of no others.
+ *
  * Products run in bf16 with fp32 accumulation.  The states are fp32, and what
  * enters them keeps 16 bits or more; where a chunk's rows are multiplied by one
  * it is rounded to bf16 (sol_lin_attn_step: it is not).  Every call repeats bit
@@ -574,6 +578,11 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
  * is read.  causal: the last row of a sequence sees its last key, the row
  * before it one key less: row i sees keys up to i + kv_lens[b] - q_lens[b], as
  * new tokens at the end of a cache do.  A row that sees no key has out = 0.
+ *
+ * Values are finite where they are read, and q . k above -10^30; one that is not may
+ * make NaN of any result of its sequence and head, or of the heads that share its key
+ * or value head (an infinite value too, where a softmax would give infinity), and of
+ * dlambda of those heads, but of no others.
  *
  * Scores and row sums are fp32; probabilities are rounded to bf16 for the
  * product with v, which is divided by the sum of the rounded ones.  Every call

@@ -843,7 +843,8 @@ def lin_attn_fwd(q, k, v, log_decay, scale=None, state=None, final_state=False, 
     [B, H, D, D] (None: zero), lens int32 [B] on the device (None: all N; rows
     of out behind a sequence are not written).  final_state: also return the
     state after the last token; True, or the tensor that receives it (state
-    itself is allowed).  Returns out, or (out, final state)."""
+    itself is allowed).  Returns out, or (out, final state), which carry no
+    autograd graph whatever the inputs do: the gradients are lin_attn_bwd's."""
     B, H, N, D = _dims("q", q, 4)
     dev = q.device
     Hk = _dims("k", k, 4)[1]
@@ -945,7 +946,8 @@ def diff_attn_fwd(q, k, v, lam, scale=None, causal=False, q_lens=None, kv_lens=N
     i + kv_len - q_len.  Rows of out behind a sequence are not written.
     Returns out, or with training (out, out2, lse), which diff_attn_bwd takes:
     out2 bf16 [B, H, N, 3, D], the second map's own output, what its rounding
-    left and what that of out left, and the rows' log sums, float32 [B, 2H, N]."""
+    left and what that of out left, and the rows' log sums, float32 [B, 2H, N].
+    They carry no autograd graph whatever the inputs do."""
     B, H, Hv, Hk, N, M, D = _diff_shape(q, k, v)
     dev = q.device
     qp, qs = _rows("q", q)

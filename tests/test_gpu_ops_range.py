@@ -34,3 +34,34 @@ def test_large_values_under_scores_far_above_the_first_keys(N, M, own_keys, trai
     out = (out[0] if training else out).double().cpu()
     assert torch.isfinite(out).all()
     assert ((out - ref).abs() <= 2 * 2.0 ** -8 * (1 + lam) * most).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("name", ["q", "k", "v", "do"])
+def test_a_value_that_is_not_finite_stays_in_its_sequence_and_heads(name, bad):
+    """One such value in a sequence's last token: every result of other sequences and
+    of heads that do not read it keeps its bits."""
+    B, H, Hv, N = 2, 4, 2, 700
+    x = {n: t.cuda() for n, t in inputs(B, H, Hv, True, N, N, seed=1).items()}
+    S = torch.randn(B, H, D, D, generator=torch.Generator().manual_seed(2)).cuda()
+    dec = torch.tensor([-0.5, -0.1, -0.01, 0.0]).cuda()
+
+    def run(y):
+        args = (y["q"], y["k"], y["v"], y["lam"])
+        fwd = sol.diff_attn_fwd(*args, causal=True, training=True)
+        lin = (y["q"][:, ::2].contiguous(), y["k"][:, ::2].contiguous(), y["v"], dec)
+        few = sol.diff_attn_fwd(y["q"][:, :, -1:], *args[1:], causal=True)
+        return {"diff": (*fwd[:2], few, *sol.diff_attn_bwd(y["do"], *args, *fwd, causal=True)[:3]),
+                "lin": (*sol.lin_attn_fwd(*lin, state=S, final_state=True),
+                        *sol.lin_attn_bwd(y["do"], *lin, state=S, dfinal_state=S))}
+
+    want = run(x)
+    y = {n: t.clone() for n, t in x.items()}
+    y[name][1, 0, N - 1, 5] = bad  # sequence 1; its first head, map or value head
+    got = run(y)
+    for op, results in want.items():
+        for a, b in zip(results, got[op]):
+            assert torch.equal(a[0], b[0]), op
+            # the heads of the second value head (of q and dq two for each, of k and dk likewise)
+            assert torch.equal(a[1, a.shape[1] // 2:], b[1, b.shape[1] // 2:]), op
+        assert any(not torch.isfinite(b[1].float()).all() for b in got[op])
