@@ -81,7 +81,6 @@ def test_differential(causal):
     assert torch.equal(sol.diff_attn_fwd(q, k, v, lam, causal=causal), out)
     dq, dk, dv, dlam = sol.diff_attn_bwd(do, q, k, v, lam, out, out2, lse, causal=causal)
     picks = torch.tensor(sorted({0, 1, 31, 32, 127, 128, N - 1, N - 2, N - 113, N // 2} | set(range(977, N, 3989))), device="cuda")
-    K, V, w = k[0].double(), v[0, 0].double(), (s, -lam.item() * s)
     K, V, w = k[0].double(), v[0, 0].double(), (s, -lam.double().item() * s)
     sums = {n: torch.zeros(3, len(picks), D, dtype=torch.float64, device="cuda") for n in ("dk0", "dk1", "dv")}
     dl, size, top = 0.0, 0.0, 0.0
