@@ -571,7 +571,7 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
  * [B][Hv][M][D], H a multiple of Hv, output head h reading value head
  * hv = h / (H / Hv); k [B][Hk][M][D] with Hk = 2 Hv (the maps read key heads
  * 2 hv and 2 hv + 1) or Hk = Hv (both read key head hv); out [B][H][N][D].
- * lambda: H floats on the device; scale > 0.
+ * lambda: H floats on the device; scale: 10^-30 to 10^8.
  *
  * Masks: q_lens, kv_lens: B int32 on the device, or NULL (all N, all M): the
  * rows and keys of each sequence (taken into 0..N, 0..M); nothing behind them
@@ -584,8 +584,10 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
  * or value head (an infinite value too, where a softmax would give infinity), and of
  * dlambda of those heads, but of no others.
  *
- * Scores and row sums are fp32; probabilities are rounded to bf16 for the
- * product with v, which is divided by the sum of the rounded ones.  Every call
+ * Scores and row sums are fp32 (a probability is off by up to 2^-21 of its row's
+ * largest |scale q . k|); probabilities are rounded to bf16 for the product
+ * with v, which is divided by the sum of the rounded ones, and backwards what the
+ * products with k, q and dout take is.  Every call
  * repeats bit for bit.  A call with few rows over many keys splits the keys over
  * workgroups and joins them through the workspace.
  *

@@ -198,6 +198,8 @@ int check_launch(size_t need) {
 int check_diff(const sol::DiffShape& s, int D) {
   SOL_TRY(check_diff_sizes(s, D));
   if (!std::isfinite(s.scale) || !(s.scale > 0.0f)) return fail(SOL_ERR_INVALID_ARG, "scale must be finite and > 0");
+  // a row's log sum over the scale and the lowest maximum, -1e30, times it stay in fp32
+  if (s.scale < 1e-30f || s.scale > 1e8f) return fail(SOL_ERR_INVALID_ARG, "scale must be 1e-30 to 1e8 (got %g)", s.scale);
   SOL_TRY(check_small("lambda", s.lambda, false));
   SOL_TRY(check_small("q_lens", s.q_lens, true));
   SOL_TRY(check_small("kv_lens", s.kv_lens, true));

@@ -65,3 +65,37 @@ def test_a_value_that_is_not_finite_stays_in_its_sequence_and_heads(name, bad):
             # the heads of the second value head (of q and dq two for each, of k and dk likewise)
             assert torch.equal(a[1, a.shape[1] // 2:], b[1, b.shape[1] // 2:]), op
         assert any(not torch.isfinite(b[1].float()).all() for b in got[op])
+
+
+@pytest.mark.parametrize("N,M", [(3, 40), (300, 200)])
+@pytest.mark.parametrize("power", [-93, 26])
+def test_scales_at_the_ends(N, M, power):
+    """Queries times 2^-power and the scale times 2^power: the same numbers, bit for bit, the
+    queries' gradient times 2^power (causal: the first rows of 300 on 200 see no key)."""
+    x = {n: t.cuda() for n, t in inputs(1, 2, 1, True, N, M, seed=N).items()}
+
+    def run(q, scale):
+        args = (q, x["k"], x["v"], x["lam"])
+        fwd = sol.diff_attn_fwd(*args, scale=scale, causal=True, training=True)
+        return (*fwd, *sol.diff_attn_bwd(x["do"], *args, *fwd, scale=scale, causal=True))
+
+    want = run(x["q"], 0.125)
+    out, out2, lse, dq, *rest = run((x["q"].double() * 2.0 ** -power).bfloat16(), 0.125 * 2.0 ** power)
+    assert all(torch.equal(a, b) for a, b in zip((out, out2, lse, *rest), want[:3] + want[4:]))
+    assert torch.equal(dq.double(), want[3].double() * 2.0 ** power)
+
+
+def test_the_smallest_scale():
+    """1e-30: all keys weigh the same, forwards and backwards (1 / M and lam / M are off by 2^-8, rounded to bf16,
+    and the sums once more)."""
+    N, M = 70, 200
+    x = inputs(1, 2, 1, True, N, M, seed=N)
+    y = {n: t.cuda() for n, t in x.items()}
+    args = (y["q"], y["k"], y["v"], y["lam"])
+    fwd = sol.diff_attn_fwd(*args, scale=1e-30, training=True)
+    got = sol.diff_attn_bwd(y["do"], *args, *fwd, scale=1e-30)
+    lam, do, v = x["lam"].double()[:, None, None], x["do"].double(), x["v"].double()
+    assert ((fwd[0].double().cpu() - (1 - lam) * v.mean(2, keepdim=True)).abs() <= 2.0 ** -7 * (1 + lam) * v.abs().mean(2, keepdim=True)).all()
+    ref, size = ((1 - lam) * do / M).sum((1, 2)), ((1 + lam) * do.abs() / M).sum((1, 2))
+    assert ((got[2].double().cpu()[:, 0] - ref[:, None]).abs() <= 2.0 ** -7 * size[:, None]).all()
+    assert all(torch.isfinite(t).all() for t in got)

@@ -66,3 +66,10 @@ def test_linear_queries_of_sizes_that_calls_refuse():
     assert sol.sol_lin_attn_bwd_workspace_bytes(1, 8, 8, 8 * K * K, 128) > 0        # (heads of their own: no such sum)
     assert sol.sol_lin_attn_bwd_workspace_bytes(2 ** 31 - 1, 2 ** 31 - 1, 1, 8 * K * K, 128) == 0
     assert sol.sol_lin_attn_fwd_workspace_bytes(2 ** 31 - 1, 2 ** 31 - 1, 8 * K * K, 128) == 0
+
+
+@pytest.mark.parametrize("call", [diff_fwd, diff_bwd])
+@pytest.mark.parametrize("scale", [1e-31, 1e-38, 1.1e8, 3e38])
+def test_scales_past_the_kernels_numbers(call, scale):
+    """Below, a row's log sum over the scale leaves fp32; above, the mask's lowest maximum times the scale does."""
+    refused(-1, "scale", call(scale=scale))
