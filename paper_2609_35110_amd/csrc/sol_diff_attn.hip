@@ -285,10 +285,11 @@ __device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
 // exponent), or whose products with the values leave fp32, has its workgroup walk the
 // keys again, held to the rows' own maxima, found by a walk for scores alone.
 //
-// 12,480 rows x 24 heads: 3.28 ms, 1,165 TFLOP/s, 90 % of a large bf16 product's
-// rate here; the matrix cores are busy 60 % of the cycles at 1.7 GHz, which the
-// chip's power sets (4.2 vector instructions an MFMA).  For training, with the
-// second sum and two more outputs, 3 heads take 457 us instead of 419.
+// 12,480 rows x 24 heads: 3.25 to 3.5 ms by box and what ran before, 1,100 to 1,180
+// TFLOP/s, 84 to 90 % of a large bf16 product's rate here; the matrix cores are busy
+// 60 % of the cycles at 1.7 GHz, which the chip's power sets (4.3 vector instructions
+// an MFMA).  For training, with the second sum and two more outputs, 24 heads take
+// 3,361 us instead of 3,250; causal 2 x 4,097 rows x 8 heads 163 instead of 147.
 constexpr int kFwdKeys = 32;
 constexpr float kTooMuch = 1.2089258e24f;
 template <bool kShared, bool kTrain>
@@ -588,8 +589,9 @@ __host__ __device__ inline int few_groups(const DiffShape& s) {
 // would give every head a tile of 128).  The keys' bytes bound it, so each wave
 // of the workgroup walks every fourth block of 32 keys with both maps on its
 // own, through LDS of its own (no barriers), the next block's bytes in flight
-// in its registers; the four waves' rows are joined at the end.  5.9 TB/s over
-// 111,600 keys (570 us), 5.4 over 32 caches of 256 to 8,192 (102 us).
+// in its registers; the four waves' rows are joined at the end.  5.7 to 5.9 TB/s over
+// 111,600 keys of 40 heads (580 to 600 us), 5.3 over 32 caches of 256 to 8,192 (104 us);
+// P in two bf16 parts, as exact as the outputs' own rounding, costs 2 to 12 % there.
 template <bool kShared>
 __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit) {
   constexpr int kBlock = 32, kWaves = 4;
@@ -751,8 +753,8 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd A, int nsplit)
 }
 
 // The pieces' results joined: a wave takes a row of an output head, two dims a
-// lane, both maps; of few rows, which have many pieces, four waves do.  Bound by its bytes and, of few rows, by latency: 5 to 13 us in
-// the calls above.
+// lane, both maps; of few rows, which have many pieces, four waves do.  Bound by its
+// bytes and, of few rows, by latency: 5 to 13 us in the calls above.
 template <bool kFew>
 __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, DiffTiles plan) {
   __shared__ float2 of[kFew ? 8 : 1][64];
@@ -833,9 +835,11 @@ __global__ __launch_bounds__(256) void diff_join_kernel(DiffFwd A, DiffTiles pla
 //   dS_0 = P_0 (X - delta_0),  dS_1 = -lambda P_1 (X - delta_1),
 //   dq_s = scale dS_s k_s,  dk_s = scale dS_s^T q_s,
 //   dv = (P_0 - lambda P_1)^T dout,  dlambda = - sum P_1 X.
-// P is found again from the rows' log sums.  Two halves, one that owns rows (dq)
-// and one that owns keys (dk, dv, dlambda): no atomics, and every sum in a fixed
-// order.
+// P is found again from the rows' log sums.  dS and P_0 - lambda P_1 are rounded to
+// bf16 for their products with k, q and dout, which are bf16: a result's error is its
+// terms' roundings and its own, of one size (0.0024 of its norm together).  Two
+// halves, one that owns rows (dq) and one that owns keys (dk, dv, dlambda): no
+// atomics, and every sum in a fixed order.
 
 // What the backward kernels know of a row, 32 rows together: kStatLse0, kStatLse1:
 // -lse / scale of the maps, which added to raw scores and scaled gives log2 P
@@ -1390,9 +1394,10 @@ __device__ __forceinline__ void dkv_of(const DiffBwd& A, uint8_t (*lds)[3][kTile
 // Both in one launch, the keys' workgroups first: what either leaves of the last
 // round of the chip's 256 CUs the other fills.
 //
-// 12,480 rows x 3 heads: 1.34 ms; the eight products that the gradients are make
-// 714 TFLOP/s of it, the eleven that it executes (scores and X in both halves)
-// 982, 76 % of a large bf16 product's rate, at the clock that power leaves.
+// 12,480 rows x 3 heads: 1.24 ms, of peaked rows 1.32 to 1.35; the eight products
+// that the gradients are make 710 to 770 TFLOP/s of it, the eleven that it executes
+// (scores and X in both halves) 980 to 1,060, 75 to 82 % of a large bf16 product's
+// rate, at the clock that power leaves.
 template <bool kShared>
 __global__ __launch_bounds__(256, 1) void diff_bwd_kernel(DiffBwd A, int key_wgs) {
   struct Keys {

@@ -239,10 +239,11 @@ constexpr int kAhead = 6;  // operand reads on their way in the slots of a chunk
 // state and one half of the turn's rows each, the halves' states added up at the
 // end.
 //
-// Bound by its bytes when they come from HBM: 111,600 tokens x 40 heads 440 us,
-// 4.3 TB/s (370 us where the rows' second part is left out, which costs the
-// states half their bits); 12,480 x 24 from the caches 34 us, 4.5 TB/s.  One wave
-// a SIMD, 64 rows a turn, took 507 and 37.
+// Bound by its bytes when they come from HBM: 111,600 tokens x 40 heads 420 to 440
+// us, 4.4 to 4.6 TB/s (370 us where the rows' second part is left out, which costs
+// the states half their bits); 12,480 x 24 from the caches 34 us, 5.0 TB/s.  One wave
+// a SIMD, 64 rows a turn, took 507 and 37.  Every row is read, those of a fast head
+// too that leave nothing at the segment's end.
 constexpr int kStateRows = 2 * kC;
 __global__ __launch_bounds__(kScanThreads, 2) void lin_state_kernel(StateArgs A) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][2][kTile];  // ring of two; b, c; halves
@@ -331,7 +332,7 @@ __global__ __launch_bounds__(kScanThreads, 2) void lin_state_kernel(StateArgs A)
 
 // The states before each segment, from what their parts add: in place, one
 // workgroup per slab and 1,024 of its state's values, eight parts' loads in
-// flight.  Few bytes and one chain: 24 heads x 10 segments 7.6 us.
+// flight.  Few bytes and one chain: 24 heads x 10 segments 8 us.
 __global__ __launch_bounds__(kThreads) void lin_join_kernel(StateArgs A) {
   const SegmentStates& S = A.st[blockIdx.x % A.n];
   const int slab = blockIdx.x / A.n >> 4, part = (blockIdx.x / A.n) & 15;
@@ -385,8 +386,9 @@ __device__ __forceinline__ void tile_product(f32x16 (&s)[2], const bf16x8 (&bf)[
 //
 // Waves 0 to 3 own 32 columns each of the state and of y: the state stays in
 // registers (64 a lane), where an MFMA leaves it and the next one takes it as an
-// operand (rounded to bf16 there, as y is a bf16 result: both roundings are of
-// the same size).  Waves 4 to 7 copy the chunks straight into LDS (a ring of
+// operand (rounded to bf16 there, as the C x C product is where c takes it, since y
+// is a bf16 result: the roundings are of the same size, 0.0023 of y's norm together
+// where y's own is 0.0017).  Waves 4 to 7 copy the chunks straight into LDS (a ring of
 // three, two on their way) and find the three 32 x 32 tiles on and below the
 // diagonal of the C x C product, which they pass on in the order the next
 // product reads them, while the others multiply by the state.
@@ -397,10 +399,10 @@ __device__ __forceinline__ void tile_product(f32x16 (&s)[2], const bf16x8 (&bf)[
 //   32  S += b^T (c w) with the next weighted c; the C x C tiles arrive on the way
 //    6  z = P c        after half of those; the others add y and z up
 //
-// Bound by its bytes where the chip is full: 111,600 tokens x 40 heads 1,030 us,
-// 4.4 TB/s of a copy's 4.94; 12,480 x 24 68 us, 4.5.  One workgroup alone takes
-// 1.95 us a chunk (four waves that did all of it, one after the other, 2.75).
-// The gradients' three scans of 12,480 x 24: 190 us for 0.72 GB past L2.
+// Bound by its bytes where the chip is full: 111,600 tokens x 40 heads 1,030 to
+// 1,070 us, 4.3 to 4.5 TB/s of a copy's 4.94; 12,480 x 24 69 us, 4.7.  One workgroup
+// alone takes 1.9 us a chunk (four waves that did all of it, one after the other,
+// 2.75).  The gradients' three scans of 12,480 x 24: 190 to 195 us for 0.76 GB past L2.
 constexpr int kScanRing = 3;
 __global__ __launch_bounds__(kScanThreads, 2) void lin_scan_kernel(ScanArgs A) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kScanRing][3][kTile];
@@ -644,8 +646,8 @@ __global__ __launch_bounds__(kThreads) void lin_group_sum_kernel(GroupSum A) {
 // One token for each request: the state is read, decayed, added to and written,
 // and multiplied by q on the way.  Its bytes bound it (64 KB in and out against
 // 66 kflop), so a workgroup takes a quarter of a state's columns, four 16-byte
-// loads a thread all in flight: 10,240 states 250 us, 5.4 TB/s; 24 of them 3.9 us,
-// a launch and a load's latency.
+// loads a thread all in flight: 10,240 states 270 to 280 us, 4.8 to 5.0 TB/s; 24 of
+// them 4 us, a launch and a load's latency.
 //
 // The decay is taken off as a difference, as in the chunks' states (fade_state):
 // a factor next to 1 rounds the same way for every token, by up to 2^-25 of the
@@ -751,14 +753,15 @@ static int lin_sets(int scans) { return scans > 1 ? 2 : 1; }
 
 // Segments: as many as give each of the 256 CUs one workgroup of the launch's
 // scans, of 256 tokens at least, where that is the faster way.  In times of a
-// chunk (1.75 us), n segments take C / n of the scan, 0.75 as many of the state
+// chunk (1.9 us), n segments take C / n of the scan, 0.75 as many of the state
 // pass, and 7 + workgroups / 64 for two more launches and the states' bytes.
-// Measured, in us, one segment against n: forward of 2 heads x 512 tokens 18
-// against 24 (n = 2), x 1,024 31 against 24 (4); 24 heads x 1,024 31 against 31
-// (4), x 2,048 64 against 36 (8); 64 heads x 1,024 35 against 40 (4), x 2,048 65
-// against 53 (4); 128 heads x 2,048 74 against 86 (2), x 12,480 512 against 446
-// (2).  Gradients of 24 heads x 1,024 34 against 36 (3), x 2,048 63 against 52
-// (3; 69 in 8); 64 heads x 2,048 70 against 111 (4).
+// Measured, in us, one segment against n: forward of 2 heads x 512 tokens 20
+// against 27 (n = 2), x 1,024 35 against 28 (4); 8 heads x 4,096 125 against 37 (16);
+// 24 heads x 1,024 35 against 35 (4), x 2,048 67 against 39 (8); 64 heads x 1,024 37
+// against 43 (4), x 2,048 67 against 58 (4); 128 heads x 2,048 71 against 91 (2), x
+// 12,480 509 against 474 (2).  Gradients of 8 heads x 4,096 127 against 47 (8), 24
+// heads x 1,024 37 against 41 (3), x 2,048 67 against 57 (3; 76 in 8); 64 heads x
+// 2,048 85 against 116 (2).
 LinPlan lin_plan(int64_t slabs, int N, int scans) {
   const int chunks = (N + kC - 1) / kC, most = (chunks + 3) / 4;
   const LinPlan one = {chunks * kC, 1, 1};
