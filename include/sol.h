@@ -579,10 +579,10 @@ int sol_lin_attn_step(const void* q, const sol_strides* q_strides, const void* k
  * before it one key less: row i sees keys up to i + kv_lens[b] - q_lens[b], as
  * new tokens at the end of a cache do.  A row that sees no key has out = 0.
  *
- * Values are finite where they are read, and q . k above -10^30; one that is not may
- * make NaN of any result of its sequence and head, or of the heads that share its key
- * or value head (an infinite value too, where a softmax would give infinity), and of
- * dlambda of those heads, but of no others.
+ * Values are finite where they are read, v below 2^96 in size and q . k above -10^30;
+ * one that is not may make NaN of any result of its sequence and head, or of the heads
+ * that share its key or value head (an infinite value too, where a softmax would give
+ * infinity), and of dlambda of those heads, but of no others.
  *
  * Scores and row sums are fp32 (a probability is off by up to 2^-21 of its row's
  * largest |scale q . k|); probabilities are rounded to bf16 for the product
