@@ -189,3 +189,58 @@ def test_caches_far_apart():
     out = sol.lin_attn_step(*a, rate, pool, slots=slots)
     assert torch.equal(out, sol.lin_attn_step(*a, rate, first))
     assert torch.equal(pool[slots.long()], first)
+
+
+def test_linear_most_slabs():
+    """2^21 sequences of one head: out = scale (q . k) v, dq = scale (do . v) k and its like; the next token of each."""
+    B = 1 << 21
+    g = torch.Generator(device="cuda").manual_seed(7)
+    q, k, v, do = (rand(g, B, 1, 1, D) for _ in range(4))
+    rate, s = torch.tensor([-0.25], device="cuda"), D ** -0.5
+    assert sol.sol_lin_attn_bwd_workspace_bytes(B, 1, 1, 1, D) == 0
+    out = sol.lin_attn_fwd(q, k, v, rate)
+    dq, dk, dv = sol.lin_attn_bwd(do, q, k, v, rate)
+    dot = lambda a, b: s * (a.double() * b.double()).sum(-1, keepdim=True)  # noqa: E731
+    for got, a, b, c in ((out, q, k, v), (dq, do, v, k), (dk, do, v, q), (dv, q, k, do)):
+        for i in range(0, B, B // 8):  # the product is rounded to bf16 once and so is the result, 2^-8 each
+            ref = dot(a[i:i + B // 8], b[i:i + B // 8]) * c[i:i + B // 8].double()
+            # (fp32 dots: 2^-18 of the terms' sizes, where they cancel)
+            slack = 2.0 ** -18 * dot(a[i:i + B // 8].abs(), b[i:i + B // 8].abs()) * c[i:i + B // 8].abs().double()
+            assert ((got[i:i + B // 8].double() - ref).abs() <= 2.02 * 2.0 ** -8 * ref.abs() + slack + 1e-30).all()
+    R = 1 << 17
+    pool = torch.zeros(R, 1, D, D, device="cuda")
+    step = sol.lin_attn_step(q[:R, :, 0], k[:R, :, 0], v[:R, :, 0], rate, pool)
+    ref = dot(q[:R, :, 0], k[:R, :, 0]) * v[:R, :, 0].double()
+    slack = 2.0 ** -18 * dot(q[:R, :, 0].abs(), k[:R, :, 0].abs()) * v[:R, :, 0].abs().double()
+    assert ((step.double() - ref).abs() <= 1.01 * 2.0 ** -8 * ref.abs() + slack + 1e-30).all()
+
+
+@pytest.mark.parametrize("B,H", [(1 << 22, 1), (1 << 10, 1 << 12)])
+def test_differential_most_slabs(B, H):
+    """2^22 output heads of one row and key: out = (1 - lam) v."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q, k, v = rand(g, B, 2, 1, D).expand(B, 2, 1, D), rand(g, B, 2, 1, D), rand(g, B, 1, 1, D)
+    if H > 1:  # one q for all heads, which share a value head
+        q = q[:, :1].expand(B, 2 * H, 1, D)
+    lam = torch.rand(H, generator=g, device="cuda")
+    out = sol.diff_attn_fwd(q, k, v, lam)
+    ref = (1 - lam.double())[None, :, None, None]
+    step = B // 8
+    for i in range(0, B, step):
+        want = ref * v[i:i + step].double()
+        assert ((out[i:i + step].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -22 * v[i:i + step].abs().double()).all()
+
+
+def test_differential_gradients_of_many_slabs():
+    """2^18 sequences of one row and key: dv = (1 - lam) dout, dlam = -sum v . dout, dq and dk zero."""
+    B = 1 << 18
+    g = torch.Generator(device="cuda").manual_seed(9)
+    q, k, v, do = rand(g, B, 2, 1, D), rand(g, B, 2, 1, D), rand(g, B, 1, 1, D), rand(g, B, 1, 1, D)
+    lam = torch.tensor([0.375], device="cuda")
+    dq, dk, dv, dlam = sol.diff_attn_bwd(do, q, k, v, lam, *sol.diff_attn_fwd(q, k, v, lam, training=True))
+    assert torch.equal(dv, (0.625 * do.float()).bfloat16())
+    dot = v.double() * do.double()
+    assert abs(dlam.item() + dot.sum().item()) <= 1e-6 * dot.abs().sum().item()
+    # X - delta cancels: 2^-16 of its terms' sizes (two bf16 parts of o_s and out), times scale k
+    size = (2.0 ** -15 * dot.abs().sum(-1, keepdim=True) + 1e-30) * D ** -0.5
+    assert (dq.double().abs() <= size * k.double().abs()).all() and (dk.double().abs() <= size * q.double().abs()).all()
