@@ -629,6 +629,132 @@ int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const v
                       void* workspace, size_t workspace_bytes, sol_stream_t stream);
 
 /*
+ * Queries and keys normalised and rotated at positions of their own, in one pass
+ * over both: sol_qknorm_rope3d for tokens that are no single raster grid (clips and
+ * images of several sizes in one batch, text among them, the next token of each of
+ * many requests), for tensors that lie in a projection's output, and with its
+ * gradients.  For every row x of q and k, with r = 1/sqrt(mean_d(x_d^2) + eps),
+ *     y = bf16(R(pos) (gamma r x)),
+ * fp32 but for the rotation, which is sol_rope3d's (the same bits; without gamma
+ * r = gamma = 1, and a token that does not turn is copied).
+ *
+ * Tensors: q, q_out [B][H][N][D] and k, k_out [B][Hk][N][D] bf16 with strides,
+ * alignment and overlaps as in sol_lin_attn_fwd above, except that an output may be
+ * its own input, row for row (q_out = q).  Hk = 0: there is no k, and its pointers
+ * are not looked at.  H and Hk need not be multiples of each other.
+ * q_gamma, k_gamma: D floats on the device, 16-byte aligned, or NULL (that tensor is
+ * not normalised).  lens: B int32 on the device, or NULL (all N): sequence b has its
+ * first lens[b] tokens (taken into 0..N); rows of the outputs behind them are left
+ * as they are.
+ *
+ * Positions: pos, int32 on the device, the coordinates (t, h, w) of token (b, n) at
+ * pos[b * pos_stride_b + 3 n], pos_stride_b 0 (one set for all) or at least 3 N; NULL:
+ * nothing turns.  rope_tab is the device copy of sol_rope3d_table_ex(D, T, Hl, Wl, dt,
+ * dh, dw), 16-byte aligned, whose extents need only bound the coordinates.  A
+ * coordinate below 0 turns its axis by nothing (text: -1, -1, -1).  A token with one
+ * at or past its extent gets NaN in all of its rows (an axis without dims has no
+ * coordinate); no memory outside the table is read.
+ *
+ * sol_qk_norm_rope_bwd: from dq_out and dk_out, the gradients of the outputs, and the
+ * call's q and k: dq and dk (bf16, zero behind a sequence; dq may be dq_out itself,
+ * dk dk_out), and the norm weights' gradients dq_gamma and dk_gamma (D floats, 4-byte
+ * aligned, summed over batch, heads and tokens; NULL: not wanted, and so where there
+ * is no gamma).  fp32, rounded once; sums in one order, the same bits every call.
+ * Without q_gamma (k_gamma) q (k) is not looked at.
+ * A token with a coordinate past its extent makes its rows NaN, and the weights'
+ * gradients.  workspace: sol_qk_norm_rope_bwd_workspace_bytes(B, N) bytes of device
+ * memory (0 for invalid sizes), 16-byte aligned, where dq_gamma or dk_gamma is given,
+ * not overlapping any tensor; its contents are scratch.
+ *
+ * D = 128; 1 <= N <= SOL_MAX_TOKENS; B*N <= 2^28; H, Hk <= 2^16; a table of at most
+ * 2^28 pairs; 0 <= eps finite (a row of zeros with eps = 0 gives NaN, as the formula
+ * does).
+ */
+int sol_qk_norm_rope(const void* q, const sol_strides* q_strides, const void* k,
+                     const sol_strides* k_strides, void* q_out,
+                     const sol_strides* q_out_strides, void* k_out,
+                     const sol_strides* k_out_strides, const float* q_gamma,
+                     const float* k_gamma, float eps, const int32_t* pos, int64_t pos_stride_b,
+                     const float* rope_tab, int T, int Hl, int Wl, int dt, int dh, int dw,
+                     const int32_t* lens, int B, int H, int Hk, int N, int D, sol_stream_t stream);
+size_t sol_qk_norm_rope_bwd_workspace_bytes(int B, int N);
+int sol_qk_norm_rope_bwd(const void* dq_out, const sol_strides* dq_out_strides,
+                         const void* dk_out, const sol_strides* dk_out_strides,
+                         const void* q, const sol_strides* q_strides, const void* k,
+                         const sol_strides* k_strides, void* dq,
+                         const sol_strides* dq_strides, void* dk,
+                         const sol_strides* dk_strides, const float* q_gamma,
+                         const float* k_gamma, float* dq_gamma, float* dk_gamma, float eps,
+                         const int32_t* pos, int64_t pos_stride_b, const float* rope_tab, int T,
+                         int Hl, int Wl, int dt, int dh, int dw, const int32_t* lens, int B, int H,
+                         int Hk, int N, int D, void* workspace, size_t workspace_bytes,
+                         sol_stream_t stream);
+
+/*
+ * Cross attention: softmax attention of one sequence's rows to the keys and values of
+ * another, of a length of its own (a text encoder's states, another clip's tokens),
+ *     out = softmax(scale q k^T) v,
+ * over the keys that are visible.  q and k enter as they are: sol_qk_norm_rope
+ * normalises and rotates them.
+ *
+ * Tensors (bf16, strides, alignment and overlaps as in sol_lin_attn_fwd): q, out
+ * [B][H][N][D], k, v [B][Hk][M][D], H a multiple of Hk (query head h reads key and
+ * value head h / (H / Hk)); a stride of 0 shares an encoder's states between
+ * sequences or heads.  scale: 10^-30 to 10^8.
+ *
+ * Masks: q_lens, kv_lens: B int32 on the device, or NULL (all N, all M): the rows and
+ * keys of each sequence (taken into 0..N, 0..M).  key_mask: B * M bytes on the device,
+ * [B][M], or NULL: a key whose byte is 0 is hidden from all of its sequence's rows.
+ * No row or key behind a sequence and no hidden key is read.  A row that sees no key
+ * has out = 0.
+ *
+ * Values are finite where they are read, v below 2^96 in size and q . k above -10^30;
+ * one that is not may make NaN of any result of its sequence and head, or of the heads
+ * that share its key head (an infinite value too, where a softmax would give infinity),
+ * but of no others.
+ *
+ * Scores and row sums are fp32 (a probability is off by up to 2^-21 of its row's
+ * largest |scale q . k|); probabilities are rounded to bf16 for the product with v,
+ * which is divided by the sum of the rounded ones, and backwards what the products
+ * with k, q and dout take is.  Every call repeats bit for bit.
+ *
+ * sol_cross_attn_fwd: rows of out behind a sequence are left as they are.  For
+ * training, out_left ([B][H][N][D] bf16, contiguous) receives what rounding to bf16
+ * left of out, and lse ([B][H][N] floats) the logarithm of each row's sum of
+ * exponentials, -inf for a row that sees no key; both are NULL or neither, and both
+ * are left as they are behind a sequence.
+ *
+ * sol_cross_attn_bwd: from dout, the gradient of out, and the forward call's out,
+ * out_left and lse: dq, dk, dv (bf16, zero behind a sequence and for a hidden key;
+ * shared heads' gradients summed in fp32.  Sequences that share their keys by a stride
+ * of 0 get gradients of their own).
+ *
+ * workspace: sol_cross_attn_fwd_workspace_bytes / _bwd_workspace_bytes bytes of
+ * device memory (masked: whether there is a key_mask; 0: none is needed and NULL is
+ * taken), 16-byte aligned, not overlapping any tensor; its contents are scratch.  Those
+ * return 0 for invalid sizes too.  D = 128; 1 <= N, M <= SOL_MAX_TOKENS; B*H <= 2^22,
+ * B*H*N and B*Hk*M < 2^31, and no launch of 2^32 threads: B*H*N and B*Hk*M <= 2^25 with
+ * B*H <= 2^20 are always taken.
+ */
+size_t sol_cross_attn_fwd_workspace_bytes(int B, int H, int Hk, int N, int M, int D, int masked);
+size_t sol_cross_attn_bwd_workspace_bytes(int B, int H, int Hk, int N, int M, int D, int masked);
+int sol_cross_attn_fwd(const void* q, const sol_strides* q_strides, const void* k,
+                       const sol_strides* k_strides, const void* v, const sol_strides* v_strides,
+                       void* out, const sol_strides* out_strides, void* out_left, float* lse,
+                       const int32_t* q_lens, const int32_t* kv_lens, const uint8_t* key_mask,
+                       int B, int H, int Hk, int N, int M, int D, float scale, void* workspace,
+                       size_t workspace_bytes, sol_stream_t stream);
+int sol_cross_attn_bwd(const void* dout, const sol_strides* dout_strides, const void* q,
+                       const sol_strides* q_strides, const void* k, const sol_strides* k_strides,
+                       const void* v, const sol_strides* v_strides, const void* out,
+                       const sol_strides* out_strides, const void* out_left, const float* lse,
+                       void* dq, const sol_strides* dq_strides, void* dk,
+                       const sol_strides* dk_strides, void* dv, const sol_strides* dv_strides,
+                       const int32_t* q_lens, const int32_t* kv_lens, const uint8_t* key_mask,
+                       int B, int H, int Hk, int N, int M, int D, float scale, void* workspace,
+                       size_t workspace_bytes, sol_stream_t stream);
+
+/*
  * Measurement aid: the dense matrix rate of this GPU at the attention
  * kernels' launch shape.  Launches `workgroups` workgroups of four waves (one
  * per SIMD, as the attention kernels run), each wave issuing iters * 16 fp16

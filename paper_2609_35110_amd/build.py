@@ -12,7 +12,8 @@ LIB = os.path.join(PKG, "libsol.so")
 # debug build: LDS arrays that hold values are filled with NaN at kernel entry
 POISON_LIB = os.path.join(PKG, "libsol_poison.so")
 SOURCES = ["sol_kernels.hip", "sol_sparse.hip", "sol_records.hip", "sol_probe.hip", "sol_noalloc.hip",
-           "sol_lin_attn.hip", "sol_diff_attn.hip", "sol_api.cpp", "sol_api_ops.cpp"]
+           "sol_lin_attn.hip", "sol_diff_attn.hip", "sol_norm_rope.hip", "sol_cross_attn.hip", "sol_api.cpp",
+           "sol_api_ops.cpp", "sol_api_cross.cpp"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

@@ -1,0 +1,1074 @@
+// Cross attention (sol_cross_attn_fwd, _bwd): softmax attention of one sequence's
+// rows to another's keys and values, of a length of its own,
+//   out = softmax(scale q k^T) v over the keys that are visible.
+//
+// As in the differential attention one pass over the keys with the running maximum
+// and sum of each row; scores S^T = K Q^T and outputs O^T = V^T P^T, so that a lane
+// owns a row and P as the score MFMA leaves it is the operand of the next.  fp32
+// throughout but for the operands: P is rounded to bf16, as the values are bf16, and
+// its product divided by the sum of the rounded ones.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "sol_cross.h"
+#include "sol_softmax.h"
+
+namespace sol {
+namespace {
+
+__device__ __forceinline__ int query_len(const CrossShape& s, int b) {
+  return s.q_lens ? min(max(s.q_lens[b], 0), s.N) : s.N;
+}
+__device__ __forceinline__ int key_len(const CrossShape& s, int b) {
+  return s.kv_lens ? min(max(s.kv_lens[b], 0), s.M) : s.M;
+}
+
+// Results of pieces of the keys, to be joined: o fp32 [piece][row][128], then the
+// log2 of the sums that o was divided by, [piece][row], and of the exact ones (for
+// training), for `rows` rows: those of the tiles that are split (tile after tile),
+// or, where the few-row kernel splits, all [B][H][N].
+struct Parts {
+  float *o, *l, *exact;
+  int64_t rows;
+};
+__device__ __forceinline__ Parts parts_of(float* ws, int64_t rows, int pieces) {
+  return {ws, ws + rows * pieces * D, ws + rows * pieces * (D + 1), rows};
+}
+
+// out, and for training what its rounding left, of two dims from `d` of row (b, h, n).
+__device__ __forceinline__ void store_two(const CrossFwd& A, int b, int h, int n, int d, float2 o) {
+  const uint32_t w = pack_bf16x2(o.x, o.y);
+  *reinterpret_cast<uint32_t*>(A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)n * A.out.sn + d) = w;
+  if (A.left)
+    *reinterpret_cast<uint32_t*>(A.left + (((int64_t)b * A.s.H + h) * A.s.N + n) * D + d) = left2(o.x, o.y, w);
+}
+
+// ------------------------------------------------------------------- forward
+
+// Groups of rows of one key head's query heads in the few-row kernel.
+__host__ __device__ inline int64_t few_groups(const CrossShape& s) {
+  return ((int64_t)(s.H / s.Hk) * s.N + kFewRows - 1) / kFewRows;
+}
+
+// Rows in groups of 32 of all heads that share a key head -- row r is token r % N of
+// head hk per + r / N --, a workgroup each: each wave walks every fourth block of 32
+// keys on its own, through LDS of its own (no barriers), the next block's bytes in
+// flight in its registers; the four waves' rows are joined at the end.  A key that is
+// masked is not read.
+template <bool kMasked>
+__global__ __launch_bounds__(256, 2) void cross_few_kernel(CrossFwd A, int nsplit) {
+  constexpr int kBlock = 32, kWaves = 4;
+  constexpr int kTileElems = kBlock * kStride;
+  constexpr int kRow = D + 4;
+  struct Joined {
+    float o[kWaves][kFewRows][kRow];
+    float m[kWaves][kFewRows], l[kWaves][kFewRows], exact[kWaves][kFewRows];
+  };
+  union Lds {
+    uint16_t tiles[kWaves][2 * kTileElems];
+    Joined j;
+  };
+  __shared__ __attribute__((aligned(16))) Lds lds;
+  lds_poison(&lds, sizeof(lds));
+  lds_poison_done();
+  const CrossShape& s = A.s;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
+  // (sequence, key head, piece of the keys) after another over the XCDs, but the
+  // groups of rows that read the same keys on one, side by side
+  const int per = s.H / s.Hk, groups = (int)few_groups(s);
+  int id = blockIdx.x / (8 * groups) * 8 + blockIdx.x % 8;
+  const int64_t row_base = (int64_t)(blockIdx.x / 8 % groups) * kFewRows;
+  const int n_rows = (int)min((int64_t)per * s.N - row_base, (int64_t)kFewRows);
+  if (id >= s.B * s.Hk * nsplit) return;
+  const int split = id % nsplit;
+  id /= nsplit;
+  const int hk = id % s.Hk, b = id / s.Hk;
+  const int qlen = query_len(s, b), klen = key_len(s, b);
+  const float c = s.scale * kLog2e;
+  const int64_t my = row_base + min(l32, n_rows - 1);
+  const int h = hk * per + (int)(my / s.N), row = (int)(my % s.N);
+  const bool valid = l32 < n_rows && row < qlen;
+
+  const uint16_t* k = A.k.p + b * A.k.sb + hk * A.k.sh;
+  const uint16_t* v = A.v.p + b * A.v.sb + hk * A.v.sh;
+  const uint8_t* mk = kMasked ? s.mask + (int64_t)b * s.M : nullptr;
+  bf16x8 qf[8];
+  if (!__any(valid)) return;  // (the same in all four waves)
+  load_row(qf, A.q.p + b * A.q.sb + h * A.q.sh + (int64_t)row * A.q.sn, valid, hh);
+
+  const int2 range = split_keys(klen, split, nsplit, kBlock * kWaves);
+  MapRows x;
+  clear(x);
+  uint16_t* tk = lds.tiles[wave];
+  uint16_t* tv = tk + kTileElems;
+  const int tr = column_offset(lane);
+  // Which keys of a block are visible, a bit each.
+  auto seen_byte = [&](int key) __attribute__((always_inline)) {
+    const int i = key + l32;
+    return kMasked ? (i < range.y ? (int)mk[i] : 0) : (int)(i < range.y);
+  };
+  auto seen_word = [&](int byte) __attribute__((always_inline)) { return (uint32_t)__ballot(byte != 0); };
+  constexpr int kLoads = kBlock / 4;  // rows of a lane's: lane / 16 + 4 u
+  uint4 xk[kLoads], xv[kLoads];
+  const int lr = lane >> 4, cc = lane & 15;
+  auto load = [&](int key, uint32_t seen) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int r = lr + 4 * u;
+      xk[u] = xv[u] = make_uint4(0, 0, 0, 0);
+      if (seen >> r & 1) {
+        xk[u] = *reinterpret_cast<const uint4*>(k + (int64_t)(key + r) * A.k.sn + cc * 8);
+        xv[u] = *reinterpret_cast<const uint4*>(v + (int64_t)(key + r) * A.v.sn + cc * 8);
+      }
+    }
+  };
+  int key = range.x + wave * kBlock;
+  uint32_t seen = seen_word(seen_byte(key));
+  int next_byte = seen_byte(key + kBlock * kWaves);
+  load(key, seen);
+  for (; key < range.y; key += kBlock * kWaves) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      *reinterpret_cast<uint4*>(tk + (lr + 4 * u) * kStride + cc * 8) = xk[u];
+      *reinterpret_cast<uint4*>(tv + (lr + 4 * u) * kStride + cc * 8) = xv[u];
+    }
+    // the wave's own LDS: its reads below follow its writes above, and those
+    // the reads of the turn before (a wave's LDS operations stay in order; this
+    // keeps the compiler from moving them past each other)
+    asm volatile("" ::: "memory");
+    const uint32_t now = seen;
+    seen = seen_word(next_byte);
+    load(key + kBlock * kWaves, seen);
+    next_byte = seen_byte(key + 2 * kBlock * kWaves);
+    f32x16 sc[1] = {scores(tk, qf, lane)};
+    if (now != 0xffffffffu) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (!(now >> (8 * (r >> 2) + 4 * hh + (r & 3)) & 1)) sc[0][r] = -__builtin_inff();
+    }
+    raise_max(x, sc, c);
+    exponentials(x, sc[0], c);
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const bf16x8 p = operand8(sc[0], y);
+      x.l = add_bf16x8(p, x.l);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) x.o[d] = mfma(column8(tv + 16 * y * kStride + 32 * d + tr), p, x.o[d]);
+    }
+    asm volatile("" ::: "memory");
+  }
+
+  // join the waves' rows
+  __syncthreads();
+  const float l = both_sum(x.l), exact = both_sum(x.exact);
+  if (l32 < n_rows) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(&lds.j.o[wave][l32][32 * d + 8 * q + 4 * hh]) =
+            make_float4(x.o[d][4 * q], x.o[d][4 * q + 1], x.o[d][4 * q + 2], x.o[d][4 * q + 3]);
+    if (hh == 0) {
+      lds.j.m[wave][l32] = x.m;
+      lds.j.l[wave][l32] = l;
+      lds.j.exact[wave][l32] = exact;
+    }
+  }
+  __syncthreads();
+  const Parts p = parts_of(A.ws, (int64_t)s.B * s.H * s.N, nsplit);
+  // one pair of dims of one row a thread and turn
+  for (int i = t; i < n_rows * (D / 2); i += 256) {
+    const int r = i / (D / 2), d = 2 * (i % (D / 2));
+    const int hr = hk * per + (int)((row_base + r) / s.N), n = (int)((row_base + r) % s.N);
+    if (n >= qlen) continue;
+    float top = kNoMax, sum = 0.0f, exact_sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds.j.m[w][r]);
+    float2 o = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f((lds.j.m[w][r] - top) * c);
+      sum = __builtin_fmaf(f, lds.j.l[w][r], sum);
+      exact_sum = __builtin_fmaf(f, lds.j.exact[w][r], exact_sum);
+      o.x = __builtin_fmaf(f, lds.j.o[w][r][d], o.x);
+      o.y = __builtin_fmaf(f, lds.j.o[w][r][d + 1], o.y);
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    o.x *= inv;
+    o.y *= inv;
+    const int64_t at = ((int64_t)b * s.H + hr) * s.N + n;
+    if (nsplit > 1) {
+      const int64_t am = split * p.rows + at;
+      *reinterpret_cast<float2*>(p.o + am * D + d) = o;
+      if (d == 0) p.l[am] = log2_sum(top, sum, c);
+      if (d == 0 && A.lse) p.exact[am] = log2_sum(top, exact_sum, c);
+    } else {
+      store_two(A, b, hr, n, d, o);
+      if (A.lse && d == 0) A.lse[at] = log2_sum(top, exact_sum, c) * kLn2;
+    }
+  }
+}
+
+// The pieces' results joined: four waves take a row, two dims a lane.
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossFwd A, DiffTiles plan) {
+  __shared__ float2 of[4][64];
+  __shared__ float sums[4][3];
+  lds_poison(of, sizeof(of));
+  lds_poison(sums, sizeof(sums));
+  lds_poison_done();
+  const CrossShape& s = A.s;
+  const int64_t rows = (int64_t)s.B * s.H * s.N, i = blockIdx.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int n = (int)(i % s.N), bh = (int)(i / s.N), h = bh % s.H, b = bh / s.H;
+  if (n >= query_len(s, b)) return;
+  const Parts p = parts_of(A.ws, rows, plan.pieces);
+  float top = kNoMax, sum = 0.0f, exact = 0.0f;
+  // (loads of eight pieces at a time)
+#pragma unroll 8
+  for (int u = wave; u < plan.pieces; u += 4) top = fmaxf(top, p.l[u * rows + i]);
+  float2 o = make_float2(0.0f, 0.0f);
+#pragma unroll 8
+  for (int u = wave; u < plan.pieces; u += 4) {
+    const int64_t am = u * rows + i;
+    const float f = __builtin_amdgcn_exp2f(p.l[am] - top);
+    const float2 x = *reinterpret_cast<const float2*>(p.o + am * D + 2 * lane);
+    sum += f;
+    if (A.lse) exact += __builtin_amdgcn_exp2f(p.exact[am] - top);
+    o.x = __builtin_fmaf(f, x.x, o.x);
+    o.y = __builtin_fmaf(f, x.y, o.y);
+  }
+  of[wave][lane] = o;
+  if (lane == 0) sums[wave][0] = top, sums[wave][1] = sum, sums[wave][2] = exact;
+  __syncthreads();
+  if (wave) return;
+  top = fmaxf(fmaxf(sums[0][0], sums[1][0]), fmaxf(sums[2][0], sums[3][0]));
+  sum = exact = 0.0f;
+  o = make_float2(0.0f, 0.0f);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(sums[w][0] - top);
+    sum = __builtin_fmaf(f, sums[w][1], sum);
+    exact = __builtin_fmaf(f, sums[w][2], exact);
+    o.x = __builtin_fmaf(f, of[w][lane].x, o.x);
+    o.y = __builtin_fmaf(f, of[w][lane].y, o.y);
+  }
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  o.x *= inv;
+  o.y *= inv;
+  store_two(A, b, h, n, 2 * lane, o);
+  if (A.lse && lane == 0) A.lse[i] = sum > 0.0f ? (top + log2f(exact)) * kLn2 : -__builtin_inff();
+}
+
+// ------------------------------------------------------ visible keys in order
+//
+// Where keys are masked the tile kernels walk the visible ones alone: order[b] holds
+// them first, in order, and then the others, counts[b] how many are visible.  So a
+// masked key costs nothing and is not read, and a sequence's visible keys are as a
+// shorter sequence's, their rows found through order.
+
+constexpr int kOrderThreads = 1024;
+__global__ __launch_bounds__(kOrderThreads) void cross_order_kernel(CrossShape s, int32_t* order, int32_t* counts) {
+  __shared__ int waves[kOrderThreads / 64];
+  const int b = blockIdx.x, t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  const int klen = key_len(s, b);
+  const uint8_t* m = s.mask + (int64_t)b * s.M;
+  int32_t* to = order + (int64_t)b * s.M;
+  int seen = 0;  // visible keys before this step's
+  for (int at = 0; at < s.M; at += kOrderThreads) {
+    const int key = at + t;
+    const bool on = key < klen && m[key] != 0;
+    const uint64_t ones = __ballot(on);
+    if (lane == 0) waves[wave] = __popcll(ones);
+    __syncthreads();
+    int before = seen, all = 0;
+#pragma unroll
+    for (int w = 0; w < kOrderThreads / 64; ++w) {
+      if (w < wave) before += waves[w];
+      all += waves[w];
+    }
+    before += __popcll(ones & ((1ull << lane) - 1));  // visible keys before this one
+    if (key < s.M) to[on ? before : s.M - 1 - (key - before)] = key;  // (the others from the end)
+    seen += all;
+    __syncthreads();
+  }
+  if (t == 0) counts[b] = seen;
+}
+
+// A sequence's keys as the tile kernels walk them.
+template <bool kMasked>
+struct Keys {
+  const int32_t* order;  // kMasked
+  int len;
+  __device__ __forceinline__ Keys(const CrossShape& s, const int32_t* o, const int32_t* counts, int b) {
+    order = kMasked ? o + (int64_t)b * s.M : nullptr;
+    len = kMasked ? counts[b] : key_len(s, b);
+  }
+  __device__ __forceinline__ int at(int i) const { return kMasked ? order[i] : i; }
+};
+
+// Tiles of 32 keys and their values, one after the other from key `from` on, on their
+// way into a ring in LDS, one kilobyte at a time: copy 0, 1 the halves of K's tile, 2, 3
+// V's.  A wave brings 8 rows.  Past the last tile it comes again, and is not used; keys
+// past the sequence are its last key again (their scores are masked).
+constexpr int kTileKeys = 32;
+constexpr int kRing = 4;
+template <bool kMasked>
+struct KeyCopies {
+  const uint16_t *k, *v;  // the head's; without a mask, of the tile's first key
+  int64_t ksn, vsn;
+  Keys<kMasked> keys;
+  int key, row, lane, turns;
+  uint32_t at0, to, ok, ov;
+  int next;  // kMasked: this lane's row of the tile to come
+  const uint16_t *mk, *mv;
+
+  __device__ __forceinline__ KeyCopies(const Rows& kr, const Rows& vr, int b, int hk, const Keys<kMasked>& ks, int from,
+                                       int n, uint32_t lds, int wave, int l)
+      : k(kr.p + b * kr.sb + hk * kr.sh), v(vr.p + b * vr.sb + hk * vr.sh), ksn(kr.sn), vsn(vr.sn), keys(ks), key(from),
+        row(8 * wave + (l >> 3)), lane(l), turns(n), at0(lds + wave * kRowBlock), to(0), ok(0), ov(0), next(0), mk(nullptr),
+        mv(nullptr) {
+    restart(from);
+  }
+  __device__ __forceinline__ void fetch(int tile_key) {
+    if (kMasked && turns > 0) next = keys.at(min(tile_key + row, keys.len - 1));
+  }
+  const uint16_t *k0, *v0;
+  __device__ __forceinline__ void restart(int from) {
+    key = from;
+    if (kMasked) {
+      fetch(from);
+    } else {
+      k0 = k + (int64_t)from * ksn;
+      v0 = v + (int64_t)from * vsn;
+      ok = copy_offset(row, ksn, lane);
+      ov = copy_offset(row, vsn, lane);
+    }
+  }
+  // Tile i (after i - 1, or the same again) into place `place` of a ring of kRing.
+  __device__ __forceinline__ void start(int i, int place) {
+    const bool on = i > 0 && i < turns;
+    key += on ? kTileKeys : 0;
+    to = __builtin_amdgcn_readfirstlane(at0 + (place % kRing) * (2 * kTile32));
+    if (kMasked) {
+      const int chunk = 8 * ((lane & 7) ^ swizzle(lane >> 3));
+      mk = k + (int64_t)next * ksn + chunk;
+      mv = v + (int64_t)next * vsn + chunk;
+      fetch(i + 1 < turns ? key + kTileKeys : key);
+    } else {
+      k0 += on ? kTileKeys * ksn : 0;
+      v0 += on ? kTileKeys * vsn : 0;
+      if (key + kTileKeys > keys.len) {
+        const int r = min(row, keys.len - 1 - key);
+        ok = copy_offset(r, ksn, lane);
+        ov = copy_offset(r, vsn, lane);
+      }
+    }
+  }
+  __device__ __forceinline__ void part(int n) const {
+    const uint32_t lds = to + n / 2 * kTile32 + n % 2 * 1024;
+    if (kMasked) copy_1k_from(lds, (n / 2 ? mv : mk) + n % 2 * 64);
+    else copy_1k(lds, n / 2 ? v0 : k0, (n / 2 ? ov : ok) + n % 2 * 128);
+  }
+  __device__ __forceinline__ void all(int i, int place) {
+    start(i, place);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) part(n);
+  }
+};
+
+// Tiles of 256 rows, a head's one after the other; where lengths differ head after
+// head, so that every XCD has some of each sequence.
+struct RowTile {
+  int b, h, row0;
+};
+__host__ __device__ inline int tiles_of(int n, int rows) { return (n + rows - 1) / rows; }
+__host__ __device__ inline int64_t row_tiles_of(const CrossShape& s) { return (int64_t)s.B * s.H * tiles_of(s.N, kCrossRows); }
+__device__ __forceinline__ int2 slab_of(int slab, int heads, const CrossShape& s) {  // (b, h)
+  return s.q_lens || s.kv_lens || s.mask ? make_int2(slab % s.B, slab / s.B) : make_int2(slab / heads, slab % heads);
+}
+__device__ __forceinline__ RowTile row_tile(int tile, const CrossShape& s) {
+  const int per_head = tiles_of(s.N, kCrossRows), slab = tile / per_head;
+  const int2 bh = slab_of(slab, s.H, s);
+  return {bh.x, bh.y, (tile - slab * per_head) * kCrossRows};
+}
+// The tile and piece of a workgroup: tiles [0, full) whole, the rest in pieces; a run
+// of consecutive ones to an XCD.
+struct Piece {
+  int tile, piece, pieces;
+};
+__device__ __forceinline__ Piece piece_of(int wg, int tiles, const DiffTiles& p) {
+  if (wg < p.full) return {xcd_local_id(wg, p.full), 0, 1};
+  const int id = xcd_local_id(wg - p.full, (tiles - p.full) * p.pieces);
+  return {p.full + id / p.pieces, id % p.pieces, p.pieces};
+}
+
+// ------------------------------------------------------------------ backward
+//
+// With X = dout v^T, P the probabilities and delta = dout . out of a row,
+//   dS = P (X - delta),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T dout.
+// P is found again from the rows' log sums.  dS and P are rounded to bf16 for their
+// products with k, q and dout, which are bf16: a result's error is its terms'
+// roundings and its own, of one size (0.0024 of its norm together).  Two halves, one
+// that owns rows (dq) and one that owns keys (dk, dv): no atomics, and every sum in
+// a fixed order.
+
+// What the backward kernels know of a row, 32 rows together: kStatLse: -lse / scale,
+// which added to raw scores and scaled gives log2 P (-inf, and so P = 0, where the
+// row has no keys or is not the sequence's); kStatDelta: -delta; 32 floats each.
+constexpr int kBwdRows = 32;
+constexpr int kStatFloats = 2 * kBwdRows;
+enum { kStatLse = 0, kStatDelta = kBwdRows };
+
+__global__ __launch_bounds__(16 * kBwdRows) void cross_stats_kernel(CrossBwd A) {
+  const CrossShape& s = A.s;
+  const int row_tiles = tiles_of(s.N, kBwdRows);
+  const int r = threadIdx.x >> 4, cc = threadIdx.x & 15;
+  const int n = (int)(blockIdx.x % row_tiles) * kBwdRows + r;
+  const int bh = blockIdx.x / row_tiles, h = bh % s.H, b = bh / s.H;
+  const bool valid = n < query_len(s, b);
+  float d = 0.0f;
+  if (valid) {
+    float o[8], g[8], left[8];
+    auto load = [](float (&f)[8], const uint16_t* p) { unpack_bf16x8(*reinterpret_cast<const uint4*>(p), f); };
+    load(o, A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)n * A.out.sn + 8 * cc);
+    load(g, A.dout.p + b * A.dout.sb + h * A.dout.sh + (int64_t)n * A.dout.sn + 8 * cc);
+    load(left, A.left + ((int64_t)bh * s.N + n) * D + 8 * cc);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) d = __builtin_fmaf(g[u], o[u] + left[u], d);
+  }
+  d = row_sumsq_lanes16(d);
+  if (cc < 2) {
+    const float lse = valid ? A.lse[(int64_t)bh * s.N + n] : 0.0f;
+    const bool some = valid && lse > -3e38f;
+    A.stats[(int64_t)blockIdx.x * kStatFloats + cc * kBwdRows + r] =
+        cc ? (some ? -d : 0.0f) : some ? -lse / s.scale : -__builtin_inff();
+  }
+}
+
+// A backward turn t finds the scores and X of tile t, the exponentials of tile t
+// (from the slot where its scores are done), what is left of tile t - 1 to its
+// operands, and the gradient products of tile t - 1.  The barrier stands where the
+// last eight slots begin, so that the next tile's first fragments are read before
+// the turn ends.
+
+// dq of 256 rows of one head, 64 a wave in two blocks of 32 (a fragment of K or V is
+// read once for two MFMAs), over all the keys.
+template <bool kMasked>
+__device__ __forceinline__ void dq_of(const CrossBwd& A, uint8_t (*lds)[2][kTile32], int wg) {
+  constexpr int kAhead = 6, kHold = 8;
+  const CrossShape& s = A.s;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
+  const Piece pc = piece_of(wg, (int)row_tiles_of(s), A.plan);
+  const RowTile rt = row_tile(pc.tile, s);
+  const int b = rt.b, h = rt.h, hk = h / (s.H / s.Hk);
+  const int qlen = query_len(s, b);
+  const Keys<kMasked> keys(s, A.order, A.counts, b);
+  const int row = rt.row0 + 64 * wave + l32;  // and 32 more
+  const float c = s.scale * kLog2e;
+
+  bf16x8 qf[2][8], gf[2][8];
+  float lse[2], del[2];
+  const int row_tiles = tiles_of(s.N, kBwdRows);
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    const int n = row + 32 * m;
+    const bool valid = n < qlen;
+    load_row(qf[m], A.q.p + b * A.q.sb + h * A.q.sh + (int64_t)n * A.q.sn, valid, hh);
+    load_row(gf[m], A.dout.p + b * A.dout.sb + h * A.dout.sh + (int64_t)n * A.dout.sn, valid, hh);
+    lse[m] = -__builtin_inff();
+    del[m] = 0.0f;
+    if (valid) {
+      const float* st = A.stats + ((int64_t)(b * s.H + h) * row_tiles + n / kBwdRows) * kStatFloats + n % kBwdRows;
+      lse[m] = st[kStatLse] * c;
+      del[m] = st[kStatDelta];
+    }
+  }
+  const int2 range = split_keys(rt.row0 < qlen ? keys.len : 0, pc.piece, pc.pieces, kTileKeys);
+  const int turns = tiles_of(range.y - range.x, kTileKeys);
+  KeyCopies<kMasked> copy(A.k, A.v, b, hk, keys, range.x, turns, lds_address(&lds[0][0][0]), wave, lane);
+
+  struct Scores {
+    f32x16 s[2], x[2];  // scores, then P; X
+  } sa, sb;
+  f32x16 dq[2][4] = {};
+  bf16x8 ring[kHold];
+  uint32_t pw[2][8];  // dS, but for the factor scale
+  const RowPlace rp = row_place(lane);
+  const int cp = col_place(lane);
+  // the fragment of slots 2 f and 2 f + 1 of a turn on tile `now` whose products read tile `then`
+  auto fragment = [&](int f, const uint8_t* now, const uint8_t* then) __attribute__((always_inline)) {
+    if (f < 8) return row_frag(now, rp, f);
+    if (f < 16) return row_frag(now + kTile32, rp, f - 8);
+    return col_frag(then + cp, (f - 16) >> 2, f & 3);
+  };
+  auto finish = [&](const Scores& old, int m, int r) __attribute__((always_inline)) {  // keys r, r + 1
+    pw[m][r >> 1] = pack_bf16x2(old.s[m][r] * (old.x[m][r] + del[m]), old.s[m][r + 1] * (old.x[m][r + 1] + del[m]));
+    pin(pw[m][r >> 1]);
+  };
+  auto hold_operands = [&]() __attribute__((always_inline)) {
+    hold_in_agprs(qf[0]);
+    hold_in_agprs(qf[1]);
+    hold_in_agprs(gf[0]);
+    hold_in_agprs(gf[1]);
+  };
+  auto turn = [&](int i, Scores& now, Scores& old) __attribute__((always_inline)) {
+    constexpr int kSlots = 48;
+    const uint8_t* tn = &lds[i % kRing][0][0];
+    const uint8_t* to = &lds[(i + kRing - 1) % kRing][0][0];
+    const uint8_t* next = &lds[(i + 1) % kRing][0][0];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) asm volatile("" : "+a"(dq[0][d]), "+a"(dq[1][d]));
+    hold_operands();
+    each<0, kSlots>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int j = slot.value, f = j / 2, m = j & 1;
+      if constexpr (j == kSlots - 14) {
+        copies_landed<0>();
+        copy.start(i + 2, i + 2);
+        slot_end();
+      }
+      if constexpr (j >= kSlots - 13 && j < kSlots - 9) copy.part(j - (kSlots - 13));
+      const bf16x8 a = ring[f % kHold];
+      if constexpr (j < 16) {
+        if constexpr (j < 2) score_first_a(now.s[m], a, qf[m][f]);
+        else score_a(now.s[m], a, qf[m][f]);
+      } else if constexpr (j < 32) {
+        if constexpr (j < 18) score_first_a(now.x[m], a, gf[m][f - 8]);
+        else score_a(now.x[m], a, gf[m][f - 8]);
+      } else {
+        constexpr int d = f & 3, y = (f - 16) >> 2;
+        const uint4 w = make_uint4(pw[m][4 * y], pw[m][4 * y + 1], pw[m][4 * y + 2], pw[m][4 * y + 3]);
+        dq[m][d] = mfma(a, __builtin_bit_cast(bf16x8, w), dq[m][d]);
+      }
+      if constexpr (m == 0) {
+        constexpr int g = f + kAhead;
+        ring[g % kHold] = g < kSlots / 2 ? fragment(g, tn, to) : fragment(g - kSlots / 2, next, tn);
+      }
+      if constexpr (j < 32 && j % 2 == 0) finish(old, (j >> 1) & 1, (j >> 2) * 2);
+      if constexpr (j >= 18) {  // the exponentials: 32 in 30 slots
+#pragma unroll
+        for (int e = (j - 18) * 16 / 15; e < (j - 17) * 16 / 15; ++e) {
+          float p = __builtin_amdgcn_exp2f(__builtin_fmaf(now.s[e & 1][e >> 1], c, lse[e & 1]));
+          pin(p);
+          now.s[e & 1][e >> 1] = p;
+        }
+      }
+      slot_end();
+    });
+    const int key = range.x + i * kTileKeys;
+    if (key + kTileKeys > keys.len || i >= turns) {
+      const int to_key = i < turns ? keys.len : 0;  // (past the last tile: none)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (key + 4 * hh + 8 * (r >> 2) + (r & 3) >= to_key) now.s[0][r] = now.s[1][r] = 0.0f;
+    }
+  };
+  if (turns > 0) {
+    copy.all(0, 0);
+    copy.all(0, kRing - 1);  // turn 0's products, of dS = 0
+    copies_landed<0>();
+    hold_operands();
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      pin(lse[m]);
+      pin(del[m]);
+    }
+    all_landed();
+    copy.all(1, 1);
+    sb = Scores{};
+#pragma unroll
+    for (int f = 0; f < kAhead; ++f) ring[f] = fragment(f, &lds[0][0][0], nullptr);
+    for (int i = 0; i <= turns; i += 2) {
+      turn(i, sa, sb);
+      turn(i + 1, sb, sa);
+    }
+    copies_landed<0>();  // none is under way when the wave ends
+  }
+  const int first = rt.row0 + 64 * wave;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    if (pc.pieces > 1) {
+      float* o = A.dq_parts +
+                 (((int64_t)(pc.tile - A.plan.full) * pc.pieces + pc.piece) * kCrossRows + row + 32 * m - rt.row0) * D + 4 * hh;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4*>(o + 32 * d + 8 * q) =
+              make_float4(dq[m][d][4 * q], dq[m][d][4 * q + 1], dq[m][d][4 * q + 2], dq[m][d][4 * q + 3]);
+    } else {  // zero behind the sequence
+      const bool valid = row + 32 * m < qlen;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dq[m][d][r] = valid ? dq[m][d][r] * s.scale : 0.0f;
+      store_rows(reinterpret_cast<uint8_t*>(lds) + wave * kOutBytes, lane,
+                 A.dq.p + b * A.dq.sb + h * A.dq.sh + (int64_t)(first + 32 * m) * A.dq.sn, A.dq.sn, 0, s.N - first - 32 * m,
+                 [&](int d, int q) { return pack4(dq[m][d], q); });
+    }
+  }
+}
+
+// A wave's 32 rows (of keys) to the rows of memory that order[i] names, i < rows.
+template <class Words>
+__device__ __forceinline__ void store_ordered(uint8_t* mine, int lane, uint16_t* to, int64_t sn, const int32_t* order,
+                                              int rows, Words&& words) {
+  uint8_t* row = mine + (lane & 31) * kOutStride + (lane >> 5) * 8;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint2*>(row + 64 * d + 16 * q) = words(d, q);
+  asm volatile("" ::: "memory");  // the wave's LDS operations stay in order
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    const int r = 4 * u + (lane >> 4), cc = lane & 15;
+    const uint4 x = *reinterpret_cast<const uint4*>(mine + r * kOutStride + 16 * cc);
+    if (r < rows) *reinterpret_cast<uint4*>(to + (int64_t)order[r] * sn + 8 * cc) = x;
+  }
+  asm volatile("" ::: "memory");
+}
+
+// dk, dv of 128 keys of one key head, 32 keys a wave, over the rows of every head of
+// its group or of a piece of them (so a shared head's gradient is summed in registers,
+// heads in order).
+template <bool kMasked>
+__device__ __forceinline__ void dkv_of(const CrossBwd& A, uint8_t (*lds)[2][kTile32], float (*stat)[kStatFloats], int wg,
+                                       int wgs) {
+  constexpr int kAhead = 8;
+  // lds: q, dout
+  const CrossShape& s = A.s;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
+  const int tiles = tiles_of(s.M, kCrossKeys), pieces = A.head_pieces * A.row_pieces;
+  const int id = xcd_local_id(wg, wgs), at = id / pieces;
+  const int2 bh = slab_of(at / tiles, s.Hk, s);
+  const int piece = id % pieces, row_piece = piece % A.row_pieces;
+  const int hk = bh.y, b = bh.x, tile = at % tiles;
+  const int qlen = query_len(s, b);
+  const Keys<kMasked> keys(s, A.order, A.counts, b);
+  const int per = s.H / s.Hk / A.head_pieces, h0 = (hk * A.head_pieces + piece / A.row_pieces) * per;  // the piece's heads
+  const int key0 = tile * kCrossKeys, key = key0 + 32 * wave + l32;
+  const bool valid = key < keys.len;
+  const float c = s.scale * kLog2e;
+
+  bf16x8 kf[8], vf[8];
+  const int64_t key_row = valid ? keys.at(key) : 0;
+  load_row(kf, A.k.p + b * A.k.sb + hk * A.k.sh + key_row * A.k.sn, valid, hh);
+  load_row(vf, A.v.p + b * A.v.sb + hk * A.v.sh + key_row * A.v.sn, valid, hh);
+
+  // the tiles of rows, head after head
+  const int row_tiles = tiles_of(s.N, kBwdRows);
+  const int all = key0 < keys.len ? tiles_of(qlen, kBwdRows) : 0;
+  const int first = (int)((int64_t)all * row_piece / A.row_pieces);
+  const int end = (int)((int64_t)all * (row_piece + 1) / A.row_pieces);
+  const int head_turns = end - first, turns = head_turns * per;
+
+  const uint32_t at0 = lds_address(&lds[0][0][0]) + wave * kRowBlock;
+  const uint32_t stat0 = lds_address(&stat[0][0]);
+  const int copy_row = 8 * wave + (lane >> 3);
+  const uint16_t* qh = A.q.p + b * A.q.sb + (int64_t)h0 * A.q.sh;
+  const uint16_t* gh = A.dout.p + b * A.dout.sb + (int64_t)h0 * A.dout.sh;
+  const float* sth = A.stats + (int64_t)(b * s.H + h0) * row_tiles * kStatFloats;
+  // Tile after tile (head after head) into the ring, one kilobyte at a time; past
+  // the last tile it comes again, and is not used.
+  constexpr int kCopies = 5;
+  struct Copy {
+    const uint16_t *q, *g;
+    const float* st;
+    int u, t;  // head of the group and row tile
+    uint32_t to, to_st, oq, og;
+  } cp_ = {};
+  auto copy_start = [&](int i, int place) __attribute__((always_inline)) {
+    const bool on = i > 0 && i < turns;
+    if (i == 0 || (on && cp_.t + 1 == end)) {
+      cp_.u += i > 0;
+      cp_.t = first;
+      cp_.q = qh + cp_.u * A.q.sh + (int64_t)first * kBwdRows * A.q.sn;
+      cp_.g = gh + cp_.u * A.dout.sh + (int64_t)first * kBwdRows * A.dout.sn;
+      cp_.st = sth + ((int64_t)cp_.u * row_tiles + first) * kStatFloats;
+      cp_.oq = copy_offset(copy_row, A.q.sn, lane);
+      cp_.og = copy_offset(copy_row, A.dout.sn, lane);
+    } else {
+      cp_.t += on;
+      cp_.q += on ? kBwdRows * A.q.sn : 0;
+      cp_.g += on ? kBwdRows * A.dout.sn : 0;
+      cp_.st += on ? kStatFloats : 0;
+    }
+    cp_.to = __builtin_amdgcn_readfirstlane(at0 + (place % kRing) * (2 * kTile32));
+    cp_.to_st = __builtin_amdgcn_readfirstlane(stat0 + (place % kRing) * (kStatFloats * 4));
+    if (cp_.t + 1 == end) {  // rows past the sequence: its last row again (their P is 0)
+      const int r = min(copy_row, qlen - 1 - cp_.t * kBwdRows);
+      cp_.oq = copy_offset(r, A.q.sn, lane);
+      cp_.og = copy_offset(r, A.dout.sn, lane);
+    }
+  };
+  auto copy_part = [&](int n) __attribute__((always_inline)) {
+    if (n == 4) copy_256(cp_.to_st, cp_.st, lane * 4);
+    else copy_1k(cp_.to + n / 2 * kTile32 + n % 2 * 1024, n / 2 ? cp_.g : cp_.q, (n / 2 ? cp_.og : cp_.oq) + n % 2 * 128);
+  };
+  auto copy = [&](int i, int place) __attribute__((always_inline)) {
+    copy_start(i, place);
+#pragma unroll
+    for (int n = 0; n < kCopies; ++n) copy_part(n);
+  };
+
+  struct Scores {
+    f32x16 s, x;  // scores, X - delta
+    float p[16];
+  } sa, sb;
+  f32x16 dv[4] = {}, dk[4] = {};
+  bf16x8 ring[kAhead];
+  uint32_t pw[2][8];  // P, dS
+  const RowPlace rp = row_place(lane);
+  const int cp = col_place(lane);
+  auto hold_operands = [&]() __attribute__((always_inline)) {
+    hold_in_agprs(kf);
+    hold_in_agprs(vf);
+  };
+  auto fragment = [&](int i, const uint8_t* now, const uint8_t* then) __attribute__((always_inline)) {
+    if (i < 8) return row_frag(now, rp, i);
+    if (i < 16) return row_frag(now + kTile32, rp, i - 8);
+    const int j = i - 16;  // y, d, which: dv, dk
+    return col_frag(then + (j % 2 ? 0 : kTile32) + cp, j >> 3, (j >> 1) & 3);
+  };
+  // rows 4 q .. 4 q + 3 of a lane's sixteen
+  auto put = [&](f32x16& x, int q, const float* st) __attribute__((always_inline)) {
+    const float4 f = *reinterpret_cast<const float4*>(st + 8 * q + 4 * hh);
+    x[4 * q] = f.x;
+    x[4 * q + 1] = f.y;
+    x[4 * q + 2] = f.z;
+    x[4 * q + 3] = f.w;
+  };
+  // P and dS of rows r, r + 1 of a lane's sixteen of the last tile
+  auto finish = [&](const Scores& old, int r) __attribute__((always_inline)) {
+    pw[0][r >> 1] = pack_bf16x2(old.p[r], old.p[r + 1]);
+    pw[1][r >> 1] = pack_bf16x2(old.p[r] * old.x[r], old.p[r + 1] * old.x[r + 1]);
+    pin(pw[0][r >> 1]);
+    pin(pw[1][r >> 1]);
+  };
+  auto turn = [&](int i, Scores& now, Scores& old) __attribute__((always_inline)) {
+    constexpr int kSlots = 32;
+    const uint8_t* tn = &lds[i % kRing][0][0];
+    const uint8_t* to = &lds[(i + kRing - 1) % kRing][0][0];
+    const uint8_t* next = &lds[(i + 1) % kRing][0][0];
+    const float* stn = stat[i % kRing];
+    const float* next_st = stat[(i + 1) % kRing];
+    // (the gradients where only MFMAs reach them)
+#pragma unroll
+    for (int d = 0; d < 4; ++d) asm volatile("" : "+a"(dv[d]), "+a"(dk[d]));
+    hold_operands();
+    each<0, kSlots>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int j = slot.value;
+      if constexpr (j == kSlots - 8) {
+        copies_landed<0>();
+        copy_start(i + 2, i + 2);
+        slot_end();
+      }
+      if constexpr (j >= kSlots - 7 && j < kSlots - 7 + kCopies) copy_part(j - (kSlots - 7));
+      const bf16x8 f = ring[j % kAhead];
+      if constexpr (j < 8) {
+        score_a(now.s, f, kf[j]);
+      } else if constexpr (j < 16) {
+        score_a(now.x, f, vf[j - 8]);
+      } else {
+        constexpr int w = j % 2, d = ((j - 16) >> 1) & 3, y = (j - 16) >> 3;
+        const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(pw[w][4 * y], pw[w][4 * y + 1], pw[w][4 * y + 2], pw[w][4 * y + 3]));
+        if constexpr (w == 0) dv[d] = mfma(f, p, dv[d]);
+        else dk[d] = mfma(f, p, dk[d]);
+      }
+      constexpr int k = j + kAhead;
+      ring[j % kAhead] = k < kSlots ? fragment(k, tn, to) : fragment(k - kSlots, next, tn);
+      if constexpr (j < 16 && j % 2 == 0) finish(old, j);
+      if constexpr (j < 4) put(now.x, j, stn + kStatDelta);
+      // the next turn's scores start from the rows' log sums
+      if constexpr (j >= 24 && j < 28) put(old.s, j - 24, next_st + kStatLse);
+      if constexpr (j >= 10) {  // the exponentials: 16 in 22 slots
+#pragma unroll
+        for (int e = (j - 10) * 8 / 11; e < (j - 9) * 8 / 11; ++e) {
+          now.p[e] = __builtin_amdgcn_exp2f(now.s[e] * c);
+          pin(now.p[e]);
+        }
+      }
+      slot_end();
+    });
+    if (key0 + 32 * wave + 32 > keys.len || i >= turns) {
+      if (!valid || i >= turns) {  // (past the last tile: none)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) now.p[r] = 0.0f;
+      }
+    }
+  };
+  if (turns > 0) {
+    copy(0, 0);
+    copy(0, kRing - 1);  // turn 0's products, of P = dS = 0
+    copies_landed<0>();
+    hold_operands();
+    all_landed();
+    copy(1, 1);
+    sb = Scores{};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) put(sa.s, q, stat[0] + kStatLse);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) ring[j] = fragment(j, &lds[0][0][0], nullptr);
+    for (int i = 0; i <= turns; i += 2) {
+      turn(i, sa, sb);
+      turn(i + 1, sb, sa);
+    }
+    copies_landed<0>();  // none is under way when the wave ends
+  }
+  if (pieces > 1) {
+    float* o = A.dkv_parts + (((int64_t)at * pieces + piece) * 2 * kCrossKeys + key - key0) * D + 4 * hh;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x16& x = m ? dk[d] : dv[d];
+          *reinterpret_cast<float4*>(o + m * kCrossKeys * D + 32 * d + 8 * q) =
+              make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+        }
+    return;
+  }
+  // zero where a key is not visible
+  uint8_t* mine = reinterpret_cast<uint8_t*>(lds) + wave * kOutBytes;
+  const int first_key = key0 + 32 * wave;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    f32x16(&x)[4] = m ? dk : dv;
+    const Rows& y = m ? A.dk : A.dv;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[d][r] = valid ? x[d][r] * (m ? s.scale : 1.0f) : 0.0f;
+    uint16_t* base = y.p + b * y.sb + hk * y.sh;
+    auto words = [&](int d, int q) { return pack4(x[d], q); };
+    if (kMasked) store_ordered(mine, lane, base, y.sn, keys.order + first_key, s.M - first_key, words);
+    else store_rows(mine, lane, base + (int64_t)first_key * y.sn, y.sn, 0, s.M - first_key, words);
+  }
+}
+
+// Both in one launch, the keys' workgroups first: what either leaves of the last
+// round of the chip's 256 CUs the other fills.
+template <bool kMasked>
+__global__ __launch_bounds__(256, 1) void cross_bwd_kernel(CrossBwd A, int key_wgs) {
+  struct Lds {
+    uint8_t tiles[kRing][2][kTile32];
+    float stat[kRing][kStatFloats];
+  };
+  __shared__ __attribute__((aligned(1024))) Lds lds;
+  lds_poison(&lds, sizeof(lds));
+  lds_poison_done();
+  if ((int)blockIdx.x < key_wgs)
+    dkv_of<kMasked>(A, lds.tiles, lds.stat, blockIdx.x, key_wgs);
+  else
+    dq_of<kMasked>(A, lds.tiles, blockIdx.x - key_wgs);
+}
+
+// dq of a tile that was cut, the pieces summed in order, 16 rows a workgroup; then dv
+// and dk of key tiles that were, 16 rows of one of them.
+constexpr int kJoinRows = 16;
+template <bool kMasked>
+__global__ __launch_bounds__(256) void cross_end_kernel(CrossBwd A) {
+  const CrossShape& s = A.s;
+  const int64_t cut = row_tiles_of(s) - A.plan.full;
+  const int dq_blocks = (int)(cut * (kCrossRows / kJoinRows));
+  const int r16 = threadIdx.x >> 4, cc = threadIdx.x & 15;
+  auto sum = [&](float (&f)[8], const float* p, int pieces, int64_t step) __attribute__((always_inline)) {
+#pragma unroll 4
+    for (int u = 0; u < pieces; ++u) {
+      const float4* at = reinterpret_cast<const float4*>(p + u * step + 8 * cc);
+      const float4 x = at[0], y = at[1];
+      f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+      f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+    }
+  };
+  float f[8] = {};
+  if ((int)blockIdx.x >= dq_blocks) {
+    const int tiles = tiles_of(s.M, kCrossKeys), per_tile = kCrossKeys / kJoinRows;
+    const int w = blockIdx.x - dq_blocks, m = w & 1, id = (w >> 1) / per_tile;
+    const int r = (w >> 1) % per_tile * kJoinRows + r16, key = id % tiles * kCrossKeys + r;
+    const int2 bh = slab_of(id / tiles, s.Hk, s);
+    if (key >= s.M) return;
+    const Keys<kMasked> keys(s, A.order, A.counts, bh.x);
+    const int pieces = A.head_pieces * A.row_pieces;
+    if (key < keys.len)
+      sum(f, A.dkv_parts + (((int64_t)id * pieces * 2 + m) * kCrossKeys + r) * D, pieces, (int64_t)2 * kCrossKeys * D);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] *= m ? s.scale : 1.0f;
+    const Rows& y = m ? A.dk : A.dv;
+    *reinterpret_cast<uint4*>(y.p + bh.x * y.sb + bh.y * y.sh + (int64_t)keys.at(key) * y.sn + 8 * cc) = pack_bf16x8(f);
+    return;
+  }
+  const int tile = blockIdx.x / (kCrossRows / kJoinRows), r = blockIdx.x % (kCrossRows / kJoinRows) * kJoinRows + r16;
+  const RowTile rt = row_tile(A.plan.full + tile, s);
+  const int row = rt.row0 + r;
+  if (row >= s.N) return;
+  if (row < query_len(s, rt.b))
+    sum(f, A.dq_parts + ((int64_t)tile * A.plan.pieces * kCrossRows + r) * D, A.plan.pieces, (int64_t)kCrossRows * D);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] *= s.scale;
+  *reinterpret_cast<uint4*>(A.dq.p + rt.b * A.dq.sb + rt.h * A.dq.sh + (int64_t)row * A.dq.sn + 8 * cc) = pack_bf16x8(f);
+}
+
+}  // namespace
+
+constexpr int kCus = 256;  // each holds one workgroup of the tile kernels
+
+// A launch is a 1D grid of fewer than 2^32 threads.
+static bool fits(int64_t workgroups, int threads) { return workgroups < ((int64_t)1 << 32) / threads; }
+
+CrossPlan cross_plan(const CrossShape& s, bool ragged) {
+  (void)ragged;
+  CrossPlan p = {true, {0, 1}};
+  const int64_t wgs = (int64_t)s.B * s.Hk * few_groups(s);
+  int64_t n = kCus / wgs;
+  n = std::min<int64_t>(n, s.M / 128);
+  p.tiles.pieces = (int)(n < 1 ? 1 : n);
+  return p;
+}
+
+static int64_t fwd_workgroups(const CrossShape& s, const CrossPlan& p) {
+  return ((int64_t)s.B * s.Hk * p.tiles.pieces + 7) / 8 * 8 * few_groups(s);
+}
+
+size_t cross_fwd_bytes(const CrossShape& s) {
+  const CrossPlan p = cross_plan(s, false);
+  if (!fits(fwd_workgroups(s, p), 256)) return kTooLarge;
+  return p.tiles.pieces > 1 ? (size_t)s.B * s.H * s.N * p.tiles.pieces * (D + 2) * sizeof(float) : 0;
+}
+
+hipError_t launch_cross_fwd(const CrossFwd& a, hipStream_t stream) {
+  const CrossShape& s = a.s;
+  const CrossPlan p = cross_plan(s, s.kv_lens || s.mask);
+  const dim3 grid((unsigned)fwd_workgroups(s, p));
+  const auto kernel = s.mask ? cross_few_kernel<true> : cross_few_kernel<false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, p.tiles.pieces);
+  if (p.tiles.pieces > 1)
+    hipLaunchKernelGGL(cross_join_kernel, dim3((unsigned)((int64_t)s.B * s.H * s.N)), dim3(256), 0, stream, a, p.tiles);
+  return hipGetLastError();
+}
+
+// Tiles [full, tiles) cut along the keys, in pieces of 512 keys or more.
+static DiffTiles cut_tiles(int64_t tiles, int64_t full, int64_t pieces, int M) {
+  pieces = std::min<int64_t>({pieces, M / 512, 16});
+  if (pieces < 2) return {(int)tiles, 1};
+  return {(int)full, (int)pieces};
+}
+// Pieces of the last tiles, which leave part of the chip idle, that fill it.
+static int64_t filling(int64_t tiles, int64_t full) { return tiles > full ? kCus / (tiles - full) : 1; }
+
+// The backward launch: the keys' workgroups, then the rows'.  Times in slots of an
+// MFMA: a key tile 32 a block of 32 rows, times the heads that share it; a row tile 48
+// a block of 32 keys.
+struct BwdCost {
+  int64_t keys, key, row;  // key tiles; a key tile's time, a row tile's
+  double fair;             // a CU's time for everything if nothing idled
+};
+static BwdCost bwd_cost(const CrossShape& s) {
+  BwdCost c = {(int64_t)s.B * s.Hk * tiles_of(s.M, kCrossKeys), (int64_t)(s.H / s.Hk) * tiles_of(s.N, kBwdRows) * 32,
+               (int64_t)tiles_of(s.M, kTileKeys) * 48, 0.0};
+  c.fair = (double)(c.keys * c.key + row_tiles_of(s) * c.row) / kCus;
+  return c;
+}
+// A key tile walks the rows of all the query heads that share it.  Where that takes
+// longer than the chip needs for everything, its heads and then their rows (256 or
+// more) go to several workgroups, if that saves more than their sums' way through the
+// workspace costs.
+struct KeyPieces {
+  int heads, rows;
+  int all() const { return heads * rows; }
+};
+static KeyPieces key_pieces(const CrossShape& s) {
+  const BwdCost c = bwd_cost(s);
+  const int per = s.H / s.Hk;
+  KeyPieces least = {1, 1};
+  double time = std::max((double)c.key, c.fair);
+  auto consider = [&](KeyPieces p) {
+    const double t = std::max((double)c.key / p.all(), c.fair) + 600 + 4.0 * c.keys * p.all();
+    if (t < time) {
+      time = t;
+      least = p;
+    }
+  };
+  for (int p = 2; p <= std::min(per, kCus); ++p)
+    if (per % p == 0) consider({p, 1});
+  for (int p = 2; p <= std::min(64, s.N / 256); ++p) consider({per, p});
+  return least;
+}
+static DiffTiles bwd_tiles(const CrossShape& s, int pieces) {
+  const int64_t tiles = row_tiles_of(s);
+  const BwdCost c = bwd_cost(s);
+  const int64_t keys = c.keys * pieces, key_cost = c.key / pieces;
+  const int64_t best = (keys * key_cost + tiles * c.row) / kCus;
+  const int64_t round = keys / kCus, more = keys % kCus;  // `more` CUs take round + 1 key tiles
+  const int64_t a = best - round * key_cost, b = a - key_cost;
+  const int64_t full = std::min(tiles, (kCus - more) * (a > 0 ? a / c.row : 0) + more * (b > 0 ? b / c.row : 0));
+  // what is left goes to the CUs' remaining time
+  return cut_tiles(tiles, full, filling(tiles, full), s.M);
+}
+
+static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+// The visible keys' order and counts.
+static size_t order_bytes(const CrossShape& s) { return s.mask ? up256(((size_t)s.B * s.M + s.B) * sizeof(int32_t)) : 0; }
+static void launch_order(const CrossShape& s, int32_t* order, int32_t* counts, hipStream_t stream) {
+  hipLaunchKernelGGL(cross_order_kernel, dim3((unsigned)s.B), dim3(kOrderThreads), 0, stream, s, order, counts);
+}
+
+// Workgroups of the backward launches: the rows' statistics, both walks (the keys'
+// first), the end (0: none is needed).
+struct BwdGrids {
+  int64_t stats, keys, walks, end;
+};
+static BwdGrids bwd_grids(const CrossShape& s, const KeyPieces& pieces, const DiffTiles& plan) {
+  const int64_t key_tiles = bwd_cost(s).keys, rest = row_tiles_of(s) - plan.full;
+  BwdGrids g;
+  g.stats = (int64_t)s.B * s.H * tiles_of(s.N, kBwdRows);
+  g.keys = key_tiles * pieces.all();
+  g.walks = g.keys + plan.full + rest * plan.pieces;
+  g.end = rest * (kCrossRows / kJoinRows);
+  if (pieces.all() > 1) g.end += key_tiles * (kCrossKeys / kJoinRows) * 2;
+  return g;
+}
+
+size_t cross_bwd_bytes(const CrossShape& s, CrossBwd* a, void* ws) {
+  const KeyPieces pieces = key_pieces(s);
+  const DiffTiles plan = bwd_tiles(s, pieces.all());
+  const BwdGrids g = bwd_grids(s, pieces, plan);
+  if (!fits(g.stats, 16 * kBwdRows) || !fits(g.walks, 256) || !fits(g.end, 256) || !fits(s.B, kOrderThreads)) return kTooLarge;
+  size_t at[4];
+  at[0] = order_bytes(s);
+  at[1] = at[0] + up256((size_t)g.stats * kStatFloats * sizeof(float));
+  at[2] = at[1];
+  if (plan.pieces > 1) at[2] += (size_t)(row_tiles_of(s) - plan.full) * plan.pieces * kCrossRows * D * sizeof(float);
+  at[3] = at[2];
+  if (pieces.all() > 1) at[3] += (size_t)bwd_cost(s).keys * pieces.all() * 2 * kCrossKeys * D * sizeof(float);
+  if (a) {
+    char* p = static_cast<char*>(ws);
+    a->order = reinterpret_cast<int32_t*>(p);
+    a->counts = a->order + (size_t)s.B * s.M;
+    a->stats = reinterpret_cast<float*>(p + at[0]);
+    a->dq_parts = reinterpret_cast<float*>(p + at[1]);
+    a->dkv_parts = reinterpret_cast<float*>(p + at[2]);
+    a->plan = plan;
+    a->head_pieces = pieces.heads;
+    a->row_pieces = pieces.rows;
+  }
+  return at[3];
+}
+
+hipError_t launch_cross_bwd(const CrossBwd& a, hipStream_t stream) {
+  const CrossShape& s = a.s;
+  const BwdGrids g = bwd_grids(s, {a.head_pieces, a.row_pieces}, a.plan);
+  if (s.mask) launch_order(s, a.order, a.counts, stream);
+  hipLaunchKernelGGL(cross_stats_kernel, dim3((unsigned)g.stats), dim3(16 * kBwdRows), 0, stream, a);
+  const auto walk = s.mask ? cross_bwd_kernel<true> : cross_bwd_kernel<false>;
+  hipLaunchKernelGGL(walk, dim3((unsigned)g.walks), dim3(256), 0, stream, a, (int)g.keys);
+  if (g.end) {
+    const auto end = s.mask ? cross_end_kernel<true> : cross_end_kernel<false>;
+    hipLaunchKernelGGL(end, dim3((unsigned)g.end), dim3(256), 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace sol

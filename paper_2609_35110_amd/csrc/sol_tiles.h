@@ -123,6 +123,10 @@ __device__ __forceinline__ void copy_1k(uint32_t lds, const void* base, uint32_t
                : "s"(lds), "v"(off), "s"(base)
                : "memory", "m0");
 }
+// The same from an address of the lane's own.
+__device__ __forceinline__ void copy_1k_from(uint32_t lds, const void* p) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(p) : "memory", "m0");
+}
 // 64 floats, one a lane.
 __device__ __forceinline__ void copy_256(uint32_t lds, const void* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"

@@ -706,10 +706,11 @@ def attn_fwd_records(rec, k_prep, v_prep, n_kv=None, out=None, fp8=False, int8_r
     return out
 
 
-# ------------------------------------------- linear and differential attention
+# ----------------------- linear, differential and cross attention, norm and rotation
 
-# sol_lin_attn_* and sol_diff_attn_* (include/sol.h), bound when first called.
-_P, _I32, _SZ, _F32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
+# sol_lin_attn_*, sol_diff_attn_*, sol_qk_norm_rope* and sol_cross_attn_* (include/sol.h),
+# bound when first called.
+_P, _I32, _SZ, _F32, _I64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float, ctypes.c_int64
 _SIGNATURES = {
     "sol_lin_attn_fwd_workspace_bytes": ([_I32] * 4, _SZ),
     "sol_lin_attn_bwd_workspace_bytes": ([_I32] * 5, _SZ),
@@ -720,6 +721,13 @@ _SIGNATURES = {
     "sol_diff_attn_bwd_workspace_bytes": ([_I32] * 6, _SZ),
     "sol_diff_attn_fwd": ([_P] * 13 + [_I32] * 7 + [_F32, _I32, _P, _SZ, _P], _I32),
     "sol_diff_attn_bwd": ([_P] * 22 + [_I32] * 7 + [_F32, _I32, _P, _SZ, _P], _I32),
+    "sol_qk_norm_rope": ([_P] * 10 + [_F32, _P, _I64, _P] + [_I32] * 6 + [_P] + [_I32] * 5 + [_P], _I32),
+    "sol_qk_norm_rope_bwd_workspace_bytes": ([_I32] * 2, _SZ),
+    "sol_qk_norm_rope_bwd": ([_P] * 16 + [_F32, _P, _I64, _P] + [_I32] * 6 + [_P] + [_I32] * 5 + [_P, _SZ, _P], _I32),
+    "sol_cross_attn_fwd_workspace_bytes": ([_I32] * 7, _SZ),
+    "sol_cross_attn_bwd_workspace_bytes": ([_I32] * 7, _SZ),
+    "sol_cross_attn_fwd": ([_P] * 13 + [_I32] * 6 + [_F32, _P, _SZ, _P], _I32),
+    "sol_cross_attn_bwd": ([_P] * 21 + [_I32] * 6 + [_F32, _P, _SZ, _P], _I32),
 }
 
 
@@ -764,6 +772,34 @@ def sol_diff_attn_fwd(*args):
 
 def sol_diff_attn_bwd(*args):
     return _entry("sol_diff_attn_bwd")(*args)
+
+
+def sol_qk_norm_rope(*args):
+    return _entry("sol_qk_norm_rope")(*args)
+
+
+def sol_qk_norm_rope_bwd_workspace_bytes(B, N):
+    return _entry("sol_qk_norm_rope_bwd_workspace_bytes")(B, N)
+
+
+def sol_qk_norm_rope_bwd(*args):
+    return _entry("sol_qk_norm_rope_bwd")(*args)
+
+
+def sol_cross_attn_fwd_workspace_bytes(B, H, Hk, N, M, D, masked):
+    return _entry("sol_cross_attn_fwd_workspace_bytes")(B, H, Hk, N, M, D, masked)
+
+
+def sol_cross_attn_bwd_workspace_bytes(B, H, Hk, N, M, D, masked):
+    return _entry("sol_cross_attn_bwd_workspace_bytes")(B, H, Hk, N, M, D, masked)
+
+
+def sol_cross_attn_fwd(*args):
+    return _entry("sol_cross_attn_fwd")(*args)
+
+
+def sol_cross_attn_bwd(*args):
+    return _entry("sol_cross_attn_bwd")(*args)
 
 
 def strides(b, h, n):
@@ -1001,6 +1037,176 @@ def diff_attn_bwd(dout, q, k, v, lam, out, out2, lse, scale=None, causal=False, 
           _device_array("kv_lens", kv_lens, dev, torch.int32, (B,)), B, H, Hv, Hk, N, M, D, _scale(scale),
           1 if causal else 0, wp, wn)
     return dq, dk, dv, dlam
+
+
+# ---------------------------------------------- norm and rotation, cross attention
+
+def _positions(pos, dev, B, N):
+    """(pointer, elements between batches) of positions [B, N, 3], or [N, 3] for all; None: none."""
+    if pos is None:
+        return None, 0
+    if not isinstance(pos, torch.Tensor) or pos.dtype is not torch.int32 or pos.device != dev:
+        raise ValueError("pos must be an int32 tensor on %s" % dev)
+    if pos.shape == (N, 3) and pos.is_contiguous():
+        return pos.data_ptr(), 0
+    if pos.shape != (B, N, 3) or not pos[0].is_contiguous():
+        raise ValueError("pos must be [B, N, 3] or [N, 3] with contiguous tokens, got %s" % (tuple(pos.shape),))
+    return pos.data_ptr(), pos.stride(0) if B > 1 else 0
+
+
+def _norm_rope_args(pos, T, Hl, Wl, table, q_gamma, k_gamma, eps, lens, split, dev, B, N, D):
+    """The arguments that both directions share: weights, then the rest."""
+    at, step = _positions(pos, dev, B, N)
+    return ((_gamma_ptr(q_gamma, dev), _gamma_ptr(k_gamma, dev)),
+            (float(eps), at, step, _extents_table_ptr(table, dev, D, T, Hl, Wl, split), T, Hl, Wl, *_split(split),
+             _device_array("lens", lens, dev, torch.int32, (B,))))
+
+
+def _extents_table_ptr(table, dev, D, T, Hl, Wl, split):
+    """As _table_ptr, of a table whose extents bound coordinates: any of them may be 0
+    (rope3d_table gives 4 floats where none is needed)."""
+    if table is None:
+        return None
+    need = _table_floats(D, T, Hl, Wl, _split(split))
+    if (not isinstance(table, torch.Tensor) or table.dtype is not torch.float32 or table.device != dev
+            or not table.is_contiguous() or table.numel() != max(need, 4)):
+        raise ValueError("rope table must be a contiguous float32 tensor on %s, of %d floats for extents %dx%dx%d and split %s"
+                         % (dev, max(need, 4), T, Hl, Wl, _split(split)))
+    return table.data_ptr()
+
+
+def qk_norm_rope(q, k, pos, T, Hl, Wl, table, q_gamma=None, k_gamma=None, eps=1e-6, lens=None, q_out=None,
+                 k_out=None, split=None):
+    """bf16(R(pos) rms_norm(x; gamma, eps)) of q [B, H, N, D] and k [B, Hk, N, D] in
+    one pass (any strides that keep rows contiguous and 16-byte aligned).
+
+    k None: q alone.  pos int32 [B, N, 3] or [N, 3] on the device, (t, h, w) of each
+    token, below 0: that axis does not turn, at or past T, Hl, Wl: the token's rows are
+    NaN; None: nothing turns.  table: rope3d_table(T, Hl, Wl, split=split).  gammas
+    float32 [D] or None (not normalised).  lens int32 [B] on the device (None: all N);
+    rows of the outputs behind a sequence are not written.  q_out may be q, k_out k.
+    Returns (q_out, k_out), which carry no autograd graph whatever the inputs do: the
+    gradients are qk_norm_rope_bwd's."""
+    B, H, N, D = _dims("q", q, 4)
+    dev = q.device
+    qp, qs = _rows("q", q)
+    Hk, kp, ks, op, os_ = 0, None, None, None, None
+    if q_out is None:
+        q_out = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+    yp, ys = _rows("q_out", q_out, dev, (B, H, N, D))
+    if k is None:
+        if k_out is not None:
+            raise ValueError("k_out without k")
+    else:
+        Hk = _dims("k", k, 4)[1]
+        kp, ks = _rows("k", k, dev, (B, Hk, N, D))
+        if k_out is None:
+            k_out = torch.empty((B, Hk, N, D), dtype=torch.bfloat16, device=dev)
+        op, os_ = _rows("k_out", k_out, dev, (B, Hk, N, D))
+    gammas, rest = _norm_rope_args(pos, T, Hl, Wl, table, q_gamma, k_gamma, eps, lens, split, dev, B, N, D)
+    _call(sol_qk_norm_rope, dev, qp, qs, kp, ks, yp, ys, op, os_, *gammas, *rest, B, H, Hk, N, D)
+    return q_out, k_out
+
+
+def qk_norm_rope_bwd(dq_out, dk_out, q, k, pos, T, Hl, Wl, table, q_gamma=None, k_gamma=None, eps=1e-6, lens=None,
+                     dq=None, dk=None, split=None, workspace=None):
+    """The gradients of qk_norm_rope from those of its outputs and its own inputs:
+    (dq, dk, dq_gamma, dk_gamma), the first two bf16 and zero behind a sequence (dq may
+    be dq_out, dk dk_out), the others float32 [D]; None where there is no k or no gamma.
+    Without a gamma q (k) may be None."""
+    B, H, N, D = _dims("dq_out", dq_out, 4)
+    dev = dq_out.device
+    gp, gs = _rows("dq_out", dq_out)
+    shape = (B, H, N, D)
+    qp, qs = _rows("q", q, dev, shape) if q_gamma is not None else (None, None)
+    if dq is None:
+        dq = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    xp, xs = _rows("dq", dq, dev, shape)
+    Hk, hp, hs, kp, ks, yp, ys = 0, None, None, None, None, None, None
+    if dk_out is None:
+        if dk is not None or k_gamma is not None:
+            raise ValueError("dk or k_gamma without dk_out")
+    else:
+        Hk = _dims("dk_out", dk_out, 4)[1]
+        shape = (B, Hk, N, D)
+        hp, hs = _rows("dk_out", dk_out, dev, shape)
+        kp, ks = _rows("k", k, dev, shape) if k_gamma is not None else (None, None)
+        if dk is None:
+            dk = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        yp, ys = _rows("dk", dk, dev, shape)
+    gammas, rest = _norm_rope_args(pos, T, Hl, Wl, table, q_gamma, k_gamma, eps, lens, split, dev, B, N, D)
+    dgq, dgk = (None if g is None else torch.empty(D, dtype=torch.float32, device=dev) for g in (q_gamma, k_gamma))
+    need = sol_qk_norm_rope_bwd_workspace_bytes(B, N) if dgq is not None or dgk is not None else 0
+    ws, wp, wn = _scratch(workspace, need, dev)
+    _call(sol_qk_norm_rope_bwd, dev, gp, gs, hp, hs, qp, qs, kp, ks, xp, xs, yp, ys, *gammas,
+          None if dgq is None else dgq.data_ptr(), None if dgk is None else dgk.data_ptr(), *rest, B, H, Hk, N, D, wp, wn)
+    return dq, dk, dgq, dgk
+
+
+def _cross_args(q, k, v, q_lens, kv_lens, key_mask):
+    """Sizes, row arguments of q, k and v, and the masks' pointers."""
+    B, H, N, D = _dims("q", q, 4)
+    dev = q.device
+    _, Hk, M, _ = _dims("k", k, 4)
+    rows = _rows("q", q) + _rows("k", k, dev, (B, Hk, M, D)) + _rows("v", v, dev, (B, Hk, M, D))
+    if key_mask is not None and isinstance(key_mask, torch.Tensor) and key_mask.dtype is torch.bool:
+        key_mask = key_mask.view(torch.uint8)
+    return (B, H, Hk, N, M, D), rows, (_device_array("q_lens", q_lens, dev, torch.int32, (B,)),
+                                       _device_array("kv_lens", kv_lens, dev, torch.int32, (B,)),
+                                       _device_array("key_mask", key_mask, dev, torch.uint8, (B, M)))
+
+
+def cross_attn_fwd(q, k, v, scale=None, q_lens=None, kv_lens=None, key_mask=None, out=None, training=False,
+                   workspace=None):
+    """Cross attention: softmax(scale q k^T) v of q [B, H, N, D] over k, v
+    [B, Hk, M, D], bf16 (any strides that keep rows contiguous and 16-byte aligned; 0
+    shares states between sequences), H a multiple of Hk (scale None: 1/sqrt(D)).
+
+    q_lens, kv_lens int32 [B] on the device (None: all); key_mask bool or uint8 [B, M]
+    on the device (None: all visible): a key that is False or 0 is hidden, and not read.
+    Rows that see no key are zero; rows of out behind a sequence are not written.
+    Returns out, or with training (out, out_left, lse), which cross_attn_bwd takes:
+    what out's rounding left, bf16 [B, H, N, D], and the rows' log sums, float32
+    [B, H, N].  They carry no autograd graph whatever the inputs do."""
+    sizes, rows, masks = _cross_args(q, k, v, q_lens, kv_lens, key_mask)
+    B, H, _, N, _, D = sizes
+    dev = q.device
+    if out is None:
+        out = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+    op, os_ = _rows("out", out, dev, (B, H, N, D))
+    left = lse = None
+    if training:
+        left = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+        lse = torch.empty((B, H, N), dtype=torch.float32, device=dev)
+    ws, wp, wn = _scratch(workspace, sol_cross_attn_fwd_workspace_bytes(*sizes, 0 if key_mask is None else 1), dev)
+    _call(sol_cross_attn_fwd, dev, *rows, op, os_, left.data_ptr() if training else None,
+          lse.data_ptr() if training else None, *masks, *sizes, _scale(scale), wp, wn)
+    return (out, left, lse) if training else out
+
+
+def cross_attn_bwd(dout, q, k, v, out, out_left, lse, scale=None, q_lens=None, kv_lens=None, key_mask=None, dq=None,
+                   dk=None, dv=None, workspace=None):
+    """The gradients of cross_attn_fwd from dout and the out, out_left and lse of its
+    call with training: (dq, dk, dv), bf16, zero behind a sequence and for hidden keys."""
+    sizes, rows, masks = _cross_args(q, k, v, q_lens, kv_lens, key_mask)
+    B, H, Hk, N, M, D = sizes
+    dev = q.device
+    gp, gs = _rows("dout", dout, dev, (B, H, N, D))
+    op, os_ = _rows("out", out, dev, (B, H, N, D))
+    grads = []
+    for name, t, h, n in (("dq", dq, H, N), ("dk", dk, Hk, M), ("dv", dv, Hk, M)):
+        if t is None:
+            t = torch.empty((B, h, n, D), dtype=torch.bfloat16, device=dev)
+        grads.append((t,) + _rows(name, t, dev, (B, h, n, D)))
+    if out_left is None or lse is None:
+        raise ValueError("out_left and lse must be given")
+    ws, wp, wn = _scratch(workspace, sol_cross_attn_bwd_workspace_bytes(*sizes, 0 if key_mask is None else 1), dev)
+    (dq, dqp, dqs), (dk, dkp, dks), (dv, dvp, dvs) = grads
+    _call(sol_cross_attn_bwd, dev, gp, gs, *rows, op, os_,
+          _device_array("out_left", out_left, dev, torch.bfloat16, (B, H, N, D)),
+          _device_array("lse", lse, dev, torch.float32, (B, H, N)), dqp, dqs, dkp, dks, dvp, dvs, *masks, *sizes,
+          _scale(scale), wp, wn)
+    return dq, dk, dv
 
 
 # ------------------------------------------------------------ measurement aid
