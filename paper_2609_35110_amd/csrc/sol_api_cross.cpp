@@ -206,7 +206,7 @@ int sol_qk_norm_rope_bwd(const void* dq_out, const sol_strides* dq_out_strides, 
 size_t sol_cross_attn_fwd_workspace_bytes(int B, int H, int Hk, int N, int M, int D, int masked) {
   const sol::CrossShape s = cross_shape(B, H, Hk, N, M, masked);
   if (check_cross(s, D) != SOL_OK) return 0;
-  const size_t need = sol::cross_fwd_bytes(s);
+  const size_t need = sol::cross_fwd_bytes(s, nullptr, nullptr);
   return check_size(need) == SOL_OK ? need : 0;
 }
 
@@ -233,7 +233,7 @@ int sol_cross_attn_fwd(const void* q, const sol_strides* q_strides, const void* 
   if (!aligned16(out_left)) return fail(SOL_ERR_INVALID_ARG, "out_left must be 16-byte aligned");
   SOL_TRY(check_small("lse", lse, true));
   if (!out_left != !lse) return fail(SOL_ERR_INVALID_ARG, "out_left and lse are given together or not at all");
-  const size_t need = sol::cross_fwd_bytes(a.s);
+  const size_t need = sol::cross_fwd_bytes(a.s, &a, workspace);
   SOL_TRY(check_size(need));
   SOL_TRY(check_workspace(workspace, workspace_bytes, need));
   cross_spans(a.s, in + 3);
@@ -243,7 +243,6 @@ int sol_cross_attn_fwd(const void* q, const sol_strides* q_strides, const void* 
   SOL_TRY(check_apart(in, 6, outs, 4));
   a.left = static_cast<uint16_t*>(out_left);
   a.lse = lse;
-  a.ws = static_cast<float*>(workspace);
   return done(sol::launch_cross_fwd(a, reinterpret_cast<hipStream_t>(stream)), "cross_attn_fwd");
 }
 

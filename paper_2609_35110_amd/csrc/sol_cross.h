@@ -54,16 +54,17 @@ struct CrossShape {
   const uint8_t* mask;     // [B][M], 0: hidden; may be null
 };
 
-// How a forward call runs: in groups of few rows that share a key head, all of them
-// in `tiles.pieces` pieces of their keys (few), or in row tiles, from tiles.full on
-// in pieces.
+// How a forward call runs: in groups of few rows that share a key head, their keys in
+// `pieces` (few); or in tiles of rows that workgroups take in line, tiles shared at the
+// workgroups' borders (split) or not.
 struct CrossPlan {
   bool few;
-  DiffTiles tiles;
+  int pieces;
+  bool split;
+  int workgroups;  // of the tile kernel
 };
-CrossPlan cross_plan(const CrossShape& s, bool ragged);  // ragged: with kv_lens or mask
-// Bytes of workspace, with lengths or without (or kTooLarge).
-size_t cross_fwd_bytes(const CrossShape& s);
+constexpr int kCus = 256;  // compute units: each holds one workgroup of the tile kernels
+CrossPlan cross_plan(const CrossShape& s, bool ragged);  // ragged: with q_lens, kv_lens or mask
 
 struct CrossFwd {
   CrossShape s;
@@ -77,6 +78,9 @@ struct CrossFwd {
   // sequence in order and then the others; [B], how many are visible.
   int32_t *order, *counts;
 };
+// Bytes of workspace, with lengths or without (or kTooLarge); with a given, its sections
+// (from ws on) are filled in.
+size_t cross_fwd_bytes(const CrossShape& s, CrossFwd* a, void* ws);
 hipError_t launch_cross_fwd(const CrossFwd& a, hipStream_t stream);
 
 struct CrossBwd {

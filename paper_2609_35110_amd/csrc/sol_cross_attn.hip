@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256, 2) void cross_few_kernel(CrossFwd A, int nspli
 }
 
 // The pieces' results joined: four waves take a row, two dims a lane.
-__global__ __launch_bounds__(256) void cross_join_kernel(CrossFwd A, DiffTiles plan) {
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossFwd A, int pieces) {
   __shared__ float2 of[4][64];
   __shared__ float sums[4][3];
   lds_poison(of, sizeof(of));
@@ -223,14 +223,14 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossFwd A, DiffTiles p
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int n = (int)(i % s.N), bh = (int)(i / s.N), h = bh % s.H, b = bh / s.H;
   if (n >= query_len(s, b)) return;
-  const Parts p = parts_of(A.ws, rows, plan.pieces);
+  const Parts p = parts_of(A.ws, rows, pieces);
   float top = kNoMax, sum = 0.0f, exact = 0.0f;
   // (loads of eight pieces at a time)
 #pragma unroll 8
-  for (int u = wave; u < plan.pieces; u += 4) top = fmaxf(top, p.l[u * rows + i]);
+  for (int u = wave; u < pieces; u += 4) top = fmaxf(top, p.l[u * rows + i]);
   float2 o = make_float2(0.0f, 0.0f);
 #pragma unroll 8
-  for (int u = wave; u < plan.pieces; u += 4) {
+  for (int u = wave; u < pieces; u += 4) {
     const int64_t am = u * rows + i;
     const float f = __builtin_amdgcn_exp2f(p.l[am] - top);
     const float2 x = *reinterpret_cast<const float2*>(p.o + am * D + 2 * lane);
@@ -301,10 +301,13 @@ template <bool kMasked>
 struct Keys {
   const int32_t* order;  // kMasked
   int len;
-  __device__ __forceinline__ Keys(const CrossShape& s, const int32_t* o, const int32_t* counts, int b) {
+  Keys() = default;
+  __device__ __forceinline__ Keys(const CrossShape& s, const int32_t* o, int b, int n) {
     order = kMasked ? o + (int64_t)b * s.M : nullptr;
-    len = kMasked ? counts[b] : key_len(s, b);
+    len = n;
   }
+  __device__ __forceinline__ Keys(const CrossShape& s, const int32_t* o, const int32_t* counts, int b)
+      : Keys(s, o, b, kMasked ? counts[b] : key_len(s, b)) {}
   __device__ __forceinline__ int at(int i) const { return kMasked ? order[i] : i; }
 };
 
@@ -324,19 +327,20 @@ struct KeyCopies {
   int next;  // kMasked: this lane's row of the tile to come
   const uint16_t *mk, *mv;
 
-  __device__ __forceinline__ KeyCopies(const Rows& kr, const Rows& vr, int b, int hk, const Keys<kMasked>& ks, int from,
-                                       int n, uint32_t lds, int wave, int l)
-      : k(kr.p + b * kr.sb + hk * kr.sh), v(vr.p + b * vr.sb + hk * vr.sh), ksn(kr.sn), vsn(vr.sn), keys(ks), key(from),
-        row(8 * wave + (l >> 3)), lane(l), turns(n), at0(lds + wave * kRowBlock), to(0), ok(0), ov(0), next(0), mk(nullptr),
-        mv(nullptr) {
-    restart(from);
-  }
-  __device__ __forceinline__ void fetch(int tile_key) {
-    if (kMasked && turns > 0) next = keys.at(min(tile_key + row, keys.len - 1));
-  }
   const uint16_t *k0, *v0;
-  __device__ __forceinline__ void restart(int from) {
+  // n tiles from key `from` on into a ring at LDS address `lds`.
+  __device__ __forceinline__ void begin(const Rows& kr, const Rows& vr, int b, int hk, const Keys<kMasked>& ks, int from, int n,
+                                        uint32_t lds, int wave, int l) {
+    k = kr.p + b * kr.sb + hk * kr.sh;
+    v = vr.p + b * vr.sb + hk * vr.sh;
+    ksn = kr.sn;
+    vsn = vr.sn;
+    keys = ks;
     key = from;
+    row = 8 * wave + (l >> 3);
+    lane = l;
+    turns = n;
+    at0 = lds + wave * kRowBlock;
     if (kMasked) {
       fetch(from);
     } else {
@@ -345,6 +349,9 @@ struct KeyCopies {
       ok = copy_offset(row, ksn, lane);
       ov = copy_offset(row, vsn, lane);
     }
+  }
+  __device__ __forceinline__ void fetch(int tile_key) {
+    if (kMasked && turns > 0) next = keys.at(min(tile_key + row, keys.len - 1));
   }
   // Tile i (after i - 1, or the same again) into place `place` of a ring of kRing.
   __device__ __forceinline__ void start(int i, int place) {
@@ -402,6 +409,570 @@ __device__ __forceinline__ Piece piece_of(int wg, int tiles, const DiffTiles& p)
   if (wg < p.full) return {xcd_local_id(wg, p.full), 0, 1};
   const int id = xcd_local_id(wg - p.full, (tiles - p.full) * p.pieces);
   return {p.full + id / p.pieces, id % p.pieces, p.pieces};
+}
+
+// ----------------------------------------------------------- forward, row tiles
+
+// The tile kernel's work is a line of turns: sequence after sequence, head after head,
+// tile after tile of 256 rows, each as many turns as its keys make tiles of 32 (one
+// where there is none).  Workgroup i of n takes turns [i total / n, (i + 1) total / n)
+// of it, to the nearest tile's start unless tiles are split.  Lengths count where there
+// are few sequences enough to add them up; else every sequence counts as a whole one.
+constexpr int kMaxByLength = 1024;
+struct Line {
+  const CrossShape& s;
+  const int32_t* counts;  // of visible keys, or null
+  bool by_length;
+  __device__ __forceinline__ Line(const CrossShape& sh, const int32_t* c) : s(sh), counts(c) {
+    by_length = (s.q_lens || s.kv_lens || s.mask) && s.B <= kMaxByLength;
+  }
+  __device__ __forceinline__ int keys(int b) const { return counts ? counts[b] : key_len(s, b); }
+  __device__ __forceinline__ int tiles(int b) const { return tiles_of(by_length ? query_len(s, b) : s.N, kCrossRows); }
+  __device__ __forceinline__ int turns(int b) const { return max(1, tiles_of(by_length ? keys(b) : s.M, kTileKeys)); }
+  __device__ __forceinline__ int64_t cost(int b) const { return (int64_t)s.H * tiles(b) * turns(b); }
+};
+struct Place {
+  int b, h, rank, turn;
+};
+// Places of two turns of the line, and the line's length.  All lanes of a wave call it.
+struct Bounds {
+  Place from, to;
+};
+__device__ __forceinline__ Place place_in(const Line& l, int b, int64_t rest) {
+  const int per_tile = l.turns(b);
+  const int64_t tile = rest / per_tile, per_head = max(l.tiles(b), 1);
+  return {b, (int)(tile / per_head), (int)(tile % per_head), (int)(rest - tile * per_tile)};
+}
+__device__ __forceinline__ Place uniform(const Place& p) {
+  return {__builtin_amdgcn_readfirstlane(p.b), __builtin_amdgcn_readfirstlane(p.h), __builtin_amdgcn_readfirstlane(p.rank),
+          __builtin_amdgcn_readfirstlane(p.turn)};
+}
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)(((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32) | __builtin_amdgcn_readfirstlane((uint32_t)x));
+}
+__device__ __forceinline__ int64_t line_total(const Line& l) {
+  if (!l.by_length) return l.cost(0) * l.s.B;
+  const int lane = threadIdx.x & 63;
+  int64_t total = 0;
+  for (int b = lane; b < l.s.B; b += 64) total += l.cost(b);
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
+  return uniform(total);
+}
+__device__ __forceinline__ Place find(const Line& l, int64_t turn, int64_t total) {
+  const Place end = {l.s.B, 0, 0, 0};
+  if (turn >= total) return end;
+  if (!l.by_length) {
+    const int64_t one = l.cost(0);
+    return uniform(place_in(l, (int)(turn / one), turn % one));
+  }
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int base = 0; base < l.s.B; base += 64) {
+    const int b = base + lane;
+    const int64_t mine = b < l.s.B ? l.cost(b) : 0;
+    int64_t upto = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int64_t x = __shfl_up(upto, m);
+      if (lane >= m) upto += x;
+    }
+    const uint64_t past = __ballot(before + upto > turn);
+    if (past) {
+      const int at = __ffsll((unsigned long long)past) - 1;
+      const int64_t start = before + uniform(__shfl(upto - mine, at));
+      return uniform(place_in(l, base + at, turn - start));
+    }
+    before += uniform(__shfl(upto, 63));
+  }
+  return end;
+}
+// The next tile's start where the turn lies in a tile's second half, this one's otherwise.
+__device__ __forceinline__ Place nearest(const Line& l, Place p) {
+  if (p.b >= l.s.B || p.turn == 0) return p;
+  if (2 * p.turn >= __builtin_amdgcn_readfirstlane(l.turns(p.b))) {
+    if (++p.rank >= __builtin_amdgcn_readfirstlane(l.tiles(p.b))) {
+      p.rank = 0;
+      if (++p.h == l.s.H) {
+        p.h = 0;
+        do ++p.b;
+        while (p.b < l.s.B && __builtin_amdgcn_readfirstlane(l.tiles(p.b)) == 0);  // (the next one's first tile is a place of the line)
+      }
+    }
+  }
+  p.turn = 0;
+  return p;
+}
+// Workgroups that have a turn of the line.
+__device__ __forceinline__ int line_workgroups(int64_t total, int launched) { return (int)min(total, (int64_t)launched); }
+__device__ __forceinline__ int64_t line_bound(int64_t total, int i, int n) {
+  return total / n * i + total % n * i / n;
+}
+
+// A workgroup's tiles one after the other: those with rows; turns `from` .. `to` of the
+// current one are the workgroup's.
+struct Tiles {
+  Place at;
+  int qlen, klen, from, to;
+  bool done;
+  __device__ __forceinline__ int turns() const { return tiles_of(klen, kTileKeys); }
+  __device__ __forceinline__ bool whole() const { return from == 0 && to == turns(); }
+  __device__ __forceinline__ int row0() const { return at.rank * kCrossRows; }
+  __device__ __forceinline__ void lengths(const Line& l) {
+    if (at.b >= l.s.B) return;
+    qlen = __builtin_amdgcn_readfirstlane(query_len(l.s, at.b));
+    klen = __builtin_amdgcn_readfirstlane(l.keys(at.b));
+  }
+  // From `at` on, the first tile that has rows and is not past `end` (which may name a
+  // tile behind its sequence's rows, where lengths do not count).
+  __device__ __forceinline__ void settle_on(const Line& l, const Place& end) {
+    for (;;) {
+      const bool end_head = at.b == end.b && at.h == end.h;
+      if (at.b >= l.s.B || (end_head && (at.rank > end.rank || (at.rank == end.rank && at.turn >= end.turn)))) {
+        done = true;
+        return;
+      }
+      if (row0() < qlen) break;
+      if (end_head) {
+        done = true;
+        return;
+      }
+      at.rank = at.turn = 0;
+      if (++at.h == l.s.H) {
+        at.h = 0;
+        ++at.b;
+        lengths(l);
+      }
+    }
+    from = at.turn;
+    to = turns();
+    if (at.b == end.b && at.h == end.h && at.rank == end.rank) to = min(to, end.turn);
+  }
+  __device__ __forceinline__ void start(const Line& l, const Place& f, const Place& end) {
+    at = f;
+    done = false;
+    qlen = klen = from = to = 0;
+    lengths(l);
+    settle_on(l, end);
+  }
+  __device__ __forceinline__ void next(const Line& l, const Place& end) {
+    if (done) return;
+    at.turn = 0;
+    ++at.rank;
+    settle_on(l, end);
+  }
+};
+
+// Where workgroup `wg` of a split line leaves its share of a tile: before one that
+// another began (0), or after the last that it began itself (1); 256 rows of 128 and
+// two logarithms each.
+constexpr int kShareFloats = kCrossRows * (D + 2);
+__device__ __forceinline__ float* share_of(float* ws, int wg, bool began) {
+  return ws + ((int64_t)2 * wg + began) * kShareFloats;
+}
+
+// 256 rows of one head a tile, 64 a wave in two blocks of 32 (a fragment of K or V is
+// read once for two MFMAs); one wave a SIMD, so its MFMAs, exponentials and LDS reads
+// have to overlap inside the wave: a turn of the loop is a list of slots, each an MFMA,
+// the LDS read of a fragment some slots on and a share of the arithmetic on scores that
+// are done, and nothing moves between slots.  Turn i: the products P V of item i - 1,
+// the exponentials of item i, the scores of item i + 1, an item being 32 keys of a tile.
+// Items follow each other over the tiles' borders, so that a tile of few keys (a
+// prompt's 512 are 16 turns) pays for no pipeline of its own: its rows come into LDS
+// while the tile before is walked, and its outputs leave while the next one's copies
+// are on their way.
+//
+// A row is held to the maximum of its first item: P and the sums have 8 exponent bits,
+// so scores far above it cost no precision, and most rows' stay within a few binades.
+// A row whose P add up to more than 2^80 (55 above it in the exponent), or whose
+// products with the values leave fp32, has its workgroup walk the tile again, held to
+// the rows' own maxima, found by a walk for scores alone.
+constexpr float kTooMuch = 1.2089258e24f;
+template <bool kMasked, bool kTrain>
+__global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool split) {
+  constexpr int kFrags = 16, kAhead = 6, kHold = 8;
+  struct Lds {
+    uint8_t tiles[kRing][2][kTile32];
+    uint8_t rows[4][2][kTile32];  // of each wave: the next tile's q, or an output on its way
+  };
+  __shared__ __attribute__((aligned(1024))) Lds lds;
+  lds_poison(&lds, sizeof(lds));
+  lds_poison_done();
+  const CrossShape& s = A.s;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
+  const int wg = xcd_local_id(blockIdx.x, gridDim.x), per = s.H / s.Hk;
+  const float c = s.scale * kLog2e;
+  const Line line(s, kMasked ? A.counts : nullptr);
+  Place end;
+  Tiles now_at, next_at;
+  {
+    const int64_t total = line_total(line);
+    const int n = line_workgroups(total, gridDim.x);
+    if (wg >= n) return;
+    Place from = find(line, line_bound(total, wg, n), total);
+    end = find(line, line_bound(total, wg + 1, n), total);
+    if (!split) {
+      from = nearest(line, from);
+      end = nearest(line, end);
+    }
+    now_at.start(line, from, end);
+  }
+
+  // outputs of rows without keys: their tile has no turns
+  auto no_keys = [&](const Tiles& at) __attribute__((always_inline)) {
+    uint16_t* to = A.out.p + at.at.b * A.out.sb + at.at.h * A.out.sh;
+    const int64_t row = ((int64_t)at.at.b * s.H + at.at.h) * s.N;
+    for (int i = t; i < kCrossRows * kChunks; i += 256) {
+      const int n = at.row0() + i / kChunks, cc = i % kChunks;
+      if (n >= at.qlen) break;
+      *reinterpret_cast<uint4*>(to + (int64_t)n * A.out.sn + 8 * cc) = make_uint4(0, 0, 0, 0);
+      if (kTrain) *reinterpret_cast<uint4*>(A.left + (row + n) * D + 8 * cc) = make_uint4(0, 0, 0, 0);
+      if (kTrain && cc == 0) A.lse[row + n] = -__builtin_inff();
+    }
+  };
+  // on to a tile that has turns; `write`: those without are written on the way
+  auto to_turns = [&](Tiles& at, bool write) __attribute__((always_inline)) {
+    while (!at.done && at.from >= at.to) {
+      if (write && at.klen == 0) no_keys(at);
+      at.next(line, end);
+    }
+  };
+  to_turns(now_at, true);
+  if (now_at.done) return;
+
+  // the copies of now_at's tiles of keys, two ahead of the exponentials', then the next one's
+  KeyCopies<kMasked> copy;
+  auto copy_tile = [&](const Tiles& at) __attribute__((always_inline)) {
+    copy.begin(A.k, A.v, at.at.b, at.at.h / per, Keys<kMasked>(s, A.order, at.at.b, at.klen), at.from * kTileKeys,
+               at.to - at.from, lds_address(&lds.tiles[0][0][0]), wave, lane);
+  };
+  // rows of a tile's q, the wave's 64, into its place; rows behind the sequence are its last one again
+  uint8_t* mine = &lds.rows[wave][0][0];
+  auto copy_rows = [&](const Tiles& at) __attribute__((always_inline)) {
+    const uint16_t* q = A.q.p + at.at.b * A.q.sb + at.at.h * A.q.sh + 8 * ((lane & 7) ^ swizzle(lane >> 3));
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const uint16_t* p = q + (int64_t)min(at.row0() + 64 * wave + 8 * u + (lane >> 3), at.qlen - 1) * A.q.sn;
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(mine) + u * kRowBlock);
+      copy_1k_from(to, p);
+      copy_1k_from(to + 1024, p + 64);
+    }
+  };
+  bf16x8 qf[2][8];
+  const RowPlace rp = row_place(lane);
+  const int cp = col_place(lane);
+  auto load_rows = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the wave's own copies
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) qf[m][kk] = row_frag(mine + m * kTile32, rp, kk);
+    asm volatile("" ::: "memory");
+    hold_in_agprs(qf[0]);
+    hold_in_agprs(qf[1]);
+  };
+
+  struct Item {
+    f32x16 s[2];        // scores of the row blocks
+    uint32_t pw[2][8];  // P, packed
+  } ia, ib;
+  MapRows x[2];
+  float mc[2];  // the maxima held to, times c
+  bf16x8 ring[kHold];
+  int item = 0;  // of all, at the tile's start
+  int n_turns = 0, n_keys = 0, key0 = 0, n_next = 0;
+  bool begun = false;  // the next tile's copies
+  // the fragments of a turn in order: V of item i - 1, then K of item i + 1
+  auto fragment = [&](int f, const uint8_t* then, const uint8_t* next) __attribute__((always_inline)) {
+    return f < 8 ? col_frag(then + kTile32 + cp, f >> 2, f & 3) : row_frag(next, rp, f - 8);
+  };
+  auto place_of = [&](int i) __attribute__((always_inline)) {
+    return &lds.tiles[(item + min(i, n_turns - 1)) % kRing][0][0];
+  };
+  auto mask_item = [&](Item& now, int i) __attribute__((always_inline)) {
+    const int key = key0 + i * kTileKeys;
+    if (key + kTileKeys > n_keys || i >= n_turns) {
+      const int last = i < n_turns ? n_keys - 1 : -1;
+      settle(now.s[0], now.s[1]);
+      mask(now.s[0], key + 4 * hh, last);
+      mask(now.s[1], key + 4 * hh, last);
+    }
+  };
+  // one exponential; its pair is summed and packed with the next one's (an
+  // exponential's result is not there at once)
+  float e[2];
+  auto take = [&](Item& now, int m, int r) __attribute__((always_inline)) {  // keys r, r + 1
+    if (kTrain) x[m].exact += e[0];
+    now.pw[m][r >> 1] = pack_bf16x2(e[0], e[1]);
+    if (kTrain) x[m].exact += e[1];
+    pin(now.pw[m][r >> 1]);
+    x[m].l = add_bf16x2(now.pw[m][r >> 1], x[m].l);
+    pin(x[m].l);
+    if (kTrain) pin(x[m].exact);
+  };
+  auto exponential = [&](Item& now, int m, int r) __attribute__((always_inline)) {
+    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(now.s[m][r], c, -mc[m]));
+    if (r % 2 == 0 && r > 0) take(now, m, r - 2);
+    if (r == 0 && m == 1) take(now, 0, 14);
+    e[r & 1] = p;
+    pin(e[r & 1]);
+  };
+  auto operand = [&](const Item& z, int m, int y) __attribute__((always_inline)) {
+    return __builtin_bit_cast(bf16x8, make_uint4(z.pw[m][4 * y], z.pw[m][4 * y + 1], z.pw[m][4 * y + 2], z.pw[m][4 * y + 3]));
+  };
+  // scores of item i, which is in the ring's place `place`, all at once
+  auto scores_of = [&](Item& z, int i, int place) __attribute__((always_inline)) {
+    const uint8_t* tk = &lds.tiles[place % kRing][0][0];
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const bf16x8 f = row_frag(tk, rp, kk);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        if (kk == 0) score_first_a(z.s[m], f, qf[m][kk]);
+        else score_a(z.s[m], f, qf[m][kk]);
+      }
+    }
+    settle(z.s[0], z.s[1]);
+    mask_item(z, i);
+  };
+  auto raise = [&](const Item& z) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      float top = z.s[m][0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, z.s[m][r]);
+      x[m].m = fmaxf(x[m].m, both_max(top));
+    }
+  };
+  // Large values under P that pass 1 may leave fp32 with sums that stay below 2^80:
+  // looked for in waves where a row's P add up to more than its keys could at 1.
+  auto not_finite = [&]() __attribute__((always_inline)) {
+    if (!__any(x[0].l > (float)SOL_MAX_TOKENS || x[1].l > (float)SOL_MAX_TOKENS)) return false;
+    uint32_t top = 0;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        top = max(top, max(__float_as_uint(x[0].o[d][r]) & 0x7fffffffu, __float_as_uint(x[1].o[d][r]) & 0x7fffffffu));
+    return top >= 0x7f800000u;
+  };
+  // item i of the tile; old: item i - 1's P, and room for item i + 1's scores
+  auto turn = [&](int i, Item& now, Item& old) __attribute__((always_inline)) {
+    const uint8_t* to = place_of(max(i - 1, 0));
+    const uint8_t* tn = place_of(i);
+    const uint8_t* next = place_of(i + 1);
+    mask_item(now, i);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) asm volatile("" : "+a"(x[0].o[d]), "+a"(x[1].o[d]));
+    hold_in_agprs(qf[0]);
+    hold_in_agprs(qf[1]);
+    each<0, 32>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int j = slot.value, f = j / 2, m = j & 1;
+      if constexpr (j == 2) {
+        copies_landed<0>();
+        if (i < n_turns) {  // (past them, and past a tile without a next, it comes again)
+          if (i + 2 >= n_turns && !begun && !next_at.done) {
+            copy_tile(next_at);
+            begun = true;
+          }
+          copy.start(begun ? n_next : i + 2, item + (begun ? n_turns + n_next : i + 2));
+          n_next += begun;
+        }
+        slot_end();
+      }
+      if constexpr (j >= 3 && j < 7) copy.part(j - 3);
+      if constexpr (j < 16) {
+        constexpr int d = f & 3, y = j >> 3;
+        x[m].o[d] = mfma(ring[f % kHold], operand(old, m, y), x[m].o[d]);
+      } else {
+        constexpr int kk = f - 8;
+        if constexpr (kk == 0) score_first_a(old.s[m], ring[f % kHold], qf[m][kk]);
+        else score_a(old.s[m], ring[f % kHold], qf[m][kk]);
+      }
+      if constexpr (m == 0) {
+        constexpr int g = f + kAhead;
+        ring[g % kHold] = g < kFrags ? fragment(g, to, next) : fragment(g - kFrags, tn, nullptr);
+      }
+      if constexpr (j >= 2 && j < 16) {
+#pragma unroll
+        for (int u = (j - 2) * 8 / 7; u < (j - 1) * 8 / 7; ++u) exponential(now, 0, u);
+      }
+      if constexpr (j >= 16) exponential(now, 1, j - 16);
+      slot_end();
+    });
+    take(now, 1, 14);
+  };
+  auto last_products = [&](const Item& old) __attribute__((always_inline)) {
+    const uint8_t* to = place_of(n_turns - 1);
+#pragma unroll
+    for (int f = 0; f < 8; ++f) {
+      const bf16x8 v = f < kAhead ? ring[f % kHold] : fragment(f, to, nullptr);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) x[m].o[f & 3] = mfma(v, operand(old, m, f >> 2), x[m].o[f & 3]);
+    }
+  };
+  // a tile's outputs, through the wave's rows in LDS
+  auto finish = [&](const Tiles& at) __attribute__((always_inline)) {
+    const bool whole = at.whole();
+    float* share = share_of(A.ws, wg, at.from == 0);
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float l = both_sum(x[m].l), exact = kTrain ? both_sum(x[m].exact) : 0.0f;
+      const float inv = 1.0f / l;  // (a row behind the sequence is its last one again)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[m].o[d][r] *= inv;
+      const int first = 64 * wave + 32 * m, n = at.row0() + first + l32;
+      if (!whole) {
+        float* to = share + (first + l32) * D + 4 * hh;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<float4*>(to + 32 * d + 8 * q) =
+                make_float4(x[m].o[d][4 * q], x[m].o[d][4 * q + 1], x[m].o[d][4 * q + 2], x[m].o[d][4 * q + 3]);
+        if (hh == 0) {
+          share[kCrossRows * D + first + l32] = mc[m] + log2f(l);
+          if (kTrain) share[kCrossRows * (D + 1) + first + l32] = mc[m] + log2f(exact);
+        }
+        continue;
+      }
+      const int64_t row = ((int64_t)at.at.b * s.H + at.at.h) * s.N + at.row0() + first;
+      const int rows = at.qlen - at.row0() - first;
+      store_rows(mine, lane, A.out.p + at.at.b * A.out.sb + at.at.h * A.out.sh + (int64_t)(at.row0() + first) * A.out.sn,
+                 A.out.sn, 0, rows, [&](int d, int q) { return pack4(x[m].o[d], q); });
+      if (kTrain) {
+        store_rows(mine, lane, A.left + row * D, D, 0, rows,
+                   [&](int d, int q) { return left4(x[m].o[d], q, pack4(x[m].o[d], q)); });
+        if (hh == 0 && n < at.qlen) A.lse[row + l32] = (mc[m] + log2f(exact)) * kLn2;
+      }
+    }
+  };
+
+  copy_rows(now_at);
+  next_at = now_at;
+  next_at.next(line, end);
+  to_turns(next_at, true);
+  load_rows();
+  if (!next_at.done) copy_rows(next_at);
+  for (bool landed = false;; landed = true) {
+    n_turns = now_at.to - now_at.from;
+    n_keys = now_at.klen;
+    key0 = now_at.from * kTileKeys;
+    x[0].m = x[1].m = kNoMax;
+    for (int attempt = 0;; ++attempt) {
+      // the tile's first two items, but what the tile before has brought already
+      if (!begun) {
+        copy_tile(now_at);
+        copy.all(0, item);
+        n_next = 1;
+        landed = false;
+      }
+      if (!landed) {
+        copies_landed<0>();
+        all_landed();
+      }
+      if (n_next < 2) copy.all(1, item + 1);
+      begun = false;
+      n_next = 0;
+      scores_of(ia, 0, item);
+      if (attempt == 0) raise(ia);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const float held = x[m].m;
+        clear(x[m]);
+        x[m].m = held;
+        mc[m] = held * c;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) ib.pw[m][w] = 0;
+      }
+      // (turn 0's products are of P = 0 and the tile itself)
+#pragma unroll
+      for (int f = 0; f < kAhead; ++f) ring[f] = fragment(f, place_of(0), nullptr);
+      for (int i = 0; i < n_turns; i += 2) {  // (an odd tile's last turn is of no key)
+        turn(i, ia, ib);
+        turn(i + 1, ib, ia);
+      }
+      last_products(ib);
+      if (attempt || !__syncthreads_or(!(x[0].l < kTooMuch && x[1].l < kTooMuch) || not_finite())) break;
+      // the rows' own maxima, by a walk for scores alone; then the tile again
+      copies_landed<0>();
+      copy_tile(now_at);
+      for (int i = 0; i < n_turns; ++i) {
+        __syncthreads();
+        copy.all(i, 0);
+        copies_landed<0>();
+        scores_of(ia, i, 0);
+        raise(ia);
+      }
+      __syncthreads();
+      begun = false;
+    }
+    item += n_turns;
+    const Tiles past = now_at;
+    now_at = next_at;
+    if (!now_at.done) load_rows();  // (its place is free for the outputs then)
+    finish(past);
+    if (now_at.done) break;
+    next_at.next(line, end);
+    to_turns(next_at, true);
+    if (!next_at.done) copy_rows(next_at);
+  }
+  copies_landed<0>();  // none is under way when the wave ends
+}
+
+// Tiles that workgroups shared, joined: 16 rows of a tile a workgroup, a row's 16
+// chunks of 8 dims a lane each.
+__global__ __launch_bounds__(256) void cross_shares_kernel(CrossFwd A, int launched) {
+  const CrossShape& s = A.s;
+  const Line line(s, s.mask ? A.counts : nullptr);
+  const int per_head = tiles_of(s.N, kCrossRows), steps = kCrossRows / 16;
+  const int tile = blockIdx.x / steps, r = blockIdx.x % steps * 16 + (threadIdx.x >> 4), cc = threadIdx.x & 15;
+  const int rank = tile % per_head, bh = tile / per_head, h = bh % s.H, b = bh / s.H;
+  const int n = rank * kCrossRows + r, qlen = query_len(s, b);
+  if (rank * kCrossRows >= qlen) return;
+  // the tile's turns in the line, and the first and last workgroup that has some
+  const int64_t total = line_total(line), turns = line.turns(b);
+  const int wgs = line_workgroups(total, launched);
+  int64_t at = ((int64_t)h * line.tiles(b) + rank) * turns;
+  if (line.by_length) {
+    int64_t before = 0;
+    for (int i = threadIdx.x & 63; i < b; i += 64) before += line.cost(i);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) before += __shfl_xor(before, m);
+    at += before;
+  } else {
+    at += b * line.cost(0);
+  }
+  const int w0 = (int)(((at + 1) * wgs - 1) / total), w1 = (int)(((at + turns) * wgs - 1) / total);
+  if (w0 == w1 || n >= qlen) return;
+  auto share = [&](int w) { return share_of(A.ws, w, line_bound(total, w, wgs) <= at); };
+  float top = kNoMax;
+  for (int w = w0; w <= w1; ++w) top = fmaxf(top, share(w)[kCrossRows * D + r]);
+  float sum = 0.0f, exact = 0.0f, o[8] = {};
+  for (int w = w0; w <= w1; ++w) {
+    const float* x = share(w);
+    const float f = __builtin_amdgcn_exp2f(x[kCrossRows * D + r] - top);
+    sum += f;
+    if (A.lse) exact += __builtin_amdgcn_exp2f(x[kCrossRows * (D + 1) + r] - top);
+    const float4 a = *reinterpret_cast<const float4*>(x + r * D + 8 * cc), z = *reinterpret_cast<const float4*>(x + r * D + 8 * cc + 4);
+    o[0] = __builtin_fmaf(f, a.x, o[0]); o[1] = __builtin_fmaf(f, a.y, o[1]);
+    o[2] = __builtin_fmaf(f, a.z, o[2]); o[3] = __builtin_fmaf(f, a.w, o[3]);
+    o[4] = __builtin_fmaf(f, z.x, o[4]); o[5] = __builtin_fmaf(f, z.y, o[5]);
+    o[6] = __builtin_fmaf(f, z.z, o[6]); o[7] = __builtin_fmaf(f, z.w, o[7]);
+  }
+  const float inv = 1.0f / sum;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) o[u] *= inv;
+  const uint4 y = pack_bf16x8(o);
+  *reinterpret_cast<uint4*>(A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)n * A.out.sn + 8 * cc) = y;
+  if (A.lse) {
+    const int64_t row = (int64_t)bh * s.N + n;
+    *reinterpret_cast<uint4*>(A.left + row * D + 8 * cc) =
+        make_uint4(left2(o[0], o[1], y.x), left2(o[2], o[3], y.y), left2(o[4], o[5], y.z), left2(o[6], o[7], y.w));
+    if (cc == 0) A.lse[row] = (top + log2f(exact)) * kLn2;
+  }
 }
 
 // ------------------------------------------------------------------ backward
@@ -487,7 +1058,8 @@ __device__ __forceinline__ void dq_of(const CrossBwd& A, uint8_t (*lds)[2][kTile
   }
   const int2 range = split_keys(rt.row0 < qlen ? keys.len : 0, pc.piece, pc.pieces, kTileKeys);
   const int turns = tiles_of(range.y - range.x, kTileKeys);
-  KeyCopies<kMasked> copy(A.k, A.v, b, hk, keys, range.x, turns, lds_address(&lds[0][0][0]), wave, lane);
+  KeyCopies<kMasked> copy;
+  copy.begin(A.k, A.v, b, hk, keys, range.x, turns, lds_address(&lds[0][0][0]), wave, lane);
 
   struct Scores {
     f32x16 s[2], x[2];  // scores, then P; X
@@ -913,39 +1485,71 @@ __global__ __launch_bounds__(256) void cross_end_kernel(CrossBwd A) {
 
 }  // namespace
 
-constexpr int kCus = 256;  // each holds one workgroup of the tile kernels
-
 // A launch is a 1D grid of fewer than 2^32 threads.
 static bool fits(int64_t workgroups, int threads) { return workgroups < ((int64_t)1 << 32) / threads; }
+static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 CrossPlan cross_plan(const CrossShape& s, bool ragged) {
-  (void)ragged;
-  CrossPlan p = {true, {0, 1}};
-  const int64_t wgs = (int64_t)s.B * s.Hk * few_groups(s);
-  int64_t n = kCus / wgs;
-  n = std::min<int64_t>(n, s.M / 128);
-  p.tiles.pieces = (int)(n < 1 ? 1 : n);
+  CrossPlan p = {};
+  const int64_t tiles = row_tiles_of(s), turns = tiles_of(s.M, kTileKeys);
+  p.few = few_groups(s) == 1 || (int64_t)(s.H / s.Hk) * s.N <= 64;
+  if (p.few) {
+    const int64_t wgs = (int64_t)s.B * s.Hk * few_groups(s);
+    const int64_t n = std::min<int64_t>(kCus / wgs, s.M / 128);
+    p.pieces = (int)(n < 1 ? 1 : n);
+    return p;
+  }
+  p.pieces = 1;
+  p.workgroups = (int)std::min<int64_t>(kCus, tiles * turns);
+  // What whole tiles leave idle, in turns of 0.9 us, against the shares' way through memory
+  const double idle = (double)((tiles + kCus - 1) / kCus * turns) - (double)(tiles * turns) / kCus;
+  p.split = idle > 30 && !(ragged && s.B > kMaxByLength);
   return p;
 }
 
-static int64_t fwd_workgroups(const CrossShape& s, const CrossPlan& p) {
-  return ((int64_t)s.B * s.Hk * p.tiles.pieces + 7) / 8 * 8 * few_groups(s);
+static int64_t few_workgroups(const CrossShape& s, int pieces) {
+  return ((int64_t)s.B * s.Hk * pieces + 7) / 8 * 8 * few_groups(s);
+}
+// The visible keys' order and counts.
+static size_t order_bytes(const CrossShape& s) { return s.mask ? up256(((size_t)s.B * s.M + s.B) * sizeof(int32_t)) : 0; }
+static void launch_order(const CrossShape& s, int32_t* order, int32_t* counts, hipStream_t stream) {
+  hipLaunchKernelGGL(cross_order_kernel, dim3((unsigned)s.B), dim3(kOrderThreads), 0, stream, s, order, counts);
 }
 
-size_t cross_fwd_bytes(const CrossShape& s) {
-  const CrossPlan p = cross_plan(s, false);
-  if (!fits(fwd_workgroups(s, p), 256)) return kTooLarge;
-  return p.tiles.pieces > 1 ? (size_t)s.B * s.H * s.N * p.tiles.pieces * (D + 2) * sizeof(float) : 0;
+size_t cross_fwd_bytes(const CrossShape& s, CrossFwd* a, void* ws) {
+  const CrossPlan p = cross_plan(s, false);  // (the most: ragged calls never split where these do not)
+  if (a) a->ws = static_cast<float*>(ws);
+  if (p.few) {
+    if (!fits(few_workgroups(s, p.pieces), 256)) return kTooLarge;
+    return p.pieces > 1 ? (size_t)s.B * s.H * s.N * p.pieces * (D + 2) * sizeof(float) : 0;
+  }
+  if (!fits(row_tiles_of(s) * (kCrossRows / 16), 256) || !fits(s.B, kOrderThreads)) return kTooLarge;
+  const size_t order = order_bytes(s);
+  if (a) {
+    a->order = static_cast<int32_t*>(ws);
+    a->counts = a->order + (size_t)s.B * s.M;
+    a->ws = reinterpret_cast<float*>(static_cast<char*>(ws) + order);
+  }
+  return order + (p.split ? (size_t)2 * p.workgroups * kShareFloats * sizeof(float) : 0);
 }
 
 hipError_t launch_cross_fwd(const CrossFwd& a, hipStream_t stream) {
   const CrossShape& s = a.s;
-  const CrossPlan p = cross_plan(s, s.kv_lens || s.mask);
-  const dim3 grid((unsigned)fwd_workgroups(s, p));
-  const auto kernel = s.mask ? cross_few_kernel<true> : cross_few_kernel<false>;
-  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, p.tiles.pieces);
-  if (p.tiles.pieces > 1)
-    hipLaunchKernelGGL(cross_join_kernel, dim3((unsigned)((int64_t)s.B * s.H * s.N)), dim3(256), 0, stream, a, p.tiles);
+  const CrossPlan p = cross_plan(s, s.q_lens || s.kv_lens || s.mask);
+  if (p.few) {
+    const auto kernel = s.mask ? cross_few_kernel<true> : cross_few_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)few_workgroups(s, p.pieces)), dim3(256), 0, stream, a, p.pieces);
+    if (p.pieces > 1)
+      hipLaunchKernelGGL(cross_join_kernel, dim3((unsigned)((int64_t)s.B * s.H * s.N)), dim3(256), 0, stream, a, p.pieces);
+    return hipGetLastError();
+  }
+  if (s.mask) launch_order(s, a.order, a.counts, stream);
+  const auto kernel = s.mask ? (a.lse ? cross_fwd_kernel<true, true> : cross_fwd_kernel<true, false>)
+                             : (a.lse ? cross_fwd_kernel<false, true> : cross_fwd_kernel<false, false>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)p.workgroups), dim3(256), 0, stream, a, p.split);
+  if (p.split)
+    hipLaunchKernelGGL(cross_shares_kernel, dim3((unsigned)(row_tiles_of(s) * (kCrossRows / 16))), dim3(256), 0, stream, a,
+                       p.workgroups);
   return hipGetLastError();
 }
 
@@ -1006,13 +1610,6 @@ static DiffTiles bwd_tiles(const CrossShape& s, int pieces) {
   const int64_t full = std::min(tiles, (kCus - more) * (a > 0 ? a / c.row : 0) + more * (b > 0 ? b / c.row : 0));
   // what is left goes to the CUs' remaining time
   return cut_tiles(tiles, full, filling(tiles, full), s.M);
-}
-
-static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-// The visible keys' order and counts.
-static size_t order_bytes(const CrossShape& s) { return s.mask ? up256(((size_t)s.B * s.M + s.B) * sizeof(int32_t)) : 0; }
-static void launch_order(const CrossShape& s, int32_t* order, int32_t* counts, hipStream_t stream) {
-  hipLaunchKernelGGL(cross_order_kernel, dim3((unsigned)s.B), dim3(kOrderThreads), 0, stream, s, order, counts);
 }
 
 // Workgroups of the backward launches: the rows' statistics, both walks (the keys'
