@@ -312,74 +312,92 @@ struct Keys {
 };
 
 // Tiles of 32 keys and their values, one after the other from key `from` on, on their
-// way into a ring in LDS, one kilobyte at a time: copy 0, 1 the halves of K's tile, 2, 3
-// V's.  A wave brings 8 rows.  Past the last tile it comes again, and is not used; keys
-// past the sequence are its last key again (their scores are masked).
+// way into LDS, one kilobyte at a time: copy 0, 1 the halves of K's tile, 2, 3 V's.  A
+// wave brings 8 rows.  Past the last tile it comes again, and is not used; keys past the
+// sequence are its last one again (their scores are masked).  Masked keys' rows are found
+// a tile ahead, by scalar loads, which no wait for copies sees.
 constexpr int kTileKeys = 32;
 constexpr int kRing = 4;
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 template <bool kMasked>
 struct KeyCopies {
-  const uint16_t *k, *v;  // the head's; without a mask, of the tile's first key
+  const uint16_t *k, *v;  // the tile's first key (kMasked: the head's)
   int64_t ksn, vsn;
   Keys<kMasked> keys;
-  int key, row, lane, turns;
-  uint32_t at0, to, ok, ov;
-  int next;  // kMasked: this lane's row of the tile to come
+  int key, tile, turns, row, lane;
+  uint32_t at, to_k, to_v, ok, ov;
+  int next, last;  // kMasked: this lane's row of the tile to come; the last key's row
   const uint16_t *mk, *mv;
 
-  const uint16_t *k0, *v0;
-  // n tiles from key `from` on into a ring at LDS address `lds`.
+  // n tiles from key `from` on.
   __device__ __forceinline__ void begin(const Rows& kr, const Rows& vr, int b, int hk, const Keys<kMasked>& ks, int from, int n,
-                                        uint32_t lds, int wave, int l) {
+                                        int wave, int l) {
     k = kr.p + b * kr.sb + hk * kr.sh;
     v = vr.p + b * vr.sb + hk * vr.sh;
     ksn = kr.sn;
     vsn = vr.sn;
     keys = ks;
     key = from;
+    tile = 0;
     row = 8 * wave + (l >> 3);
     lane = l;
     turns = n;
-    at0 = lds + wave * kRowBlock;
+    at = wave * kRowBlock;
     if (kMasked) {
-      fetch(from);
+      if (n > 0) {
+        last = constant()[keys.len - 1];
+        fetch();
+      }
     } else {
-      k0 = k + (int64_t)from * ksn;
-      v0 = v + (int64_t)from * vsn;
+      k += (int64_t)from * ksn;
+      v += (int64_t)from * vsn;
       ok = copy_offset(row, ksn, lane);
       ov = copy_offset(row, vsn, lane);
     }
   }
-  __device__ __forceinline__ void fetch(int tile_key) {
-    if (kMasked && turns > 0) next = keys.at(min(tile_key + row, keys.len - 1));
+  __device__ __forceinline__ const __attribute__((address_space(4))) int32_t* constant() const {
+    return (const __attribute__((address_space(4))) int32_t*)(uintptr_t)keys.order;
   }
-  // Tile i (after i - 1, or the same again) into place `place` of a ring of kRing.
-  __device__ __forceinline__ void start(int i, int place) {
-    const bool on = i > 0 && i < turns;
-    key += on ? kTileKeys : 0;
-    to = __builtin_amdgcn_readfirstlane(at0 + (place % kRing) * (2 * kTile32));
+  // kMasked: rows of the tile from `key` on.  (A sequence's list is followed by 8 words or more.)
+  __device__ __forceinline__ void fetch() {
+    const auto* p = constant() + key + at / kRowBlock * 8;
+    int r = p[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) r = (lane >> 3) == j ? p[j] : r;
+    next = key + row < keys.len ? r : last;
+  }
+  // The next tile (the first, to begin with) into LDS at k_to and v_to.
+  __device__ __forceinline__ void start(uint32_t k_to, uint32_t v_to) {
+    to_k = __builtin_amdgcn_readfirstlane(k_to + at);
+    to_v = __builtin_amdgcn_readfirstlane(v_to + at);
+    const bool on = tile > 0 && tile < turns;
     if (kMasked) {
       const int chunk = 8 * ((lane & 7) ^ swizzle(lane >> 3));
       mk = k + (int64_t)next * ksn + chunk;
       mv = v + (int64_t)next * vsn + chunk;
-      fetch(i + 1 < turns ? key + kTileKeys : key);
+      if (tile + 1 < turns) {
+        key += kTileKeys;
+        fetch();
+      }
     } else {
-      k0 += on ? kTileKeys * ksn : 0;
-      v0 += on ? kTileKeys * vsn : 0;
+      key += on ? kTileKeys : 0;
+      k += on ? kTileKeys * ksn : 0;
+      v += on ? kTileKeys * vsn : 0;
       if (key + kTileKeys > keys.len) {
         const int r = min(row, keys.len - 1 - key);
         ok = copy_offset(r, ksn, lane);
         ov = copy_offset(r, vsn, lane);
       }
     }
+    ++tile;
   }
   __device__ __forceinline__ void part(int n) const {
-    const uint32_t lds = to + n / 2 * kTile32 + n % 2 * 1024;
+    const uint32_t lds = (n / 2 ? to_v : to_k) + n % 2 * 1024;
     if (kMasked) copy_1k_from(lds, (n / 2 ? mv : mk) + n % 2 * 64);
-    else copy_1k(lds, n / 2 ? v0 : k0, (n / 2 ? ov : ok) + n % 2 * 128);
+    else copy_1k(lds, n / 2 ? v : k, (n / 2 ? ov : ok) + n % 2 * 128);
   }
-  __device__ __forceinline__ void all(int i, int place) {
-    start(i, place);
+  __device__ __forceinline__ void all(uint32_t k_to, uint32_t v_to) {
+    start(k_to, v_to);
 #pragma unroll
     for (int n = 0; n < 4; ++n) part(n);
   }
@@ -585,14 +603,18 @@ __device__ __forceinline__ float* share_of(float* ws, int wg, bool began) {
 // A row is held to the maximum of its first item: P and the sums have 8 exponent bits,
 // so scores far above it cost no precision, and most rows' stay within a few binades.
 // A row whose P add up to more than 2^80 (55 above it in the exponent), or whose
-// products with the values leave fp32, has its workgroup walk the tile again, held to
-// the rows' own maxima, found by a walk for scores alone.
+// products with the values leave fp32, has its wave walk the tile again by itself,
+// raising the maxima as they come.
 constexpr float kTooMuch = 1.2089258e24f;
 template <bool kMasked, bool kTrain>
 __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool split) {
   constexpr int kFrags = 16, kAhead = 6, kHold = 8;
+  // A turn reads V of item i - 1 and K of item i + 1 and sends for item i + kLook, in four
+  // copies; items of a tile: an even number, kLook at least (past its keys the last one
+  // again, masked), so that copies reach no further than into the next tile.
+  constexpr int kLook = 4, kKPlaces = 4, kVPlaces = 8;
   struct Lds {
-    uint8_t tiles[kRing][2][kTile32];
+    uint8_t k[kKPlaces][kTile32], v[kVPlaces][kTile32];
     uint8_t rows[4][2][kTile32];  // of each wave: the next tile's q, or an output on its way
   };
   __shared__ __attribute__((aligned(1024))) Lds lds;
@@ -618,10 +640,18 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
     now_at.start(line, from, end);
   }
 
+  // This lane, where what follows from it is to be found there and not kept (in registers
+  // that the turns need) from the kernel's start on.
+  auto lane_here = [&]() __attribute__((always_inline)) {
+    int l = t & 63;
+    asm volatile("" : "+v"(l));
+    return l;
+  };
   // outputs of rows without keys: their tile has no turns
   auto no_keys = [&](const Tiles& at) __attribute__((always_inline)) {
     uint16_t* to = A.out.p + at.at.b * A.out.sb + at.at.h * A.out.sh;
     const int64_t row = ((int64_t)at.at.b * s.H + at.at.h) * s.N;
+    const int t = 64 * wave + lane_here();
     for (int i = t; i < kCrossRows * kChunks; i += 256) {
       const int n = at.row0() + i / kChunks, cc = i % kChunks;
       if (n >= at.qlen) break;
@@ -630,29 +660,64 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
       if (kTrain && cc == 0) A.lse[row + n] = -__builtin_inff();
     }
   };
-  // on to a tile that has turns; `write`: those without are written on the way
-  auto to_turns = [&](Tiles& at, bool write) __attribute__((always_inline)) {
+  // on to a tile that has turns; those without are written on the way
+  auto to_turns = [&](Tiles& at) __attribute__((always_inline)) {
     while (!at.done && at.from >= at.to) {
-      if (write && at.klen == 0) no_keys(at);
+      if (at.klen == 0) no_keys(at);
       at.next(line, end);
     }
   };
-  to_turns(now_at, true);
+  to_turns(now_at);
   if (now_at.done) return;
 
-  // the copies of now_at's tiles of keys, two ahead of the exponentials', then the next one's
+  // the items' copies: now_at's, then the next tile's
   KeyCopies<kMasked> copy;
   auto copy_tile = [&](const Tiles& at) __attribute__((always_inline)) {
     copy.begin(A.k, A.v, at.at.b, at.at.h / per, Keys<kMasked>(s, A.order, at.at.b, at.klen), at.from * kTileKeys,
-               at.to - at.from, lds_address(&lds.tiles[0][0][0]), wave, lane);
+               at.to - at.from, wave, lane);
   };
-  // rows of a tile's q, the wave's 64, into its place; rows behind the sequence are its last one again
+  int item = 0;  // of all, at the tile's start
+  auto k_place = [&](int i) __attribute__((always_inline)) { return &lds.k[(item + i) % kKPlaces][0]; };
+  auto v_place = [&](int i) __attribute__((always_inline)) { return &lds.v[(item + i) % kVPlaces][0]; };
+
+  // The wave's 64 rows in LDS, 16 KB, at a tile's end: first its outputs on their way to
+  // memory, then the q of the tile after the next on its way from there.  Both are
+  // exactly 16 operations of the wave (outputs of training twice 16 and two log sums):
+  // rows behind the sequence are its last one again, of q and so of the outputs, which are
+  // stored over it, the same bits.  So a turn knows what was sent for after the copies that
+  // it needs, and waits for nothing else: memory has three turns for the rows.
+  constexpr int kRowOps = kTrain ? 50 : 32;
   uint8_t* mine = &lds.rows[wave][0][0];
+  // Row r's 16-byte chunk c of an output lies at place c ^ (r % 16), its halves exchanged
+  // for odd r / 16: written 8 bytes a lane, a row a lane, and read a row a 16 lanes, without
+  // bank conflicts.
+  auto stage = [&](int m, auto&& words) __attribute__((always_inline)) {
+    const int lane = lane_here(), hh = lane >> 5, l32 = lane & 31;
+    uint8_t* row = mine + (32 * m + l32) * 2 * D + 8 * (hh ^ (l32 >> 4));
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) *reinterpret_cast<uint2*>(row + 16 * ((4 * d + q) ^ (l32 & 15))) = words(d, q);
+  };
+  auto store_staged = [&](uint16_t* to, int64_t sn, int last) __attribute__((always_inline)) {
+    const int lane = lane_here();
+    asm volatile("" ::: "memory");  // the wave's LDS operations stay in order
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      const int r = 4 * u + (lane >> 4);
+      const uint4 y = *reinterpret_cast<const uint4*>(mine + r * 2 * D + 16 * ((lane & 15) ^ (r & 15)));
+      *reinterpret_cast<uint4*>(to + (int64_t)min(64 * wave + r, last) * sn + 8 * (lane & 15)) =
+          4 * u & 16 ? make_uint4(y.z, y.w, y.x, y.y) : y;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
   auto copy_rows = [&](const Tiles& at) __attribute__((always_inline)) {
-    const uint16_t* q = A.q.p + at.at.b * A.q.sb + at.at.h * A.q.sh + 8 * ((lane & 7) ^ swizzle(lane >> 3));
+    const int lane = lane_here();
+    const uint16_t* q = A.q.p + at.at.b * A.q.sb + at.at.h * A.q.sh + (int64_t)at.row0() * A.q.sn + 8 * ((lane & 7) ^ swizzle(lane >> 3));
+    const int last = at.qlen - 1 - at.row0();
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const uint16_t* p = q + (int64_t)min(at.row0() + 64 * wave + 8 * u + (lane >> 3), at.qlen - 1) * A.q.sn;
+      const uint16_t* p = q + (int64_t)min(64 * wave + 8 * u + (lane >> 3), last) * A.q.sn;
       const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(mine) + u * kRowBlock);
       copy_1k_from(to, p);
       copy_1k_from(to + 1024, p + 64);
@@ -662,7 +727,8 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
   const RowPlace rp = row_place(lane);
   const int cp = col_place(lane);
   auto load_rows = [&]() __attribute__((always_inline)) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the wave's own copies
+    // the wave's own copies: three turns' at least were sent for after them
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * (kLook - 1)) : "memory");
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -679,15 +745,10 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
   MapRows x[2];
   float mc[2];  // the maxima held to, times c
   bf16x8 ring[kHold];
-  int item = 0;  // of all, at the tile's start
-  int n_turns = 0, n_keys = 0, key0 = 0, n_next = 0;
-  bool begun = false;  // the next tile's copies
+  int n_turns = 0, n_items = 0, n_keys = 0, key0 = 0;  // items with keys, and all of the tile
   // the fragments of a turn in order: V of item i - 1, then K of item i + 1
-  auto fragment = [&](int f, const uint8_t* then, const uint8_t* next) __attribute__((always_inline)) {
-    return f < 8 ? col_frag(then + kTile32 + cp, f >> 2, f & 3) : row_frag(next, rp, f - 8);
-  };
-  auto place_of = [&](int i) __attribute__((always_inline)) {
-    return &lds.tiles[(item + min(i, n_turns - 1)) % kRing][0][0];
+  auto fragment = [&](int f, const uint8_t* v, const uint8_t* k) __attribute__((always_inline)) {
+    return f < 8 ? col_frag(v + cp, f >> 2, f & 3) : row_frag(k, rp, f - 8);
   };
   auto mask_item = [&](Item& now, int i) __attribute__((always_inline)) {
     const int key = key0 + i * kTileKeys;
@@ -720,47 +781,12 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
   auto operand = [&](const Item& z, int m, int y) __attribute__((always_inline)) {
     return __builtin_bit_cast(bf16x8, make_uint4(z.pw[m][4 * y], z.pw[m][4 * y + 1], z.pw[m][4 * y + 2], z.pw[m][4 * y + 3]));
   };
-  // scores of item i, which is in the ring's place `place`, all at once
-  auto scores_of = [&](Item& z, int i, int place) __attribute__((always_inline)) {
-    const uint8_t* tk = &lds.tiles[place % kRing][0][0];
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      const bf16x8 f = row_frag(tk, rp, kk);
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        if (kk == 0) score_first_a(z.s[m], f, qf[m][kk]);
-        else score_a(z.s[m], f, qf[m][kk]);
-      }
-    }
-    settle(z.s[0], z.s[1]);
-    mask_item(z, i);
-  };
-  auto raise = [&](const Item& z) __attribute__((always_inline)) {
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      float top = z.s[m][0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) top = fmaxf(top, z.s[m][r]);
-      x[m].m = fmaxf(x[m].m, both_max(top));
-    }
-  };
-  // Large values under P that pass 1 may leave fp32 with sums that stay below 2^80:
-  // looked for in waves where a row's P add up to more than its keys could at 1.
-  auto not_finite = [&]() __attribute__((always_inline)) {
-    if (!__any(x[0].l > (float)SOL_MAX_TOKENS || x[1].l > (float)SOL_MAX_TOKENS)) return false;
-    uint32_t top = 0;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        top = max(top, max(__float_as_uint(x[0].o[d][r]) & 0x7fffffffu, __float_as_uint(x[1].o[d][r]) & 0x7fffffffu));
-    return top >= 0x7f800000u;
-  };
-  // item i of the tile; old: item i - 1's P, and room for item i + 1's scores
+  // Item i of the tile; old: item i - 1's P, and room for the next item's scores (after the
+  // last one the next tile's first).
   auto turn = [&](int i, Item& now, Item& old) __attribute__((always_inline)) {
-    const uint8_t* to = place_of(max(i - 1, 0));
-    const uint8_t* tn = place_of(i);
-    const uint8_t* next = place_of(i + 1);
+    const uint8_t* then = v_place(max(i - 1, 0));  // (turn 0's products are of P = 0)
+    const uint8_t* here = v_place(i);
+    const uint8_t* next = k_place(i + 1);
     mask_item(now, i);
 #pragma unroll
     for (int d = 0; d < 4; ++d) asm volatile("" : "+a"(x[0].o[d]), "+a"(x[1].o[d]));
@@ -769,15 +795,12 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
     each<0, 32>([&](auto slot) __attribute__((always_inline)) {
       constexpr int j = slot.value, f = j / 2, m = j & 1;
       if constexpr (j == 2) {
-        copies_landed<0>();
-        if (i < n_turns) {  // (past them, and past a tile without a next, it comes again)
-          if (i + 2 >= n_turns && !begun && !next_at.done) {
-            copy_tile(next_at);
-            begun = true;
-          }
-          copy.start(begun ? n_next : i + 2, item + (begun ? n_turns + n_next : i + 2));
-          n_next += begun;
-        }
+        // the next item, sent for three turns ago: after it two turns' copies, and in a
+        // tile's first three turns the rows'
+        if (i < kLook - 1) copies_landed<4 * (kLook - 2) + kRowOps>();
+        else copies_landed<4 * (kLook - 2)>();
+        if (i + kLook == n_items && !next_at.done) copy_tile(next_at);  // (past the last tile its last item again)
+        copy.start(lds_address(k_place(i + kLook)), lds_address(v_place(i + kLook)));
         slot_end();
       }
       if constexpr (j >= 3 && j < 7) copy.part(j - 3);
@@ -791,7 +814,7 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
       }
       if constexpr (m == 0) {
         constexpr int g = f + kAhead;
-        ring[g % kHold] = g < kFrags ? fragment(g, to, next) : fragment(g - kFrags, tn, nullptr);
+        ring[g % kHold] = g < kFrags ? fragment(g, then, next) : fragment(g - kFrags, here, nullptr);
       }
       if constexpr (j >= 2 && j < 16) {
 #pragma unroll
@@ -803,121 +826,190 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
     take(now, 1, 14);
   };
   auto last_products = [&](const Item& old) __attribute__((always_inline)) {
-    const uint8_t* to = place_of(n_turns - 1);
+    const uint8_t* then = v_place(n_items - 1);
 #pragma unroll
     for (int f = 0; f < 8; ++f) {
-      const bf16x8 v = f < kAhead ? ring[f % kHold] : fragment(f, to, nullptr);
+      const bf16x8 v = f < kAhead ? ring[f % kHold] : fragment(f, then, nullptr);
 #pragma unroll
       for (int m = 0; m < 2; ++m) x[m].o[f & 3] = mfma(v, operand(old, m, f >> 2), x[m].o[f & 3]);
     }
   };
-  // a tile's outputs, through the wave's rows in LDS
-  auto finish = [&](const Tiles& at) __attribute__((always_inline)) {
-    const bool whole = at.whole();
+  // Large values under P that pass 1 may leave fp32 with sums that stay below 2^80:
+  // looked for in waves where a row's P add up to more than its keys could at 1.
+  auto not_finite = [&]() __attribute__((always_inline)) {
+    if (!__any(x[0].l > (float)SOL_MAX_TOKENS || x[1].l > (float)SOL_MAX_TOKENS)) return false;
+    uint32_t top = 0;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        top = max(top, max(__float_as_uint(x[0].o[d][r]) & 0x7fffffffu, __float_as_uint(x[1].o[d][r]) & 0x7fffffffu));
+    return __any(top >= 0x7f800000u) != 0;
+  };
+  // o of 32 rows divided by their sums; of those, for the workspace or for training, the
+  // log2 of the sums
+  auto divide = [&](MapRows& y) __attribute__((always_inline)) {
+    const float inv = 1.0f / both_sum(y.l);  // (a row behind the sequence is its last one again)
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) y.o[d][r] *= inv;
+  };
+  // a share of a tile, 32 rows from its row `first` on, to the workspace
+  auto store_share = [&](const Tiles& at, int first, const MapRows& y, float held) __attribute__((always_inline)) {
+    const int lane = lane_here(), hh = lane >> 5, l32 = lane & 31;
     float* share = share_of(A.ws, wg, at.from == 0);
+    float* to = share + (first + l32) * D + 4 * hh;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const float l = both_sum(x[m].l), exact = kTrain ? both_sum(x[m].exact) : 0.0f;
-      const float inv = 1.0f / l;  // (a row behind the sequence is its last one again)
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(to + 32 * d + 8 * q) =
+            make_float4(y.o[d][4 * q], y.o[d][4 * q + 1], y.o[d][4 * q + 2], y.o[d][4 * q + 3]);
+    const float l2 = held + log2f(both_sum(y.l)), exact2 = kTrain ? held + log2f(both_sum(y.exact)) : 0.0f;
+    if (hh == 0) share[kCrossRows * D + first + l32] = l2;
+    if (kTrain && hh == 0) share[kCrossRows * (D + 1) + first + l32] = exact2;
+  };
+  // A tile's outputs.  (All is there when the turns that count the rows' operations come:
+  // those of a share are not counted, and waited for.)
+  auto finish = [&](const Tiles& at) __attribute__((always_inline)) {
+    divide(x[0]);
+    divide(x[1]);
+    if (!at.whole()) {
+      store_share(at, 64 * wave, x[0], mc[0]);
+      store_share(at, 64 * wave + 32, x[1], mc[1]);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      return;
+    }
+    const int last = at.qlen - 1 - at.row0();
+    if (kTrain) {
+      const int64_t row = ((int64_t)at.at.b * s.H + at.at.h) * s.N + at.row0();
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[m].o[d][r] *= inv;
-      const int first = 64 * wave + 32 * m, n = at.row0() + first + l32;
-      if (!whole) {
-        float* to = share + (first + l32) * D + 4 * hh;
+      for (int m = 0; m < 2; ++m) {
+        const float lse = (mc[m] + log2f(both_sum(x[m].exact))) * kLn2;
+        if (hh == 0) A.lse[row + min(64 * wave + 32 * m + l32, last)] = lse;
+        stage(m, [&](int d, int q) { return left4(x[m].o[d], q, pack4(x[m].o[d], q)); });
+      }
+      store_staged(A.left + row * D, D, last);
+    }
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<float4*>(to + 32 * d + 8 * q) =
-                make_float4(x[m].o[d][4 * q], x[m].o[d][4 * q + 1], x[m].o[d][4 * q + 2], x[m].o[d][4 * q + 3]);
-        if (hh == 0) {
-          share[kCrossRows * D + first + l32] = mc[m] + log2f(l);
-          if (kTrain) share[kCrossRows * (D + 1) + first + l32] = mc[m] + log2f(exact);
+    for (int m = 0; m < 2; ++m) stage(m, [&](int d, int q) { return pack4(x[m].o[d], q); });
+    store_staged(A.out.p + at.at.b * A.out.sb + at.at.h * A.out.sh + (int64_t)at.row0() * A.out.sn, A.out.sn, last);
+  };
+  // The wave's rows of a tile again, the running maxima raised as they come: the wave by
+  // itself, its rows' place for the tiles of keys, and the outputs straight to memory.
+  auto again = [&](const Tiles& at) __attribute__((always_inline)) {
+    const int lane = lane_here(), hh = lane >> 5, l32 = lane & 31;
+    const RowPlace rp = row_place(lane);
+    const int cp = col_place(lane);
+    const Keys<kMasked> keys(s, A.order, at.at.b, at.klen);
+    const int chunk = 8 * ((lane & 7) ^ swizzle(lane >> 3));
+    const uint16_t* k = A.k.p + at.at.b * A.k.sb + at.at.h / per * A.k.sh + chunk;
+    const uint16_t* v = A.v.p + at.at.b * A.v.sb + at.at.h / per * A.v.sh + chunk;
+#pragma unroll 1
+    for (int first = 64 * wave; first < 64 * wave + 64; first += 32) {
+      bf16x8 rows[8];
+      MapRows y;
+      clear(y);
+      load_row(rows, A.q.p + at.at.b * A.q.sb + at.at.h * A.q.sh + (int64_t)min(at.row0() + first + l32, at.qlen - 1) * A.q.sn,
+               true, hh);
+#pragma unroll 1
+      for (int key = at.from * kTileKeys; key < min(at.to * kTileKeys, at.klen); key += kTileKeys) {
+#pragma unroll 1
+        for (int u = 0; u < 4; ++u) {
+          const int64_t r = keys.at(min(key + 8 * u + (lane >> 3), at.klen - 1));
+          const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(mine) + u * kRowBlock);
+          copy_1k_from(to, k + r * A.k.sn);
+          copy_1k_from(to + 1024, k + r * A.k.sn + 64);
+          copy_1k_from(to + kTile32, v + r * A.v.sn);
+          copy_1k_from(to + kTile32 + 1024, v + r * A.v.sn + 64);
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        f32x16 sc[1] = {};
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) sc[0] = mfma(row_frag(mine, rp, kk), rows[kk], sc[0]);
+        mask(sc[0], key + 4 * hh, at.klen - 1);
+        raise_max(y, sc, c);
+        exponentials(y, sc[0], c);
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const bf16x8 p = operand8(sc[0], z);
+          y.l = add_bf16x8(p, y.l);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) y.o[d] = mfma(col_frag(mine + kTile32 + cp, z, d), p, y.o[d]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the place's reads, before the next copies
+      }
+      divide(y);
+      if (!at.whole()) {
+        store_share(at, first, y, y.m * c);
         continue;
       }
-      const int64_t row = ((int64_t)at.at.b * s.H + at.at.h) * s.N + at.row0() + first;
-      const int rows = at.qlen - at.row0() - first;
-      store_rows(mine, lane, A.out.p + at.at.b * A.out.sb + at.at.h * A.out.sh + (int64_t)(at.row0() + first) * A.out.sn,
-                 A.out.sn, 0, rows, [&](int d, int q) { return pack4(x[m].o[d], q); });
+      const int n = at.row0() + first, rows_left = at.qlen - n;
+      const int64_t row = ((int64_t)at.at.b * s.H + at.at.h) * s.N + n;
       if (kTrain) {
-        store_rows(mine, lane, A.left + row * D, D, 0, rows,
-                   [&](int d, int q) { return left4(x[m].o[d], q, pack4(x[m].o[d], q)); });
-        if (hh == 0 && n < at.qlen) A.lse[row + l32] = (mc[m] + log2f(exact)) * kLn2;
+        const float lse = (y.m * c + log2f(both_sum(y.exact))) * kLn2;
+        if (hh == 0 && l32 < rows_left) A.lse[row + l32] = lse;
+        store_rows(mine, lane, A.left + row * D, D, 0, rows_left, [&](int d, int q) { return left4(y.o[d], q, pack4(y.o[d], q)); });
       }
+      store_rows(mine, lane, A.out.p + at.at.b * A.out.sb + at.at.h * A.out.sh + (int64_t)n * A.out.sn, A.out.sn, 0, rows_left,
+                 [&](int d, int q) { return pack4(y.o[d], q); });
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // (not counted)
   };
 
   copy_rows(now_at);
+  copy_tile(now_at);
+#pragma unroll
+  for (int u = 0; u < kLook; ++u) copy.all(lds_address(k_place(u)), lds_address(v_place(u)));
   next_at = now_at;
   next_at.next(line, end);
-  to_turns(next_at, true);
+  to_turns(next_at);
+  copies_landed<0>();
   load_rows();
-  if (!next_at.done) copy_rows(next_at);
-  for (bool landed = false;; landed = true) {
+  all_landed();
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) {
+    const bf16x8 f = row_frag(k_place(0), rp, kk);
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      if (kk == 0) score_first_a(ia.s[m], f, qf[m][kk]);
+      else score_a(ia.s[m], f, qf[m][kk]);
+    }
+  }
+  for (;;) {
+    copy_rows(next_at.done ? now_at : next_at);  // (of no use where there is none, but of the same number)
     n_turns = now_at.to - now_at.from;
+    n_items = max(n_turns + (n_turns & 1), kLook);
     n_keys = now_at.klen;
     key0 = now_at.from * kTileKeys;
-    x[0].m = x[1].m = kNoMax;
-    for (int attempt = 0;; ++attempt) {
-      // the tile's first two items, but what the tile before has brought already
-      if (!begun) {
-        copy_tile(now_at);
-        copy.all(0, item);
-        n_next = 1;
-        landed = false;
-      }
-      if (!landed) {
-        copies_landed<0>();
-        all_landed();
-      }
-      if (n_next < 2) copy.all(1, item + 1);
-      begun = false;
-      n_next = 0;
-      scores_of(ia, 0, item);
-      if (attempt == 0) raise(ia);
+    settle(ia.s[0], ia.s[1]);
+    mask_item(ia, 0);
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const float held = x[m].m;
-        clear(x[m]);
-        x[m].m = held;
-        mc[m] = held * c;
+    for (int m = 0; m < 2; ++m) {
+      float top = ia.s[m][0];
 #pragma unroll
-        for (int w = 0; w < 8; ++w) ib.pw[m][w] = 0;
-      }
-      // (turn 0's products are of P = 0 and the tile itself)
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, ia.s[m][r]);
+      clear(x[m]);
+      mc[m] = both_max(top) * c;
 #pragma unroll
-      for (int f = 0; f < kAhead; ++f) ring[f] = fragment(f, place_of(0), nullptr);
-      for (int i = 0; i < n_turns; i += 2) {  // (an odd tile's last turn is of no key)
-        turn(i, ia, ib);
-        turn(i + 1, ib, ia);
-      }
-      last_products(ib);
-      if (attempt || !__syncthreads_or(!(x[0].l < kTooMuch && x[1].l < kTooMuch) || not_finite())) break;
-      // the rows' own maxima, by a walk for scores alone; then the tile again
-      copies_landed<0>();
-      copy_tile(now_at);
-      for (int i = 0; i < n_turns; ++i) {
-        __syncthreads();
-        copy.all(i, 0);
-        copies_landed<0>();
-        scores_of(ia, i, 0);
-        raise(ia);
-      }
-      __syncthreads();
-      begun = false;
+      for (int w = 0; w < 8; ++w) ib.pw[m][w] = 0;
     }
-    item += n_turns;
-    const Tiles past = now_at;
+#pragma unroll
+    for (int f = 0; f < kAhead; ++f) ring[f] = fragment(f, v_place(0), nullptr);
+    for (int i = 0; i < n_items; i += 2) {
+      turn(i, ia, ib);
+      if (i + 2 == n_items) load_rows();  // the next tile's, whose first scores the last turn finds
+      turn(i + 1, ib, ia);
+    }
+    last_products(ib);
+    if (__any(!(x[0].l < kTooMuch && x[1].l < kTooMuch)) != 0 || not_finite()) again(now_at);
+    else finish(now_at);
+    item += n_items;
     now_at = next_at;
-    if (!now_at.done) load_rows();  // (its place is free for the outputs then)
-    finish(past);
     if (now_at.done) break;
     next_at.next(line, end);
-    to_turns(next_at, true);
-    if (!next_at.done) copy_rows(next_at);
+    to_turns(next_at);
   }
   copies_landed<0>();  // none is under way when the wave ends
 }
@@ -1059,7 +1151,8 @@ __device__ __forceinline__ void dq_of(const CrossBwd& A, uint8_t (*lds)[2][kTile
   const int2 range = split_keys(rt.row0 < qlen ? keys.len : 0, pc.piece, pc.pieces, kTileKeys);
   const int turns = tiles_of(range.y - range.x, kTileKeys);
   KeyCopies<kMasked> copy;
-  copy.begin(A.k, A.v, b, hk, keys, range.x, turns, lds_address(&lds[0][0][0]), wave, lane);
+  copy.begin(A.k, A.v, b, hk, keys, range.x, turns, wave, lane);
+  auto place = [&](int i) __attribute__((always_inline)) { return lds_address(&lds[i % kRing][0][0]); };
 
   struct Scores {
     f32x16 s[2], x[2];  // scores, then P; X
@@ -1097,7 +1190,7 @@ __device__ __forceinline__ void dq_of(const CrossBwd& A, uint8_t (*lds)[2][kTile
       constexpr int j = slot.value, f = j / 2, m = j & 1;
       if constexpr (j == kSlots - 14) {
         copies_landed<0>();
-        copy.start(i + 2, i + 2);
+        copy.start(place(i + 2), place(i + 2) + kTile32);
         slot_end();
       }
       if constexpr (j >= kSlots - 13 && j < kSlots - 9) copy.part(j - (kSlots - 13));
@@ -1137,8 +1230,13 @@ __device__ __forceinline__ void dq_of(const CrossBwd& A, uint8_t (*lds)[2][kTile
     }
   };
   if (turns > 0) {
-    copy.all(0, 0);
-    copy.all(0, kRing - 1);  // turn 0's products, of dS = 0
+    copy.all(place(0), place(0) + kTile32);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {  // turn 0's products, of dS = 0, take the same
+      copy.to_k += n ? 0 : place(kRing - 1) - place(0);
+      copy.to_v += n ? 0 : place(kRing - 1) - place(0);
+      copy.part(n);
+    }
     copies_landed<0>();
     hold_operands();
 #pragma unroll
@@ -1147,7 +1245,7 @@ __device__ __forceinline__ void dq_of(const CrossBwd& A, uint8_t (*lds)[2][kTile
       pin(del[m]);
     }
     all_landed();
-    copy.all(1, 1);
+    copy.all(place(1), place(1) + kTile32);
     sb = Scores{};
 #pragma unroll
     for (int f = 0; f < kAhead; ++f) ring[f] = fragment(f, &lds[0][0][0], nullptr);
