@@ -53,13 +53,14 @@ __host__ __device__ inline int64_t few_groups(const CrossShape& s) {
 }
 
 // Rows in groups of 32 of all heads that share a key head -- row r is token r % N of
-// head hk per + r / N --, a workgroup each: each wave walks every fourth block of 32
-// keys on its own, through LDS of its own (no barriers), the next block's bytes in
-// flight in its registers; the four waves' rows are joined at the end.  A key that is
+// head hk per + r / N --, a workgroup each: each of its eight waves walks every eighth
+// block of 32 keys on its own, through LDS of its own (no barriers), the next block's
+// bytes in flight in its registers; the waves' rows are joined at the end.  A key that is
 // masked is not read.
+constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves;
 template <bool kMasked>
-__global__ __launch_bounds__(256, 2) void cross_few_kernel(CrossFwd A, int nsplit) {
-  constexpr int kBlock = 32, kWaves = 4;
+__global__ __launch_bounds__(kFewThreads) void cross_few_kernel(CrossFwd A, int nsplit) {
+  constexpr int kBlock = 32, kWaves = kFewWaves;
   constexpr int kTileElems = kBlock * kStride;
   constexpr int kRow = D + 4;
   struct Joined {
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(256, 2) void cross_few_kernel(CrossFwd A, int nspli
   const uint16_t* v = A.v.p + b * A.v.sb + hk * A.v.sh;
   const uint8_t* mk = kMasked ? s.mask + (int64_t)b * s.M : nullptr;
   bf16x8 qf[8];
-  if (!__any(valid)) return;  // (the same in all four waves)
+  if (!__any(valid)) return;  // (the same in all waves)
   load_row(qf, A.q.p + b * A.q.sb + h * A.q.sh + (int64_t)row * A.q.sn, valid, hh);
 
   const int2 range = split_keys(klen, split, nsplit, kBlock * kWaves);
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(256, 2) void cross_few_kernel(CrossFwd A, int nspli
   __syncthreads();
   const Parts p = parts_of(A.ws, (int64_t)s.B * s.H * s.N, nsplit);
   // one pair of dims of one row a thread and turn
-  for (int i = t; i < n_rows * (D / 2); i += 256) {
+  for (int i = t; i < n_rows * (D / 2); i += kFewThreads) {
     const int r = i / (D / 2), d = 2 * (i % (D / 2));
     const int hr = hk * per + (int)((row_base + r) / s.N), n = (int)((row_base + r) % s.N);
     if (n >= qlen) continue;
@@ -1590,10 +1591,20 @@ static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 CrossPlan cross_plan(const CrossShape& s, bool ragged) {
   CrossPlan p = {};
   const int64_t tiles = row_tiles_of(s), turns = tiles_of(s.M, kTileKeys);
-  p.few = few_groups(s) == 1 || (int64_t)(s.H / s.Hk) * s.N <= 64;
+  // Groups of 32 rows where they all stand on the chip at once, or hold all of a key
+  // head's rows: 24 heads over 512 keys, 256 rows (192 groups) 13.0 us, in tiles 22.8; 384
+  // rows (288) 23.9, 22.9; over 4,096 keys 41, 48 and 77, 53; 16 x 16 heads over 512, 32
+  // rows (256) 17.8, 25.9, 64 rows (512) 26.4, 26.1.
+  p.few = few_groups(s) == 1 || (int64_t)s.B * s.Hk * few_groups(s) <= kCus;
   if (p.few) {
+    // As many pieces as give every CU a workgroup, of 512 keys or more (one row of 24
+    // heads over 512 keys 9.4 us in one piece, 13.2 in two, with the join; 4 x 8 heads
+    // over 2,048 21.0, 16.7, 13.7 in four; 40 over 30,000 285, 110 in six).  Where lengths
+    // differ two for every CU, of 1,024 or more: 32 caches of 256 to 8,192 keys, 8 heads,
+    // 119 us in one piece, 103 in two, 113 in four; equal ones 183, 183, 187.
     const int64_t wgs = (int64_t)s.B * s.Hk * few_groups(s);
-    const int64_t n = std::min<int64_t>(kCus / wgs, s.M / 128);
+    int64_t n = std::min<int64_t>(kCus / wgs, s.M / 512);
+    if (ragged && s.B > 1) n = std::max(n, std::min<int64_t>(2 * kCus / wgs, s.M / 1024));
     p.pieces = (int)(n < 1 ? 1 : n);
     return p;
   }
@@ -1615,11 +1626,13 @@ static void launch_order(const CrossShape& s, int32_t* order, int32_t* counts, h
 }
 
 size_t cross_fwd_bytes(const CrossShape& s, CrossFwd* a, void* ws) {
-  const CrossPlan p = cross_plan(s, false);  // (the most: ragged calls never split where these do not)
   if (a) a->ws = static_cast<float*>(ws);
+  // (the most, with lengths or without: few rows' pieces with them, tiles' shares without)
+  const CrossPlan p = cross_plan(s, false);
   if (p.few) {
-    if (!fits(few_workgroups(s, p.pieces), 256)) return kTooLarge;
-    return p.pieces > 1 ? (size_t)s.B * s.H * s.N * p.pieces * (D + 2) * sizeof(float) : 0;
+    const int pieces = std::max(p.pieces, cross_plan(s, true).pieces);
+    if (!fits(few_workgroups(s, pieces), kFewThreads)) return kTooLarge;
+    return pieces > 1 ? (size_t)s.B * s.H * s.N * pieces * (D + 2) * sizeof(float) : 0;
   }
   if (!fits(row_tiles_of(s) * (kCrossRows / 16), 256) || !fits(s.B, kOrderThreads)) return kTooLarge;
   const size_t order = order_bytes(s);
@@ -1636,7 +1649,7 @@ hipError_t launch_cross_fwd(const CrossFwd& a, hipStream_t stream) {
   const CrossPlan p = cross_plan(s, s.q_lens || s.kv_lens || s.mask);
   if (p.few) {
     const auto kernel = s.mask ? cross_few_kernel<true> : cross_few_kernel<false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)few_workgroups(s, p.pieces)), dim3(256), 0, stream, a, p.pieces);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)few_workgroups(s, p.pieces)), dim3(kFewThreads), 0, stream, a, p.pieces);
     if (p.pieces > 1)
       hipLaunchKernelGGL(cross_join_kernel, dim3((unsigned)((int64_t)s.B * s.H * s.N)), dim3(256), 0, stream, a, p.pieces);
     return hipGetLastError();

@@ -1041,12 +1041,17 @@ def diff_attn_bwd(dout, q, k, v, lam, out, out2, lse, scale=None, causal=False, 
 
 # ---------------------------------------------- norm and rotation, cross attention
 
+_GAMMA_SHAPE = torch.Size([HEAD_DIM])
+
+
 def _positions(pos, dev, B, N):
     """(pointer, elements between batches) of positions [B, N, 3], or [N, 3] for all; None: none."""
     if pos is None:
         return None, 0
     if not isinstance(pos, torch.Tensor) or pos.dtype is not torch.int32 or pos.device != dev:
         raise ValueError("pos must be an int32 tensor on %s" % dev)
+    if pos.dim() == 3 and pos.shape == (B, N, 3) and pos.is_contiguous():
+        return pos.data_ptr(), 3 * N
     if pos.shape == (N, 3) and pos.is_contiguous():
         return pos.data_ptr(), 0
     if pos.shape != (B, N, 3) or not pos[0].is_contiguous():
@@ -1054,25 +1059,38 @@ def _positions(pos, dev, B, N):
     return pos.data_ptr(), pos.stride(0) if B > 1 else 0
 
 
+def _weights_ptr(gamma, dev):
+    """As _gamma_ptr, a good one in one expression."""
+    if gamma is None:
+        return None
+    if (isinstance(gamma, torch.Tensor) and gamma.dtype is torch.float32 and gamma.shape == _GAMMA_SHAPE
+            and gamma.is_contiguous() and gamma.device == dev):
+        return gamma.data_ptr()
+    return _gamma_ptr(gamma, dev)
+
+
 def _norm_rope_args(pos, T, Hl, Wl, table, q_gamma, k_gamma, eps, lens, split, dev, B, N, D):
     """The arguments that both directions share: weights, then the rest."""
     at, step = _positions(pos, dev, B, N)
-    return ((_gamma_ptr(q_gamma, dev), _gamma_ptr(k_gamma, dev)),
-            (float(eps), at, step, _extents_table_ptr(table, dev, D, T, Hl, Wl, split), T, Hl, Wl, *_split(split),
-             _device_array("lens", lens, dev, torch.int32, (B,))))
-
-
-def _extents_table_ptr(table, dev, D, T, Hl, Wl, split):
-    """As _table_ptr, of a table whose extents bound coordinates: any of them may be 0
-    (rope3d_table gives 4 floats where none is needed)."""
+    split = DEFAULT_SPLIT if split is None else _split(split)
     if table is None:
-        return None
-    need = _table_floats(D, T, Hl, Wl, _split(split))
-    if (not isinstance(table, torch.Tensor) or table.dtype is not torch.float32 or table.device != dev
-            or not table.is_contiguous() or table.numel() != max(need, 4)):
-        raise ValueError("rope table must be a contiguous float32 tensor on %s, of %d floats for extents %dx%dx%d and split %s"
-                         % (dev, max(need, 4), T, Hl, Wl, _split(split)))
-    return table.data_ptr()
+        tab = None
+    else:
+        # the extents bound coordinates, any of them may be 0 (rope3d_table gives 4 floats where none is needed)
+        need = max(_table_floats(D, T, Hl, Wl, split), 4)
+        if (not isinstance(table, torch.Tensor) or table.dtype is not torch.float32 or table.device != dev
+                or not table.is_contiguous() or table.numel() != need):
+            raise ValueError("rope table must be a contiguous float32 tensor on %s, of %d floats for extents %dx%dx%d and split %s"
+                             % (dev, need, T, Hl, Wl, split))
+        tab = table.data_ptr()
+    return ((_weights_ptr(q_gamma, dev), _weights_ptr(k_gamma, dev)),
+            (eps, at, step, tab, T, Hl, Wl, *split,
+             None if lens is None else _device_array("lens", lens, dev, torch.int32, (B,))))
+
+
+def _empty_rows(like, shape, dev):
+    """A contiguous bf16 tensor (torch.empty_like is the quicker of the two)."""
+    return torch.empty_like(like) if like.is_contiguous() else torch.empty(shape, dtype=torch.bfloat16, device=dev)
 
 
 def qk_norm_rope(q, k, pos, T, Hl, Wl, table, q_gamma=None, k_gamma=None, eps=1e-6, lens=None, q_out=None,
@@ -1092,7 +1110,7 @@ def qk_norm_rope(q, k, pos, T, Hl, Wl, table, q_gamma=None, k_gamma=None, eps=1e
     qp, qs = _rows("q", q)
     Hk, kp, ks, op, os_ = 0, None, None, None, None
     if q_out is None:
-        q_out = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+        q_out = _empty_rows(q, (B, H, N, D), dev)
     yp, ys = _rows("q_out", q_out, dev, (B, H, N, D))
     if k is None:
         if k_out is not None:
@@ -1101,7 +1119,7 @@ def qk_norm_rope(q, k, pos, T, Hl, Wl, table, q_gamma=None, k_gamma=None, eps=1e
         Hk = _dims("k", k, 4)[1]
         kp, ks = _rows("k", k, dev, (B, Hk, N, D))
         if k_out is None:
-            k_out = torch.empty((B, Hk, N, D), dtype=torch.bfloat16, device=dev)
+            k_out = _empty_rows(k, (B, Hk, N, D), dev)
         op, os_ = _rows("k_out", k_out, dev, (B, Hk, N, D))
     gammas, rest = _norm_rope_args(pos, T, Hl, Wl, table, q_gamma, k_gamma, eps, lens, split, dev, B, N, D)
     _call(sol_qk_norm_rope, dev, qp, qs, kp, ks, yp, ys, op, os_, *gammas, *rest, B, H, Hk, N, D)
@@ -1120,7 +1138,7 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, pos, T, Hl, Wl, table, q_gamma=None, 
     shape = (B, H, N, D)
     qp, qs = _rows("q", q, dev, shape) if q_gamma is not None else (None, None)
     if dq is None:
-        dq = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        dq = _empty_rows(dq_out, shape, dev)
     xp, xs = _rows("dq", dq, dev, shape)
     Hk, hp, hs, kp, ks, yp, ys = 0, None, None, None, None, None, None
     if dk_out is None:
@@ -1132,7 +1150,7 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, pos, T, Hl, Wl, table, q_gamma=None, 
         hp, hs = _rows("dk_out", dk_out, dev, shape)
         kp, ks = _rows("k", k, dev, shape) if k_gamma is not None else (None, None)
         if dk is None:
-            dk = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+            dk = _empty_rows(dk_out, shape, dev)
         yp, ys = _rows("dk", dk, dev, shape)
     gammas, rest = _norm_rope_args(pos, T, Hl, Wl, table, q_gamma, k_gamma, eps, lens, split, dev, B, N, D)
     dgq, dgk = (None if g is None else torch.empty(D, dtype=torch.float32, device=dev) for g in (q_gamma, k_gamma))
@@ -1148,12 +1166,16 @@ def _cross_args(q, k, v, q_lens, kv_lens, key_mask):
     B, H, N, D = _dims("q", q, 4)
     dev = q.device
     _, Hk, M, _ = _dims("k", k, 4)
-    rows = _rows("q", q) + _rows("k", k, dev, (B, Hk, M, D)) + _rows("v", v, dev, (B, Hk, M, D))
+    shape = (B, Hk, M, D)
+    rows = _rows("q", q) + _rows("k", k, dev, shape) + _rows("v", v, dev, shape)
     if key_mask is not None and isinstance(key_mask, torch.Tensor) and key_mask.dtype is torch.bool:
         key_mask = key_mask.view(torch.uint8)
-    return (B, H, Hk, N, M, D), rows, (_device_array("q_lens", q_lens, dev, torch.int32, (B,)),
-                                       _device_array("kv_lens", kv_lens, dev, torch.int32, (B,)),
-                                       _device_array("key_mask", key_mask, dev, torch.uint8, (B, M)))
+    masks = (None, None, None)
+    if q_lens is not None or kv_lens is not None or key_mask is not None:
+        masks = (_device_array("q_lens", q_lens, dev, torch.int32, (B,)),
+                 _device_array("kv_lens", kv_lens, dev, torch.int32, (B,)),
+                 _device_array("key_mask", key_mask, dev, torch.uint8, (B, M)))
+    return (B, H, Hk, N, M, D), rows, masks
 
 
 def cross_attn_fwd(q, k, v, scale=None, q_lens=None, kv_lens=None, key_mask=None, out=None, training=False,
@@ -1172,11 +1194,11 @@ def cross_attn_fwd(q, k, v, scale=None, q_lens=None, kv_lens=None, key_mask=None
     B, H, _, N, _, D = sizes
     dev = q.device
     if out is None:
-        out = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+        out = _empty_rows(q, (B, H, N, D), dev)
     op, os_ = _rows("out", out, dev, (B, H, N, D))
     left = lse = None
     if training:
-        left = torch.empty((B, H, N, D), dtype=torch.bfloat16, device=dev)
+        left = _empty_rows(q, (B, H, N, D), dev)
         lse = torch.empty((B, H, N), dtype=torch.float32, device=dev)
     ws, wp, wn = _scratch(workspace, sol_cross_attn_fwd_workspace_bytes(*sizes, 0 if key_mask is None else 1), dev)
     _call(sol_cross_attn_fwd, dev, *rows, op, os_, left.data_ptr() if training else None,
