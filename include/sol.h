@@ -662,8 +662,8 @@ int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const v
  * is no gamma).  fp32, rounded once; sums in one order, the same bits every call.
  * Without q_gamma (k_gamma) q (k) is not looked at.
  * A token with a coordinate past its extent makes its rows NaN, and the weights'
- * gradients.  workspace: sol_qk_norm_rope_bwd_workspace_bytes(B, N) bytes of device
- * memory (0 for invalid sizes), 16-byte aligned, where dq_gamma or dk_gamma is given,
+ * gradients.  workspace: sol_qk_norm_rope_bwd_workspace_bytes bytes of device memory (0
+ * for invalid sizes), 16-byte aligned, where dq_gamma or dk_gamma is given,
  * not overlapping any tensor; its contents are scratch.
  *
  * D = 128; 1 <= N <= SOL_MAX_TOKENS; B*N <= 2^28; H, Hk <= 2^16; a table of at most
@@ -677,7 +677,7 @@ int sol_qk_norm_rope(const void* q, const sol_strides* q_strides, const void* k,
                      const float* k_gamma, float eps, const int32_t* pos, int64_t pos_stride_b,
                      const float* rope_tab, int T, int Hl, int Wl, int dt, int dh, int dw,
                      const int32_t* lens, int B, int H, int Hk, int N, int D, sol_stream_t stream);
-size_t sol_qk_norm_rope_bwd_workspace_bytes(int B, int N);
+size_t sol_qk_norm_rope_bwd_workspace_bytes(int B, int H, int Hk, int N, int D);
 int sol_qk_norm_rope_bwd(const void* dq_out, const sol_strides* dq_out_strides,
                          const void* dk_out, const sol_strides* dk_out_strides,
                          const void* q, const sol_strides* q_strides, const void* k,

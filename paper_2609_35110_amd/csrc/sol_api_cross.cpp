@@ -10,6 +10,16 @@ namespace {
 constexpr int64_t kMaxTokens = (int64_t)1 << 28;  // of a batch: a launch has 16 threads a token and fewer than 2^32
 constexpr int kMaxHeads = 1 << 16;
 
+int check_norm_rope_sizes(int B, int H, int Hk, int N, int D) {
+  if (B < 1 || H < 1 || Hk < 0 || N < 1)
+    return fail(SOL_ERR_INVALID_ARG, "B, H, N must be >= 1 and Hk >= 0 (got %d, %d, %d, %d)", B, H, N, Hk);
+  if (D != sol::kHeadDim) return fail(SOL_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", D);
+  if (N > SOL_MAX_TOKENS) return fail(SOL_ERR_UNSUPPORTED, "N=%d exceeds %d", N, SOL_MAX_TOKENS);
+  if ((int64_t)B * N > kMaxTokens) return fail(SOL_ERR_UNSUPPORTED, "B*N too large (at most 2^28)");
+  if (H > kMaxHeads || Hk > kMaxHeads) return fail(SOL_ERR_UNSUPPORTED, "H or Hk too large (at most 2^16)");
+  return SOL_OK;
+}
+
 // The table's sections: of a grid whose extents bound the coordinates, whatever
 // the tokens are.
 sol::SeqGrid sections(int T, int Hl, int Wl, int dt, int dh, int dw) {
@@ -33,12 +43,7 @@ sol::SeqGrid sections(int T, int Hl, int Wl, int dt, int dh, int dw) {
 int take_norm_rope(sol::NormRope* s, const float* q_gamma, const float* k_gamma, float eps, const int32_t* pos,
                    int64_t pos_stride_b, const float* tab, int T, int Hl, int Wl, int dt, int dh, int dw,
                    const int32_t* lens, int B, int H, int Hk, int N, int D) {
-  if (B < 1 || H < 1 || Hk < 0 || N < 1)
-    return fail(SOL_ERR_INVALID_ARG, "B, H, N must be >= 1 and Hk >= 0 (got %d, %d, %d, %d)", B, H, N, Hk);
-  if (D != sol::kHeadDim) return fail(SOL_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", D);
-  if (N > SOL_MAX_TOKENS) return fail(SOL_ERR_UNSUPPORTED, "N=%d exceeds %d", N, SOL_MAX_TOKENS);
-  if ((int64_t)B * N > kMaxTokens) return fail(SOL_ERR_UNSUPPORTED, "B*N too large (at most 2^28)");
-  if (H > kMaxHeads || Hk > kMaxHeads) return fail(SOL_ERR_UNSUPPORTED, "H or Hk too large (at most 2^16)");
+  SOL_TRY(check_norm_rope_sizes(B, H, Hk, N, D));
   if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(SOL_ERR_INVALID_ARG, "eps must be finite and >= 0");
   for (const float* g : {q_gamma, k_gamma})
     if (!aligned16(g)) return fail(SOL_ERR_INVALID_ARG, "q_gamma and k_gamma must be 16-byte aligned");
@@ -162,9 +167,9 @@ int sol_qk_norm_rope(const void* q, const sol_strides* q_strides, const void* k,
   return done(sol::launch_norm_rope_fwd(a, reinterpret_cast<hipStream_t>(stream)), "qk_norm_rope");
 }
 
-size_t sol_qk_norm_rope_bwd_workspace_bytes(int B, int N) {
-  if (B < 1 || N < 1 || N > SOL_MAX_TOKENS || (int64_t)B * N > kMaxTokens) return 0;
-  return sol::norm_rope_bwd_bytes((int64_t)B * N);
+size_t sol_qk_norm_rope_bwd_workspace_bytes(int B, int H, int Hk, int N, int D) {
+  if (check_norm_rope_sizes(B, H, Hk, N, D) != SOL_OK) return 0;
+  return sol::norm_rope_bwd_bytes((int64_t)B * N, H + Hk);
 }
 
 int sol_qk_norm_rope_bwd(const void* dq_out, const sol_strides* dq_out_strides, const void* dk_out,
@@ -190,7 +195,7 @@ int sol_qk_norm_rope_bwd(const void* dq_out, const sol_strides* dq_out_strides, 
     return fail(SOL_ERR_INVALID_ARG, "a gradient of weights that are not there (dq_gamma, dk_gamma)");
   SOL_TRY(check_small("dq_gamma", dq_gamma, true));
   SOL_TRY(check_small("dk_gamma", dk_gamma, true));
-  const size_t need = dq_gamma || dk_gamma ? sol::norm_rope_bwd_bytes((int64_t)B * N) : 0;
+  const size_t need = dq_gamma || dk_gamma ? sol::norm_rope_bwd_bytes((int64_t)B * N, H + Hk) : 0;
   SOL_TRY(check_workspace(workspace, workspace_bytes, need));
   norm_rope_spans(a.s, in + 4);
   outs[2] = span("dq_gamma", dq_gamma, sol::kHeadDim * 4);

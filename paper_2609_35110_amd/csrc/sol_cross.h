@@ -35,10 +35,8 @@ struct NormRopeBwd {
   float *dq_gamma, *dk_gamma;  // null: no norm, or not wanted
   float* partial;              // fp32 [workgroup][2][128], where a gamma's gradient is wanted
 };
-// Workgroups of the gradients' launch, and the bytes of workspace where a gamma's
-// gradient is wanted.
-int64_t norm_rope_bwd_workgroups(int64_t tokens);
-size_t norm_rope_bwd_bytes(int64_t tokens);
+// Bytes of workspace where a gamma's gradient is wanted (heads: of q and k).
+size_t norm_rope_bwd_bytes(int64_t tokens, int heads);
 hipError_t launch_norm_rope_bwd(const NormRopeBwd& a, hipStream_t stream);
 
 // ------------------------------------------------------------ cross attention

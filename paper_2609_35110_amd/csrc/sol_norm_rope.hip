@@ -106,16 +106,18 @@ __device__ __forceinline__ void turn_back(float (&f)[8], const RopeCS& cs) {
   }
 }
 
-// The gradients: tiles of 16 tokens, every gridDim.x-th a workgroup, all heads of
-// each; gamma's gradient is summed over a thread's rows, then over the workgroup's
-// 16 tokens, then (norm_rope_gamma_kernel) over the workgroups.
+// The gradients: tiles of 16 tokens, every gridDim.x-th a workgroup, `per_wg` heads of
+// each, the next head's rows on their way while one's are worked on; gamma's gradient
+// is summed over a thread's rows, then over the workgroup's 16 tokens, then
+// (norm_rope_gamma_kernel) over the workgroups.
 template <bool kRope>
-__global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormRopeBwd A) {
+__global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormRopeBwd A, int per_wg) {
   __shared__ float sum[2][kTokens][D];
   lds_poison(sum, sizeof(sum));
   lds_poison_done();
   const NormRope& s = A.s;
   const int cc = threadIdx.x & 15, r = threadIdx.x >> 4;
+  const int from = blockIdx.y * per_wg, to = min(from + per_wg, s.H + s.Hk);
   float gq[8], gk[8], sq[8] = {}, sk[8] = {};
   if (s.q_gamma) load_gamma(s.q_gamma, cc, gq);
   if (s.k_gamma) load_gamma(s.k_gamma, cc, gk);
@@ -128,18 +130,18 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormRopeBwd A) {
     if (kRope && t.bad)
       for (int e = 0; e < 8; ++e) sq[e] = sk[e] = nan_value();
     auto walk = [&](const Rows& dy, const Rows& x, const Rows& dx, const float* gamma, const float (&gm)[8], float (&sg)[8],
-                    int heads) {
-      for (int h = 0; h < heads; ++h) {
-        uint4* to = reinterpret_cast<uint4*>(row_at(dx, t, h) + 8 * cc);
-        if (!t.inside) {  // zero behind the sequence
-          *to = make_uint4(0, 0, 0, 0);
-          continue;
-        }
+                    int h0, int h1) {
+      if (h0 >= h1) return;
+      if (!t.inside) {  // zero behind the sequence
+        for (int h = h0; h < h1; ++h) *reinterpret_cast<uint4*>(row_at(dx, t, h) + 8 * cc) = make_uint4(0, 0, 0, 0);
+        return;
+      }
+      auto load = [&](const Rows& z, int h) { return *reinterpret_cast<const uint4*>(row_at(z, t, min(h, h1 - 1)) + 8 * cc); };
+      auto step = [&](int h, const uint4& y, const uint4& v) {
         float g[8];
-        unpack_bf16x8(*reinterpret_cast<const uint4*>(row_at(dy, t, h) + 8 * cc), g);
+        unpack_bf16x8(y, g);
         if (kRope) turn_back(g, cs);
         if (gamma) {
-          const uint4 v = *reinterpret_cast<const uint4*>(row_at(x, t, h) + 8 * cc);
           const float inv = rms_inv(row_sumsq_lanes16(chunk_sumsq(v)), s.eps);
           float f[8], dot = 0.0f;
           unpack_bf16x8(v, f);
@@ -154,11 +156,20 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormRopeBwd A) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) g[e] = inv * __builtin_fmaf(-f[e], dot, g[e]);
         }
-        *to = kRope && t.bad ? nan_row() : pack_bf16x8(g);
+        *reinterpret_cast<uint4*>(row_at(dx, t, h) + 8 * cc) = kRope && t.bad ? nan_row() : pack_bf16x8(g);
+      };
+      // (two heads a trip: no load in flight moves between registers; past the last head it is read again)
+      uint4 ya = load(dy, h0), va = gamma ? load(x, h0) : ya;
+      for (int h = h0; h < h1; h += 2) {
+        const uint4 yb = load(dy, h + 1), vb = gamma ? load(x, h + 1) : yb;
+        step(h, ya, va);
+        ya = load(dy, h + 2);
+        va = gamma ? load(x, h + 2) : ya;
+        if (h + 1 < h1) step(h + 1, yb, vb);
       }
     };
-    walk(A.dq_out, A.q, A.dq, s.q_gamma, gq, sq, s.H);
-    walk(A.dk_out, A.k, A.dk, s.k_gamma, gk, sk, s.Hk);
+    walk(A.dq_out, A.q, A.dq, s.q_gamma, gq, sq, from, min(to, s.H));
+    walk(A.dk_out, A.k, A.dk, s.k_gamma, gk, sk, max(from - s.H, 0), to - s.H);
   }
   if (A.partial == nullptr) return;
 #pragma unroll
@@ -171,15 +182,15 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormRopeBwd A) {
   float x = 0.0f;
 #pragma unroll
   for (int u = 0; u < kTokens; ++u) x += sum[which][u][d];
-  A.partial[(int64_t)blockIdx.x * (2 * D) + threadIdx.x] = x;
+  A.partial[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (2 * D) + threadIdx.x] = x;
 }
 
-// The workgroups' sums of gamma's gradients joined in one order, in 64 bits: 8 of
-// the 256 columns a workgroup, 32 slices of the rows, then the slices.
-constexpr int kGammaCols = 8, kGammaSlices = 32;
+// The workgroups' sums of gamma's gradients joined in one order, in 64 bits: 4 of the
+// 256 columns a workgroup, 64 slices of the rows, the slices of a wave and then the waves.
+constexpr int kGammaCols = 4, kGammaSlices = 256 / kGammaCols;
 __global__ __launch_bounds__(256) void norm_rope_gamma_kernel(const float* __restrict__ partial, int n, float* dq_gamma,
                                                               float* dk_gamma) {
-  __shared__ double sum[kGammaSlices][kGammaCols];
+  __shared__ double sum[4][kGammaCols];
   lds_poison(sum, sizeof(sum));
   lds_poison_done();
   const int c = threadIdx.x % kGammaCols, slice = threadIdx.x / kGammaCols;
@@ -187,10 +198,12 @@ __global__ __launch_bounds__(256) void norm_rope_gamma_kernel(const float* __res
   double x = 0.0;
 #pragma unroll 8
   for (int i = slice; i < n; i += kGammaSlices) x += (double)partial[(int64_t)i * (2 * D) + col];
-  sum[slice][c] = x;
+#pragma unroll
+  for (int m = kGammaCols; m < 64; m <<= 1) x += __shfl_xor(x, m);
+  if ((threadIdx.x & 63) < kGammaCols) sum[threadIdx.x >> 6][c] = x;
   __syncthreads();
-  if (slice) return;
-  for (int u = 1; u < kGammaSlices; ++u) x += sum[u][c];
+  if (threadIdx.x >= kGammaCols) return;
+  x = (sum[0][c] + sum[1][c]) + (sum[2][c] + sum[3][c]);
   float* to = col < D ? dq_gamma : dk_gamma;
   if (to) to[col % D] = (float)x;
 }
@@ -210,20 +223,35 @@ hipError_t launch_norm_rope_fwd(const NormRopeFwd& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-int64_t norm_rope_bwd_workgroups(int64_t tokens) {
-  const int64_t tiles = (tokens + kTokens - 1) / kTokens;
-  return tiles < kStreamWgs ? tiles : kStreamWgs;
+// Tiles of tokens a round, and parts of the heads, of the gradients' launch: every CU
+// eight workgroups (512 tiles of 20 heads 25.8 us whole, 20.4 in four parts).
+static void bwd_grid(int64_t tokens, int heads, int64_t* tiles, int* per) {
+  const int64_t all = (tokens + kTokens - 1) / kTokens;
+  *tiles = all < kStreamWgs ? all : kStreamWgs;
+  const int64_t parts = kStreamWgs / *tiles;
+  *per = (int)(parts >= heads ? 1 : (heads + parts - 1) / parts);
 }
-size_t norm_rope_bwd_bytes(int64_t tokens) { return (size_t)norm_rope_bwd_workgroups(tokens) * 2 * D * sizeof(float); }
+static int64_t bwd_workgroups(int64_t tokens, int heads) {
+  int64_t tiles;
+  int per;
+  bwd_grid(tokens, heads, &tiles, &per);
+  return tiles * ((heads + per - 1) / per);
+}
+size_t norm_rope_bwd_bytes(int64_t tokens, int heads) {
+  return (size_t)bwd_workgroups(tokens, heads) * 2 * D * sizeof(float);
+}
 
 hipError_t launch_norm_rope_bwd(const NormRopeBwd& a, hipStream_t stream) {
   const NormRope& s = a.s;
-  const int64_t wgs = norm_rope_bwd_workgroups((int64_t)s.B * s.N);
+  const int heads = s.H + s.Hk;
+  int64_t tiles;
+  int per;
+  bwd_grid((int64_t)s.B * s.N, heads, &tiles, &per);
   const auto kernel = s.pos ? norm_rope_bwd_kernel<true> : norm_rope_bwd_kernel<false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)((heads + per - 1) / per)), dim3(256), 0, stream, a, per);
   if (a.partial)
-    hipLaunchKernelGGL(norm_rope_gamma_kernel, dim3(2 * D / kGammaCols), dim3(256), 0, stream, a.partial, (int)wgs, a.dq_gamma,
-                       a.dk_gamma);
+    hipLaunchKernelGGL(norm_rope_gamma_kernel, dim3(2 * D / kGammaCols), dim3(256), 0, stream, a.partial,
+                       (int)bwd_workgroups((int64_t)s.B * s.N, heads), a.dq_gamma, a.dk_gamma);
   return hipGetLastError();
 }
 

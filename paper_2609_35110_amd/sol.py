@@ -722,7 +722,7 @@ _SIGNATURES = {
     "sol_diff_attn_fwd": ([_P] * 13 + [_I32] * 7 + [_F32, _I32, _P, _SZ, _P], _I32),
     "sol_diff_attn_bwd": ([_P] * 22 + [_I32] * 7 + [_F32, _I32, _P, _SZ, _P], _I32),
     "sol_qk_norm_rope": ([_P] * 10 + [_F32, _P, _I64, _P] + [_I32] * 6 + [_P] + [_I32] * 5 + [_P], _I32),
-    "sol_qk_norm_rope_bwd_workspace_bytes": ([_I32] * 2, _SZ),
+    "sol_qk_norm_rope_bwd_workspace_bytes": ([_I32] * 5, _SZ),
     "sol_qk_norm_rope_bwd": ([_P] * 16 + [_F32, _P, _I64, _P] + [_I32] * 6 + [_P] + [_I32] * 5 + [_P, _SZ, _P], _I32),
     "sol_cross_attn_fwd_workspace_bytes": ([_I32] * 7, _SZ),
     "sol_cross_attn_bwd_workspace_bytes": ([_I32] * 7, _SZ),
@@ -778,8 +778,8 @@ def sol_qk_norm_rope(*args):
     return _entry("sol_qk_norm_rope")(*args)
 
 
-def sol_qk_norm_rope_bwd_workspace_bytes(B, N):
-    return _entry("sol_qk_norm_rope_bwd_workspace_bytes")(B, N)
+def sol_qk_norm_rope_bwd_workspace_bytes(B, H, Hk, N, D):
+    return _entry("sol_qk_norm_rope_bwd_workspace_bytes")(B, H, Hk, N, D)
 
 
 def sol_qk_norm_rope_bwd(*args):
@@ -1154,7 +1154,7 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, pos, T, Hl, Wl, table, q_gamma=None, 
         yp, ys = _rows("dk", dk, dev, shape)
     gammas, rest = _norm_rope_args(pos, T, Hl, Wl, table, q_gamma, k_gamma, eps, lens, split, dev, B, N, D)
     dgq, dgk = (None if g is None else torch.empty(D, dtype=torch.float32, device=dev) for g in (q_gamma, k_gamma))
-    need = sol_qk_norm_rope_bwd_workspace_bytes(B, N) if dgq is not None or dgk is not None else 0
+    need = sol_qk_norm_rope_bwd_workspace_bytes(B, H, Hk, N, D) if dgq is not None or dgk is not None else 0
     ws, wp, wn = _scratch(workspace, need, dev)
     _call(sol_qk_norm_rope_bwd, dev, gp, gs, hp, hs, qp, qs, kp, ks, xp, xs, yp, ys, *gammas,
           None if dgq is None else dgq.data_ptr(), None if dgk is None else dgk.data_ptr(), *rest, B, H, Hk, N, D, wp, wn)

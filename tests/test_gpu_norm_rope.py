@@ -106,7 +106,7 @@ def check(x, eps=1e-6, split=(32, 48, 48), lens=None, norm=(True, True), place=l
             assert grads[2 + i] is None
             continue
         terms = torch.where(inside, terms, 0.0)
-        chain = t.shape[1] * -(-B * N // (16 * min(STREAM_WGS, -(-B * N // 16))))
+        chain = t.shape[1] * -(-B * N // (16 * min(STREAM_WGS, -(-B * N // 16))))  # (all heads of a tile in one thread: the most)
         off = (grads[2 + i].cpu().double() - terms.sum((0, 1, 2))).abs()
         assert (off <= 2.0 ** -24 * (chain + 24) * torch.where(inside, tsize, 0.0).sum((0, 1, 2))).all()
     return outs, grads
