@@ -666,8 +666,8 @@ int sol_diff_attn_bwd(const void* dout, const sol_strides* dout_strides, const v
  * for invalid sizes), 16-byte aligned, where dq_gamma or dk_gamma is given,
  * not overlapping any tensor; its contents are scratch.
  *
- * D = 128; 1 <= N <= SOL_MAX_TOKENS; B*N <= 2^28; H, Hk <= 2^16; a table of at most
- * 2^28 pairs; 0 <= eps finite (a row of zeros with eps = 0 gives NaN, as the formula
+ * D = 128; 1 <= N <= SOL_MAX_TOKENS; B*N <= 2^28 - 16; H + Hk < 2^16; a table of at
+ * most 2^28 pairs; 0 <= eps finite (a row of zeros with eps = 0 gives NaN, as the formula
  * does).
  */
 int sol_qk_norm_rope(const void* q, const sol_strides* q_strides, const void* k,

@@ -7,16 +7,16 @@
 
 namespace {
 
-constexpr int64_t kMaxTokens = (int64_t)1 << 28;  // of a batch: a launch has 16 threads a token and fewer than 2^32
-constexpr int kMaxHeads = 1 << 16;
+constexpr int64_t kMaxTokens = ((int64_t)1 << 28) - 16;  // of a batch: a launch has 16 threads a token and fewer than 2^32
+constexpr int kMaxHeads = (1 << 16) - 1;                 // of q and k: a head may be a workgroup of a grid's second axis
 
 int check_norm_rope_sizes(int B, int H, int Hk, int N, int D) {
   if (B < 1 || H < 1 || Hk < 0 || N < 1)
     return fail(SOL_ERR_INVALID_ARG, "B, H, N must be >= 1 and Hk >= 0 (got %d, %d, %d, %d)", B, H, N, Hk);
   if (D != sol::kHeadDim) return fail(SOL_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", D);
   if (N > SOL_MAX_TOKENS) return fail(SOL_ERR_UNSUPPORTED, "N=%d exceeds %d", N, SOL_MAX_TOKENS);
-  if ((int64_t)B * N > kMaxTokens) return fail(SOL_ERR_UNSUPPORTED, "B*N too large (at most 2^28)");
-  if (H > kMaxHeads || Hk > kMaxHeads) return fail(SOL_ERR_UNSUPPORTED, "H or Hk too large (at most 2^16)");
+  if ((int64_t)B * N > kMaxTokens) return fail(SOL_ERR_UNSUPPORTED, "B*N too large (at most 2^28 - 16)");
+  if ((int64_t)H + Hk > kMaxHeads) return fail(SOL_ERR_UNSUPPORTED, "H + Hk too large (at most 2^16 - 1)");
   return SOL_OK;
 }
 

@@ -315,11 +315,13 @@ struct Keys {
 // Tiles of 32 keys and their values, one after the other from key `from` on, on their
 // way into LDS, one kilobyte at a time: copy 0, 1 the halves of K's tile, 2, 3 V's.  A
 // wave brings 8 rows.  Past the last tile it comes again, and is not used; keys past the
-// sequence are its last one again (their scores are masked).  Masked keys' rows are found
-// a tile ahead, by scalar loads, which no wait for copies sees.
+// sequence are its last one again (their scores are masked).  Masked keys' rows are
+// looked up for eight tiles at a time, a lane each, and passed on by ds_bpermute: a
+// look-up waits for all the copies before it (40 heads of 111,600 rows over 512 keys, all
+// visible, looked up tile by tile 1,745 us, so 1,527; sooner, and waited for a tile later,
+// 1,530).
 constexpr int kTileKeys = 32;
 constexpr int kRing = 4;
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 template <bool kMasked>
 struct KeyCopies {
   const uint16_t *k, *v;  // the tile's first key (kMasked: the head's)
@@ -327,7 +329,7 @@ struct KeyCopies {
   Keys<kMasked> keys;
   int key, tile, turns, row, lane;
   uint32_t at, to_k, to_v, ok, ov;
-  int next, last;  // kMasked: this lane's row of the tile to come; the last key's row
+  int rows, next;  // kMasked: rows of eight tiles, lane / 8 the tile; this lane's of the tile to come
   const uint16_t *mk, *mv;
 
   // n tiles from key `from` on.
@@ -345,10 +347,7 @@ struct KeyCopies {
     turns = n;
     at = wave * kRowBlock;
     if (kMasked) {
-      if (n > 0) {
-        last = constant()[keys.len - 1];
-        fetch();
-      }
+      if (n > 0) look_up(0);
     } else {
       k += (int64_t)from * ksn;
       v += (int64_t)from * vsn;
@@ -356,16 +355,13 @@ struct KeyCopies {
       ov = copy_offset(row, vsn, lane);
     }
   }
-  __device__ __forceinline__ const __attribute__((address_space(4))) int32_t* constant() const {
-    return (const __attribute__((address_space(4))) int32_t*)(uintptr_t)keys.order;
-  }
-  // kMasked: rows of the tile from `key` on.  (A sequence's list is followed by 8 words or more.)
-  __device__ __forceinline__ void fetch() {
-    const auto* p = constant() + key + at / kRowBlock * 8;
-    int r = p[0];
-#pragma unroll
-    for (int j = 1; j < 8; ++j) r = (lane >> 3) == j ? p[j] : r;
-    next = key + row < keys.len ? r : last;
+  // kMasked: this lane's row of tile i, whose keys are from `key` on.
+  __device__ __forceinline__ void look_up(int i) {
+    if (i % 8 == 0) {
+      rows = keys.order[min(key + kTileKeys * (lane >> 3) + (int)(at / kRowBlock) * 8 + (lane & 7), keys.len - 1)];
+      asm volatile("" : "+v"(rows));  // (waited for here, not in every turn)
+    }
+    next = __builtin_amdgcn_ds_bpermute(4 * (i % 8 * 8 + (lane >> 3)), rows);
   }
   // The next tile (the first, to begin with) into LDS at k_to and v_to.
   __device__ __forceinline__ void start(uint32_t k_to, uint32_t v_to) {
@@ -378,7 +374,7 @@ struct KeyCopies {
       mv = v + (int64_t)next * vsn + chunk;
       if (tile + 1 < turns) {
         key += kTileKeys;
-        fetch();
+        look_up(tile + 1);
       }
     } else {
       key += on ? kTileKeys : 0;
@@ -452,10 +448,6 @@ struct Line {
 };
 struct Place {
   int b, h, rank, turn;
-};
-// Places of two turns of the line, and the line's length.  All lanes of a wave call it.
-struct Bounds {
-  Place from, to;
 };
 __device__ __forceinline__ Place place_in(const Line& l, int b, int64_t rest) {
   const int per_tile = l.turns(b);
@@ -643,9 +635,9 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
 
   // This lane, where what follows from it is to be found there and not kept (in registers
   // that the turns need) from the kernel's start on.
-  auto lane_here = [&]() __attribute__((always_inline)) {
-    int l = t & 63;
-    asm volatile("" : "+v"(l));
+  auto lane_here = []() __attribute__((always_inline)) {
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
     return l;
   };
   // outputs of rows without keys: their tile has no turns
@@ -689,6 +681,7 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
   // it needs, and waits for nothing else: memory has three turns for the rows.
   constexpr int kRowOps = kTrain ? 50 : 32;
   uint8_t* mine = &lds.rows[wave][0][0];
+  auto mine_at = [&]() __attribute__((always_inline)) { return lds_address(&lds.rows[0][0][0]) + wave * (uint32_t)sizeof(lds.rows[0]); };
   // Row r's 16-byte chunk c of an output lies at place c ^ (r % 16), its halves exchanged
   // for odd r / 16: written 8 bytes a lane, a row a lane, and read a row a 16 lanes, without
   // bank conflicts.
@@ -719,7 +712,7 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const uint16_t* p = q + (int64_t)min(64 * wave + 8 * u + (lane >> 3), last) * A.q.sn;
-      const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(mine) + u * kRowBlock);
+      const uint32_t to = __builtin_amdgcn_readfirstlane(mine_at() + u * kRowBlock);
       copy_1k_from(to, p);
       copy_1k_from(to + 1024, p + 64);
     }
@@ -919,7 +912,7 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
 #pragma unroll 1
         for (int u = 0; u < 4; ++u) {
           const int64_t r = keys.at(min(key + 8 * u + (lane >> 3), at.klen - 1));
-          const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(mine) + u * kRowBlock);
+          const uint32_t to = __builtin_amdgcn_readfirstlane(mine_at() + u * kRowBlock);
           copy_1k_from(to, k + r * A.k.sn);
           copy_1k_from(to + 1024, k + r * A.k.sn + 64);
           copy_1k_from(to + kTile32, v + r * A.v.sn);
