@@ -1,0 +1,142 @@
+"""Calls of the norm and rotation at given positions and of cross attention side by
+side and replayed, on the GPU: two streams at once, lengths, masks and positions that
+change between a graph's replays, graphs that share a workspace."""
+import pytest
+import torch
+
+from paper_2609_35110_amd import sol
+
+pytestmark = pytest.mark.gpu
+D = 128
+GRID = (6, 5, 7)
+
+
+def rand(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda").bfloat16()
+
+
+def rope(x, pos, lens=None):
+    q, k, gq, gk, tab = x
+    args = (pos, *GRID, tab, gq, gk)
+    out = sol.qk_norm_rope(q, k, *args, lens=lens, q_out=torch.zeros_like(q), k_out=torch.zeros_like(k))
+    return (*out, *sol.qk_norm_rope_bwd(*out, q, k, *args, lens=lens))
+
+
+def rope_case(seed, B=3, N=700):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    pos = torch.stack([torch.randint(-1, n, (B, N), generator=g, device="cuda") for n in GRID], -1).int()
+    return (rand(g, B, 4, N, D), rand(g, B, 2, N, D), 1 + 0.1 * torch.randn(D, generator=g, device="cuda"),
+            1 + 0.1 * torch.randn(D, generator=g, device="cuda"), sol.rope3d_table(*GRID).cuda()), pos
+
+
+def cross(x, q_lens=None, kv_lens=None, key_mask=None, ws=(None, None, None)):
+    """The tile kernels, the few-row kernel in pieces and the backward pass."""
+    q, k, v, do = x
+    m = dict(kv_lens=kv_lens, key_mask=key_mask)
+    fwd = sol.cross_attn_fwd(q, k, v, q_lens=q_lens, out=torch.zeros_like(q), training=True, workspace=ws[0], **m)
+    few = sol.cross_attn_fwd(q[:, :, :1], k, v, workspace=ws[1], **m)
+    rows = torch.arange(q.shape[2], device="cuda") < (q.shape[2] if q_lens is None else q_lens[:, None])
+    left = fwd[1] if q_lens is None else torch.where(rows[:, None, :, None], fwd[1], 0)
+    return (fwd[0], left, few, *sol.cross_attn_bwd(do, q, k, v, *fwd, q_lens=q_lens, workspace=ws[2], **m))
+
+
+def cross_case(seed, B=3, H=8, Hk=2, N=1100, M=1200):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return rand(g, B, H, N, D), rand(g, B, Hk, M, D), rand(g, B, Hk, M, D), rand(g, B, H, N, D)
+
+
+def same(a, b):
+    return all((x is None and y is None) or torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_two_streams_at_once():
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    work = []
+    for i in range(2):
+        r, c = rope_case(i), cross_case(i)
+        work.append([lambda r=r: rope(*r), lambda c=c: cross(c)])
+    want = [[f() for f in w] for w in work]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = [[], []]
+        for i in range(2):  # the operators in turn, so that both streams have some of each
+            for s, stream in enumerate(streams):
+                with torch.cuda.stream(stream):
+                    got[s].append(work[s][(i + s) % 2]())
+        torch.cuda.synchronize()
+        for s in range(2):
+            for i in range(2):
+                assert same(got[s][i], want[s][(i + s) % 2])
+
+
+def test_lengths_masks_and_states_change_between_replays():
+    x = cross_case(3)
+    B, _, N, _ = x[0].shape
+    M = x[1].shape[2]
+    ql, kl = (torch.tensor([n, n // 2, 1], dtype=torch.int32, device="cuda") for n in (N, M))
+    mask = torch.ones(B, M, dtype=torch.bool, device="cuda")
+    cross(x, ql, kl, mask)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = cross(x, ql, kl, mask)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for new_q, new_k, share in (([N, N // 2, 1], [M, M // 2, 1], 1.0), ([0, N, 65], [M, 0, 33], 0.5), ([7, 0, N - 1], [1, 9, M], 0.01),
+                                ([N, N, N], [M, M, M], 0.0), ([0, 0, 0], [M, 1, 0], 1.0)):
+        ql.copy_(torch.tensor(new_q, dtype=torch.int32))
+        kl.copy_(torch.tensor(new_k, dtype=torch.int32))
+        mask.copy_(torch.rand(B, M, generator=g, device="cuda") < share)
+        for t in x:
+            t.copy_(rand(g, *t.shape))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = cross(x, ql, kl, mask)
+        assert torch.isfinite(want[0].float()).all()
+        assert same(got, want), (new_q, new_k, share)
+
+
+def test_positions_and_lengths_change_between_replays():
+    x, pos = rope_case(4)
+    B, N = pos.shape[:2]
+    lens = torch.tensor([N, N // 2, 1], dtype=torch.int32, device="cuda")
+    rope(x, pos, lens)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = rope(x, pos, lens)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    for new in ([N, N // 2, 1], [0, N, 65], [0, 0, 0], [N, N, N]):
+        lens.copy_(torch.tensor(new, dtype=torch.int32))
+        pos.copy_(torch.stack([torch.randint(-1, n, (B, N), generator=g, device="cuda") for n in GRID], -1).int())
+        graph.replay()
+        torch.cuda.synchronize()
+        want = rope(x, pos, lens)
+        assert torch.isfinite(want[4]).all()
+        assert same(got, want), new
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_graphs_share_a_workspace(masked):
+    """Two graphs of different sizes on one workspace, replayed in turn with eager calls on it between them."""
+    cases = [cross_case(7), cross_case(8, B=2, H=6, Hk=6, N=800, M=700)]
+    g = torch.Generator(device="cuda").manual_seed(9)
+    masks = [torch.rand(c[1].shape[0], c[1].shape[2], generator=g, device="cuda") < 0.7 if masked else None for c in cases]
+    sizes = [(c[0].shape[0], c[0].shape[1], c[1].shape[1], c[0].shape[2], c[1].shape[2], D, int(masked)) for c in cases]
+    most = max(max(sol.sol_cross_attn_fwd_workspace_bytes(*s), sol.sol_cross_attn_bwd_workspace_bytes(*s),
+                   sol.sol_cross_attn_fwd_workspace_bytes(*s[:3], 1, *s[4:])) for s in sizes)
+    ws = torch.empty(most, dtype=torch.uint8, device="cuda")
+    want = [cross(c, key_mask=m) for c, m in zip(cases, masks)]
+    graphs, got = [], []
+    for c, m in zip(cases, masks):
+        cross(c, key_mask=m, ws=(ws, ws, ws))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            got.append(cross(c, key_mask=m, ws=(ws, ws, ws)))
+    for turn in range(6):
+        i = turn % 2
+        for t in got[i]:
+            t.zero_()
+        graphs[i].replay()
+        if turn % 3 == 0:
+            assert same(cross(cases[1 - i], key_mask=masks[1 - i], ws=(ws, ws, ws)), want[1 - i])
+        ws.fill_(255)  # what is in it between calls is nothing
+        torch.cuda.synchronize()
+        assert same(got[i], want[i]), turn
