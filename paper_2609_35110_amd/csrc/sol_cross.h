@@ -53,11 +53,13 @@ struct CrossShape {
 };
 
 // How a forward call runs: in groups of few rows that share a key head, their keys in
-// `pieces` (few); or in tiles of rows that workgroups take in line, tiles shared at the
-// workgroups' borders (split) or not.
+// `pieces` (few); or in tiles of rows that workgroups take in line, all of a head's keys in
+// LDS (brief), or a ring of them, tiles shared at the workgroups' borders (split) or not.
+constexpr int kShortKeys = 256;
 struct CrossPlan {
   bool few;
   int pieces;
+  bool brief;
   bool split;
   int workgroups;  // of the tile kernel
 };

@@ -437,13 +437,14 @@ constexpr int kMaxByLength = 1024;
 struct Line {
   const CrossShape& s;
   const int32_t* counts;  // of visible keys, or null
+  bool even;              // a tile is one turn, whatever its keys
   bool by_length;
-  __device__ __forceinline__ Line(const CrossShape& sh, const int32_t* c) : s(sh), counts(c) {
+  __device__ __forceinline__ Line(const CrossShape& sh, const int32_t* c, bool e = false) : s(sh), counts(c), even(e) {
     by_length = (s.q_lens || s.kv_lens || s.mask) && s.B <= kMaxByLength;
   }
   __device__ __forceinline__ int keys(int b) const { return counts ? counts[b] : key_len(s, b); }
   __device__ __forceinline__ int tiles(int b) const { return tiles_of(by_length ? query_len(s, b) : s.N, kCrossRows); }
-  __device__ __forceinline__ int turns(int b) const { return max(1, tiles_of(by_length ? keys(b) : s.M, kTileKeys)); }
+  __device__ __forceinline__ int turns(int b) const { return even ? 1 : max(1, tiles_of(by_length ? keys(b) : s.M, kTileKeys)); }
   __device__ __forceinline__ int64_t cost(int b) const { return (int64_t)s.H * tiles(b) * turns(b); }
 };
 struct Place {
@@ -573,6 +574,156 @@ struct Tiles {
     settle_on(l, end);
   }
 };
+
+// Few keys (kShortKeys at most; a prompt's 77 tokens): all of a head's are in LDS, staged
+// once for the tiles of it that a workgroup takes one after the other, so a tile is a read
+// of its rows, a softmax and a write, and memory bounds it up to some 128 keys.  Eight
+// waves of 32 rows, two a SIMD, that meet at a change of heads alone; a wave's next rows
+// are on their way, in registers, while it works on the last.  Hidden keys are zeros in
+// LDS, and not read.
+//
+// 40 heads of 111,600 rows: over 32 keys 468 us (4.9 TB/s of rows, as a copy), 77 476, 128
+// 503, 192 586, 256 683 (860 TFLOP/s, as the tile kernel over more keys); the tile kernel,
+// which has a tile's rows wait for memory no longer than its few turns, 663, 623, 587, 742,
+// 852.  (Blocks of keys as a loop: 643 over 192, 760 over 256.)
+constexpr int kShortWaves = kCrossRows / 32, kShortThreads = 64 * kShortWaves;
+template <int kBlocks, bool kTrain>  // blocks of 32 keys
+__global__ __launch_bounds__(kShortThreads) void cross_short_kernel(CrossFwd A) {
+  struct Lds {
+    uint8_t k[kBlocks][kTile32], v[kBlocks][kTile32];
+    uint8_t out[kShortWaves][32 * D];  // half of the dims of a wave's rows, on their way out
+  };
+  __shared__ __attribute__((aligned(1024))) Lds lds;
+  lds_poison(&lds, sizeof(lds));
+  lds_poison_done();
+  const CrossShape& s = A.s;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
+  const int wg = xcd_local_id(blockIdx.x, gridDim.x), per = s.H / s.Hk;
+  const float c = s.scale * kLog2e;
+  const Line line(s, nullptr, true);
+  Place end;
+  Tiles at, next;
+  {
+    const int64_t total = line_total(line);
+    const int n = line_workgroups(total, gridDim.x);
+    if (wg >= n) return;
+    const Place from = find(line, line_bound(total, wg, n), total);
+    end = find(line, line_bound(total, wg + 1, n), total);
+    at.start(line, from, end);
+  }
+  bf16x8 q[8], q_next[8];
+  auto load = [&](bf16x8(&f)[8], const Tiles& a) __attribute__((always_inline)) {
+    const int n = a.row0() + 32 * wave + l32;
+    load_row(f, A.q.p + a.at.b * A.q.sb + a.at.h * A.q.sh + (int64_t)n * A.q.sn, !a.done && n < a.qlen, hh);
+  };
+  uint32_t seen[kBlocks];  // visible keys, a bit each
+  int held_b = -1, held_hk = -1;
+  auto stage = [&](int b, int hk, int klen) __attribute__((always_inline)) {
+    const uint16_t* k = A.k.p + b * A.k.sb + hk * A.k.sh;
+    const uint16_t* v = A.v.p + b * A.v.sb + hk * A.v.sh;
+    const int r = t >> 4, cc = t & 15;
+    const int to = (r >> 3) * kRowBlock + (cc >> 3) * 1024 + (r & 7) * 128 + ((cc & 7) ^ swizzle(r)) * 16;
+    constexpr int kStep = kBlocks < 4 ? kBlocks : 4;
+#pragma unroll
+    for (int from = 0; from < kBlocks; from += kStep) {
+      uint4 xk[kStep], xv[kStep];
+#pragma unroll
+      for (int w = 0; w < kStep; ++w) {
+        const int u = from + w, key = 32 * u + l32;
+        seen[u] = (uint32_t)__ballot(key < klen && (!s.mask || s.mask[(int64_t)b * s.M + key] != 0));
+        xk[w] = xv[w] = make_uint4(0, 0, 0, 0);
+        if (seen[u] >> r & 1) {
+          xk[w] = *reinterpret_cast<const uint4*>(k + (int64_t)(32 * u + r) * A.k.sn + 8 * cc);
+          xv[w] = *reinterpret_cast<const uint4*>(v + (int64_t)(32 * u + r) * A.v.sn + 8 * cc);
+        }
+      }
+      if (from == 0) __syncthreads();  // the last head's are done with
+#pragma unroll
+      for (int w = 0; w < kStep; ++w) {
+        *reinterpret_cast<uint4*>(lds.k[from + w] + to) = xk[w];
+        *reinterpret_cast<uint4*>(lds.v[from + w] + to) = xv[w];
+      }
+    }
+    __syncthreads();
+  };
+  // The wave's rows to memory, 64 dims at a time through its LDS: the 16-byte chunk c of
+  // row r lies at place c ^ (r % 8), so that 8 lanes write 128 bytes of a row.
+  auto store_halves = [&](uint16_t* to, int64_t sn, int rows, auto&& words) __attribute__((always_inline)) {
+    uint8_t* mine = lds.out[wave];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int z = 0; z < 4; ++z)
+          *reinterpret_cast<uint2*>(mine + l32 * D + 16 * ((4 * d + z) ^ (l32 & 7)) + 8 * hh) = words(2 * half + d, z);
+      asm volatile("" ::: "memory");  // the wave's LDS operations stay in order
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int r = 8 * u + (lane >> 3), cc = lane & 7;
+        const uint4 x = *reinterpret_cast<const uint4*>(mine + r * D + 16 * (cc ^ (r & 7)));
+        if (r < rows) *reinterpret_cast<uint4*>(to + (int64_t)r * sn + 64 * half + 8 * cc) = x;
+      }
+      asm volatile("" ::: "memory");
+    }
+  };
+  const RowPlace rp = row_place(lane);
+  const int cp = col_place(lane);
+  load(q_next, at);
+  while (!at.done) {
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) q[kk] = q_next[kk];
+    next = at;
+    next.next(line, end);
+    const int b = at.at.b, h = at.at.h, hk = h / per, first = at.row0() + 32 * wave;
+    if (b != held_b || hk != held_hk) {
+      held_b = b;
+      held_hk = hk;
+      stage(b, hk, at.klen);
+    }
+    load(q_next, next);
+    if (first < at.qlen) {
+      MapRows x;
+      clear(x);
+#pragma unroll
+      for (int u = 0; u < kBlocks; ++u) {
+        if (u > 0 && 32 * u >= at.klen) break;
+        f32x16 sc[1] = {};
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) sc[0] = mfma(row_frag(lds.k[u], rp, kk), q[kk], sc[0]);
+        if (seen[u] != 0xffffffffu) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!(seen[u] >> (8 * (r >> 2) + 4 * hh + (r & 3)) & 1)) sc[0][r] = -__builtin_inff();
+        }
+        raise_max(x, sc, c);
+        exponentials(x, sc[0], c);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const bf16x8 p = operand8(sc[0], y);
+          x.l = add_bf16x8(p, x.l);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) x.o[d] = mfma(col_frag(lds.v[u] + cp, y, d), p, x.o[d]);
+        }
+      }
+      const float l = both_sum(x.l), inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x.o[d][r] *= inv;
+      const int rows = at.qlen - first;
+      if (kTrain) {
+        const int64_t row = ((int64_t)b * s.H + h) * s.N + first;
+        const float lse = log2_sum(x.m, both_sum(x.exact), c) * kLn2;
+        if (hh == 0 && l32 < rows) A.lse[row + l32] = lse;
+        store_halves(A.left + row * D, D, rows, [&](int d, int z) { return left4(x.o[d], z, pack4(x.o[d], z)); });
+      }
+      store_halves(A.out.p + b * A.out.sb + h * A.out.sh + (int64_t)first * A.out.sn, A.out.sn, rows,
+                   [&](int d, int z) { return pack4(x.o[d], z); });
+    }
+    at = next;
+  }
+}
 
 // Where workgroup `wg` of a split line leaves its share of a tile: before one that
 // another began (0), or after the last that it began itself (1); 256 rows of 128 and
@@ -1602,7 +1753,11 @@ CrossPlan cross_plan(const CrossShape& s, bool ragged) {
     return p;
   }
   p.pieces = 1;
-  p.workgroups = (int)std::min<int64_t>(kCus, tiles * turns);
+  // Few keys: 24 heads of 12,480 rows over 77 45 us, over 256 53, for training 51 and 66;
+  // in the ring 57, 70, 68 and 82.  64 x 24 heads of 300 rows over 200 127, 197.
+  p.brief = s.M <= kShortKeys;
+  p.workgroups = (int)std::min<int64_t>(kCus, p.brief ? tiles : tiles * turns);
+  if (p.brief) return p;
   // What whole tiles leave idle, in turns of 0.9 us, against the shares' way through memory
   const double idle = (double)((tiles + kCus - 1) / kCus * turns) - (double)(tiles * turns) / kCus;
   p.split = idle > 30 && !(ragged && s.B > kMaxByLength);
@@ -1627,6 +1782,7 @@ size_t cross_fwd_bytes(const CrossShape& s, CrossFwd* a, void* ws) {
     if (!fits(few_workgroups(s, pieces), kFewThreads)) return kTooLarge;
     return pieces > 1 ? (size_t)s.B * s.H * s.N * pieces * (D + 2) * sizeof(float) : 0;
   }
+  if (p.brief) return 0;
   if (!fits(row_tiles_of(s) * (kCrossRows / 16), 256) || !fits(s.B, kOrderThreads)) return kTooLarge;
   const size_t order = order_bytes(s);
   if (a) {
@@ -1645,6 +1801,14 @@ hipError_t launch_cross_fwd(const CrossFwd& a, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)few_workgroups(s, p.pieces)), dim3(kFewThreads), 0, stream, a, p.pieces);
     if (p.pieces > 1)
       hipLaunchKernelGGL(cross_join_kernel, dim3((unsigned)((int64_t)s.B * s.H * s.N)), dim3(256), 0, stream, a, p.pieces);
+    return hipGetLastError();
+  }
+  if (p.brief) {
+    const auto kernel = s.M <= 32   ? (a.lse ? cross_short_kernel<1, true> : cross_short_kernel<1, false>)
+                        : s.M <= 64 ? (a.lse ? cross_short_kernel<2, true> : cross_short_kernel<2, false>)
+                        : s.M <= 128 ? (a.lse ? cross_short_kernel<4, true> : cross_short_kernel<4, false>)
+                                    : (a.lse ? cross_short_kernel<8, true> : cross_short_kernel<8, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.workgroups), dim3(kShortThreads), 0, stream, a);
     return hipGetLastError();
   }
   if (s.mask) launch_order(s, a.order, a.counts, stream);

@@ -191,12 +191,13 @@ def cross_fwd(**kw):
     (dict(lse=at(5) + 64), -1, "lse overlaps out_left"),
     (dict(q_lens=at(4) + 64), -1, "out overlaps q_lens"),
     (dict(mask=at(4) + 65, N=1), -1, "out overlaps key_mask"),
-    (dict(mask=at(7) + 1, N=2000), -1, "workspace is NULL"),      # (the visible keys' order)
+    (dict(mask=at(7) + 1, N=2000, M=300), -1, "workspace is NULL"),  # (the visible keys' order)
     (dict(N=1, M=30000), -1, "workspace is NULL"),                # pieces of the keys
     (dict(N=1, M=30000, ws=at(9) + 8, ws_bytes=1 << 30), -1, "workspace must be 16-byte"),
     (dict(N=1, M=30000, ws=at(9), ws_bytes=64), -1, "workspace needs"),
     (dict(N=1, M=30000, ws=at(3), ws_bytes=1 << 30), -1, "workspace overlaps"),
-    (dict(B=1 << 20, H=2, Hk=1, N=65, M=1, left=None, lse=None), -2, "too large together"),
+    (dict(B=1 << 20, H=2, Hk=1, N=65, M=300, q=at(1), out=1 << 46, k=1 << 47, v=1 << 48, left=None, lse=None), -2,
+     "too large together"),
 ])
 def test_cross_fwd_refusals(kw, status, fragment):
     refused(status, fragment, cross_fwd(**kw))
@@ -243,8 +244,9 @@ def test_cross_workspaces():
     assert fwd(1, 24, 24, 1, 512, 128, 1) == 0          # (which reads the mask itself)
     assert fwd(1, 1, 1, 1, 30000, 128, 0) > 0           # pieces
     assert fwd(4, 24, 24, 8192, 512, 128, 0) == 0       # whole tiles
+    assert fwd(4, 24, 24, 8192, 256, 128, 1) == 0       # all keys at once
     # the visible keys' lists and how many there are, in 256 bytes
-    for B, M in ((1, 1), (3, 63), (2, 97), (5, 512)):
+    for B, M in ((1, 257), (3, 263), (2, 397), (5, 512)):
         assert fwd(B, 16, 16, 4096, M, 128, 1) - fwd(B, 16, 16, 4096, M, 128, 0) == (4 * (B * M + B) + 255) // 256 * 256
         assert bwd(B, 16, 16, 4096, M, 128, 1) - bwd(B, 16, 16, 4096, M, 128, 0) == (4 * (B * M + B) + 255) // 256 * 256
     for bad in ((0, 1, 1, 1, 1, 128, 0), (1, 1, 1, 1, 0, 128, 0), (1, 3, 2, 1, 1, 128, 0), (1, 1, 1, 1, 1, 64, 0),

@@ -40,11 +40,11 @@ static void norm_rope(const CrossShape& s) {
   CHECK((int64_t)sol_qk_norm_rope_bwd_workspace_bytes(s.B, s.H, s.Hk, s.N, 128) == (taken ? need : 0));
 }
 
-static bool few, split, pieces, masked_tiles, large;
+static bool few, brief, split, pieces, masked_tiles, large;
 static void fwd(const CrossShape& s) {
   const int64_t tiles = (int64_t)s.B * s.H * up(s.N, kCrossRows), turns = up(s.M, 32);
   const int64_t got = cross_fwd_bytes(s, nullptr, nullptr);
-  const int64_t order = s.mask ? up(((int64_t)s.B * s.M + s.B) * 4, 256) * 256 : 0;
+  const int64_t order = s.mask && s.M > kShortKeys ? up(((int64_t)s.B * s.M + s.B) * 4, 256) * 256 : 0;
   for (bool ragged : {false, true}) {
     const CrossPlan p = cross_plan(s, ragged);
     if (p.few) {
@@ -59,8 +59,14 @@ static void fwd(const CrossShape& s) {
       few = true;
       pieces |= p.pieces > 1;
     } else {
+      CHECK(p.brief == (s.M <= kShortKeys) && !(p.brief && p.split));
       // every workgroup has a turn: a share that is joined is one that was written
-      CHECK(p.workgroups >= 1 && p.workgroups <= kCus && p.workgroups <= tiles * turns);
+      CHECK(p.workgroups >= 1 && p.workgroups <= kCus && p.workgroups <= (p.brief ? tiles : tiles * turns));
+      if (p.brief) {
+        CHECK(got == 0);
+        brief = true;
+        continue;
+      }
       if (got == (int64_t)kTooLarge) { large = true; continue; }
       CHECK(got >= order + (p.split ? (int64_t)2 * p.workgroups * kCrossRows * (128 + 2) * 4 : 0));
       CHECK(tiles * (kCrossRows / 16) * 256 < kThreads && (int64_t)s.B * 1024 < kThreads);
@@ -70,7 +76,7 @@ static void fwd(const CrossShape& s) {
   }
   const int64_t told = sol_cross_attn_fwd_workspace_bytes(s.B, s.H, s.Hk, s.N, s.M, 128, s.mask != nullptr);
   CHECK(told == (got == (int64_t)kTooLarge ? 0 : got));
-  if (got == (int64_t)kTooLarge || cross_plan(s, true).few) return;
+  if (got == (int64_t)kTooLarge || cross_plan(s, true).few || cross_plan(s, true).brief) return;
   CrossFwd a = {};
   char* at = reinterpret_cast<char*>(1 << 20);
   CHECK((int64_t)cross_fwd_bytes(s, &a, at) == got);
@@ -140,9 +146,9 @@ int main() {
     fwd(s);
     bwd(s);
   }
-  printf("few %d pieces %d split %d masked tiles %d head pieces %d row pieces %d cut %d large %d\n", few, pieces, split, masked_tiles,
+  printf("few %d brief %d pieces %d split %d masked tiles %d head pieces %d row pieces %d cut %d large %d\n", few, brief, pieces, split, masked_tiles,
          head_pieces, row_pieces, cut, large);
-  if (!(few && pieces && split && masked_tiles && head_pieces && row_pieces && cut && large)) return 1;  // each kind was met
+  if (!(few && brief && pieces && split && masked_tiles && head_pieces && row_pieces && cut && large)) return 1;  // each kind was met
   puts("plans hold");
 }
 """

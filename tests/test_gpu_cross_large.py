@@ -24,7 +24,7 @@ def near(name, a, ref, var, size, top):
     assert (d <= 6 * var.sqrt() + 2.0 ** -8 * ref.abs() + 2.0 ** -21 * (1 + top) * size).all(), name
 
 
-@pytest.mark.parametrize("N,M", [(LONG, 512), (600, LONG)])
+@pytest.mark.parametrize("N,M", [(LONG, 512), (LONG, 77), (600, LONG)])
 def test_long_rows_and_long_keys(N, M):
     """Forwards every row, backwards the values of picked rows and keys (the roundings as for short ones: the
     probabilities' and dS's of each term, delta's of a row)."""
@@ -62,24 +62,28 @@ def test_long_rows_and_long_keys(N, M):
         assert not a[0, 0, ~on].any()
 
 
-def test_rows_far_apart():
+@pytest.mark.parametrize("H,Hk", [(2, 1), (40, 20)])  # (groups of few rows, tiles)
+def test_rows_far_apart(H, Hk):
     """2^24 elements between tokens (the most): offsets past 2^31 elements and 2^32 bytes."""
     N, far = 300, 1 << 24
     g = torch.Generator(device="cuda").manual_seed(1)
     buf = torch.empty(N, far, dtype=torch.bfloat16, device="cuda")
     part = lambda a, h: buf[:, a:a + h * D].view(N, h, D).transpose(0, 1)[None]  # noqa: E731
-    q, k, v, do, out, dq, dk, dv = (part(2048 * i, h) for i, h in enumerate((2, 1, 1, 2, 2, 2, 1, 1)))
-    c = [rand(g, 1, h, N, D) for h in (2, 1, 1, 2)]
+    q, k, v, do, out, dq, dk, dv = (part(8192 * i, h) for i, h in enumerate((H, Hk, Hk, H, H, H, Hk, Hk)))
+    c = [rand(g, 1, h, N, D) for h in (H, Hk, Hk, H)]
     for a, b in zip((q, k, v, do), c):
         a.copy_(b)
     for mask in (None, torch.rand(1, N, generator=g, device="cuda") < 0.7):
-        fwd = sol.cross_attn_fwd(q, k, v, key_mask=mask, training=True, out=out)
-        want = sol.cross_attn_fwd(*c[:3], key_mask=mask, training=True)
-        assert all(torch.equal(a, b) for a, b in zip(fwd, want))
-        got = sol.cross_attn_bwd(do, q, k, v, *fwd, key_mask=mask, dq=dq, dk=dk, dv=dv)
-        assert all(torch.equal(a, b) for a, b in zip(got, sol.cross_attn_bwd(c[3], *c[:3], *want, key_mask=mask)))
-        few = sol.cross_attn_fwd(q[:, :, -3:], k, v, key_mask=mask)
-        assert torch.equal(few, sol.cross_attn_fwd(c[0][:, :, -3:].contiguous(), *c[1:3], key_mask=mask))
+        for M in (N, 200):
+            m = None if mask is None else mask[:, :M].contiguous()
+            few = [t[:, :, :M] for t in (k, v, c[1], c[2])]
+            fwd = sol.cross_attn_fwd(q, *few[:2], key_mask=m, training=True, out=out)
+            want = sol.cross_attn_fwd(c[0], *few[2:], key_mask=m, training=True)
+            assert all(torch.equal(a, b) for a, b in zip(fwd, want))
+            got = sol.cross_attn_bwd(do, q, *few[:2], *fwd, key_mask=m, dq=dq, dk=dk[:, :, :M], dv=dv[:, :, :M])
+            assert all(torch.equal(a, b) for a, b in zip(got, sol.cross_attn_bwd(c[3], c[0], *few[2:], *want, key_mask=m)))
+        last = sol.cross_attn_fwd(q[:, :, -3:], k, v, key_mask=mask)
+        assert torch.equal(last, sol.cross_attn_fwd(c[0][:, :, -3:].contiguous(), *c[1:3], key_mask=mask))
     pos = torch.randint(0, 5, (N, 3), generator=g, device="cuda").int()
     args = (pos, 5, 5, 5, sol.rope3d_table(5, 5, 5).cuda(), torch.rand(D, generator=g, device="cuda"),
             torch.rand(D, generator=g, device="cuda"))
@@ -100,10 +104,12 @@ def test_sequences_far_apart():
     k.copy_(ck)
     v.copy_(cv)
     mask = torch.rand(2, M, generator=g, device="cuda") < 0.5
-    for N in (1, 200, 2000):
+    for N in (1, 200, 2200):
         q = rand(g, 2, 2, N, D)
-        for m in (None, mask):
-            assert torch.equal(sol.cross_attn_fwd(q, k, v, key_mask=m), sol.cross_attn_fwd(q, ck, cv, key_mask=m))
+        for n in (M, 200):
+            for m in (None, mask[:, :n].contiguous()):
+                far_rows, near_rows = ((x[:, :, :n], y[:, :, :n]) for x, y in ((k, v), (ck, cv)))
+                assert torch.equal(sol.cross_attn_fwd(q, *far_rows, key_mask=m), sol.cross_attn_fwd(q, *near_rows, key_mask=m))
     got = sol.qk_norm_rope(q[:, :, :M], k, None, 0, 0, 0, None, k_gamma=torch.ones(D, device="cuda"), k_out=v)
     assert torch.equal(got[1], sol.qk_norm_rope(q[:, :, :M], ck, None, 0, 0, 0, None, k_gamma=torch.ones(D, device="cuda"))[1])
 

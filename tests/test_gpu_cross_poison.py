@@ -13,8 +13,8 @@ import pytest
 from paper_2609_35110_amd import build as pkg_build
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-CASES = ["tests/test_gpu_norm_rope.py", "tests/test_gpu_cross_attn.py", "tests/test_gpu_cross_grads.py",
-         "tests/test_gpu_cross_run.py"]
+CASES = ["tests/test_gpu_norm_rope.py", "tests/test_gpu_cross_attn.py", "tests/test_gpu_cross_tiles.py",
+         "tests/test_gpu_cross_grads.py", "tests/test_gpu_cross_run.py"]
 
 
 @pytest.mark.gpu

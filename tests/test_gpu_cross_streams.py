@@ -69,10 +69,10 @@ def test_two_streams_at_once():
                 assert same(got[s][i], want[s][(i + s) % 2])
 
 
-def test_lengths_masks_and_states_change_between_replays():
-    x = cross_case(3)
+@pytest.mark.parametrize("M", [1200, 200])
+def test_lengths_masks_and_states_change_between_replays(M):
+    x = cross_case(3, M=M)
     B, _, N, _ = x[0].shape
-    M = x[1].shape[2]
     ql, kl = (torch.tensor([n, n // 2, 1], dtype=torch.int32, device="cuda") for n in (N, M))
     mask = torch.ones(B, M, dtype=torch.bool, device="cuda")
     cross(x, ql, kl, mask)
