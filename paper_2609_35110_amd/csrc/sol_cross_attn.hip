@@ -434,17 +434,22 @@ __device__ __forceinline__ Piece piece_of(int wg, int tiles, const DiffTiles& p)
 // of it, to the nearest tile's start unless tiles are split.  Lengths count where there
 // are few sequences enough to add them up; else every sequence counts as a whole one.
 constexpr int kMaxByLength = 1024;
+// What a whole tile takes beside its keys' turns, while its rows come and go (3 x 16 heads
+// of up to 4,097 rows over 333 masked keys 60 us where it counts for nothing, 49; 4 x 16 of
+// 2,047 over 301 49, 38).  A split line has its turns alone.
+constexpr int kTileTurns = 4;
 struct Line {
   const CrossShape& s;
   const int32_t* counts;  // of visible keys, or null
-  bool even;              // a tile is one turn, whatever its keys
+  int tile_turns;         // turns that a tile counts for beside those of its keys; kEven: it is one
   bool by_length;
-  __device__ __forceinline__ Line(const CrossShape& sh, const int32_t* c, bool e = false) : s(sh), counts(c), even(e) {
+  static constexpr int kEven = -1;
+  __device__ __forceinline__ Line(const CrossShape& sh, const int32_t* c, int per_tile) : s(sh), counts(c), tile_turns(per_tile) {
     by_length = (s.q_lens || s.kv_lens || s.mask) && s.B <= kMaxByLength;
   }
   __device__ __forceinline__ int keys(int b) const { return counts ? counts[b] : key_len(s, b); }
   __device__ __forceinline__ int tiles(int b) const { return tiles_of(by_length ? query_len(s, b) : s.N, kCrossRows); }
-  __device__ __forceinline__ int turns(int b) const { return even ? 1 : max(1, tiles_of(by_length ? keys(b) : s.M, kTileKeys)); }
+  __device__ __forceinline__ int turns(int b) const { return tile_turns == kEven ? 1 : tile_turns + max(1, tiles_of(by_length ? keys(b) : s.M, kTileKeys)); }
   __device__ __forceinline__ int64_t cost(int b) const { return (int64_t)s.H * tiles(b) * turns(b); }
 };
 struct Place {
@@ -600,7 +605,7 @@ __global__ __launch_bounds__(kShortThreads) void cross_short_kernel(CrossFwd A) 
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
   const int wg = xcd_local_id(blockIdx.x, gridDim.x), per = s.H / s.Hk;
   const float c = s.scale * kLog2e;
-  const Line line(s, nullptr, true);
+  const Line line(s, nullptr, Line::kEven);
   Place end;
   Tiles at, next;
   {
@@ -768,7 +773,7 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
   const int wg = xcd_local_id(blockIdx.x, gridDim.x), per = s.H / s.Hk;
   const float c = s.scale * kLog2e;
-  const Line line(s, kMasked ? A.counts : nullptr);
+  const Line line(s, kMasked ? A.counts : nullptr, split ? 0 : kTileTurns);
   Place end;
   Tiles now_at, next_at;
   {
@@ -1163,7 +1168,7 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
 // chunks of 8 dims a lane each.
 __global__ __launch_bounds__(256) void cross_shares_kernel(CrossFwd A, int launched) {
   const CrossShape& s = A.s;
-  const Line line(s, s.mask ? A.counts : nullptr);
+  const Line line(s, s.mask ? A.counts : nullptr, 0);
   const int per_head = tiles_of(s.N, kCrossRows), steps = kCrossRows / 16;
   const int tile = blockIdx.x / steps, r = blockIdx.x % steps * 16 + (threadIdx.x >> 4), cc = threadIdx.x & 15;
   const int rank = tile % per_head, bh = tile / per_head, h = bh % s.H, b = bh / s.H;
@@ -1759,8 +1764,14 @@ CrossPlan cross_plan(const CrossShape& s, bool ragged) {
   p.workgroups = (int)std::min<int64_t>(kCus, p.brief ? tiles : tiles * turns);
   if (p.brief) return p;
   // What whole tiles leave idle, in turns of 0.9 us, against the shares' way through memory
-  const double idle = (double)((tiles + kCus - 1) / kCus * turns) - (double)(tiles * turns) / kCus;
-  p.split = idle > 30 && !(ragged && s.B > kMaxByLength);
+  // (20 to 30 us), and against the clock, which rises where part of the chip idles: 24 heads
+  // over 4,096 keys, 1,024 rows (80 turns idle) 111 us whole, 79 split, 12,480 rows (52, a
+  // twelfth of all) 577, 604; 8 heads of 4,097 over 12,480 (183) 312, 224; 24 of 1,024 over
+  // 2,048 (40) 62, 58, over 1,024 (20) 37, 47.
+  const double all = (double)((tiles + kCus - 1) / kCus * turns), idle = all - (double)(tiles * turns) / kCus;
+  // Lengths, which are not known here, change nothing: 2 x 8 heads of up to 4,000 rows over
+  // 8,000 masked keys would gain (171, 148), 4 x 24 heads lose (528, 576).
+  p.split = idle > 30 && 8 * idle > all && !(ragged && s.B > kMaxByLength);
   return p;
 }
 
@@ -1846,7 +1857,9 @@ static BwdCost bwd_cost(const CrossShape& s) {
 // A key tile walks the rows of all the query heads that share it.  Where that takes
 // longer than the chip needs for everything, its heads and then their rows (256 or
 // more) go to several workgroups, if that saves more than their sums' way through the
-// workspace costs.
+// workspace costs: 24 heads of 12,480 rows on 4 key heads of 512 keys 1,648 us whole, 343
+// in pieces; on 24 381, 367; 8 heads of 4,097 rows over 12,480 keys 801, 735; 16 of 1,024
+// over 1,024 51, 47.
 struct KeyPieces {
   int heads, rows;
   int all() const { return heads * rows; }
@@ -1876,7 +1889,8 @@ static DiffTiles bwd_tiles(const CrossShape& s, int pieces) {
   const int64_t round = keys / kCus, more = keys % kCus;  // `more` CUs take round + 1 key tiles
   const int64_t a = best - round * key_cost, b = a - key_cost;
   const int64_t full = std::min(tiles, (kCus - more) * (a > 0 ? a / c.row : 0) + more * (b > 0 ? b / c.row : 0));
-  // what is left goes to the CUs' remaining time
+  // what is left goes to the CUs' remaining time (2 x 8 heads of 300 rows over 4,000 keys 161
+  // us whole, 75 cut; 8 of 2,048 over 2,048 81, 78)
   return cut_tiles(tiles, full, filling(tiles, full), s.M);
 }
 
