@@ -1885,6 +1885,15 @@ static DiffTiles bwd_tiles(const CrossShape& s, int pieces) {
   const int64_t tiles = row_tiles_of(s);
   const BwdCost c = bwd_cost(s);
   const int64_t keys = c.keys * pieces, key_cost = c.key / pieces;
+  if (keys + tiles <= kCus) {
+    // All stand on the chip at once: rows are cut while that holds and their walks are the
+    // longer ones, in pieces of 128 keys or more, if it saves more turns than the join takes
+    // (4 x 3 heads of 6 rows over 1,021 keys 43 us whole, 24 cut; 8 of 512 over 512 31, 29).
+    const int64_t turns = tiles_of(s.M, kTileKeys);
+    const int64_t n = std::min<int64_t>({(kCus - keys) / tiles, s.M / 128, (c.row + key_cost - 1) / key_cost, 32});
+    if (n < 2 || turns - turns / n < 8) return {(int)tiles, 1};
+    return {0, (int)n};
+  }
   const int64_t best = (keys * key_cost + tiles * c.row) / kCus;
   const int64_t round = keys / kCus, more = keys % kCus;  // `more` CUs take round + 1 key tiles
   const int64_t a = best - round * key_cost, b = a - key_cost;

@@ -98,7 +98,7 @@ static void bwd(const CrossShape& s) {
   const int64_t tiles = (int64_t)s.B * s.H * up(s.N, kCrossRows), rest = tiles - a.plan.full;
   CHECK(rest >= 0 && a.plan.full >= 0 && a.plan.pieces >= 1);
   if (a.plan.pieces == 1) CHECK(rest == 0);
-  else CHECK(a.plan.pieces <= 16 && s.M / a.plan.pieces >= 512);
+  else CHECK(a.plan.pieces <= 32 && s.M / a.plan.pieces >= 64);
   const int64_t key_tiles = (int64_t)s.B * s.Hk * up(s.M, kCrossKeys), all = (int64_t)a.head_pieces * a.row_pieces;
   CHECK(a.head_pieces >= 1 && a.row_pieces >= 1 && (s.H / s.Hk) % a.head_pieces == 0);
   if (a.row_pieces > 1) CHECK(a.head_pieces == s.H / s.Hk && s.N / a.row_pieces >= 256);
