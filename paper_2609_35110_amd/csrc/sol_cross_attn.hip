@@ -531,7 +531,7 @@ __device__ __forceinline__ int64_t line_bound(int64_t total, int i, int n) {
 struct Tiles {
   Place at;
   int qlen, klen, from, to;
-  bool done;
+  int done;  // (as a bool the struct's copies went through scratch memory)
   __device__ __forceinline__ int turns() const { return tiles_of(klen, kTileKeys); }
   __device__ __forceinline__ bool whole() const { return from == 0 && to == turns(); }
   __device__ __forceinline__ int row0() const { return at.rank * kCrossRows; }
@@ -1685,6 +1685,234 @@ __global__ __launch_bounds__(256, 1) void cross_bwd_kernel(CrossBwd A, int key_w
     dq_of<kMasked>(A, lds.tiles, blockIdx.x - key_wgs);
 }
 
+// Few keys (kShortBwdKeys at most): one workgroup has all of a key head's, 32 a wave, and
+// takes blocks of 32 rows of its heads, every parts-th one, so that a row is read once and
+// the five products are five (the walks above, which meet the rows twice, take seven).  A
+// wave finds S and X of its keys as Q K^T and dout V^T, whose registers are the operands of
+// dv and dk; dS goes through LDS, where every wave takes all the keys' for dq of 32 dims.
+// delta is found from the rows on their way into LDS, the next block's bytes in flight.
+constexpr int kShortBwdKeys = kCrossKeys;
+__global__ __launch_bounds__(256, 1) void cross_short_bwd_kernel(CrossBwd A) {
+  struct Lds {
+    uint8_t rows[2][2][kTile32];  // q and dout of a block and the next
+    uint8_t ds[4][kTile32];          // dS of a wave's keys, a key's 32 rows at the start of its 256 bytes; K to begin with
+    uint8_t dq[kOutBytes];           // the last block's dq, on its way out
+    float lse[kBwdRows], delta[kBwdRows];  // -log2 of the rows' sums (-inf: P is 0); -delta
+  };
+  __shared__ __attribute__((aligned(1024))) Lds lds;
+  lds_poison(&lds, sizeof(lds));
+  lds_poison_done();
+  const CrossShape& s = A.s;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
+  const int parts = A.row_pieces, slab = blockIdx.x / parts, part = blockIdx.x % parts;
+  const int2 bh = slab_of(slab, s.Hk, s);
+  const int b = bh.x, hk = bh.y, per = s.H / s.Hk;
+  const int qlen = query_len(s, b), klen = key_len(s, b);
+  const float c = s.scale * kLog2e;
+  const RowPlace rp = row_place(lane);
+  const int cp = col_place(lane);
+
+  // the keys: rows of K and V in registers as the scores take them, and 32 dims of all of K
+  const uint16_t* k = A.k.p + b * A.k.sb + hk * A.k.sh;
+  const int r16 = t >> 4, cc = t & 15;  // of 16 threads a row
+  const int own0 = 8 * wave + (lane >> 4);  // of the block's rows this thread has chunk cc of this one and the fourth after
+  auto place = [&](int row) __attribute__((always_inline)) {  // of chunk cc of a tile's row
+    return (row >> 3) * kRowBlock + (cc >> 3) * 1024 + (row & 7) * 128 + ((cc & 7) ^ swizzle(row & 7)) * 16;
+  };
+  auto seen = [&](int key) __attribute__((always_inline)) {
+    return key < klen && (!s.mask || s.mask[(int64_t)b * s.M + key] != 0);
+  };
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    const int key = 16 * u + r16;
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (seen(key)) x = *reinterpret_cast<const uint4*>(k + (int64_t)key * A.k.sn + 8 * cc);
+    *reinterpret_cast<uint4*>(lds.ds[u >> 1] + place(16 * (u & 1) + r16)) = x;
+  }
+  const int key = 32 * wave + l32;
+  const bool valid = seen(key), any = __any(valid) != 0, all = __all(valid) != 0;
+  bf16x8 kf[8], vf[8], kt[8];
+  load_row(vf, A.v.p + b * A.v.sb + hk * A.v.sh + (int64_t)key * A.v.sn, valid, hh);
+  __syncthreads();
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) {
+    kf[kk] = row_frag(lds.ds[wave], rp, kk);
+    kt[kk] = col_frag(lds.ds[kk >> 1] + cp, kk & 1, wave);
+  }
+  f32x16 dv[4] = {}, dk[4] = {};
+
+  // the blocks that have rows; those that have none get zeros
+  const int with_rows = tiles_of(qlen, kBwdRows), blocks = per * with_rows, none = per * (tiles_of(s.N, kBwdRows) - with_rows);
+  for (int i = part; i < none; i += parts) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int n = (with_rows + i / per) * kBwdRows + r16 + 16 * u;
+      if (n < s.N)
+        *reinterpret_cast<uint4*>(A.dq.p + b * A.dq.sb + (hk * per + i % per) * A.dq.sh + (int64_t)n * A.dq.sn + 8 * cc) =
+            make_uint4(0, 0, 0, 0);
+    }
+  }
+  struct Block {
+    int h, row0;
+  };
+  auto block = [&](int i) __attribute__((always_inline)) {
+    const int u = i / with_rows;
+    return Block{hk * per + u, (i - u * with_rows) * kBwdRows};
+  };
+  // Rows of block x on their way, those behind the sequence as its last one (their P is 0):
+  // q and dout into LDS, a wave eight of them; of out, what it left and the log sums a
+  // thread its own rows.
+  uint4 xo[2], xl[2];
+  float xs[2];
+  auto load = [&](const Block& x, int to) __attribute__((always_inline)) {
+    const int64_t row0 = ((int64_t)b * s.H + x.h) * s.N;
+    const int last = qlen - 1 - x.row0, copied = min(8 * wave + (lane >> 3), last);
+    const uint16_t* q = A.q.p + b * A.q.sb + x.h * A.q.sh + (int64_t)x.row0 * A.q.sn;
+    const uint16_t* g = A.dout.p + b * A.dout.sb + x.h * A.dout.sh + (int64_t)x.row0 * A.dout.sn;
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(&lds.rows[0][0][0]) + to * 2 * kTile32 + wave * kRowBlock);
+    const uint32_t oq = copy_offset(copied, A.q.sn, lane), og = copy_offset(copied, A.dout.sn, lane);
+    copy_1k(at, q, oq);
+    copy_1k(at + 1024, q, oq + 128);
+    copy_1k(at + kTile32, g, og);
+    copy_1k(at + kTile32 + 1024, g, og + 128);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int n = x.row0 + min(own0 + 4 * u, last);
+      xo[u] = *reinterpret_cast<const uint4*>(A.out.p + b * A.out.sb + x.h * A.out.sh + (int64_t)n * A.out.sn + 8 * cc);
+      xl[u] = *reinterpret_cast<const uint4*>(A.left + (row0 + n) * D + 8 * cc);
+      xs[u] = A.lse[row0 + n];
+    }
+  };
+  // dq of block x, which all waves have left in LDS, to memory
+  auto flush = [&](const Block& x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = own0 + 4 * u, n = x.row0 + r;
+      uint4 y = *reinterpret_cast<const uint4*>(lds.dq + r * kOutStride + 16 * cc);
+      if (n >= qlen) y = make_uint4(0, 0, 0, 0);
+      if (n < s.N) *reinterpret_cast<uint4*>(A.dq.p + b * A.dq.sb + x.h * A.dq.sh + (int64_t)n * A.dq.sn + 8 * cc) = y;
+    }
+  };
+
+  if (part < blocks) load(block(part), 0);
+  int now = 0;
+  for (int i = part; i < blocks; i += parts, now ^= 1) {
+    const Block at = block(i);
+    const uint8_t *tq = lds.rows[now][0], *tg = lds.rows[now][1];
+    // (what only MFMAs reach, where the rows on their way need no room)
+#pragma unroll
+    for (int d = 0; d < 4; ++d) asm volatile("" : "+a"(dv[d]), "+a"(dk[d]));
+    hold_in_agprs(kt);
+    copies_landed<0>();  // this wave's rows
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = own0 + 4 * u;
+      float o[8], g[8], left[8], d = 0.0f;
+      unpack_bf16x8(xo[u], o);
+      unpack_bf16x8(*reinterpret_cast<const uint4*>(tg + place(r)), g);
+      unpack_bf16x8(xl[u], left);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d = __builtin_fmaf(g[e], o[e] + left[e], d);
+      d = row_sumsq_lanes16(d);
+      if (cc == 0) {
+        const bool some = at.row0 + r < qlen && xs[u] > -3e38f;
+        lds.lse[r] = some ? -xs[u] * kLog2e : -__builtin_inff();
+        lds.delta[r] = some ? -d : 0.0f;
+      }
+    }
+    __syncthreads();
+    load(block(i + parts < blocks ? i + parts : i), now ^ 1);  // (the last one again is not used)
+    if (i != part) flush(block(i - parts));
+    if (any) {
+      f32x16 sc, x;
+      hold_in_agprs(kf);
+      hold_in_agprs(vf);
+      score_first_a(sc, row_frag(tq, rp, 0), kf[0]);
+      score_first_a(x, row_frag(tg, rp, 0), vf[0]);
+#pragma unroll
+      for (int kk = 1; kk < 8; ++kk) {
+        score_a(sc, row_frag(tq, rp, kk), kf[kk]);
+        score_a(x, row_frag(tg, rp, kk), vf[kk]);
+      }
+      settle(sc, x);
+      uint32_t pw[2][8];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {  // rows 8 g + 4 hh on
+        const float4 l = *reinterpret_cast<const float4*>(lds.lse + 8 * g + 4 * hh);
+        const float4 e = *reinterpret_cast<const float4*>(lds.delta + 8 * g + 4 * hh);
+        float p[4] = {__builtin_fmaf(sc[4 * g], c, l.x), __builtin_fmaf(sc[4 * g + 1], c, l.y),
+                      __builtin_fmaf(sc[4 * g + 2], c, l.z), __builtin_fmaf(sc[4 * g + 3], c, l.w)};
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          p[z] = __builtin_amdgcn_exp2f(p[z]);
+          if (!all) p[z] = valid ? p[z] : 0.0f;
+        }
+        pw[0][2 * g] = pack_bf16x2(p[0], p[1]);
+        pw[0][2 * g + 1] = pack_bf16x2(p[2], p[3]);
+        pw[1][2 * g] = pack_bf16x2(p[0] * (x[4 * g] + e.x), p[1] * (x[4 * g + 1] + e.y));
+        pw[1][2 * g + 1] = pack_bf16x2(p[2] * (x[4 * g + 2] + e.z), p[3] * (x[4 * g + 3] + e.w));
+        *reinterpret_cast<uint2*>(lds.ds[wave] + (l32 >> 3) * kRowBlock + (l32 & 7) * 128 + (g ^ swizzle(l32 & 7)) * 16 + 8 * hh) =
+            make_uint2(pw[1][2 * g], pw[1][2 * g + 1]);
+      }
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(pw[0][4 * y], pw[0][4 * y + 1], pw[0][4 * y + 2], pw[0][4 * y + 3]));
+        const bf16x8 ds = __builtin_bit_cast(bf16x8, make_uint4(pw[1][4 * y], pw[1][4 * y + 1], pw[1][4 * y + 2], pw[1][4 * y + 3]));
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          dv[d] = mfma(col_frag(tg + cp, y, d), p, dv[d]);
+          dk[d] = mfma(col_frag(tq + cp, y, d), ds, dk[d]);
+        }
+      }
+    }
+    __syncthreads();
+    f32x16 dq = {};
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (32 * u < klen) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) dq = mfma(kt[2 * u + y], col_frag(lds.ds[u] + cp, y, 0), dq);
+      }
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<uint2*>(lds.dq + l32 * kOutStride + 64 * wave + 16 * g + 8 * hh) =
+          make_uint2(pack_bf16x2(dq[4 * g] * s.scale, dq[4 * g + 1] * s.scale),
+                     pack_bf16x2(dq[4 * g + 2] * s.scale, dq[4 * g + 3] * s.scale));
+  }
+  all_landed();  // none is under way when the wave ends
+  __syncthreads();
+  if (part < blocks) flush(block(part + (blocks - 1 - part) / parts * parts));
+  __syncthreads();
+  if (32 * wave >= s.M) return;
+  // zero where a key is not visible
+  if (parts > 1) {
+    float* o = A.dkv_parts + (((int64_t)slab * parts + part) * 2 * kCrossKeys + key) * D + 4 * hh;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x16& x = m ? dk[d] : dv[d];
+          *reinterpret_cast<float4*>(o + m * kCrossKeys * D + 32 * d + 8 * g) =
+              valid ? make_float4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+    return;
+  }
+  uint8_t* mine = reinterpret_cast<uint8_t*>(&lds) + wave * kOutBytes;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    f32x16(&x)[4] = m ? dk : dv;
+    const Rows& y = m ? A.dk : A.dv;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[d][i] = valid ? x[d][i] * (m ? s.scale : 1.0f) : 0.0f;
+    store_rows(mine, lane, y.p + b * y.sb + hk * y.sh + (int64_t)(32 * wave) * y.sn, y.sn, 0, s.M - 32 * wave,
+               [&](int d, int g) { return pack4(x[d], g); });
+  }
+}
+
 // dq of a tile that was cut, the pieces summed in order, 16 rows a workgroup; then dv
 // and dk of key tiles that were, 16 rows of one of them.
 constexpr int kJoinRows = 16;
@@ -1919,7 +2147,27 @@ static BwdGrids bwd_grids(const CrossShape& s, const KeyPieces& pieces, const Di
   return g;
 }
 
+// Workgroups of a key head of few keys: as many as the chip has room for, of two blocks of
+// rows or more, up to kMostParts, whose sums are joined.  Few key heads of many rows, which
+// that would leave part of the chip idle with, walk as more keys do.
+static int short_parts(const CrossShape& s) {
+  const int64_t slabs = (int64_t)s.B * s.Hk, blocks = (int64_t)(s.H / s.Hk) * tiles_of(s.N, kBwdRows);
+  constexpr int kMostParts = 32;
+  if (s.M > kShortBwdKeys || (slabs * kMostParts < kCus && blocks > 2 * kMostParts)) return 0;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({kCus / slabs, blocks / 2, kMostParts}));
+}
+
 size_t cross_bwd_bytes(const CrossShape& s, CrossBwd* a, void* ws) {
+  if (const int parts = short_parts(s)) {
+    const int64_t slabs = (int64_t)s.B * s.Hk;
+    if (a) {
+      a->dkv_parts = static_cast<float*>(ws);
+      a->plan = {(int)row_tiles_of(s), 1};
+      a->head_pieces = 1;
+      a->row_pieces = parts;
+    }
+    return parts > 1 ? (size_t)slabs * parts * 2 * kCrossKeys * D * sizeof(float) : 0;
+  }
   const KeyPieces pieces = key_pieces(s);
   const DiffTiles plan = bwd_tiles(s, pieces.all());
   const BwdGrids g = bwd_grids(s, pieces, plan);
@@ -1948,6 +2196,11 @@ size_t cross_bwd_bytes(const CrossShape& s, CrossBwd* a, void* ws) {
 hipError_t launch_cross_bwd(const CrossBwd& a, hipStream_t stream) {
   const CrossShape& s = a.s;
   const BwdGrids g = bwd_grids(s, {a.head_pieces, a.row_pieces}, a.plan);
+  if (short_parts(s)) {
+    hipLaunchKernelGGL(cross_short_bwd_kernel, dim3((unsigned)(s.B * s.Hk * a.row_pieces)), dim3(256), 0, stream, a);
+    if (g.end) hipLaunchKernelGGL(cross_end_kernel<false>, dim3((unsigned)g.end), dim3(256), 0, stream, a);
+    return hipGetLastError();
+  }
   if (s.mask) launch_order(s, a.order, a.counts, stream);
   hipLaunchKernelGGL(cross_stats_kernel, dim3((unsigned)g.stats), dim3(16 * kBwdRows), 0, stream, a);
   const auto walk = s.mask ? cross_bwd_kernel<true> : cross_bwd_kernel<false>;

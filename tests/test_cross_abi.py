@@ -232,7 +232,7 @@ def cross_bwd(**kw):
     (dict(ws_bytes=100), -1, "workspace needs"),
     (dict(ws=at(2)), -1, "workspace overlaps k"),
     (dict(ws=at(6)), -1, "workspace overlaps lse"),
-    (dict(B=1 << 20, H=4, N=65, M=1), -2, "too large together"),
+    (dict(B=1 << 20, H=4, N=65, M=300), -2, "too large together"),
 ])
 def test_cross_bwd_refusals(kw, status, fragment):
     refused(status, fragment, cross_bwd(**kw))
@@ -249,6 +249,8 @@ def test_cross_workspaces():
     for B, M in ((1, 257), (3, 263), (2, 397), (5, 512)):
         assert fwd(B, 16, 16, 4096, M, 128, 1) - fwd(B, 16, 16, 4096, M, 128, 0) == (4 * (B * M + B) + 255) // 256 * 256
         assert bwd(B, 16, 16, 4096, M, 128, 1) - bwd(B, 16, 16, 4096, M, 128, 0) == (4 * (B * M + B) + 255) // 256 * 256
+    assert bwd(1, 24, 24, 32, 77, 128, 1) == 0          # a key head's rows in one workgroup
+    assert bwd(1, 24, 24, 4096, 77, 128, 1) == 24 * 10 * 2 * 128 * 128 * 4  # in ten, joined
     for bad in ((0, 1, 1, 1, 1, 128, 0), (1, 1, 1, 1, 0, 128, 0), (1, 3, 2, 1, 1, 128, 0), (1, 1, 1, 1, 1, 64, 0),
                 (1 << 12, 1 << 11, 1, 1, 1, 128, 0), (1 << 10, 1, 1, 1 << 22, 1, 128, 0)):
         assert fwd(*bad) == 0 and bwd(*bad) == 0

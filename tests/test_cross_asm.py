@@ -18,7 +18,7 @@ NAMES = {"cross_fwd_kernel": 4, "cross_bwd_kernel": 2}  # instances: masked or n
 
 
 @pytest.fixture(scope="module")
-def kernels(tmp_path_factory):
+def text(tmp_path_factory):
     hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
     if not os.path.exists(hipcc):
         pytest.skip("hipcc not available")
@@ -28,7 +28,11 @@ def kernels(tmp_path_factory):
     res = subprocess.run([hipcc] + flags + ["--cuda-device-only", "-S", "-I", pkg_build.INCLUDE, "-I", pkg_build.CSRC,
                                             "-x", "hip", src, "-o", out], capture_output=True, text=True)
     assert res.returncode == 0, res.stderr[-2000:]
-    text = open(out).read()
+    return open(out).read()
+
+
+@pytest.fixture(scope="module")
+def kernels(text):
     found = []
     for name, n in NAMES.items():
         instances = checks.functions(text, name)
@@ -41,8 +45,12 @@ def test_mfma_latency(kernels):
     checks.check_mfma_latency(kernels, past_branches=False)
 
 
-def test_no_spills(kernels):
+def test_no_spills(kernels, text):
     checks.check_no_spills(kernels)
+    for name, n in (("cross_short_kernel", 8), ("cross_short_bwd_kernel", 1), ("cross_few_kernel", 2)):
+        instances = checks.functions(text, name)
+        assert len(instances) == n, name
+        checks.check_no_spills(instances)
 
 
 def test_operands_settled_before_inline_mfmas(kernels):

@@ -84,7 +84,7 @@ static void fwd(const CrossShape& s) {
   if (s.mask) CHECK(reinterpret_cast<char*>(a.order) == at && a.counts == a.order + (int64_t)s.B * s.M);
 }
 
-static bool head_pieces, row_pieces, cut;
+static bool head_pieces, row_pieces, cut, brief_parts;
 static void bwd(const CrossShape& s) {
   CrossBwd a = {};
   char* at = reinterpret_cast<char*>(1 << 20);
@@ -95,6 +95,16 @@ static void bwd(const CrossShape& s) {
   if (always) CHECK(got != (int64_t)kTooLarge && (int64_t)cross_fwd_bytes(s, nullptr, nullptr) != (int64_t)kTooLarge);
   if (got == (int64_t)kTooLarge) return;
   CHECK((int64_t)cross_bwd_bytes(s, nullptr, nullptr) == got);
+  const int64_t slabs = (int64_t)s.B * s.Hk, blocks = (s.H / s.Hk) * up(s.N, 32);
+  if (s.M <= kCrossKeys && (slabs >= 8 || blocks <= 64)) {  // a key head's rows in parts, which have blocks of 32
+    const int64_t parts = a.row_pieces;
+    CHECK(a.head_pieces == 1 && parts >= 1 && parts <= blocks && (parts == 1 || slabs * parts <= kCus));
+    CHECK(a.plan.full == (int64_t)s.B * s.H * up(s.N, kCrossRows) && a.plan.pieces == 1);
+    CHECK(got == (parts > 1 ? slabs * parts * 2 * kCrossKeys * 128 * 4 : 0) && slabs * parts * 256 < kThreads);
+    CHECK(reinterpret_cast<char*>(a.dkv_parts) == at);
+    brief_parts |= parts > 1;
+    return;
+  }
   const int64_t tiles = (int64_t)s.B * s.H * up(s.N, kCrossRows), rest = tiles - a.plan.full;
   CHECK(rest >= 0 && a.plan.full >= 0 && a.plan.pieces >= 1);
   if (a.plan.pieces == 1) CHECK(rest == 0);
@@ -148,7 +158,7 @@ int main() {
   }
   printf("few %d brief %d pieces %d split %d masked tiles %d head pieces %d row pieces %d cut %d large %d\n", few, brief, pieces, split, masked_tiles,
          head_pieces, row_pieces, cut, large);
-  if (!(few && brief && pieces && split && masked_tiles && head_pieces && row_pieces && cut && large)) return 1;  // each kind was met
+  if (!(few && brief && pieces && split && masked_tiles && head_pieces && row_pieces && cut && brief_parts && large)) return 1;  // each kind was met
   puts("plans hold");
 }
 """
