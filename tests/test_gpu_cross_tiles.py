@@ -140,15 +140,23 @@ def test_strides(order, M):
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
-@pytest.mark.parametrize("name", ["q", "k", "v"])
-@pytest.mark.parametrize("M", [500, 150])
+@pytest.mark.parametrize("name", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("M", [500, 150, 100])
 def test_a_value_that_is_not_finite_stays_in_its_sequence_and_heads(name, bad, M):
     """One such value in a sequence's last token, whose tile others follow."""
     x = {n: t.cuda() for n, t in inputs(2, 16, 8, 700, M, seed=1).items()}
-    want = sol.cross_attn_fwd(x["q"], x["k"], x["v"])
+
+    def run():
+        args = (x["q"], x["k"], x["v"])
+        fwd = sol.cross_attn_fwd(*args, training=True)
+        return (*fwd, *sol.cross_attn_bwd(x["do"], *args, *fwd))
+
+    want = run()
     x[name][0, 2, -1, 5] = bad
-    got = sol.cross_attn_fwd(x["q"], x["k"], x["v"])
-    mine = [2, 3] if name == "q" else [4, 5]  # the heads of that key head
-    assert not torch.isfinite(got[0, mine].float()).all()
-    others = [h for h in range(16) if h not in mine]
-    assert torch.equal(got[1], want[1]) and torch.equal(got[0, others], want[0, others])
+    got = run()
+    key_head = 1 if name in ("q", "do") else 2  # of 8, which two heads share
+    assert not torch.isfinite(got[3][0, [2 * key_head, 2 * key_head + 1]].float()).all()
+    for a, b in zip(want, got):
+        per = a.shape[1] // 8
+        others = [h for h in range(a.shape[1]) if h // per != key_head]
+        assert torch.equal(b[1], a[1]) and torch.equal(b[0, others], a[0, others])
