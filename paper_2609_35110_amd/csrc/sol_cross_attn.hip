@@ -25,6 +25,12 @@ __device__ __forceinline__ int key_len(const CrossShape& s, int b) {
   return s.kv_lens ? min(max(s.kv_lens[b], 0), s.M) : s.M;
 }
 
+// Sequence and head of slab `slab`; where lengths differ head after head, so that every
+// XCD has some of each sequence.
+__device__ __forceinline__ int2 slab_of(int slab, int heads, const CrossShape& s) {  // (b, h)
+  return s.q_lens || s.kv_lens || s.mask ? make_int2(slab % s.B, slab / s.B) : make_int2(slab / heads, slab % heads);
+}
+
 // Results of pieces of the keys, to be joined: o fp32 [piece][row][128], then the
 // log2 of the sums that o was divided by, [piece][row], and of the exact ones (for
 // training), for `rows` rows: those of the tiles that are split (tile after tile),
@@ -76,16 +82,19 @@ __global__ __launch_bounds__(kFewThreads) void cross_few_kernel(CrossFwd A, int 
   lds_poison_done();
   const CrossShape& s = A.s;
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, hh = lane >> 5, l32 = lane & 31;
-  // (sequence, key head, piece of the keys) after another over the XCDs, but the
-  // groups of rows that read the same keys on one, side by side
+  // (sequence, key head, piece of the keys) after another over the XCDs; where several
+  // groups of rows read the same keys they are side by side on one, as many on each XCD
+  // (whole heads on an XCD: 20 heads of 11 groups over 901 keys 30 us, so 18; one head of
+  // 81 over 1,182 47, 21)
   const int per = s.H / s.Hk, groups = (int)few_groups(s);
-  int id = blockIdx.x / (8 * groups) * 8 + blockIdx.x % 8;
-  const int64_t row_base = (int64_t)(blockIdx.x / 8 % groups) * kFewRows;
+  int id = groups > 1 ? xcd_local_id(blockIdx.x, gridDim.x) : blockIdx.x;
+  const int64_t row_base = (int64_t)(id % groups) * kFewRows;
   const int n_rows = (int)min((int64_t)per * s.N - row_base, (int64_t)kFewRows);
-  if (id >= s.B * s.Hk * nsplit) return;
+  id /= groups;
   const int split = id % nsplit;
   id /= nsplit;
-  const int hk = id % s.Hk, b = id / s.Hk;
+  const int2 bh = groups > 1 ? slab_of(id, s.Hk, s) : make_int2(id / s.Hk, id % s.Hk);
+  const int hk = bh.y, b = bh.x;
   const int qlen = query_len(s, b), klen = key_len(s, b);
   const float c = s.scale * kLog2e;
   const int64_t my = row_base + min(l32, n_rows - 1);
@@ -407,9 +416,6 @@ struct RowTile {
 };
 __host__ __device__ inline int tiles_of(int n, int rows) { return (n + rows - 1) / rows; }
 __host__ __device__ inline int64_t row_tiles_of(const CrossShape& s) { return (int64_t)s.B * s.H * tiles_of(s.N, kCrossRows); }
-__device__ __forceinline__ int2 slab_of(int slab, int heads, const CrossShape& s) {  // (b, h)
-  return s.q_lens || s.kv_lens || s.mask ? make_int2(slab % s.B, slab / s.B) : make_int2(slab / heads, slab % heads);
-}
 __device__ __forceinline__ RowTile row_tile(int tile, const CrossShape& s) {
   const int per_head = tiles_of(s.N, kCrossRows), slab = tile / per_head;
   const int2 bh = slab_of(slab, s.H, s);
@@ -2009,7 +2015,7 @@ CrossPlan cross_plan(const CrossShape& s, bool ragged) {
 }
 
 static int64_t few_workgroups(const CrossShape& s, int pieces) {
-  return ((int64_t)s.B * s.Hk * pieces + 7) / 8 * 8 * few_groups(s);
+  return (int64_t)s.B * s.Hk * pieces * few_groups(s);
 }
 // The visible keys' order and counts.
 static size_t order_bytes(const CrossShape& s) { return s.mask ? up256(((size_t)s.B * s.M + s.B) * sizeof(int32_t)) : 0; }

@@ -51,7 +51,7 @@ static void fwd(const CrossShape& s) {
       const int64_t groups = up((int64_t)(s.H / s.Hk) * s.N, kFewRows);
       CHECK(p.pieces >= 1 && (p.pieces == 1 || s.M / p.pieces >= 512));
       if (got == (int64_t)kTooLarge) continue;
-      CHECK(up((int64_t)s.B * s.Hk * p.pieces, 8) * 8 * groups * 512 < kThreads);
+      CHECK((int64_t)s.B * s.Hk * p.pieces * groups * 512 < kThreads);
       if (p.pieces > 1) {
         CHECK(got >= (int64_t)s.B * s.H * s.N * p.pieces * (128 + 2) * 4);  // o, the sums and the exact ones
         CHECK((int64_t)s.B * s.H * s.N * 256 < kThreads);
