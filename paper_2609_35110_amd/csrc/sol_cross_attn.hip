@@ -2125,13 +2125,24 @@ static DiffTiles bwd_tiles(const CrossShape& s, int pieces) {
   const BwdCost c = bwd_cost(s);
   const int64_t keys = c.keys * pieces, key_cost = c.key / pieces;
   if (keys + tiles <= kCus) {
-    // All stand on the chip at once: rows are cut while that holds and their walks are the
-    // longer ones, in pieces of 128 keys or more, if it saves more turns than the join takes
-    // (4 x 3 heads of 6 rows over 1,021 keys 43 us whole, 24 cut; 8 of 512 over 512 31, 29).
-    const int64_t turns = tiles_of(s.M, kTileKeys);
-    const int64_t n = std::min<int64_t>({(kCus - keys) / tiles, s.M / 128, (c.row + key_cost - 1) / key_cost, 32});
-    if (n < 2 || turns - turns / n < 8) return {(int)tiles, 1};
-    return {0, (int)n};
+    // The chip has room for all: rows are cut (in pieces of 128 keys or more) where that
+    // ends sooner, a start and the join taking some six turns each; past one round the
+    // workgroups' mean and half of a last one.  (4 x 3 heads of 6 rows over 1,021 keys 43 us
+    // whole, 24 cut; 3 x 4 on 2 of 274 over 4,375 142, 58; 8 of 512 over 512 31, 29.)
+    constexpr double kStart = 6 * 48;
+    int least = 1;
+    double time = (double)std::max(key_cost, c.row) + kStart;
+    for (int n = 2; n <= std::min(32, s.M / 128); ++n) {
+      const double piece = (double)c.row / n;
+      const double t = kStart + (keys + tiles * n <= kCus ? std::max((double)key_cost, piece) + kStart
+                                                          : (keys * (key_cost + kStart) + tiles * n * (piece + kStart)) / kCus +
+                                                                (piece + kStart) / 2);
+      if (t < time) {
+        time = t;
+        least = n;
+      }
+    }
+    return least > 1 ? DiffTiles{0, least} : DiffTiles{(int)tiles, 1};
   }
   const int64_t best = (keys * key_cost + tiles * c.row) / kCus;
   const int64_t round = keys / kCus, more = keys % kCus;  // `more` CUs take round + 1 key tiles
