@@ -1195,7 +1195,7 @@ __global__ __launch_bounds__(256) void cross_shares_kernel(CrossFwd A, int launc
   }
   const int w0 = (int)(((at + 1) * wgs - 1) / total), w1 = (int)(((at + turns) * wgs - 1) / total);
   if (w0 == w1 || n >= qlen) return;
-  auto share = [&](int w) { return share_of(A.ws, w, line_bound(total, w, wgs) <= at); };
+  auto share = [&](int w) { return share_of(A.ws, w, w == w0); };  // (the first has the tile's first turn, no other one)
   float top = kNoMax;
   for (int w = w0; w <= w1; ++w) top = fmaxf(top, share(w)[kCrossRows * D + r]);
   float sum = 0.0f, exact = 0.0f, o[8] = {};
