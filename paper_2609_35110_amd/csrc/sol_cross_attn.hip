@@ -838,9 +838,11 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
   // The wave's 64 rows in LDS, 16 KB, at a tile's end: first its outputs on their way to
   // memory, then the q of the tile after the next on its way from there.  Both are
   // exactly 16 operations of the wave (outputs of training twice 16 and two log sums):
-  // rows behind the sequence are its last one again, of q and so of the outputs, which are
-  // stored over it, the same bits.  So a turn knows what was sent for after the copies that
-  // it needs, and waits for nothing else: memory has three turns for the rows.
+  // rows behind the sequence are its last one again, of q and so of the outputs, which the
+  // wave that has that row stores over it, the same bits.  So a turn knows what was sent for
+  // after the copies that it needs, and waits for nothing else: memory has three turns for
+  // the rows.  (A wave whose rows all lie behind the sequence stores none of them: the last
+  // row's own wave may walk again, and round otherwise.)
   constexpr int kRowOps = kTrain ? 50 : 32;
   uint8_t* mine = &lds.rows[wave][0][0];
   auto mine_at = [&]() __attribute__((always_inline)) { return lds_address(&lds.rows[0][0][0]) + wave * (uint32_t)sizeof(lds.rows[0]); };
@@ -1159,7 +1161,8 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_kernel(CrossFwd A, bool spli
       turn(i + 1, ib, ia);
     }
     last_products(ib);
-    if (__any(!(x[0].l < kTooMuch && x[1].l < kTooMuch)) != 0 || not_finite()) again(now_at);
+    if (now_at.row0() + 64 * wave >= now_at.qlen) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no row of its own (not counted)
+    else if (__any(!(x[0].l < kTooMuch && x[1].l < kTooMuch)) != 0 || not_finite()) again(now_at);
     else finish(now_at);
     item += n_items;
     now_at = next_at;
