@@ -733,8 +733,10 @@ int sol_qk_norm_rope_bwd(const void* dq_out, const sol_strides* dq_out_strides,
  * device memory (masked: whether there is a key_mask; 0: none is needed and NULL is
  * taken), 16-byte aligned, not overlapping any tensor; its contents are scratch.  Those
  * return 0 for invalid sizes too.  D = 128; 1 <= N, M <= SOL_MAX_TOKENS; B*H <= 2^22,
- * B*H*N and B*Hk*M < 2^31, and no launch of 2^32 threads: B*H*N and B*Hk*M <= 2^25 with
- * B*H <= 2^20 are always taken.
+ * B*H*N and B*Hk*M < 2^31; forwards, over more than 256 keys, at most 2^20 tiles of 256
+ * rows of a head (but for calls of few rows, N H / Hk <= 32); and no launch of 2^32
+ * threads (backwards 512 for 32 rows of a head; 1,024 a sequence with a key_mask):
+ * B*H*N and B*Hk*M <= 2^25 with B*H <= 2^20 are always taken.
  */
 size_t sol_cross_attn_fwd_workspace_bytes(int B, int H, int Hk, int N, int M, int D, int masked);
 size_t sol_cross_attn_bwd_workspace_bytes(int B, int H, int Hk, int N, int M, int D, int masked);

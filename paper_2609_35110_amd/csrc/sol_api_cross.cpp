@@ -129,7 +129,7 @@ int check_cross_call(const sol::CrossShape& s, int D) {
 }
 int check_size(size_t need) {
   if (need == sol::kTooLarge)
-    return fail(SOL_ERR_UNSUPPORTED, "B, H, N, M too large together (a launch of 2^32 threads or more)");
+    return fail(SOL_ERR_UNSUPPORTED, "B, H, N, M too large together (more than 2^20 tiles of 256 rows, or a launch of 2^32 threads)");
   return SOL_OK;
 }
 // Their spans: in[0 .. 2].

@@ -1977,6 +1977,8 @@ __global__ __launch_bounds__(256) void cross_end_kernel(CrossBwd A) {
 
 // A launch is a 1D grid of fewer than 2^32 threads.
 static bool fits(int64_t workgroups, int threads) { return workgroups < ((int64_t)1 << 32) / threads; }
+// Row tiles of a forward call that runs in line.
+constexpr int64_t kMostTiles = 1 << 20;
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 CrossPlan cross_plan(const CrossShape& s, bool ragged) {
@@ -2036,7 +2038,8 @@ size_t cross_fwd_bytes(const CrossShape& s, CrossFwd* a, void* ws) {
     return pieces > 1 ? (size_t)s.B * s.H * s.N * pieces * (D + 2) * sizeof(float) : 0;
   }
   if (p.brief) return 0;
-  if (!fits(row_tiles_of(s) * (kCrossRows / 16), 256) || !fits(s.B, kOrderThreads)) return kTooLarge;
+  // (shared tiles, which a launch of 16 rows a workgroup joins, are far fewer)
+  if (row_tiles_of(s) > kMostTiles || (s.mask && !fits(s.B, kOrderThreads))) return kTooLarge;
   const size_t order = order_bytes(s);
   if (a) {
     a->order = static_cast<int32_t*>(ws);
@@ -2197,7 +2200,8 @@ size_t cross_bwd_bytes(const CrossShape& s, CrossBwd* a, void* ws) {
   const KeyPieces pieces = key_pieces(s);
   const DiffTiles plan = bwd_tiles(s, pieces.all());
   const BwdGrids g = bwd_grids(s, pieces, plan);
-  if (!fits(g.stats, 16 * kBwdRows) || !fits(g.walks, 256) || !fits(g.end, 256) || !fits(s.B, kOrderThreads)) return kTooLarge;
+  if (!fits(g.stats, 16 * kBwdRows) || !fits(g.walks, 256) || !fits(g.end, 256) || (s.mask && !fits(s.B, kOrderThreads)))
+    return kTooLarge;
   size_t at[4];
   at[0] = order_bytes(s);
   at[1] = at[0] + up256((size_t)g.stats * kStatFloats * sizeof(float));
