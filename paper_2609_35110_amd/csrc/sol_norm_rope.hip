@@ -95,8 +95,8 @@ __global__ __launch_bounds__(256) void norm_rope_fwd_kernel(NormRopeFwd A, int p
   walk(A.k, A.k_out, s.k_gamma, gk, max(from - s.H, 0), to - s.H);
 }
 
-// R(pos)^T of a chunk, in fp32 with the table's hi plane (gradients are rounded to
-// bf16 once, and sums of them are fp32: 2^-24 of a pair is far below either).
+// R(pos)^T of a chunk, in fp32 with cosines and sines rounded to it (gradients are
+// rounded to bf16 once, and sums of them are fp32: 2^-24 of a pair is far below either).
 __device__ __forceinline__ void turn_back(float (&f)[8], const RopeCS& cs) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
@@ -214,7 +214,7 @@ hipError_t launch_norm_rope_fwd(const NormRopeFwd& a, hipStream_t stream) {
   const NormRope& s = a.s;
   const int64_t tiles = ((int64_t)s.B * s.N + kTokens - 1) / kTokens;
   const int heads = s.H + s.Hk;
-  // as many heads a workgroup as leave every CU eight of them
+  // as many heads a workgroup as make eight workgroups a CU (of which it holds seven at once)
   int64_t per = tiles * heads / kStreamWgs;
   per = per < 1 ? 1 : per > heads ? heads : per;
   const int64_t groups = (heads + per - 1) / per;
@@ -223,8 +223,9 @@ hipError_t launch_norm_rope_fwd(const NormRopeFwd& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Tiles of tokens a round, and parts of the heads, of the gradients' launch: every CU
-// eight workgroups (512 tiles of 20 heads 25.8 us whole, 20.4 in four parts).
+// Tiles of tokens a round, and parts of the heads, of the gradients' launch: eight
+// workgroups a CU, of which its registers hold four at once (five without positions), in
+// two rounds (512 tiles of 20 heads 25.8 us whole, 20.4 in four parts).
 static void bwd_grid(int64_t tokens, int heads, int64_t* tiles, int* per) {
   const int64_t all = (tokens + kTokens - 1) / kTokens;
   *tiles = all < kStreamWgs ? all : kStreamWgs;

@@ -1,6 +1,6 @@
 // Tiles of bf16 rows staged in LDS and the MFMA fragments read from them:
-// shared by the linear (sol_lin_attn.hip) and differential
-// (sol_diff_attn.hip) attention.
+// shared by the linear (sol_lin_attn.hip), differential (sol_diff_attn.hip) and
+// cross (sol_cross_attn.hip) attention.
 #pragma once
 
 #include <type_traits>
